@@ -539,6 +539,156 @@ typedef struct heddle_profile_info {
 } heddle_profile_info;
 int heddle_profile_info_get(const heddle_profile *p, heddle_profile_info *info);
 
+/* ======================================================================
+ * Feed-forward and gradient operators: the work whose times a profile holds.
+ *
+ * A profile's layer_ns and xlayer_ns are times of a layer's forward and
+ * backward pass on a GPU type; on this GPU these operators are the gated
+ * feed-forward block of a layer and of its experts, the matrix product it is
+ * made of, and the gradient clipping that ends a step.
+ *
+ * Matrices are DEVICE memory, row-major, of 16-bit values (HEDDLE_T_BF16 or
+ * HEDDLE_T_F16); `ld` is the distance between rows in elements (>= the
+ * row's length, at most 4,194,304; where no memory is shared between rows
+ * any address and any ld will do: sums run at full speed for rows that start
+ * on 4-byte boundaries, others are copied to scratch first). Sums are fp32;
+ * every output is rounded once, to nearest even. Inputs and outputs must not
+ * overlap, except that residual may be the output itself.
+ *
+ * Expert groups: with d_offsets (DEVICE [groups + 1] int32, non-decreasing,
+ * from 0 to the row count) rows d_offsets[e] .. d_offsets[e+1] - 1 use the
+ * weights of expert e, which lie stride elements apart. A group may be
+ * empty; the gradients of its weights are zero. The values are read on the
+ * device only. Values out of order or range are clamped: no access leaves
+ * the tensors, but rows that then belong to no group are not written and
+ * those in two groups hold the product of either.
+ *
+ * Scratch is the caller's: the *_workspace call tells how many bytes the call
+ * with the same descriptor needs (0 often; d_workspace may then be NULL). It
+ * must be 256-byte aligned, unused by other work until the call's work is
+ * done, and needs no initial value. All calls are asynchronous on `stream`
+ * and allocate nothing, so they can be captured into a graph.
+ *
+ * Errors: HEDDLE_E_INVAL (null pointer, a size, type, activation or ld out of
+ * range, misaligned pointer or too little workspace), HEDDLE_E_RANGE (more
+ * tiles than a launch holds) or HEDDLE_E_DEVICE; with the first nothing is
+ * enqueued.
+ * ====================================================================== */
+#define HEDDLE_T_BF16 0
+#define HEDDLE_T_F16  1
+#define HEDDLE_T_F32  2   /* gradient tensors only */
+
+#define HEDDLE_A_NONE      0
+#define HEDDLE_A_RELU      1
+#define HEDDLE_A_GELU      2   /* z/2 (1 + erf(z / sqrt 2)) */
+#define HEDDLE_A_GELU_TANH 3   /* z/2 (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))) */
+#define HEDDLE_A_SILU      4   /* z / (1 + exp(-z)) */
+
+#define HEDDLE_MAX_LD      (1 << 22)
+#define HEDDLE_MAX_GROUPS  65536
+
+/* Y = act(Z) + R with Z = X W^T + b, and its gradients. */
+typedef struct heddle_linear_desc {
+    int32_t dtype, act;
+    int64_t m, n, k;                                  /* rows of X; columns of Y and of X; m >= 0, n, k >= 1 */
+    const void *x; int64_t ldx;                       /* [m][k] */
+    const void *w; int64_t ldw;                       /* [n][k]; grouped: [groups][n][k] */
+    const void *bias;                                 /* [n] ([groups][n]) or NULL */
+    const void *residual; int64_t ldr;                /* [m][n] or NULL */
+    void *preact; int64_t ldp;                        /* [m][n] Z: output of heddle_linear or NULL, input of
+                                                         heddle_linear_backward unless act is NONE */
+    void *y; int64_t ldy;                             /* [m][n] output of heddle_linear */
+    int32_t groups;                                   /* >= 1 with d_offsets, else ignored */
+    const int32_t *d_offsets; int64_t stride_w;       /* expert groups, or NULL */
+    const void *dy; int64_t lddy;                     /* [m][n] gradient of Y (it is that of R too) */
+    void *dx; int64_t lddx;                           /* [m][k] or NULL */
+    void *dw; int64_t lddw; int64_t stride_dw;        /* [n][k] ([groups][n][k]) or NULL */
+    void *db;                                         /* [n] ([groups][n]) or NULL */
+} heddle_linear_desc;
+
+/*
+ * heddle_linear -- the product with bias, activation and residual in its
+ * epilogue. Reads x, w, bias, residual; writes y and, where given, preact.
+ */
+int heddle_linear(const heddle_linear_desc *d, void *d_workspace, int64_t workspace_bytes, hipStream_t stream);
+/*
+ * heddle_linear_backward -- with dZ = dY act'(Z): dX = dZ W, dW = dZ^T X,
+ * db = the sum of dZ's rows; each of the three only where its pointer is
+ * given. Reads dy, preact (unless act is NONE), w for dx, x for dw. dZ is
+ * rounded to dtype, as an operand of the products.
+ */
+int heddle_linear_backward(const heddle_linear_desc *d, void *d_workspace, int64_t workspace_bytes, hipStream_t stream);
+int heddle_linear_workspace(const heddle_linear_desc *d, int32_t backward, int64_t *h_bytes);
+
+/*
+ * The gated block: P = X Win^T of 2 f columns (row j of Win is the gate of
+ * unit j, row f + j its up projection), H = act(P_gate) P_up,
+ * Y = H Wout^T + R, and its gradients.
+ */
+typedef struct heddle_gated_ffn_desc {
+    int32_t dtype, act;
+    int64_t t, d, f;                                  /* rows, model width, hidden units; t >= 0, d, f >= 1 */
+    const void *x; int64_t ldx;                       /* [t][d] */
+    const void *w_in; int64_t ldw_in;                 /* [2 f][d]; grouped: [groups][2 f][d] */
+    const void *w_out; int64_t ldw_out;               /* [d][f]; grouped: [groups][d][f] */
+    const void *residual; int64_t ldr;                /* [t][d] or NULL */
+    void *preact; int64_t ldp;                        /* [t][2 f] P: output of heddle_gated_ffn or NULL, input of
+                                                         heddle_gated_ffn_backward */
+    void *y; int64_t ldy;                             /* [t][d] */
+    int32_t groups;
+    const int32_t *d_offsets; int64_t stride_in, stride_out;
+    const void *dy; int64_t lddy;                     /* [t][d] */
+    void *dx; int64_t lddx;                           /* [t][d] or NULL */
+    void *dw_in; int64_t lddw_in; int64_t stride_dw_in;      /* like w_in, or NULL */
+    void *dw_out; int64_t lddw_out; int64_t stride_dw_out;   /* like w_out, or NULL */
+} heddle_gated_ffn_desc;
+
+/*
+ * heddle_gated_ffn -- both projections, the activation and the product in one
+ * kernel, then the output projection with the residual in its epilogue. H is
+ * rounded to dtype in scratch, as an operand of the second product.
+ */
+int heddle_gated_ffn(const heddle_gated_ffn_desc *d, void *d_workspace, int64_t workspace_bytes, hipStream_t stream);
+/*
+ * heddle_gated_ffn_backward -- dH = dY Wout, dP = [dH P_up act'(P_gate) |
+ * dH act(P_gate)] in that product's epilogue (with H again), then
+ * dX = dP Win, dWin = dP^T X, dWout = dY^T H; each only where its pointer is
+ * given. dP and H are rounded to dtype, as operands. The gradient of the
+ * residual is dy.
+ */
+int heddle_gated_ffn_backward(const heddle_gated_ffn_desc *d, void *d_workspace, int64_t workspace_bytes, hipStream_t stream);
+int heddle_gated_ffn_workspace(const heddle_gated_ffn_desc *d, int32_t backward, int64_t *h_bytes);
+
+/* A gradient tensor: n contiguous values, aligned to their own size. */
+typedef struct heddle_grad_desc {
+    const void *g;
+    void *out;                                        /* clipped values; NULL or g: in place */
+    int64_t n;                                        /* >= 0 */
+    int32_t dtype;                                    /* HEDDLE_T_* */
+} heddle_grad_desc;
+
+/*
+ * heddle_grad_norm -- the 2-norm over all values of all tensors, one float at
+ * d_norm. Sums are in fp64, in a fixed order: the same tensors give the same
+ * bits, and squares of fp32 values do not overflow. NaN and infinity come
+ * through. grads is HOST memory, read during the call. Sharded gradients:
+ * all-reduce the squares of the ranks' norms, then heddle_clip_grads.
+ */
+int heddle_grad_norm(const heddle_grad_desc *grads, int32_t count, float *d_norm,
+                     void *d_workspace, int64_t workspace_bytes, hipStream_t stream);
+/*
+ * heddle_clip_grads -- out = g min(1, max_norm / (norm + 1e-6)), formed in
+ * fp32 and rounded once. In place nothing is written where the factor is 1.
+ * A NaN norm makes every value NaN, an infinite one 0 (infinities NaN).
+ * max_norm is finite and > 0.
+ */
+int heddle_clip_grads(const heddle_grad_desc *grads, int32_t count, const float *d_norm, float max_norm,
+                      hipStream_t stream);
+/* heddle_clip_grad_norm -- both in one call; d_norm receives the norm before clipping. */
+int heddle_clip_grad_norm(const heddle_grad_desc *grads, int32_t count, float max_norm, float *d_norm,
+                          void *d_workspace, int64_t workspace_bytes, hipStream_t stream);
+int heddle_grad_norm_workspace(const heddle_grad_desc *grads, int32_t count, int64_t *h_bytes);
+
 /* Message of the last negative return on this host thread ("" if none). */
 const char *heddle_last_error(void);
 

@@ -1,0 +1,323 @@
+// Global gradient norm over many tensors, and clipping by it, on gfx950.
+//
+// norm = sqrt(sum over tensors of sum g^2); out = g min(1, max_norm / (norm + 1e-6)).
+// Bound by memory: every value is read for the norm and read again, and
+// written, for the clipping. The tensors' table goes to the kernels as an
+// argument (kTensors a launch), so no copy to the device precedes them.
+// A tensor is cut into chunks of kChunk bytes at 16-byte addresses; workgroup
+// b of G takes chunks b, b + G, ... and leaves one fp64 sum. Squares are
+// summed in fp64 throughout: fp32 squares overflow from 1.9e19, and at two
+// fp64 operations a value the sums stay far below the vector units' rate. The
+// clipping's workgroups each add up the at most kParts sums by themselves, in
+// one order, which saves a launch between the two passes.
+#include <cmath>
+
+#include "heddle_internal.h"
+
+namespace heddle {
+
+constexpr int kTensors = 128, kParts = 2048;
+constexpr int64_t kChunk = 32768;
+
+struct GradTable {
+    const void *g[kTensors];
+    void *out[kTensors];
+    int64_t n[kTensors];
+    int32_t first[kTensors + 1];              // a tensor's first chunk in the launch
+    uint8_t dtype[kTensors];
+    int32_t count;
+};
+
+__device__ inline float grad_value(float v) { return v; }
+__device__ inline float grad_value(__bf16 v) { return (float)v; }
+__device__ inline float grad_value(_Float16 v) { return (float)v; }
+
+// the 16-byte pieces of chunk c of a tensor, one lane a piece: f(elements, first, from, to)
+template <typename T, typename F> __device__ inline void chunk_pieces(const void *g, int64_t n, int64_t c, F f)
+{
+    constexpr int V = 16 / sizeof(T);
+    const uintptr_t p = (uintptr_t)g;
+    const int64_t skew = (int64_t)(p & 15) / (int64_t)sizeof(T);        // values before g in its first piece
+    const T *base = (const T *)(p & ~(uintptr_t)15);
+    const int64_t end = skew + n;
+    const int64_t v0 = c * (kChunk / (int64_t)sizeof(T));
+#pragma unroll 4
+    for (int i = 0; i < kChunk / 16 / 256; i++) {
+        const int64_t v = v0 + (i * 256 + threadIdx.x) * V;
+        if (v >= end) return;
+        const int from = v < skew ? (int)(skew - v) : 0, to = end - v < V ? (int)(end - v) : V;
+        f(base + v, v - skew, from, to);
+    }
+}
+
+template <typename T> struct Piece { typedef T type __attribute__((ext_vector_type(16 / sizeof(T)))); };
+
+template <typename T> __device__ inline void read_piece(const T *p, int from, int to, float *v)
+{
+    constexpr int V = 16 / sizeof(T);
+    if (from == 0 && to == V) {
+        const typename Piece<T>::type x = *(const typename Piece<T>::type *)p;
+#pragma unroll
+        for (int i = 0; i < V; i++) v[i] = grad_value(x[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; i++) v[i] = i >= from && i < to ? grad_value(p[i]) : 0.0f;
+    }
+}
+
+template <typename T> __device__ inline double chunk_squares(const void *g, int64_t n, int64_t c)
+{
+    double s = 0;
+    chunk_pieces<T>(g, n, c, [&](const T *p, int64_t, int from, int to) {
+        constexpr int V = 16 / sizeof(T);
+        float v[V];
+        read_piece(p, from, to, v);
+#pragma unroll
+        for (int i = 0; i < V; i++) s = fma((double)v[i], (double)v[i], s);
+    });
+    return s;
+}
+
+// sum over the workgroup's 256 lanes, in a fixed order, in every lane
+__device__ inline double block_sum(double s, double *lds)
+{
+#pragma unroll
+    for (int d = 32; d; d /= 2) s += __shfl_xor(s, d);
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = s;
+    __syncthreads();
+    s = (lds[0] + lds[1]) + (lds[2] + lds[3]);
+    __syncthreads();
+    return s;
+}
+
+__global__ void __launch_bounds__(256) grad_squares_kernel(GradTable t, double *parts)
+{
+    __shared__ double lds[4];
+    double s = 0;
+    int k = 0;
+    for (int c = blockIdx.x; c < t.first[t.count]; c += gridDim.x) {
+        while (c >= t.first[k + 1]) k++;
+        const int64_t local = c - t.first[k];
+        if (t.dtype[k] == HEDDLE_T_BF16) s += chunk_squares<__bf16>(t.g[k], t.n[k], local);
+        else if (t.dtype[k] == HEDDLE_T_F16) s += chunk_squares<_Float16>(t.g[k], t.n[k], local);
+        else s += chunk_squares<float>(t.g[k], t.n[k], local);
+    }
+    s = block_sum(s, lds);
+    if (threadIdx.x == 0) parts[blockIdx.x] = s;
+}
+
+__device__ inline float norm_of(const double *parts, int count, double *lds)
+{
+    double s = 0;
+    for (int i = threadIdx.x; i < count; i += 256) s += parts[i];
+    return (float)sqrt(block_sum(s, lds));
+}
+
+__global__ void __launch_bounds__(256) grad_norm_kernel(const double *parts, int count, float *norm)
+{
+    __shared__ double lds[4];
+    const float v = norm_of(parts, count, lds);
+    if (threadIdx.x == 0) *norm = v;
+}
+
+template <typename T>
+__device__ inline void clip_chunk(const void *g, void *out, int64_t n, int64_t c, float factor)
+{
+    chunk_pieces<T>(g, n, c, [&](const T *p, int64_t first, int from, int to) {
+        constexpr int V = 16 / sizeof(T);
+        float v[V];
+        read_piece(p, from, to, v);
+        T *o = (T *)out + first;
+        if (from == 0 && to == V) {
+            typename Piece<T>::type x;
+#pragma unroll
+            for (int i = 0; i < V; i++) x[i] = (T)(v[i] * factor);
+            __builtin_memcpy(o, &x, 16);      // out may start anywhere its values may
+        } else {
+#pragma unroll
+            for (int i = 0; i < V; i++)
+                if (i >= from && i < to) o[i] = (T)(v[i] * factor);
+        }
+    });
+}
+
+// The factor from d_norm, or from the parts (then the first workgroup of the
+// first launch writes the norm).
+__global__ void __launch_bounds__(256) clip_kernel(GradTable t, const double *parts, int count, float *norm, int write,
+                                                   float max_norm)
+{
+    __shared__ double lds[4];
+    float v;
+    if (parts) {
+        v = norm_of(parts, count, lds);
+        if (write && blockIdx.x == 0 && threadIdx.x == 0) *norm = v;
+    } else {
+        v = *norm;
+    }
+    float factor = max_norm / (v + 1e-6f);
+    if (factor >= 1.0f) factor = 1.0f;                                  // a NaN stays
+    int k = 0;
+    for (int c = blockIdx.x; c < t.first[t.count]; c += gridDim.x) {
+        while (c >= t.first[k + 1]) k++;
+        if (factor == 1.0f && t.out[k] == t.g[k]) continue;
+        const int64_t local = c - t.first[k];
+        if (t.dtype[k] == HEDDLE_T_BF16) clip_chunk<__bf16>(t.g[k], t.out[k], t.n[k], local, factor);
+        else if (t.dtype[k] == HEDDLE_T_F16) clip_chunk<_Float16>(t.g[k], t.out[k], t.n[k], local, factor);
+        else clip_chunk<float>(t.g[k], t.out[k], t.n[k], local, factor);
+    }
+}
+
+static int check_grads(const heddle_grad_desc *g, int32_t count)
+{
+    if (count < 0) return fail(HEDDLE_E_INVAL, "count < 0");
+    if (count > 0 && !g) return fail(HEDDLE_E_INVAL, "grads is NULL");
+    for (int32_t i = 0; i < count; i++) {
+        if (g[i].dtype != HEDDLE_T_BF16 && g[i].dtype != HEDDLE_T_F16 && g[i].dtype != HEDDLE_T_F32)
+            return fail(HEDDLE_E_INVAL, "unknown dtype of a gradient tensor");
+        const uintptr_t mask = g[i].dtype == HEDDLE_T_F32 ? 3 : 1;
+        if (g[i].n < 0 || g[i].n > (int64_t(1) << 40)) return fail(HEDDLE_E_INVAL, "size of a gradient tensor out of range");
+        if (g[i].n > 0 && !g[i].g) return fail(HEDDLE_E_INVAL, "a gradient tensor is NULL");
+        if (((uintptr_t)g[i].g | (uintptr_t)g[i].out) & mask)
+            return fail(HEDDLE_E_INVAL, "a gradient tensor is not aligned to its values");
+    }
+    return HEDDLE_OK;
+}
+
+static int64_t chunks_of(const heddle_grad_desc &g)
+{
+    const int64_t size = g.dtype == HEDDLE_T_F32 ? 4 : 2, skew = (int64_t)((uintptr_t)g.g & 15);
+    return g.n > 0 ? (skew + g.n * size + kChunk - 1) / kChunk : 0;
+}
+
+// tables of up to kTensors tensors (and 2^30 chunks) each; f(table) launches
+template <typename F> static int each_table(const heddle_grad_desc *g, int32_t count, F f)
+{
+    int32_t i = 0;
+    do {
+        GradTable t;
+        t.count = 0;
+        t.first[0] = 0;
+        for (; i < count && t.count < kTensors; i++) {
+            const int64_t c = chunks_of(g[i]);
+            if (c == 0) continue;
+            if (t.first[t.count] + c > (int64_t(1) << 30)) break;
+            const int k = t.count++;
+            t.g[k] = g[i].g;
+            t.out[k] = g[i].out ? g[i].out : const_cast<void *>(g[i].g);
+            t.n[k] = g[i].n;
+            t.dtype[k] = (uint8_t)g[i].dtype;
+            t.first[k + 1] = (int32_t)(t.first[k] + c);
+        }
+        const int rc = f(t);
+        if (rc) return rc;
+    } while (i < count);
+    return HEDDLE_OK;
+}
+
+static int tables_of(const heddle_grad_desc *g, int32_t count)
+{
+    int n = 0;
+    each_table(g, count, [&](const GradTable &) { n++; return HEDDLE_OK; });
+    return n;
+}
+
+static int check_parts(const void *ws, int64_t bytes, int tables)
+{
+    if (!ws || ((uintptr_t)ws & 255)) return fail(HEDDLE_E_INVAL, "workspace is NULL or not 256-byte aligned");
+    if (bytes < (int64_t)(kParts + tables) * 8) return fail(HEDDLE_E_INVAL, "workspace smaller than the call needs");
+    return HEDDLE_OK;
+}
+
+// the sums of squares; *parts: how many
+static int launch_squares(const heddle_grad_desc *g, int32_t count, double *ws, int *parts, hipStream_t stream)
+{
+    int64_t all = 0;
+    for (int32_t i = 0; i < count; i++) all += chunks_of(g[i]);
+    *parts = 0;
+    return each_table(g, count, [&](const GradTable &t) {
+        // every launch has its share of the kParts sums
+        const int64_t mine = t.first[t.count];
+        int64_t blocks = all > kParts ? (int64_t)((double)mine / (double)all * kParts) : mine;
+        if (blocks < 1) blocks = 1;
+        if (blocks > kParts) blocks = kParts;
+        hipLaunchKernelGGL(grad_squares_kernel, dim3((unsigned)blocks), dim3(256), 0, stream, t, ws + *parts);
+        *parts += (int)blocks;
+        const hipError_t e = hipGetLastError();
+        return e == hipSuccess ? HEDDLE_OK : hip_fail(e, "grad_squares_kernel");
+    });
+}
+
+static int launch_clip(const heddle_grad_desc *g, int32_t count, const double *parts, int n_parts, float *norm, float max_norm,
+                       hipStream_t stream)
+{
+    int write = 1;
+    return each_table(g, count, [&](const GradTable &t) {
+        const int64_t mine = t.first[t.count];
+        const int64_t blocks = mine < 1 ? 1 : mine < kParts ? mine : kParts;
+        hipLaunchKernelGGL(clip_kernel, dim3((unsigned)blocks), dim3(256), 0, stream, t, parts, n_parts, norm, write, max_norm);
+        write = 0;
+        const hipError_t e = hipGetLastError();
+        return e == hipSuccess ? HEDDLE_OK : hip_fail(e, "clip_kernel");
+    });
+}
+
+static int check_max_norm(float max_norm)
+{
+    return std::isfinite(max_norm) && max_norm > 0 ? HEDDLE_OK : fail(HEDDLE_E_INVAL, "max_norm is not finite and > 0");
+}
+
+}  // namespace heddle
+
+using namespace heddle;
+
+extern "C" int heddle_grad_norm_workspace(const heddle_grad_desc *grads, int32_t count, int64_t *h_bytes)
+{
+    if (!h_bytes) return fail(HEDDLE_E_INVAL, "h_bytes is NULL");
+    const int rc = check_grads(grads, count);
+    if (rc) return rc;
+    *h_bytes = (int64_t)(kParts + tables_of(grads, count)) * 8;
+    return HEDDLE_OK;
+}
+
+extern "C" int heddle_grad_norm(const heddle_grad_desc *grads, int32_t count, float *d_norm, void *ws, int64_t bytes,
+                                hipStream_t stream)
+{
+    int rc = check_grads(grads, count);
+    if (rc) return rc;
+    if (!d_norm || ((uintptr_t)d_norm & 3)) return fail(HEDDLE_E_INVAL, "d_norm is NULL or misaligned");
+    rc = check_parts(ws, bytes, tables_of(grads, count));
+    if (rc) return rc;
+    int parts = 0;
+    rc = launch_squares(grads, count, (double *)ws, &parts, stream);
+    if (rc) return rc;
+    hipLaunchKernelGGL(grad_norm_kernel, dim3(1), dim3(256), 0, stream, (const double *)ws, parts, d_norm);
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess ? HEDDLE_OK : hip_fail(e, "grad_norm_kernel");
+}
+
+extern "C" int heddle_clip_grads(const heddle_grad_desc *grads, int32_t count, const float *d_norm, float max_norm,
+                                 hipStream_t stream)
+{
+    int rc = check_grads(grads, count);
+    if (rc) return rc;
+    if (!d_norm || ((uintptr_t)d_norm & 3)) return fail(HEDDLE_E_INVAL, "d_norm is NULL or misaligned");
+    rc = check_max_norm(max_norm);
+    if (rc) return rc;
+    return launch_clip(grads, count, nullptr, 0, const_cast<float *>(d_norm), max_norm, stream);
+}
+
+extern "C" int heddle_clip_grad_norm(const heddle_grad_desc *grads, int32_t count, float max_norm, float *d_norm, void *ws,
+                                     int64_t bytes, hipStream_t stream)
+{
+    int rc = check_grads(grads, count);
+    if (rc) return rc;
+    if (!d_norm || ((uintptr_t)d_norm & 3)) return fail(HEDDLE_E_INVAL, "d_norm is NULL or misaligned");
+    rc = check_max_norm(max_norm);
+    if (rc) return rc;
+    rc = check_parts(ws, bytes, tables_of(grads, count));
+    if (rc) return rc;
+    int parts = 0;
+    rc = launch_squares(grads, count, (double *)ws, &parts, stream);
+    if (rc) return rc;
+    return launch_clip(grads, count, (const double *)ws, parts, d_norm, max_norm, stream);
+}

@@ -1,0 +1,168 @@
+// The gated feed-forward block and its gradients on gfx950's matrix cores.
+//
+// Forward, 6 t d f flops: one product over [gate | up] rows whose tiles
+// alternate 16 gate and 16 up rows of Win, so that a lane holds a unit's gate
+// and up sums side by side and writes H = act(gate) up; then H Wout^T.
+// Backward, 12 t d f flops: dY Wout forms dP and H again in its epilogue
+// (P is what the forward pass kept; H costs t f values less to keep), then the
+// three products over them.
+#include "linear.h"
+
+namespace heddle {
+namespace mm {
+
+static int check_ffn(const heddle_gated_ffn_desc *d, bool backward)
+{
+    if (!d) return fail(HEDDLE_E_INVAL, "descriptor is NULL");
+    if (d->dtype != HEDDLE_T_BF16 && d->dtype != HEDDLE_T_F16) return fail(HEDDLE_E_INVAL, "dtype is neither BF16 nor F16");
+    if (d->act < HEDDLE_A_NONE || d->act > HEDDLE_A_SILU) return fail(HEDDLE_E_INVAL, "unknown activation");
+    if (d->t < 0 || d->d < 1 || d->f < 1 || d->t > kMaxRows || d->d > HEDDLE_MAX_LD || 2 * d->f > HEDDLE_MAX_LD)
+        return fail(HEDDLE_E_INVAL, "t, d or f out of range");
+    if (d->d_offsets && (d->groups < 1 || d->groups > HEDDLE_MAX_GROUPS)) return fail(HEDDLE_E_INVAL, "groups out of range");
+    if (((uintptr_t)d->d_offsets & 3)) return fail(HEDDLE_E_INVAL, "d_offsets is misaligned");
+    const bool grouped = d->d_offsets != nullptr;
+    int rc = HEDDLE_OK;
+    auto matrix = [&](const char *name, const void *p, int64_t ld, int64_t cols) {
+        if (rc == HEDDLE_OK && d->t > 0) rc = check_matrix(name, p, ld, cols);
+    };
+    auto weights = [&](const char *name, const void *p, int64_t ld, int64_t stride, int64_t rows, int64_t cols) {
+        if (rc == HEDDLE_OK) rc = check_matrix(name, p, ld, cols);
+        if (rc == HEDDLE_OK && grouped && d->groups > 1 && stride < (rows - 1) * ld + cols)
+            rc = fail(HEDDLE_E_INVAL, std::string(name) + ": the groups overlap");
+    };
+    if (!backward) {
+        matrix("x", d->x, d->ldx, d->d);
+        weights("w_in", d->w_in, d->ldw_in, d->stride_in, 2 * d->f, d->d);
+        weights("w_out", d->w_out, d->ldw_out, d->stride_out, d->d, d->f);
+        if (d->residual) matrix("residual", d->residual, d->ldr, d->d);
+        if (d->preact) matrix("preact", d->preact, d->ldp, 2 * d->f);
+        matrix("y", d->y, d->ldy, d->d);
+    } else {
+        matrix("dy", d->dy, d->lddy, d->d);
+        matrix("preact", d->preact, d->ldp, 2 * d->f);
+        weights("w_out", d->w_out, d->ldw_out, d->stride_out, d->d, d->f);
+        if (d->dx) {
+            weights("w_in", d->w_in, d->ldw_in, d->stride_in, 2 * d->f, d->d);
+            matrix("dx", d->dx, d->lddx, d->d);
+        }
+        if (d->dw_in) {
+            matrix("x", d->x, d->ldx, d->d);
+            weights("dw_in", d->dw_in, d->lddw_in, d->stride_dw_in, 2 * d->f, d->d);
+        }
+        if (d->dw_out) weights("dw_out", d->dw_out, d->lddw_out, d->stride_dw_out, d->d, d->f);
+    }
+    return rc;
+}
+
+template <typename T, typename Epi, bool BCOL>
+static int hidden(const Operand &a, const Operand &b, int64_t t, int64_t f, int64_t k, int groups, const int32_t *offsets,
+                  const Epi &epi, Scratch &s, bool run, hipStream_t stream)
+{
+    const Shape sh = shape_of(t, f, k, offsets ? groups : 1, Epi::gated, false);
+    Args x = {};
+    x.partial = (float *)s.take(partial_bytes(sh, t, f, Epi::gated));
+    if (!run || t == 0) return HEDDLE_OK;
+    x.a = a.p, x.lda = a.ld;
+    x.b = b.p, x.ldb = b.ld, x.stride_b = b.stride;
+    x.M = (int)t, x.N = (int)f, x.K = (int)k, x.F = (int)f;
+    x.offsets = offsets;
+    x.groups = offsets ? groups : 1;
+    return launch_gemm<false, BCOL, kGroupRows, T>(x, sh, epi, stream);
+}
+
+template <typename T> static int forward(const heddle_gated_ffn_desc *d, Scratch &s, bool run, hipStream_t stream)
+{
+    const int groups = d->d_offsets ? d->groups : 1;
+    if (d->t == 0) return HEDDLE_OK;
+    Operand x = {d->x, d->ldx, 0}, wi = {d->w_in, d->ldw_in, d->stride_in}, wo = {d->w_out, d->ldw_out, d->stride_out};
+    int rc = copy_rows(x, d->t, d->d, 1, s, run, stream);
+    if (rc == HEDDLE_OK) rc = copy_rows(wi, 2 * d->f, d->d, groups, s, run, stream);
+    if (rc == HEDDLE_OK) rc = copy_rows(wo, d->d, d->f, groups, s, run, stream);
+    if (rc) return rc;
+    EpiGated<T> e = {};
+    e.ldh = up8(d->f), e.h = (T *)s.take((size_t)d->t * e.ldh * 2), e.wide_h = 8;
+    e.pre = (T *)d->preact, e.ldp = d->ldp, e.wide_p = width_of(d->preact, d->ldp, d->f);
+    e.act = d->act, e.N = (int)d->f;
+    rc = hidden<T, EpiGated<T>, false>(x, wi, d->t, d->f, d->d, groups, d->d_offsets, e, s, run, stream);
+    if (rc) return rc;
+    EpiLinear<T> o = plain_output<T>(d->y, d->ldy, d->d);
+    o.residual = (const T *)d->residual, o.ldr = d->ldr, o.wide_r = width_of(d->residual, d->ldr);
+    return product<T>(false, {e.h, e.ldh, 0}, wo, d->t, d->d, d->f, groups, d->d_offsets, o, s, run, stream);
+}
+
+template <typename T> static int backward(const heddle_gated_ffn_desc *d, Scratch &s, bool run, hipStream_t stream)
+{
+    const int groups = d->d_offsets ? d->groups : 1;
+    Operand dy = {d->dy, d->lddy, 0}, x = {d->x, d->ldx, 0}, wi = {d->w_in, d->ldw_in, d->stride_in},
+            wo = {d->w_out, d->ldw_out, d->stride_out};
+    int rc = HEDDLE_OK;
+    if (!d->dx && !d->dw_in && !d->dw_out) return rc;
+    if (d->t > 0) {
+        rc = copy_rows(dy, d->t, d->d, 1, s, run, stream);
+        if (rc == HEDDLE_OK) rc = copy_rows(wo, d->d, d->f, groups, s, run, stream);
+        if (rc == HEDDLE_OK && d->dx) rc = copy_rows(wi, 2 * d->f, d->d, groups, s, run, stream);
+        if (rc == HEDDLE_OK && d->dw_in) rc = copy_rows(x, d->t, d->d, 1, s, run, stream);
+        if (rc) return rc;
+    }
+    EpiGatedGrad<T> e = {};
+    e.ldd = up8(2 * d->f), e.ldh = up8(d->f);
+    e.dp = (T *)s.take((size_t)d->t * e.ldd * 2), e.wide_d = width_of(nullptr, e.ldd, d->f);
+    e.h = (T *)s.take((size_t)d->t * e.ldh * 2), e.wide_h = 8;
+    e.pre = (const T *)d->preact, e.ldp = d->ldp, e.wide_p = width_of(d->preact, d->ldp, d->f);
+    e.act = d->act, e.N = (int)d->f;
+    rc = hidden<T, EpiGatedGrad<T>, true>(dy, wo, d->t, d->f, d->d, groups, d->d_offsets, e, s, run, stream);
+    if (rc) return rc;
+    const Operand dp = {e.dp, e.ldd, 0}, h = {e.h, e.ldh, 0};
+    if (d->dx)
+        rc = product<T>(true, dp, wi, d->t, d->d, 2 * d->f, groups, d->d_offsets, plain_output<T>(d->dx, d->lddx, d->d), s,
+                        run, stream);
+    if (rc == HEDDLE_OK && d->dw_in)
+        rc = product_sum<T>(dp, x, 2 * d->f, d->d, d->t, groups, d->d_offsets,
+                            plain_output<T>(d->dw_in, d->lddw_in, d->d, groups > 1 ? d->stride_dw_in : 0), s, run, stream);
+    if (rc == HEDDLE_OK && d->dw_out)
+        rc = product_sum<T>(dy, h, d->d, d->f, d->t, groups, d->d_offsets,
+                            plain_output<T>(d->dw_out, d->lddw_out, d->f, groups > 1 ? d->stride_dw_out : 0), s, run, stream);
+    return rc;
+}
+
+static int gated_ffn(const heddle_gated_ffn_desc *d, bool back, void *ws, int64_t bytes, bool run, hipStream_t stream,
+                     int64_t *need)
+{
+    int rc = check_ffn(d, back);
+    if (rc) return rc;
+    for (int pass = 0; pass < 2; pass++) {
+        Scratch s = {pass ? (char *)ws : nullptr, 0};
+        const bool go = pass == 1;
+        rc = d->dtype == HEDDLE_T_BF16 ? (back ? backward<__bf16>(d, s, go, stream) : forward<__bf16>(d, s, go, stream))
+                                       : (back ? backward<_Float16>(d, s, go, stream) : forward<_Float16>(d, s, go, stream));
+        if (rc) return rc;
+        if (pass == 0) {
+            if (need) *need = (int64_t)s.used;
+            if (!run) return HEDDLE_OK;
+            rc = check_scratch(s.used, ws, bytes);
+            if (rc) return rc;
+        }
+    }
+    return HEDDLE_OK;
+}
+
+}  // namespace mm
+}  // namespace heddle
+
+using namespace heddle;
+
+extern "C" int heddle_gated_ffn(const heddle_gated_ffn_desc *d, void *ws, int64_t bytes, hipStream_t stream)
+{
+    return mm::gated_ffn(d, false, ws, bytes, true, stream, nullptr);
+}
+
+extern "C" int heddle_gated_ffn_backward(const heddle_gated_ffn_desc *d, void *ws, int64_t bytes, hipStream_t stream)
+{
+    return mm::gated_ffn(d, true, ws, bytes, true, stream, nullptr);
+}
+
+extern "C" int heddle_gated_ffn_workspace(const heddle_gated_ffn_desc *d, int32_t backward, int64_t *h_bytes)
+{
+    if (!h_bytes) return fail(HEDDLE_E_INVAL, "h_bytes is NULL");
+    return mm::gated_ffn(d, backward != 0, nullptr, 0, false, nullptr, h_bytes);
+}

@@ -1,0 +1,604 @@
+// Tiled matrix products on gfx950's matrix cores (16-bit operands, fp32 sums):
+// C[i][j] = sum over k of A(i, k) B(j, k), with the operand's memory order as
+// a template parameter, expert groups, a split reduction and a fused epilogue.
+//
+// Operands. An operand is "rows" (row i holds its k contiguous: X and W of a
+// forward product) or "columns" (row k holds its i contiguous: W in dX = dZ W,
+// both operands of dW = dZ^T X). Tiles of 64 k go from global memory straight
+// to LDS, 16 bytes a lane, through a buffer resource whose size is the
+// operand's remaining bytes: what lies past the end arrives as zero, so no
+// address needs a test. Rows tiles are [row][64] with the 16-byte pieces of a
+// row exchanged by row & 7; a lane reads its 8 k with one 16-byte read.
+// Columns tiles are [64][column] with the 32-byte pieces exchanged by 3 bits of
+// k; the transposing LDS read hands each lane 4 k of its column. Either way a
+// quarter-wave's reads touch every bank once.
+//
+// Groups. With offsets, rows offsets[g] .. offsets[g+1] of the "row" dimension
+// (kGroupRows) or of the reduction (kGroupSum) belong to group g. The offsets
+// are device data: every workgroup finds its group by itself, clamps what it
+// reads to the tensors, and a group without rows costs no product.
+#pragma once
+
+#include "heddle_internal.h"
+
+namespace heddle {
+namespace mm {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+
+template <typename T> struct pack8;
+template <> struct pack8<__bf16> { typedef bf16x8 type; };
+template <> struct pack8<_Float16> { typedef f16x8 type; };
+
+__device__ inline f32x4 mfma(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+__device__ inline f32x4 mfma(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+
+constexpr int kBK = 64;                       // k of a tile
+
+// what the offsets split: rows of the output, or the reduction (one output per group)
+enum Grouping { kGroupRows = 1, kGroupSum = 2 };
+
+struct Args {
+    const void *a, *b;
+    int64_t lda, ldb;                         // elements between rows in memory, even, at most kMaxLd
+    int64_t stride_a, stride_b;               // elements from a group's operand to the next one's
+    int32_t M, N, K;                          // K: the reduction (kGroupSum: of all groups together)
+    int32_t F;                                // gated: rows of B from a gate row to its up row (N = F)
+    const int32_t *offsets;                   // device [groups + 1], or NULL
+    int32_t groups;                           // 1 without offsets
+    int32_t tiles_m, tiles_n;                 // (kGroupRows: an upper bound over all groups)
+    int32_t splits, split_tiles;              // parts of the reduction and k-tiles of each
+    float *partial;                           // [splits][M][columns()]: sums of each part (splits > 1)
+};
+// columns of a partial sum's row: whole eights; gated: the up columns after the gate ones
+__host__ __device__ inline int64_t partial_cols(int n, bool gated) { return (int64_t)((n + 7) & ~7) * (gated ? 2 : 1); }
+constexpr int64_t kMaxLd = int64_t(1) << 22;  // 256 rows stay below 2^31 bytes
+
+// ---- activations (fp32) ----
+__device__ inline float sigmoid(float z) { return 1.0f / (1.0f + __expf(-z)); }
+__device__ inline float act_of(int act, float z)
+{
+    switch (act) {
+    case HEDDLE_A_RELU: return z > 0 ? z : (z != z ? z : 0.0f);
+    case HEDDLE_A_SILU: return z * sigmoid(z);
+    case HEDDLE_A_GELU: return 0.5f * z * (1.0f + erff(z * 0.70710678118654752f));
+    case HEDDLE_A_GELU_TANH: {
+        // 0.5 (1 + tanh u) = sigmoid(2 u)
+        const float u = 0.79788456080286536f * (z + 0.044715f * z * z * z);
+        return z * sigmoid(2.0f * u);
+    }
+    default: return z;
+    }
+}
+// value and derivative; the derivative is that at +-88 beyond, where it is 0 or 1 to fp32
+// but its factors leave the type's range
+__device__ inline void act_both(int act, float z, float &v, float &d)
+{
+    const float y = z > 88.0f ? 88.0f : z < -88.0f ? -88.0f : z;
+    switch (act) {
+    case HEDDLE_A_RELU:
+        v = z > 0 ? z : (z != z ? z : 0.0f);
+        d = z > 0 ? 1.0f : (z != z ? z : 0.0f);
+        break;
+    case HEDDLE_A_SILU: {
+        const float s = sigmoid(z);
+        v = z * s;
+        d = s * (1.0f + y * (1.0f - s));
+        break;
+    }
+    case HEDDLE_A_GELU: {
+        const float c = 0.5f * (1.0f + erff(z * 0.70710678118654752f));
+        v = z * c;
+        d = c + y * 0.39894228040143268f * __expf(-0.5f * y * y);
+        break;
+    }
+    case HEDDLE_A_GELU_TANH: {
+        const float u = 0.79788456080286536f * (z + 0.044715f * z * z * z);
+        const float s = sigmoid(2.0f * u);
+        v = z * s;
+        d = s + 2.0f * y * s * (1.0f - s) * 0.79788456080286536f * (1.0f + 0.134145f * y * y);
+        break;
+    }
+    default:
+        v = z;
+        d = 1.0f;
+    }
+}
+
+// ---- eight neighbouring values of a row; `width`: elements of a memory access ----
+template <typename T, int W> struct packed { typedef T type __attribute__((ext_vector_type(W))); };
+template <int W, typename T> __device__ inline void load_by(const T *p, float v[8])
+{
+    typedef typename packed<T, W>::type P;
+#pragma unroll
+    for (int i = 0; i < 8; i += W) {
+        const P x = *(const P *)(p + i);
+#pragma unroll
+        for (int j = 0; j < W; j++) v[i + j] = (float)x[j];
+    }
+}
+template <int W, typename T> __device__ inline void store_by(T *p, const float v[8])
+{
+    typedef typename packed<T, W>::type P;
+#pragma unroll
+    for (int i = 0; i < 8; i += W) {
+        P x;
+#pragma unroll
+        for (int j = 0; j < W; j++) x[j] = (T)v[i + j];
+        *(P *)(p + i) = x;
+    }
+}
+template <typename T> __device__ inline void load8(const T *p, int count, int width, float v[8])
+{
+    if (count >= 8 && width == 8) load_by<8>(p, v);
+    else if (count >= 8 && width == 4) load_by<4>(p, v);
+    else if (count >= 8 && width == 2) load_by<2>(p, v);
+    else {
+#pragma unroll
+        for (int i = 0; i < 8; i++) v[i] = i < count ? (float)p[i] : 0.0f;
+    }
+}
+template <typename T> __device__ inline void store8(T *p, int count, int width, const float v[8])
+{
+    if (count >= 8 && width == 8) store_by<8>(p, v);
+    else if (count >= 8 && width == 4) store_by<4>(p, v);
+    else if (count >= 8 && width == 2) store_by<2>(p, v);
+    else {
+#pragma unroll
+        for (int i = 0; i < 8; i++)
+            if (i < count) p[i] = (T)v[i];
+    }
+}
+// the widest access that suits a pointer and every distance added to it (elements)
+inline uint8_t width_of(const void *p, int64_t a, int64_t b = 0, int64_t c = 0)
+{
+    const uint64_t bits = (uint64_t)(uintptr_t)p | (uint64_t)(a | b | c) * 2;
+    return bits % 16 == 0 ? 8 : bits % 8 == 0 ? 4 : bits % 4 == 0 ? 2 : 1;
+}
+
+// ---- epilogues: one call finishes eight columns n .. n+7 of row m ----
+// y = act(z + bias) + residual, z rounded once where it is kept for the
+// backward pass (`pre`), the outputs once.
+template <typename T> struct EpiLinear {
+    static constexpr bool gated = false;
+    T *y, *pre;
+    const T *bias, *residual;
+    int64_t ldy, ldp, ldr, stride_y;          // stride_y: from a group's output to the next one's (kGroupSum)
+    int32_t act, N;
+    uint8_t wide_y, wide_p, wide_r, wide_b;   // width_of the output, preact, residual and bias
+    __device__ inline void operator()(int64_t m, int n, int g, float v[8]) const
+    {
+        const int count = N - n;
+        if (bias) {
+            float b[8];
+            load8(bias + (int64_t)g * N + n, count, wide_b, b);
+#pragma unroll
+            for (int i = 0; i < 8; i++) v[i] += b[i];
+        }
+        if (pre) store8(pre + m * ldp + n, count, wide_p, v);
+        if (act) {
+#pragma unroll
+            for (int i = 0; i < 8; i++) v[i] = act_of(act, v[i]);
+        }
+        if (residual) {
+            float r[8];
+            load8(residual + m * ldr + n, count, wide_r, r);
+#pragma unroll
+            for (int i = 0; i < 8; i++) v[i] += r[i];
+        }
+        store8(y + (int64_t)g * stride_y + m * ldy + n, count, wide_y, v);
+    }
+};
+
+// h = act(gate) * up, with both kept for the backward pass where `pre` is given
+template <typename T> struct EpiGated {
+    static constexpr bool gated = true;
+    T *h, *pre;
+    int64_t ldh, ldp;
+    int32_t act, N;                           // N = F
+    uint8_t wide_h, wide_p;
+    __device__ inline void operator()(int64_t m, int n, int, float gate[8], const float up[8]) const
+    {
+        const int count = N - n;
+        if (pre) {
+            store8(pre + m * ldp + n, count, wide_p, gate);
+            store8(pre + m * ldp + N + n, count, wide_p, up);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; i++) gate[i] = act_of(act, gate[i]) * up[i];
+        store8(h + m * ldh + n, count, wide_h, gate);
+    }
+};
+
+// From dh (the product) and the kept gate and up values: the gradients of
+// both, and h again for the output weights' gradient. dp and h are rounded to
+// the operands' type here because the next products read them as operands.
+template <typename T> struct EpiGatedGrad {
+    static constexpr bool gated = false;
+    T *dp, *h;
+    const T *pre;
+    int64_t ldd, ldh, ldp;
+    int32_t act, N;
+    uint8_t wide_d, wide_h, wide_p;
+    __device__ inline void operator()(int64_t m, int n, int, float v[8]) const
+    {
+        const int count = N - n;
+        float g[8], u[8], dg[8], hh[8];
+        load8(pre + m * ldp + n, count, wide_p, g);
+        load8(pre + m * ldp + N + n, count, wide_p, u);
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            float a, d;
+            act_both(act, g[i], a, d);
+            dg[i] = v[i] * u[i] * d;
+            hh[i] = a * u[i];
+            v[i] *= a;
+        }
+        store8(dp + m * ldd + n, count, wide_d, dg);
+        store8(dp + m * ldd + N + n, count, wide_d, v);
+        store8(h + m * ldh + n, count, wide_h, hh);
+    }
+};
+
+// ---- groups ----
+// rows of group g, inside 0 .. total whatever the offsets hold
+__device__ inline void group_range(const int32_t *offsets, int g, int total, int &lo, int &hi)
+{
+    lo = min(max(offsets[g], 0), total);
+    hi = min(max(offsets[g + 1], lo), total);
+}
+
+// the group and first row of tile t of BM rows; false past the last tile.
+// All lanes of a wavefront call it; 64 groups are summed at a time.
+__device__ inline bool find_tile(const int32_t *offsets, int groups, int total, int bm, int t, int &g, int &row, int &end)
+{
+    const int lane = threadIdx.x & 63;
+    int before = 0;
+    for (int g0 = 0; g0 < groups; g0 += 64) {
+        int lo = 0, hi = 0;
+        if (g0 + lane < groups) group_range(offsets, g0 + lane, total, lo, hi);
+        const int mine = (hi - lo + bm - 1) / bm;
+        int sum = mine;
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) {
+            const int o = __shfl_up(sum, d);
+            if (lane >= d) sum += o;
+        }
+        const uint64_t past = __ballot(before + sum > t);
+        if (past) {
+            const int l = __builtin_ctzll(past);
+            g = g0 + l;
+            const int first = before + __shfl(sum - mine, l);
+            row = __shfl(lo, l) + (t - first) * bm;
+            end = __shfl(hi, l);
+            g = __builtin_amdgcn_readfirstlane(g);
+            row = __builtin_amdgcn_readfirstlane(row);
+            end = __builtin_amdgcn_readfirstlane(end);
+            return true;
+        }
+        before += __shfl(sum, 63);
+    }
+    return false;
+}
+
+// ---- tile loads ----
+typedef __attribute__((address_space(3))) void *lds_ptr;
+
+__device__ inline __amdgpu_buffer_rsrc_t resource(const char *base, int64_t bytes)
+{
+    // whole 4-byte words: the word of the last value never crosses a page
+    const int64_t n = bytes <= 0 ? 0 : (bytes + 3) & ~int64_t(3);
+    return __builtin_amdgcn_make_buffer_rsrc((void *)base, 0, (int)(uint32_t)(n > 0xFFFFFFFCll ? 0xFFFFFFFCll : n), 0x00020000);
+}
+
+// columns tiles: the exchange of a row's 32-byte pieces
+template <int ROWS> __device__ inline int swz(int k) { return ((k & 3) | ((k >> 3 & 1) << 2)) & (ROWS / 16 - 1); }
+
+// One operand's tile of ROWS x 64, loaded by NW wavefronts. COLS: the operand
+// is "columns". PAIR: 16-row blocks alternate between gate and up rows.
+template <int ROWS, int NW, bool COLS, bool PAIR> struct Loader {
+    static constexpr int kLoads = ROWS * 8 / (NW * 64);   // 16-byte pieces of a lane
+    static constexpr int kBytes = ROWS * kBK * 2;
+    int voff[kLoads];
+    __device__ inline void init(int64_t ld, int wave)
+    {
+        const int lane = threadIdx.x & 63;
+#pragma unroll
+        for (int i = 0; i < kLoads; i++) {
+            const int c = (i * NW + wave) * 64 + lane;
+            if (COLS) {
+                const int k = c / (ROWS / 8), pos = c % (ROWS / 8);
+                voff[i] = (int)(k * ld * 2) + (pos ^ (swz<ROWS>(k) << 1)) * 16;
+            } else {
+                const int r = c / 8, pos = c % 8;
+                const int src = PAIR ? (r / 32) * 16 + r % 16 : r;
+                voff[i] = (int)(src * ld * 2) + (pos ^ (r & 7)) * 16;
+            }
+        }
+    }
+    // base: the tile's first value; bytes: from there to the operand's end;
+    // up: from a gate row to its up row, in bytes
+    __device__ inline void load(const char *base, int64_t bytes, int64_t up, char *lds, int wave) const
+    {
+        const __amdgpu_buffer_rsrc_t r = resource(base, bytes);
+        const __amdgpu_buffer_rsrc_t ru = PAIR ? resource(base + up, bytes - up) : r;
+#pragma unroll
+        for (int i = 0; i < kLoads; i++) {
+            const int piece = i * NW + wave;              // 1024 bytes, 8 rows of a rows tile
+            lds_ptr to = (lds_ptr)(lds + piece * 1024);
+            if (PAIR && (piece / 2) % 2)
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(ru, to, 16, voff[i], 0, 0, 0);
+            else
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(r, to, 16, voff[i], 0, 0, 0);
+        }
+    }
+    // a rows tile's values with k >= valid hold the next row's: make them zero
+    __device__ static inline void clear_tail(char *lds, int valid)
+    {
+        for (int c = threadIdx.x; c < ROWS * kBK; c += NW * 64) {
+            const int r = c / kBK, k = c % kBK;
+            if (k >= valid) *(short *)(lds + r * 128 + (((k / 8) ^ (r & 7)) * 16) + (k % 8) * 2) = 0;
+        }
+    }
+};
+
+// fragment of 16 rows (block `rb` of the tile), k-step s, for one lane
+template <int ROWS, bool COLS, typename T>
+__device__ inline typename pack8<T>::type fragment(const char *lds, int rb, int s)
+{
+    const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
+    if (COLS) {
+        const int q = i >> 2, f = swz<ROWS>(g * 8 + q);
+        const char *p = lds + (s * 32 + g * 8 + q) * (ROWS * 2) + ((rb ^ f) << 5) + (i & 3) * 8;
+        typedef __attribute__((address_space(3))) s16x4 *rd;
+        const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((rd)p);
+        const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((rd)(p + 4 * ROWS * 2));
+        const s16x8 z = __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+        return __builtin_bit_cast(typename pack8<T>::type, z);
+    }
+    return *(const typename pack8<T>::type *)(lds + (rb * 16 + i) * 128 + (((s * 4 + g) ^ (i & 7)) << 4));
+}
+
+// Workgroup order: consecutive workgroups go to the 8 XCDs in turn, so each
+// XCD is given a contiguous range of tiles, walked 8 row-tiles wide, and its
+// L2 holds the operands that neighbouring tiles share.
+__device__ inline int xcd_order(int id, int total)
+{
+    const int per = total / 8, extra = total % 8, x = id % 8;
+    return x * per + min(x, extra) + id / 8;
+}
+__device__ inline void tile_of(int t, int tiles_m, int tiles_n, int &tm, int &tn)
+{
+    constexpr int kWide = 8;
+    const int band = t / (kWide * tiles_n), first = band * kWide, width = min(kWide, tiles_m - first);
+    const int in = t - band * kWide * tiles_n;
+    tm = first + in % width;
+    tn = in / width;
+}
+
+template <int BM, int BN, int WM, int WN, bool ACOL, bool BCOL, Grouping GR, typename T, typename Epi>
+__global__ void __launch_bounds__(WM * WN * 64) gemm_kernel(Args x, Epi epi)
+{
+#ifdef __HIP_DEVICE_COMPILE__   // the host pass has no buffer resources
+    constexpr int NW = WM * WN, TM = BM / WM / 16, TN = BN / WN / 16, kOut = BN / WN;
+    constexpr bool PAIR = Epi::gated;
+    typedef Loader<BM, NW, ACOL, false> LA;
+    typedef Loader<BN, NW, BCOL, PAIR> LB;
+    constexpr int kStage = LA::kBytes + LB::kBytes;
+    static_assert(TM % 4 == 0 && (!PAIR || TN % 2 == 0), "a wavefront's part");
+    static_assert(NW * 64 * kOut * 4 <= 2 * kStage, "the epilogue's part of LDS");
+    __shared__ __align__(1024) char smem[2 * kStage];
+
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int per = x.tiles_m * x.tiles_n;
+    int t = xcd_order(blockIdx.x, gridDim.x);
+    const int outer = t / per;                              // split, or group of kGroupSum
+    t -= outer * per;
+    int tm, tn;
+    tile_of(t, x.tiles_m, x.tiles_n, tm, tn);
+
+    int g = 0, m0 = tm * BM, m_end = x.M, k_lo = 0, k_hi = x.K;
+    if (GR == kGroupRows && x.offsets && !find_tile(x.offsets, x.groups, x.M, BM, tm, g, m0, m_end)) return;
+    const bool grouped_sum = GR == kGroupSum && x.offsets;
+    if (grouped_sum) {
+        g = __builtin_amdgcn_readfirstlane(outer);
+        group_range(x.offsets, g, x.K, k_lo, k_hi);
+    }
+    const int split = grouped_sum ? 0 : outer;              // a grouped product is not split
+    const int k_first = k_lo + split * x.split_tiles * kBK;
+    const int k_last = grouped_sum ? k_hi : min(k_hi, k_first + x.split_tiles * kBK);
+    const int tiles = k_last > k_first ? (k_last - k_first + kBK - 1) / kBK : 0;
+    const int n0 = PAIR ? tn * (BN / 2) : tn * BN;          // PAIR: first gate row
+
+    // the tiles' first values, and the bytes from there to the operand's end
+    const int64_t eb = 2;
+    const char *pa = (const char *)x.a, *pb = (const char *)x.b + (GR == kGroupRows ? g * x.stride_b * eb : 0);
+    int64_t na, nb;
+    if (ACOL) {
+        pa += ((int64_t)k_first * x.lda + m0) * eb;
+        na = ((int64_t)(k_hi - k_first - 1) * x.lda + (x.M - m0)) * eb;
+    } else {
+        pa += ((int64_t)m0 * x.lda + k_first) * eb;
+        na = ((int64_t)(m_end - m0 - 1) * x.lda + (k_hi - k_first)) * eb;
+    }
+    const int brows = PAIR ? x.F + x.N : x.N;
+    if (BCOL) {
+        pb += ((int64_t)k_first * x.ldb + n0) * eb;
+        nb = ((int64_t)(k_hi - k_first - 1) * x.ldb + (x.N - n0)) * eb;
+    } else {
+        pb += ((int64_t)n0 * x.ldb + k_first) * eb;
+        nb = ((int64_t)(brows - n0 - 1) * x.ldb + (k_hi - k_first)) * eb;
+    }
+    const int64_t step_a = (ACOL ? x.lda * kBK : kBK) * eb, step_b = (BCOL ? x.ldb * kBK : kBK) * eb;
+    const int64_t up = PAIR ? (int64_t)x.F * x.ldb * eb : 0;
+
+    LA la;
+    LB lb;
+    la.init(x.lda, wave);
+    lb.init(x.ldb, wave);
+    const int wm = wave / WN, wn = wave % WN;
+
+    f32x4 acc[TM][TN];
+#pragma unroll
+    for (int i = 0; i < TM; i++)
+#pragma unroll
+        for (int j = 0; j < TN; j++) acc[i][j] = f32x4{0, 0, 0, 0};
+
+    if (tiles) {
+        la.load(pa, na, 0, smem, wave);
+        lb.load(pb, nb, up, smem + LA::kBytes, wave);
+    }
+    for (int kt = 0; kt < tiles; kt++) {
+        char *cur = smem + (kt & 1) * kStage, *nxt = smem + (~kt & 1) * kStage;
+        __builtin_amdgcn_s_waitcnt(0);
+        __syncthreads();
+        if (kt + 1 < tiles) {
+            pa += step_a, na -= step_a, pb += step_b, nb -= step_b;
+            la.load(pa, na, 0, nxt, wave);
+            lb.load(pb, nb, up, nxt + LA::kBytes, wave);
+        } else if ((!ACOL || !BCOL) && (k_last - k_first) % kBK && k_last == k_hi) {
+            const int valid = (k_last - k_first) % kBK;
+            if (!ACOL) LA::clear_tail(cur, valid);
+            if (!BCOL) LB::clear_tail(cur + LA::kBytes, valid);
+            __syncthreads();
+        }
+#pragma unroll
+        for (int s = 0; s < kBK / 32; s++) {
+            typename pack8<T>::type fa[TM], fb[TN];
+#pragma unroll
+            for (int i = 0; i < TM; i++) fa[i] = fragment<BM, ACOL, T>(cur, wm * TM + i, s);
+#pragma unroll
+            for (int j = 0; j < TN; j++) fb[j] = fragment<BN, BCOL, T>(cur + LA::kBytes, wn * TN + j, s);
+#pragma unroll
+            for (int i = 0; i < TM; i++)
+#pragma unroll
+                for (int j = 0; j < TN; j++) acc[i][j] = mfma(fb[j], fa[i], acc[i][j]);
+        }
+    }
+    __syncthreads();
+
+    // Epilogue: a wavefront takes 64 of its rows at a time through its own part
+    // of LDS, so that a lane finishes eight neighbouring columns. The product
+    // was formed transposed: a lane holds row lane % 16, columns 4 (lane / 16)
+    // .. + 3 of a block. 16-byte pieces of a row are exchanged by row & (pieces - 1).
+    constexpr int kPieces = kOut / 4;
+    float *own = (float *)smem + wave * 64 * kOut;
+    const int nw = n0 + (PAIR ? wn * kOut / 2 : wn * kOut);
+#pragma unroll
+    for (int h = 0; h < TM / 4; h++) {
+#pragma unroll
+        for (int i = 0; i < 4; i++)
+#pragma unroll
+            for (int j = 0; j < TN; j++) {
+                const int r = i * 16 + (lane & 15), p = j * 4 + (lane >> 4);
+                *(f32x4 *)(own + r * kOut + ((p ^ (r & (kPieces - 1))) << 2)) = acc[h * 4 + i][j];
+            }
+        __builtin_amdgcn_wave_barrier();
+        constexpr int kUnits = (PAIR ? kOut / 2 : kOut) / 8;    // eights of a row
+#pragma unroll 1
+        for (int c = lane; c < 64 * kUnits; c += 64) {
+            const int r = c / kUnits, q = c % kUnits;
+            const int m = m0 + wm * (TM * 16) + h * 64 + r;
+            const int n = nw + q * 8;
+            auto piece = [&](int p) { return *(const f32x4 *)(own + r * kOut + ((p ^ (r & (kPieces - 1))) << 2)); };
+            // PAIR: gate columns 16 b .. + 15 are pieces 8 b .. + 3, the up columns the four after
+            const int p0 = PAIR ? (q / 2) * 8 + (q % 2) * 2 : q * 2;
+            const f32x4 v0 = piece(p0), v1 = piece(p0 + 1);
+            float v[8] = {v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
+            if (m >= m_end || n >= x.N) continue;
+            if constexpr (PAIR) {
+                const f32x4 u0 = piece(p0 + 4), u1 = piece(p0 + 5);
+                float u[8] = {u0[0], u0[1], u0[2], u0[3], u1[0], u1[1], u1[2], u1[3]};
+                if (x.splits > 1) {
+                    float *to = x.partial + ((int64_t)split * x.M + m) * partial_cols(x.N, true) + n;
+                    float *tu = to + partial_cols(x.N, false);
+                    *(f32x4 *)to = v0, *(f32x4 *)(to + 4) = v1, *(f32x4 *)tu = u0, *(f32x4 *)(tu + 4) = u1;
+                } else {
+                    epi(m, n, g, v, u);
+                }
+            } else {
+                if (x.splits > 1) {
+                    float *to = x.partial + ((int64_t)split * x.M + m) * partial_cols(x.N, false) + n;
+                    *(f32x4 *)to = v0, *(f32x4 *)(to + 4) = v1;
+                } else {
+                    epi(m, n, g, v);
+                }
+            }
+        }
+        __builtin_amdgcn_wave_barrier();
+    }
+#endif
+}
+
+// Joins the parts of a split reduction, in their order, and finishes them.
+template <typename Epi> __global__ void __launch_bounds__(256) join_kernel(Args x, Epi epi)
+{
+    const int eights = (x.N + 7) / 8;
+    const int64_t total = (int64_t)x.M * eights, cols = partial_cols(x.N, Epi::gated);
+    for (int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x; c < total; c += (int64_t)gridDim.x * 256) {
+        const int m = (int)(c / eights), n = (int)(c - (int64_t)m * eights) * 8;
+        f32x4 v0 = {0, 0, 0, 0}, v1 = v0, u0 = v0, u1 = v0;
+        for (int s = 0; s < x.splits; s++) {
+            const float *from = x.partial + ((int64_t)s * x.M + m) * cols + n;
+            v0 += *(const f32x4 *)from, v1 += *(const f32x4 *)(from + 4);
+            if (Epi::gated) from += cols / 2, u0 += *(const f32x4 *)from, u1 += *(const f32x4 *)(from + 4);
+        }
+        float v[8] = {v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
+        if constexpr (Epi::gated) {
+            float u[8] = {u0[0], u0[1], u0[2], u0[3], u1[0], u1[1], u1[2], u1[3]};
+            epi(m, n, 0, v, u);
+        } else {
+            epi(m, n, 0, v);
+        }
+    }
+}
+
+// ---- host side ----
+// A tile shape and the parts of the reduction.
+struct Shape { int cfg, splits, split_tiles; };
+Shape shape_of(int64_t M, int64_t N, int64_t K, int groups, bool gated, bool sum);
+inline size_t partial_bytes(const Shape &s, int64_t M, int64_t N, bool gated)
+{
+    return s.splits > 1 ? (size_t)s.splits * M * partial_cols((int)N, gated) * 4 : 0;
+}
+
+template <int BM, int BN, int WM, int WN, bool ACOL, bool BCOL, Grouping GR, typename T, typename Epi>
+inline int launch_cfg(Args x, const Shape &s, const Epi &epi, hipStream_t stream)
+{
+    const int64_t cols = Epi::gated ? 2 * (int64_t)x.N : x.N;
+    const bool grouped = x.offsets != nullptr;
+    x.tiles_m = (int)((x.M + BM - 1) / BM) + (GR == kGroupRows && grouped ? x.groups : 0);
+    x.tiles_n = (int)((cols + BN - 1) / BN);
+    x.splits = s.splits;
+    x.split_tiles = s.split_tiles;
+    const int64_t blocks = (int64_t)x.tiles_m * x.tiles_n * (GR == kGroupSum && grouped ? x.groups : s.splits);
+    if (blocks > 0x7FFFFFFF) return fail(HEDDLE_E_RANGE, "more tiles than a launch holds");
+    hipLaunchKernelGGL((gemm_kernel<BM, BN, WM, WN, ACOL, BCOL, GR, T, Epi>), dim3((unsigned)blocks), dim3(WM * WN * 64), 0,
+                       stream, x, epi);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return hip_fail(e, "gemm_kernel");
+    if (s.splits > 1) {
+        const int64_t want = ((int64_t)x.M * ((x.N + 7) / 8) + 255) / 256;
+        hipLaunchKernelGGL((join_kernel<Epi>), dim3((unsigned)(want < 4096 ? want : 4096)), dim3(256), 0, stream, x, epi);
+        e = hipGetLastError();
+        if (e != hipSuccess) return hip_fail(e, "join_kernel");
+    }
+    return HEDDLE_OK;
+}
+
+template <bool ACOL, bool BCOL, Grouping GR, typename T, typename Epi>
+inline int launch_gemm(const Args &x, const Shape &s, const Epi &epi, hipStream_t stream)
+{
+    switch (s.cfg) {
+    case 0: return launch_cfg<256, 256, 2, 4, ACOL, BCOL, GR, T>(x, s, epi, stream);
+    case 1: return launch_cfg<128, 128, 2, 2, ACOL, BCOL, GR, T>(x, s, epi, stream);
+    default: return launch_cfg<64, 128, 1, 4, ACOL, BCOL, GR, T>(x, s, epi, stream);
+    }
+}
+
+}  // namespace mm
+}  // namespace heddle

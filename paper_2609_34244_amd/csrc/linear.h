@@ -1,0 +1,81 @@
+// Internal host side of the feed-forward operators: operands as the products
+// want them, scratch layout, and the launches the entry points are made of.
+#pragma once
+
+#include "gemm.h"
+
+namespace heddle {
+namespace mm {
+
+constexpr int64_t kMaxRows = 0x7FFFFFFF - 512;
+
+inline int64_t up8(int64_t n) { return (n + 7) & ~int64_t(7); }
+
+// Caller's scratch, handed out in 256-byte steps. With base NULL it only measures.
+struct Scratch {
+    char *base;
+    size_t used;
+    void *take(size_t bytes)
+    {
+        void *p = base ? base + used : nullptr;
+        used += (bytes + 255) & ~size_t(255);
+        return p;
+    }
+};
+
+// An operand of a product: rows of ld elements, groups stride apart.
+struct Operand { const void *p; int64_t ld, stride; };
+
+// Rows that do not start on 4-byte boundaries are copied to scratch, in
+// rows of whole 16 bytes: one pass over the operand at memory speed, against
+// products whose loads would otherwise be single values.
+inline bool needs_copy(const Operand &o, int groups)
+{
+    return ((uintptr_t)o.p & 3) || (o.ld & 1) || (groups > 1 && (o.stride & 1));
+}
+int copy_rows(Operand &o, int64_t rows, int64_t cols, int groups, Scratch &s, bool run, hipStream_t stream);
+
+// dZ = dY act'(Z) (written where dz is given) and its column sums per group
+struct BiasGrad {
+    const void *dy, *pre;
+    int64_t lddy, ldp, lddz;
+    void *dz, *db;
+    const int32_t *offsets;
+    int32_t groups, act, m, n;
+    int32_t chunks, chunk_rows;               // parts of the rows (1 with offsets)
+    float *partial;                           // [chunks][groups][n]
+};
+int64_t bias_grad_bytes(int64_t m, int64_t n, bool grouped, int groups);
+int launch_bias_grad(int dtype, BiasGrad b, hipStream_t stream);
+
+int check_matrix(const char *name, const void *p, int64_t ld, int64_t cols);
+
+// C = A B^T of plain row-major outputs with EpiLinear; sum: C = A^T B over rows
+template <typename T>
+int product(bool cols_b, const Operand &a, const Operand &b, int64_t m, int64_t n, int64_t k, int groups,
+            const int32_t *offsets, EpiLinear<T> epi, Scratch &s, bool run, hipStream_t stream);
+template <typename T>
+int product_sum(const Operand &a, const Operand &b, int64_t m, int64_t n, int64_t k, int groups, const int32_t *offsets,
+                EpiLinear<T> epi, Scratch &s, bool run, hipStream_t stream);
+
+template <typename T> inline EpiLinear<T> plain_output(void *y, int64_t ld, int64_t n, int64_t stride = 0)
+{
+    EpiLinear<T> e = {};
+    e.y = (T *)y;
+    e.ldy = ld;
+    e.stride_y = stride;
+    e.N = (int32_t)n;
+    e.wide_y = width_of(y, ld, stride);
+    return e;
+}
+
+inline int check_scratch(size_t need, const void *ws, int64_t bytes)
+{
+    if (need == 0) return HEDDLE_OK;
+    if (!ws || bytes < 0 || (size_t)bytes < need) return fail(HEDDLE_E_INVAL, "workspace smaller than the call needs");
+    if ((uintptr_t)ws & 255) return fail(HEDDLE_E_INVAL, "workspace is not 256-byte aligned");
+    return HEDDLE_OK;
+}
+
+}  // namespace mm
+}  // namespace heddle

@@ -1,0 +1,341 @@
+// Y = act(X W^T + b) + R and its gradients on gfx950's matrix cores.
+//
+// Forward: 2 m n k flops over m k + n k + m n values, one launch: bias,
+// activation and residual are applied to the sums before they are rounded.
+// Backward: dZ = dY act'(Z) is formed once, in the pass that sums db (without
+// an activation dZ is dY itself), then dX = dZ W and dW = dZ^T X.
+#include "linear.h"
+
+namespace heddle {
+namespace mm {
+
+Shape shape_of(int64_t M, int64_t N, int64_t K, int groups, bool gated, bool sum)
+{
+    const int bm[3] = {256, 128, 64}, bn[3] = {256, 128, 128}, per_cu[3] = {1, 2, 3};
+    const int64_t cols = gated ? 2 * N : N;
+    Shape best = {0, 1, 1};
+    double least = 0;
+    const int64_t kt = (K + kBK - 1) / kBK > 0 ? (K + kBK - 1) / kBK : 1;
+    for (int c = 0; c < 3; c++) {
+        const bool rows_grouped = groups > 1 && !sum;
+        // a group's rows end inside a tile: half a tile is lost on average
+        const int64_t tm = (M + bm[c] - 1) / bm[c] + (rows_grouped ? groups : 0), tn = (cols + bn[c] - 1) / bn[c];
+        const int64_t tiles = tm * tn * (groups > 1 && sum ? groups : 1);
+        const int64_t steps = groups > 1 && sum ? (kt + groups - 1) / groups : kt;
+        const int max_split = groups > 1 ? 1 : (int)(kt < 16 ? kt : 16);
+        for (int s = 1; s <= max_split; s *= 2) {
+            const int64_t part = (steps + s - 1) / s;
+            const double rounds = (double)((tiles * s + 256 * per_cu[c] - 1) / (256 * per_cu[c]));
+            // time of a k-tile in one workgroup, all of a CU's slots taken
+            const double step = bm[c] * bn[c] * per_cu[c] / (c == 0 ? 1.0 : c == 1 ? 0.75 : 0.6);
+            const double t = rounds * (part * step + 3e5) + (s > 1 ? 2e6 + 1.5 * s * M * cols / 256 : 0);
+            if (least == 0 || t < least) {
+                least = t;
+                best = {c, s, (int)((kt + s - 1) / s)};
+            }
+        }
+    }
+    return best;
+}
+
+int check_matrix(const char *name, const void *p, int64_t ld, int64_t cols)
+{
+    if (!p) return fail(HEDDLE_E_INVAL, std::string(name) + " is NULL");
+    if ((uintptr_t)p & 1) return fail(HEDDLE_E_INVAL, std::string(name) + " is not aligned to its values");
+    if (ld < cols || ld > HEDDLE_MAX_LD) return fail(HEDDLE_E_INVAL, std::string(name) + ": ld out of range");
+    return HEDDLE_OK;
+}
+
+__global__ void __launch_bounds__(256) copy_rows_kernel(const uint16_t *src, int64_t ld, int64_t stride, int64_t rows,
+                                                        int64_t cols, uint16_t *dst, int64_t ldd, int64_t all)
+{
+    const int64_t eights = ldd / 8;
+    for (int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x; c < all * eights; c += (int64_t)gridDim.x * 256) {
+        const int64_t r = c / eights, j = (c - r * eights) * 8, g = r / rows;
+        const uint16_t *from = src + g * stride + (r - g * rows) * ld + j;
+        s16x8 v;
+#pragma unroll
+        for (int i = 0; i < 8; i++) v[i] = j + i < cols ? (short)from[i] : (short)0;
+        *(s16x8 *)(dst + r * ldd + j) = v;
+    }
+}
+
+int copy_rows(Operand &o, int64_t rows, int64_t cols, int groups, Scratch &s, bool run, hipStream_t stream)
+{
+    if (!needs_copy(o, groups)) return HEDDLE_OK;
+    const int64_t ldd = up8(cols), all = rows * groups;
+    uint16_t *to = (uint16_t *)s.take((size_t)all * ldd * 2);
+    if (run && all > 0) {
+        const int64_t want = (all * (ldd / 8) + 255) / 256;
+        hipLaunchKernelGGL(copy_rows_kernel, dim3((unsigned)(want < 16384 ? want : 16384)), dim3(256), 0, stream,
+                           (const uint16_t *)o.p, o.ld, o.stride, rows, cols, to, ldd, all);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return hip_fail(e, "copy_rows_kernel");
+    }
+    o = {to, ldd, rows * ldd};
+    return HEDDLE_OK;
+}
+
+// A workgroup takes 256 columns (32 lanes of eight) and its chunk of rows, 8
+// rows at a time; its lanes' sums are joined in LDS in a fixed order.
+template <typename T> __global__ void __launch_bounds__(256) bias_grad_kernel(BiasGrad b, int wide_dy, int wide_p, int wide_z)
+{
+    __shared__ float part[8][256 + 8];
+    const int col = threadIdx.x & 31, row = threadIdx.x >> 5;
+    const int n = blockIdx.x * 256 + col * 8, count = b.n - n;
+    const int g = blockIdx.y / b.chunks, chunk = blockIdx.y - g * b.chunks;
+    int lo = 0, hi = b.m;
+    if (b.offsets) group_range(b.offsets, g, b.m, lo, hi);
+    const int first = lo + chunk * b.chunk_rows;
+    const int last = b.offsets ? hi : min(hi, first + b.chunk_rows);
+    float sum[8] = {};
+    if (count > 0)
+        for (int m = first + row; m < last; m += 8) {
+            float v[8];
+            load8((const T *)b.dy + m * b.lddy + n, count, wide_dy, v);
+            if (b.act) {
+                float z[8];
+                load8((const T *)b.pre + m * b.ldp + n, count, wide_p, z);
+#pragma unroll
+                for (int i = 0; i < 8; i++) {
+                    float a, d;
+                    act_both(b.act, z[i], a, d);
+                    v[i] *= d;
+                }
+            }
+            if (b.dz) store8((T *)b.dz + m * b.lddz + n, count, wide_z, v);
+#pragma unroll
+            for (int i = 0; i < 8; i++) sum[i] += v[i];
+        }
+    if (!b.db) return;
+#pragma unroll
+    for (int i = 0; i < 8; i++) part[row][col * 8 + i] = sum[i];
+    __syncthreads();
+    const int c = blockIdx.x * 256 + threadIdx.x;
+    if (c >= b.n) return;
+    float v = 0;
+#pragma unroll
+    for (int r = 0; r < 8; r++) v += part[r][threadIdx.x];
+    if (b.chunks > 1) b.partial[(int64_t)chunk * b.n + c] = v;
+    else ((T *)b.db)[(int64_t)g * b.n + c] = (T)v;
+}
+
+template <typename T> __global__ void __launch_bounds__(256) bias_join_kernel(BiasGrad b)
+{
+    const int c = blockIdx.x * 256 + threadIdx.x;
+    if (c >= b.n) return;
+    float v = 0;
+    for (int i = 0; i < b.chunks; i++) v += b.partial[(int64_t)i * b.n + c];
+    ((T *)b.db)[c] = (T)v;
+}
+
+// enough chunks of rows to fill the chip, at least 16 rows in each
+static void bias_chunks(int64_t m, int64_t n, bool grouped, int &chunks, int &rows)
+{
+    const int64_t blocks = (n + 255) / 256, want = grouped ? 1 : (2048 + blocks - 1) / blocks, most = (m + 15) / 16;
+    chunks = (int)(want < most ? want : most);
+    if (chunks < 1) chunks = 1;
+    rows = (int)((m + chunks - 1) / chunks);
+}
+
+int64_t bias_grad_bytes(int64_t m, int64_t n, bool grouped, int)
+{
+    int chunks, rows;
+    bias_chunks(m, n, grouped, chunks, rows);
+    return chunks > 1 ? (int64_t)chunks * n * 4 : 0;
+}
+
+template <typename T> static int run_bias_grad(BiasGrad b, hipStream_t stream)
+{
+    bias_chunks(b.m, b.n, b.offsets != nullptr, b.chunks, b.chunk_rows);
+    const int groups = b.offsets ? b.groups : 1;
+    const dim3 grid((unsigned)((b.n + 255) / 256), (unsigned)(groups * b.chunks));
+    hipLaunchKernelGGL((bias_grad_kernel<T>), grid, dim3(256), 0, stream, b, (int)width_of(b.dy, b.lddy),
+                       (int)width_of(b.pre, b.ldp), (int)width_of(b.dz, b.lddz));
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return hip_fail(e, "bias_grad_kernel");
+    if (b.db && b.chunks > 1) {
+        hipLaunchKernelGGL((bias_join_kernel<T>), dim3((unsigned)((b.n + 255) / 256)), dim3(256), 0, stream, b);
+        e = hipGetLastError();
+        if (e != hipSuccess) return hip_fail(e, "bias_join_kernel");
+    }
+    return HEDDLE_OK;
+}
+
+int launch_bias_grad(int dtype, BiasGrad b, hipStream_t stream)
+{
+    return dtype == HEDDLE_T_BF16 ? run_bias_grad<__bf16>(b, stream) : run_bias_grad<_Float16>(b, stream);
+}
+
+template <typename T>
+int product(bool cols_b, const Operand &a, const Operand &b, int64_t m, int64_t n, int64_t k, int groups,
+            const int32_t *offsets, EpiLinear<T> epi, Scratch &s, bool run, hipStream_t stream)
+{
+    const Shape sh = shape_of(m, n, k, offsets ? groups : 1, false, false);
+    Args x = {};
+    x.partial = (float *)s.take(partial_bytes(sh, m, n, false));
+    if (!run || m == 0) return HEDDLE_OK;
+    x.a = a.p, x.lda = a.ld;
+    x.b = b.p, x.ldb = b.ld, x.stride_b = b.stride;
+    x.M = (int)m, x.N = (int)n, x.K = (int)k;
+    x.offsets = offsets;
+    x.groups = offsets ? groups : 1;
+    return cols_b ? launch_gemm<false, true, kGroupRows, T>(x, sh, epi, stream)
+                  : launch_gemm<false, false, kGroupRows, T>(x, sh, epi, stream);
+}
+
+template <typename T>
+int product_sum(const Operand &a, const Operand &b, int64_t m, int64_t n, int64_t k, int groups, const int32_t *offsets,
+                EpiLinear<T> epi, Scratch &s, bool run, hipStream_t stream)
+{
+    const Shape sh = shape_of(m, n, k, offsets ? groups : 1, false, true);
+    Args x = {};
+    x.partial = (float *)s.take(partial_bytes(sh, m, n, false));
+    if (!run) return HEDDLE_OK;
+    x.a = a.p, x.lda = a.ld;
+    x.b = b.p, x.ldb = b.ld;
+    x.M = (int)m, x.N = (int)n, x.K = (int)k;
+    x.offsets = offsets;
+    x.groups = offsets ? groups : 1;
+    return launch_gemm<true, true, kGroupSum, T>(x, sh, epi, stream);
+}
+
+#define HEDDLE_PRODUCTS(T)                                                                                             \
+    template int product<T>(bool, const Operand &, const Operand &, int64_t, int64_t, int64_t, int, const int32_t *,   \
+                            EpiLinear<T>, Scratch &, bool, hipStream_t);                                               \
+    template int product_sum<T>(const Operand &, const Operand &, int64_t, int64_t, int64_t, int, const int32_t *,     \
+                                EpiLinear<T>, Scratch &, bool, hipStream_t);
+HEDDLE_PRODUCTS(__bf16)
+HEDDLE_PRODUCTS(_Float16)
+
+static int check_linear(const heddle_linear_desc *d, bool backward)
+{
+    if (!d) return fail(HEDDLE_E_INVAL, "descriptor is NULL");
+    if (d->dtype != HEDDLE_T_BF16 && d->dtype != HEDDLE_T_F16) return fail(HEDDLE_E_INVAL, "dtype is neither BF16 nor F16");
+    if (d->act < HEDDLE_A_NONE || d->act > HEDDLE_A_SILU) return fail(HEDDLE_E_INVAL, "unknown activation");
+    if (d->m < 0 || d->n < 1 || d->k < 1 || d->m > kMaxRows || d->n > HEDDLE_MAX_LD || d->k > HEDDLE_MAX_LD)
+        return fail(HEDDLE_E_INVAL, "m, n or k out of range");
+    if (d->d_offsets && (d->groups < 1 || d->groups > HEDDLE_MAX_GROUPS)) return fail(HEDDLE_E_INVAL, "groups out of range");
+    if (((uintptr_t)d->d_offsets & 3)) return fail(HEDDLE_E_INVAL, "d_offsets is misaligned");
+    const bool grouped = d->d_offsets != nullptr;
+    int rc = HEDDLE_OK;
+    auto matrix = [&](const char *name, const void *p, int64_t ld, int64_t cols) {
+        if (rc == HEDDLE_OK && d->m > 0) rc = check_matrix(name, p, ld, cols);
+    };
+    auto weights = [&](const char *name, const void *p, int64_t ld, int64_t stride) {
+        if (rc == HEDDLE_OK) rc = check_matrix(name, p, ld, d->k);
+        if (rc == HEDDLE_OK && grouped && d->groups > 1 && stride < (d->n - 1) * ld + d->k)
+            rc = fail(HEDDLE_E_INVAL, std::string(name) + ": the groups overlap");
+    };
+    if (!backward) {
+        matrix("x", d->x, d->ldx, d->k);
+        weights("w", d->w, d->ldw, d->stride_w);
+        if (d->residual) matrix("residual", d->residual, d->ldr, d->n);
+        if (d->preact) matrix("preact", d->preact, d->ldp, d->n);
+        matrix("y", d->y, d->ldy, d->n);
+        if (rc == HEDDLE_OK && ((uintptr_t)d->bias & 1)) rc = fail(HEDDLE_E_INVAL, "bias is not aligned to its values");
+    } else {
+        matrix("dy", d->dy, d->lddy, d->n);
+        if (d->act != HEDDLE_A_NONE) matrix("preact", d->preact, d->ldp, d->n);
+        if (d->dx) {
+            weights("w", d->w, d->ldw, d->stride_w);
+            matrix("dx", d->dx, d->lddx, d->k);
+        }
+        if (d->dw) {
+            matrix("x", d->x, d->ldx, d->k);
+            weights("dw", d->dw, d->lddw, d->stride_dw);
+        }
+        if (rc == HEDDLE_OK && ((uintptr_t)d->db & 1)) rc = fail(HEDDLE_E_INVAL, "db is not aligned to its values");
+    }
+    return rc;
+}
+
+template <typename T> static int forward(const heddle_linear_desc *d, Scratch &s, bool run, hipStream_t stream)
+{
+    const int groups = d->d_offsets ? d->groups : 1;
+    Operand x = {d->x, d->ldx, 0}, w = {d->w, d->ldw, d->stride_w};
+    int rc = copy_rows(x, d->m, d->k, 1, s, run, stream);
+    if (rc == HEDDLE_OK && d->m > 0) rc = copy_rows(w, d->n, d->k, groups, s, run, stream);
+    if (rc) return rc;
+    EpiLinear<T> e = plain_output<T>(d->y, d->ldy, d->n);
+    e.pre = (T *)d->preact, e.ldp = d->ldp, e.wide_p = width_of(d->preact, d->ldp);
+    e.bias = (const T *)d->bias, e.wide_b = width_of(d->bias, groups > 1 ? d->n : 0);
+    e.residual = (const T *)d->residual, e.ldr = d->ldr, e.wide_r = width_of(d->residual, d->ldr);
+    e.act = d->act;
+    return product<T>(false, x, w, d->m, d->n, d->k, groups, d->d_offsets, e, s, run, stream);
+}
+
+template <typename T> static int backward(const heddle_linear_desc *d, Scratch &s, bool run, hipStream_t stream)
+{
+    const int groups = d->d_offsets ? d->groups : 1;
+    int rc = HEDDLE_OK;
+    Operand dz = {d->dy, d->lddy, 0};
+    const bool act = d->act != HEDDLE_A_NONE, products = d->dx || d->dw;
+    BiasGrad b = {};
+    b.dy = d->dy, b.lddy = d->lddy, b.pre = d->preact, b.ldp = d->ldp, b.db = d->db, b.act = d->act;
+    b.m = (int)d->m, b.n = (int)d->n, b.offsets = d->d_offsets, b.groups = groups;
+    if (products && (act || needs_copy(dz, 1))) {
+        // dZ, or dY in rows that the products can read
+        b.lddz = up8(d->n);
+        b.dz = s.take((size_t)d->m * b.lddz * 2);
+        dz = {b.dz, b.lddz, 0};
+    }
+    if (b.db) b.partial = (float *)s.take(bias_grad_bytes(d->m, d->n, d->d_offsets != nullptr, groups));
+    if (run && (b.db || (b.dz && d->m > 0))) rc = launch_bias_grad(d->dtype, b, stream);
+    if (rc == HEDDLE_OK && d->dx) {
+        Operand w = {d->w, d->ldw, d->stride_w};
+        if (d->m > 0) rc = copy_rows(w, d->n, d->k, groups, s, run, stream);
+        if (rc == HEDDLE_OK)
+            rc = product<T>(true, dz, w, d->m, d->k, d->n, groups, d->d_offsets, plain_output<T>(d->dx, d->lddx, d->k), s,
+                            run, stream);
+    }
+    if (rc == HEDDLE_OK && d->dw) {
+        Operand x = {d->x, d->ldx, 0};
+        rc = copy_rows(x, d->m, d->k, 1, s, run, stream);
+        if (rc == HEDDLE_OK)
+            rc = product_sum<T>(dz, x, d->n, d->k, d->m, groups, d->d_offsets,
+                                plain_output<T>(d->dw, d->lddw, d->k, groups > 1 ? d->stride_dw : 0), s, run, stream);
+    }
+    return rc;
+}
+
+static int linear(const heddle_linear_desc *d, bool back, void *ws, int64_t bytes, bool run, hipStream_t stream, int64_t *need)
+{
+    int rc = check_linear(d, back);
+    if (rc) return rc;
+    for (int pass = 0; pass < 2; pass++) {
+        Scratch s = {pass ? (char *)ws : nullptr, 0};
+        const bool go = pass == 1;
+        rc = d->dtype == HEDDLE_T_BF16 ? (back ? backward<__bf16>(d, s, go, stream) : forward<__bf16>(d, s, go, stream))
+                                       : (back ? backward<_Float16>(d, s, go, stream) : forward<_Float16>(d, s, go, stream));
+        if (rc) return rc;
+        if (pass == 0) {
+            if (need) *need = (int64_t)s.used;
+            if (!run) return HEDDLE_OK;
+            rc = check_scratch(s.used, ws, bytes);
+            if (rc) return rc;
+        }
+    }
+    return HEDDLE_OK;
+}
+
+}  // namespace mm
+}  // namespace heddle
+
+using namespace heddle;
+
+extern "C" int heddle_linear(const heddle_linear_desc *d, void *ws, int64_t bytes, hipStream_t stream)
+{
+    return mm::linear(d, false, ws, bytes, true, stream, nullptr);
+}
+
+extern "C" int heddle_linear_backward(const heddle_linear_desc *d, void *ws, int64_t bytes, hipStream_t stream)
+{
+    return mm::linear(d, true, ws, bytes, true, stream, nullptr);
+}
+
+extern "C" int heddle_linear_workspace(const heddle_linear_desc *d, int32_t backward, int64_t *h_bytes)
+{
+    if (!h_bytes) return fail(HEDDLE_E_INVAL, "h_bytes is NULL");
+    return mm::linear(d, backward != 0, nullptr, 0, false, nullptr, h_bytes);
+}

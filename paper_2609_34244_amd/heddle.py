@@ -26,7 +26,15 @@ EXPORTS = ["heddle_load_profile", "heddle_free_profile", "heddle_price_plans", "
            "heddle_best_plan", "heddle_count_work", "heddle_profile_info_get", "heddle_last_error",
            "heddle_enum_count", "heddle_enum_templates", "heddle_best_enumerated", "heddle_tile_plans",
            "heddle_count_tile_work",
-           "heddle_load_cluster", "heddle_free_cluster", "heddle_fill_dp", "heddle_fill_plans"]
+           "heddle_load_cluster", "heddle_free_cluster", "heddle_fill_dp", "heddle_fill_plans",
+           "heddle_linear", "heddle_linear_backward", "heddle_linear_workspace",
+           "heddle_gated_ffn", "heddle_gated_ffn_backward", "heddle_gated_ffn_workspace",
+           "heddle_grad_norm", "heddle_clip_grads", "heddle_clip_grad_norm", "heddle_grad_norm_workspace"]
+
+HEDDLE_T_BF16, HEDDLE_T_F16, HEDDLE_T_F32 = 0, 1, 2
+HEDDLE_A_NONE, HEDDLE_A_RELU, HEDDLE_A_GELU, HEDDLE_A_GELU_TANH, HEDDLE_A_SILU = 0, 1, 2, 3, 4
+ACTIVATIONS = {"none": HEDDLE_A_NONE, "relu": HEDDLE_A_RELU, "gelu": HEDDLE_A_GELU, "gelu_tanh": HEDDLE_A_GELU_TANH,
+               "silu": HEDDLE_A_SILU}
 
 
 class HeddleError(RuntimeError):
@@ -62,6 +70,31 @@ class heddle_profile_info(C.Structure):
                 ("narrow_tile", C.c_int32)]
 
 
+class heddle_linear_desc(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("act", C.c_int32), ("m", C.c_int64), ("n", C.c_int64), ("k", C.c_int64),
+                ("x", C.c_void_p), ("ldx", C.c_int64), ("w", C.c_void_p), ("ldw", C.c_int64), ("bias", C.c_void_p),
+                ("residual", C.c_void_p), ("ldr", C.c_int64), ("preact", C.c_void_p), ("ldp", C.c_int64),
+                ("y", C.c_void_p), ("ldy", C.c_int64), ("groups", C.c_int32), ("d_offsets", C.c_void_p),
+                ("stride_w", C.c_int64), ("dy", C.c_void_p), ("lddy", C.c_int64), ("dx", C.c_void_p),
+                ("lddx", C.c_int64), ("dw", C.c_void_p), ("lddw", C.c_int64), ("stride_dw", C.c_int64),
+                ("db", C.c_void_p)]
+
+
+class heddle_gated_ffn_desc(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("act", C.c_int32), ("t", C.c_int64), ("d", C.c_int64), ("f", C.c_int64),
+                ("x", C.c_void_p), ("ldx", C.c_int64), ("w_in", C.c_void_p), ("ldw_in", C.c_int64),
+                ("w_out", C.c_void_p), ("ldw_out", C.c_int64), ("residual", C.c_void_p), ("ldr", C.c_int64),
+                ("preact", C.c_void_p), ("ldp", C.c_int64), ("y", C.c_void_p), ("ldy", C.c_int64),
+                ("groups", C.c_int32), ("d_offsets", C.c_void_p), ("stride_in", C.c_int64), ("stride_out", C.c_int64),
+                ("dy", C.c_void_p), ("lddy", C.c_int64), ("dx", C.c_void_p), ("lddx", C.c_int64),
+                ("dw_in", C.c_void_p), ("lddw_in", C.c_int64), ("stride_dw_in", C.c_int64),
+                ("dw_out", C.c_void_p), ("lddw_out", C.c_int64), ("stride_dw_out", C.c_int64)]
+
+
+class heddle_grad_desc(C.Structure):
+    _fields_ = [("g", C.c_void_p), ("out", C.c_void_p), ("n", C.c_int64), ("dtype", C.c_int32)]
+
+
 _lib = None
 
 
@@ -94,6 +127,19 @@ def lib():
         L.heddle_enum_templates.argtypes = [C.POINTER(heddle_enum_spec), I64, I64, P, P, P]
         L.heddle_best_enumerated.argtypes = [P, C.POINTER(heddle_enum_spec), P, I32, U32, I64,
                                              C.POINTER(C.c_int64), C.POINTER(C.c_int32), P, C.POINTER(C.c_int64), P]
+        for op, desc in (("linear", heddle_linear_desc), ("gated_ffn", heddle_gated_ffn_desc)):
+            for back in ("", "_backward"):
+                f = getattr(L, f"heddle_{op}{back}")
+                f.argtypes, f.restype = [C.POINTER(desc), P, I64, P], C.c_int
+            f = getattr(L, f"heddle_{op}_workspace")
+            f.argtypes, f.restype = [C.POINTER(desc), I32, C.POINTER(C.c_int64)], C.c_int
+        G = C.POINTER(heddle_grad_desc)
+        L.heddle_grad_norm.argtypes = [G, I32, P, P, I64, P]
+        L.heddle_clip_grads.argtypes = [G, I32, P, C.c_float, P]
+        L.heddle_clip_grad_norm.argtypes = [G, I32, C.c_float, P, P, I64, P]
+        L.heddle_grad_norm_workspace.argtypes = [G, I32, C.POINTER(C.c_int64)]
+        for f in ("heddle_grad_norm", "heddle_clip_grads", "heddle_clip_grad_norm", "heddle_grad_norm_workspace"):
+            getattr(L, f).restype = C.c_int
         L.heddle_last_error.restype = C.c_char_p
         for f in ("heddle_load_profile", "heddle_price_plans", "heddle_price_plans_noalloc", "heddle_argmin_plans",
                   "heddle_best_plan",
@@ -392,3 +438,244 @@ def heddle_fill_plans(profiles, mbs, cl, global_batch, dp_cap, n_stages, stages,
                                    _ptr(out["bottleneck"]), _ptr(out["peak_mem"]), _ptr(out["layers"]),
                                    _ptr(out["status"]), _ptr(out["dp"]), _ptr(out["mbs_index"]), _stream(stream)))
     return out
+
+
+# ---- feed-forward and gradient operators ----
+
+def _dtype(t, what):
+    import torch
+    code = {torch.bfloat16: HEDDLE_T_BF16, torch.float16: HEDDLE_T_F16, torch.float32: HEDDLE_T_F32}.get(t.dtype)
+    if code is None:
+        raise HeddleError(HEDDLE_E_INVAL, f"{what}: type {t.dtype} is not supported")
+    return code
+
+
+def _matrix(t, what, shape, like):
+    """(data pointer, ld) of a device matrix whose rows are contiguous"""
+    if t.dtype != like.dtype or t.device != like.device or not t.is_cuda:
+        raise HeddleError(HEDDLE_E_INVAL, f"{what}: {t.dtype} on {t.device}, not {like.dtype} on the GPU of {like.device}")
+    if tuple(t.shape) != tuple(shape):
+        raise HeddleError(HEDDLE_E_INVAL, f"{what}: shape {tuple(t.shape)}, not {tuple(shape)}")
+    rows, cols = t.shape[-2], t.shape[-1]
+    if cols > 1 and t.stride(-1) != 1:
+        raise HeddleError(HEDDLE_E_INVAL, f"{what}: rows are not contiguous")
+    return t.data_ptr(), t.stride(-2) if rows > 1 else cols
+
+
+def _weights(t, what, shape, groups, like):
+    """(data pointer, ld, distance between groups)"""
+    p, ld = _matrix(t, what, shape, like)
+    return p, ld, t.stride(0) if groups and t.shape[0] > 1 else shape[-2] * ld
+
+
+def _vector(t, what, shape, like):
+    if t.dtype != like.dtype or t.device != like.device or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise HeddleError(HEDDLE_E_INVAL, f"{what}: not a contiguous {like.dtype} tensor of shape {tuple(shape)} on {like.device}")
+    return t.data_ptr()
+
+
+def _groups(offsets, w, like):
+    """number of expert groups, 0 without offsets"""
+    import torch
+    if offsets is None:
+        return 0
+    if offsets.dtype != torch.int32 or offsets.device != like.device or offsets.dim() != 1 or not offsets.is_contiguous():
+        raise HeddleError(HEDDLE_E_INVAL, "offsets: not a contiguous int32 vector on the inputs' device")
+    if w.dim() != 3 or offsets.numel() != w.shape[0] + 1:
+        raise HeddleError(HEDDLE_E_INVAL, f"offsets: {offsets.numel()} entries for weights of shape {tuple(w.shape)}")
+    return w.shape[0]
+
+
+def _fresh(shape, like, stream):
+    import torch
+    t = torch.empty(shape, dtype=like.dtype, device=like.device)
+    if stream is not None:
+        t.record_stream(stream)
+    return t
+
+
+def _run(name, desc, backward, like, stream):
+    """scratch from torch's allocator, then the call"""
+    import torch
+    L, need = lib(), C.c_int64()
+    with torch.cuda.device(like.device):
+        _check(getattr(L, f"heddle_{name}_workspace")(C.byref(desc), backward, C.byref(need)))
+        ws = None
+        if need.value:
+            ws = torch.empty(need.value, dtype=torch.uint8, device=like.device)
+            if stream is not None:
+                ws.record_stream(stream)
+        f = getattr(L, f"heddle_{name}_backward" if backward else f"heddle_{name}")
+        _check(f(C.byref(desc), _ptr(ws), need.value, _stream(stream)))
+
+
+def _two(x, w, what):
+    if x.dim() != 2 or w.dim() not in (2, 3) or not x.is_cuda:
+        raise HeddleError(HEDDLE_E_INVAL, f"{what}: rows must be a matrix and weights a matrix, or one for each group, on the GPU")
+
+
+def heddle_linear(x, w, bias=None, act=HEDDLE_A_NONE, residual=None, preact=None, out=None, offsets=None, stream=None):
+    """act(x @ w.T + bias) + residual. x: [m, k]; w: [n, k], or with offsets
+    [groups, n, k] for rows sorted by expert; bias: [n] ([groups, n]);
+    preact: [m, n] to keep the values before the activation for the backward
+    pass. Matrices may have any distance between rows. Returns out ([m, n])."""
+    _two(x, w, "heddle_linear")
+    m, k, n = x.shape[0], x.shape[1], w.shape[-2]
+    e = _groups(offsets, w, x)
+    lead = (e,) if e else ()
+    out = _fresh((m, n), x, stream) if out is None else out
+    d = heddle_linear_desc(dtype=_dtype(x, "x"), act=act, m=m, n=n, k=k, groups=e, d_offsets=offsets.data_ptr() if e else None)
+    d.x, d.ldx = _matrix(x, "x", (m, k), x)
+    d.w, d.ldw, d.stride_w = _weights(w, "w", (*lead, n, k), e, x)
+    d.y, d.ldy = _matrix(out, "out", (m, n), x)
+    if bias is not None:
+        d.bias = _vector(bias, "bias", (*lead, n), x)
+    if residual is not None:
+        d.residual, d.ldr = _matrix(residual, "residual", (m, n), x)
+    if preact is not None:
+        d.preact, d.ldp = _matrix(preact, "preact", (m, n), x)
+    _run("linear", d, 0, x, stream)
+    return out
+
+
+def heddle_linear_backward(dy, x, w, act=HEDDLE_A_NONE, preact=None, offsets=None, want_dx=True, want_dw=True, want_db=False,
+                           dx=None, dw=None, db=None, stream=None):
+    """Gradients of heddle_linear: a dict with dx, dw and db (those wanted;
+    given tensors are written). preact: what heddle_linear kept (any act but
+    HEDDLE_A_NONE). The residual's gradient is dy itself."""
+    _two(x, w, "heddle_linear_backward")
+    m, k, n = x.shape[0], x.shape[1], w.shape[-2]
+    e = _groups(offsets, w, x)
+    lead = (e,) if e else ()
+    d = heddle_linear_desc(dtype=_dtype(x, "x"), act=act, m=m, n=n, k=k, groups=e, d_offsets=offsets.data_ptr() if e else None)
+    d.x, d.ldx = _matrix(x, "x", (m, k), x)
+    d.w, d.ldw, d.stride_w = _weights(w, "w", (*lead, n, k), e, x)
+    d.dy, d.lddy = _matrix(dy, "dy", (m, n), x)
+    if preact is not None:
+        d.preact, d.ldp = _matrix(preact, "preact", (m, n), x)
+    out = {}
+    if want_dx or dx is not None:
+        out["dx"] = _fresh((m, k), x, stream) if dx is None else dx
+        d.dx, d.lddx = _matrix(out["dx"], "dx", (m, k), x)
+    if want_dw or dw is not None:
+        out["dw"] = _fresh((*lead, n, k), x, stream) if dw is None else dw
+        d.dw, d.lddw, d.stride_dw = _weights(out["dw"], "dw", (*lead, n, k), e, x)
+    if want_db or db is not None:
+        out["db"] = _fresh((*lead, n), x, stream) if db is None else db
+        d.db = _vector(out["db"], "db", (*lead, n), x)
+    _run("linear", d, 1, x, stream)
+    return out
+
+
+def _ffn_desc(x, w_in, w_out, act, offsets):
+    _two(x, w_in, "heddle_gated_ffn")
+    t, dim = x.shape
+    if w_in.shape[-2] % 2:
+        raise HeddleError(HEDDLE_E_INVAL, "w_in: an odd number of gate and up rows")
+    f, e = w_in.shape[-2] // 2, _groups(offsets, w_in, x)
+    lead = (e,) if e else ()
+    d = heddle_gated_ffn_desc(dtype=_dtype(x, "x"), act=act, t=t, d=dim, f=f, groups=e,
+                              d_offsets=offsets.data_ptr() if e else None)
+    d.x, d.ldx = _matrix(x, "x", (t, dim), x)
+    d.w_in, d.ldw_in, d.stride_in = _weights(w_in, "w_in", (*lead, 2 * f, dim), e, x)
+    d.w_out, d.ldw_out, d.stride_out = _weights(w_out, "w_out", (*lead, dim, f), e, x)
+    return d, t, dim, f, e, lead
+
+
+def heddle_gated_ffn(x, w_in, w_out, act=HEDDLE_A_SILU, residual=None, preact=None, out=None, offsets=None, stream=None):
+    """(act(x @ gate.T) * (x @ up.T)) @ w_out.T + residual. x: [t, d]; w_in:
+    [2 f, d], gate rows then up rows; w_out: [d, f]; with offsets both have a
+    leading dimension of expert groups. preact: [t, 2 f] to keep the two
+    projections for the backward pass. Returns out ([t, d])."""
+    d, t, dim, f, _, _ = _ffn_desc(x, w_in, w_out, act, offsets)
+    out = _fresh((t, dim), x, stream) if out is None else out
+    d.y, d.ldy = _matrix(out, "out", (t, dim), x)
+    if residual is not None:
+        d.residual, d.ldr = _matrix(residual, "residual", (t, dim), x)
+    if preact is not None:
+        d.preact, d.ldp = _matrix(preact, "preact", (t, 2 * f), x)
+    _run("gated_ffn", d, 0, x, stream)
+    return out
+
+
+def heddle_gated_ffn_backward(dy, x, w_in, w_out, preact, act=HEDDLE_A_SILU, offsets=None, want_dx=True, want_dw=True,
+                              dx=None, dw_in=None, dw_out=None, stream=None):
+    """Gradients of heddle_gated_ffn: a dict with dx, dw_in and dw_out (those
+    wanted; given tensors are written). preact: what heddle_gated_ffn kept."""
+    d, t, dim, f, e, lead = _ffn_desc(x, w_in, w_out, act, offsets)
+    d.dy, d.lddy = _matrix(dy, "dy", (t, dim), x)
+    d.preact, d.ldp = _matrix(preact, "preact", (t, 2 * f), x)
+    out = {}
+    if want_dx or dx is not None:
+        out["dx"] = _fresh((t, dim), x, stream) if dx is None else dx
+        d.dx, d.lddx = _matrix(out["dx"], "dx", (t, dim), x)
+    if want_dw or dw_in is not None:
+        out["dw_in"] = _fresh((*lead, 2 * f, dim), x, stream) if dw_in is None else dw_in
+        d.dw_in, d.lddw_in, d.stride_dw_in = _weights(out["dw_in"], "dw_in", (*lead, 2 * f, dim), e, x)
+    if want_dw or dw_out is not None:
+        out["dw_out"] = _fresh((*lead, dim, f), x, stream) if dw_out is None else dw_out
+        d.dw_out, d.lddw_out, d.stride_dw_out = _weights(out["dw_out"], "dw_out", (*lead, dim, f), e, x)
+    _run("gated_ffn", d, 1, x, stream)
+    return out
+
+
+def _grads(grads, out=None):
+    """descriptor array of a list of gradient tensors, and their device"""
+    if out is not None and len(out) != len(grads):
+        raise HeddleError(HEDDLE_E_INVAL, f"{len(out)} outputs for {len(grads)} gradient tensors")
+    table = (heddle_grad_desc * max(len(grads), 1))()
+    device = grads[0].device if len(grads) else None
+    for i, g in enumerate(grads):
+        if not g.is_cuda or g.device != device or not g.is_contiguous():
+            raise HeddleError(HEDDLE_E_INVAL, f"gradient tensor {i}: not contiguous on the GPU of the first one")
+        e = table[i]
+        e.g, e.n, e.dtype = g.data_ptr(), g.numel(), _dtype(g, f"gradient tensor {i}")
+        if out is not None:
+            o = out[i]
+            if o.dtype != g.dtype or o.device != device or o.numel() != e.n or not o.is_contiguous():
+                raise HeddleError(HEDDLE_E_INVAL, f"output {i}: not contiguous, or unlike its gradient tensor")
+            e.out = o.data_ptr()
+    return table, device
+
+
+def _norm_call(table, count, device, stream, call):
+    import torch
+    L, need = lib(), C.c_int64()
+    with torch.cuda.device(device):
+        _check(L.heddle_grad_norm_workspace(table, count, C.byref(need)))
+        norm = torch.empty(1, dtype=torch.float32, device="cuda" if device is None else device)
+        ws = torch.empty(need.value, dtype=torch.uint8, device=norm.device)
+        if stream is not None:
+            norm.record_stream(stream)
+            ws.record_stream(stream)
+        _check(call(L, _ptr(norm), _ptr(ws), need.value, _stream(stream)))
+    return norm
+
+
+def heddle_grad_norm(grads, stream=None):
+    """The 2-norm over all values of all gradient tensors, as a float32 tensor
+    of one value on their device."""
+    table, device = _grads(grads)
+    return _norm_call(table, len(grads), device, stream,
+                      lambda L, norm, ws, n, s: L.heddle_grad_norm(table, len(grads), norm, ws, n, s))
+
+
+def heddle_clip_grads(grads, norm, max_norm, out=None, stream=None):
+    """Scale the gradient tensors by min(1, max_norm / (norm + 1e-6)), in
+    place or into out. norm: float32 tensor of one value on their device (of
+    all ranks' shards, say)."""
+    import torch
+    table, device = _grads(grads, out)
+    if not norm.is_cuda or norm.dtype != torch.float32 or norm.numel() != 1 or device not in (None, norm.device):
+        raise HeddleError(HEDDLE_E_INVAL, "norm: not one float32 value on the gradients' device")
+    with torch.cuda.device(norm.device):
+        _check(lib().heddle_clip_grads(table, len(grads), _ptr(norm), max_norm, _stream(stream)))
+    return grads if out is None else out
+
+
+def heddle_clip_grad_norm(grads, max_norm, out=None, stream=None):
+    """heddle_grad_norm and heddle_clip_grads in one call; returns the norm
+    before clipping."""
+    table, device = _grads(grads, out)
+    return _norm_call(table, len(grads), device, stream,
+                      lambda L, norm, ws, n, s: L.heddle_clip_grad_norm(table, len(grads), max_norm, norm, ws, n, s))
