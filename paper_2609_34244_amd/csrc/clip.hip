@@ -28,53 +28,38 @@ struct GradTable {
     int32_t count;
 };
 
-__device__ inline float grad_value(float v) { return v; }
-__device__ inline float grad_value(__bf16 v) { return (float)v; }
-__device__ inline float grad_value(_Float16 v) { return (float)v; }
-
-// the 16-byte pieces of chunk c of a tensor, one lane a piece: f(elements, first, from, to)
-template <typename T, typename F> __device__ inline void chunk_pieces(const void *g, int64_t n, int64_t c, F f)
+// Chunk c of a tensor, one 16-byte piece a lane at a time. A whole chunk is eight
+// loads before the first use, f(values, index of the first); at a tensor's ends
+// the values come one by one, g(value, index).
+template <typename T, typename F, typename G> __device__ inline void each_of_chunk(const void *g, int64_t n, int64_t c, F f, G one)
 {
-    constexpr int V = 16 / sizeof(T);
+    constexpr int V = 16 / sizeof(T), kPieces = kChunk / 16 / 256;
+    typedef T piece __attribute__((ext_vector_type(V)));
     const uintptr_t p = (uintptr_t)g;
     const int64_t skew = (int64_t)(p & 15) / (int64_t)sizeof(T);        // values before g in its first piece
     const T *base = (const T *)(p & ~(uintptr_t)15);
-    const int64_t end = skew + n;
-    const int64_t v0 = c * (kChunk / (int64_t)sizeof(T));
-#pragma unroll 4
-    for (int i = 0; i < kChunk / 16 / 256; i++) {
-        const int64_t v = v0 + (i * 256 + threadIdx.x) * V;
-        if (v >= end) return;
-        const int from = v < skew ? (int)(skew - v) : 0, to = end - v < V ? (int)(end - v) : V;
-        f(base + v, v - skew, from, to);
-    }
-}
-
-template <typename T> struct Piece { typedef T type __attribute__((ext_vector_type(16 / sizeof(T)))); };
-
-template <typename T> __device__ inline void read_piece(const T *p, int from, int to, float *v)
-{
-    constexpr int V = 16 / sizeof(T);
-    if (from == 0 && to == V) {
-        const typename Piece<T>::type x = *(const typename Piece<T>::type *)p;
+    const int64_t end = skew + n, v0 = c * (kChunk / (int64_t)sizeof(T)) + threadIdx.x * V;
+    if ((c > 0 || skew == 0) && (c + 1) * (kChunk / (int64_t)sizeof(T)) <= end) {
+        piece x[kPieces];
 #pragma unroll
-        for (int i = 0; i < V; i++) v[i] = grad_value(x[i]);
-    } else {
+        for (int i = 0; i < kPieces; i++) x[i] = *(const piece *)(base + v0 + i * 256 * V);
 #pragma unroll
-        for (int i = 0; i < V; i++) v[i] = i >= from && i < to ? grad_value(p[i]) : 0.0f;
+        for (int i = 0; i < kPieces; i++) f(x[i], v0 + i * 256 * V - skew);
+        return;
     }
+    for (int i = 0; i < kPieces; i++)
+        for (int64_t v = v0 + i * 256 * V, j = 0; j < V; j++)
+            if (v + j >= skew && v + j < end) one(base[v + j], v + j - skew);
 }
 
 template <typename T> __device__ inline double chunk_squares(const void *g, int64_t n, int64_t c)
 {
     double s = 0;
-    chunk_pieces<T>(g, n, c, [&](const T *p, int64_t, int from, int to) {
-        constexpr int V = 16 / sizeof(T);
-        float v[V];
-        read_piece(p, from, to, v);
+    auto add = [&](float v) { s = fma((double)v, (double)v, s); };
+    each_of_chunk<T>(g, n, c, [&](auto x, int64_t) {
 #pragma unroll
-        for (int i = 0; i < V; i++) s = fma((double)v[i], (double)v[i], s);
-    });
+        for (int i = 0; i < 16 / (int)sizeof(T); i++) add((float)x[i]);
+    }, [&](T x, int64_t) { add((float)x); });
     return s;
 }
 
@@ -90,7 +75,8 @@ __device__ inline double block_sum(double s, double *lds)
     return s;
 }
 
-__global__ void __launch_bounds__(256) grad_squares_kernel(GradTable t, double *parts)
+// held: sums that earlier launches left
+__global__ void __launch_bounds__(256) grad_squares_kernel(GradTable t, double *parts, int held)
 {
     __shared__ double lds[4];
     double s = 0;
@@ -103,7 +89,7 @@ __global__ void __launch_bounds__(256) grad_squares_kernel(GradTable t, double *
         else s += chunk_squares<float>(t.g[k], t.n[k], local);
     }
     s = block_sum(s, lds);
-    if (threadIdx.x == 0) parts[blockIdx.x] = s;
+    if (threadIdx.x == 0) parts[blockIdx.x] = (int)blockIdx.x < held ? parts[blockIdx.x] + s : s;
 }
 
 __device__ inline float norm_of(const double *parts, int count, double *lds)
@@ -123,22 +109,11 @@ __global__ void __launch_bounds__(256) grad_norm_kernel(const double *parts, int
 template <typename T>
 __device__ inline void clip_chunk(const void *g, void *out, int64_t n, int64_t c, float factor)
 {
-    chunk_pieces<T>(g, n, c, [&](const T *p, int64_t first, int from, int to) {
-        constexpr int V = 16 / sizeof(T);
-        float v[V];
-        read_piece(p, from, to, v);
-        T *o = (T *)out + first;
-        if (from == 0 && to == V) {
-            typename Piece<T>::type x;
+    each_of_chunk<T>(g, n, c, [&](auto x, int64_t at) {
 #pragma unroll
-            for (int i = 0; i < V; i++) x[i] = (T)(v[i] * factor);
-            __builtin_memcpy(o, &x, 16);      // out may start anywhere its values may
-        } else {
-#pragma unroll
-            for (int i = 0; i < V; i++)
-                if (i >= from && i < to) o[i] = (T)(v[i] * factor);
-        }
-    });
+        for (int i = 0; i < 16 / (int)sizeof(T); i++) x[i] = (T)((float)x[i] * factor);
+        __builtin_memcpy((T *)out + at, &x, 16);      // out may start anywhere its values may
+    }, [&](T x, int64_t at) { ((T *)out)[at] = (T)((float)x * factor); });
 }
 
 // The factor from d_norm, or from the parts (then the first workgroup of the
@@ -156,11 +131,13 @@ __global__ void __launch_bounds__(256) clip_kernel(GradTable t, const double *pa
     }
     float factor = max_norm / (v + 1e-6f);
     if (factor >= 1.0f) factor = 1.0f;                                  // a NaN stays
+    // The table runs from the last tensor to the first, and so do a tensor's chunks here: what
+    // the norm read last is still in the 256 MB memory-side cache.
     int k = 0;
     for (int c = blockIdx.x; c < t.first[t.count]; c += gridDim.x) {
         while (c >= t.first[k + 1]) k++;
         if (factor == 1.0f && t.out[k] == t.g[k]) continue;
-        const int64_t local = c - t.first[k];
+        const int64_t local = t.first[k + 1] - 1 - c;
         if (t.dtype[k] == HEDDLE_T_BF16) clip_chunk<__bf16>(t.g[k], t.out[k], t.n[k], local, factor);
         else if (t.dtype[k] == HEDDLE_T_F16) clip_chunk<_Float16>(t.g[k], t.out[k], t.n[k], local, factor);
         else clip_chunk<float>(t.g[k], t.out[k], t.n[k], local, factor);
@@ -189,59 +166,48 @@ static int64_t chunks_of(const heddle_grad_desc &g)
     return g.n > 0 ? (skew + g.n * size + kChunk - 1) / kChunk : 0;
 }
 
-// tables of up to kTensors tensors (and 2^30 chunks) each; f(table) launches
-template <typename F> static int each_table(const heddle_grad_desc *g, int32_t count, F f)
+// tables of up to kTensors tensors (and 2^30 chunks) each, from the first tensor or from
+// the last; f(table) launches
+template <typename F> static int each_table(const heddle_grad_desc *g, int32_t count, bool backward, F f)
 {
-    int32_t i = 0;
+    int32_t done = 0;
     do {
         GradTable t;
         t.count = 0;
         t.first[0] = 0;
-        for (; i < count && t.count < kTensors; i++) {
-            const int64_t c = chunks_of(g[i]);
+        for (; done < count && t.count < kTensors; done++) {
+            const heddle_grad_desc &d = g[backward ? count - 1 - done : done];
+            const int64_t c = chunks_of(d);
             if (c == 0) continue;
             if (t.first[t.count] + c > (int64_t(1) << 30)) break;
             const int k = t.count++;
-            t.g[k] = g[i].g;
-            t.out[k] = g[i].out ? g[i].out : const_cast<void *>(g[i].g);
-            t.n[k] = g[i].n;
-            t.dtype[k] = (uint8_t)g[i].dtype;
+            t.g[k] = d.g;
+            t.out[k] = d.out ? d.out : const_cast<void *>(d.g);
+            t.n[k] = d.n;
+            t.dtype[k] = (uint8_t)d.dtype;
             t.first[k + 1] = (int32_t)(t.first[k] + c);
         }
         const int rc = f(t);
         if (rc) return rc;
-    } while (i < count);
+    } while (done < count);
     return HEDDLE_OK;
 }
 
-static int tables_of(const heddle_grad_desc *g, int32_t count)
-{
-    int n = 0;
-    each_table(g, count, [&](const GradTable &) { n++; return HEDDLE_OK; });
-    return n;
-}
-
-static int check_parts(const void *ws, int64_t bytes, int tables)
+static int check_parts(const void *ws, int64_t bytes)
 {
     if (!ws || ((uintptr_t)ws & 255)) return fail(HEDDLE_E_INVAL, "workspace is NULL or not 256-byte aligned");
-    if (bytes < (int64_t)(kParts + tables) * 8) return fail(HEDDLE_E_INVAL, "workspace smaller than the call needs");
+    if (bytes < (int64_t)kParts * 8) return fail(HEDDLE_E_INVAL, "workspace smaller than the call needs");
     return HEDDLE_OK;
 }
 
 // the sums of squares; *parts: how many
 static int launch_squares(const heddle_grad_desc *g, int32_t count, double *ws, int *parts, hipStream_t stream)
 {
-    int64_t all = 0;
-    for (int32_t i = 0; i < count; i++) all += chunks_of(g[i]);
     *parts = 0;
-    return each_table(g, count, [&](const GradTable &t) {
-        // every launch has its share of the kParts sums
-        const int64_t mine = t.first[t.count];
-        int64_t blocks = all > kParts ? (int64_t)((double)mine / (double)all * kParts) : mine;
-        if (blocks < 1) blocks = 1;
-        if (blocks > kParts) blocks = kParts;
-        hipLaunchKernelGGL(grad_squares_kernel, dim3((unsigned)blocks), dim3(256), 0, stream, t, ws + *parts);
-        *parts += (int)blocks;
+    return each_table(g, count, false, [&](const GradTable &t) {
+        const int mine = t.first[t.count], blocks = mine < 1 ? 1 : mine < kParts ? mine : kParts;
+        hipLaunchKernelGGL(grad_squares_kernel, dim3((unsigned)blocks), dim3(256), 0, stream, t, ws, *parts);
+        if (blocks > *parts) *parts = blocks;
         const hipError_t e = hipGetLastError();
         return e == hipSuccess ? HEDDLE_OK : hip_fail(e, "grad_squares_kernel");
     });
@@ -251,7 +217,7 @@ static int launch_clip(const heddle_grad_desc *g, int32_t count, const double *p
                        hipStream_t stream)
 {
     int write = 1;
-    return each_table(g, count, [&](const GradTable &t) {
+    return each_table(g, count, true, [&](const GradTable &t) {
         const int64_t mine = t.first[t.count];
         const int64_t blocks = mine < 1 ? 1 : mine < kParts ? mine : kParts;
         hipLaunchKernelGGL(clip_kernel, dim3((unsigned)blocks), dim3(256), 0, stream, t, parts, n_parts, norm, write, max_norm);
@@ -275,7 +241,7 @@ extern "C" int heddle_grad_norm_workspace(const heddle_grad_desc *grads, int32_t
     if (!h_bytes) return fail(HEDDLE_E_INVAL, "h_bytes is NULL");
     const int rc = check_grads(grads, count);
     if (rc) return rc;
-    *h_bytes = (int64_t)(kParts + tables_of(grads, count)) * 8;
+    *h_bytes = (int64_t)kParts * 8;
     return HEDDLE_OK;
 }
 
@@ -285,7 +251,7 @@ extern "C" int heddle_grad_norm(const heddle_grad_desc *grads, int32_t count, fl
     int rc = check_grads(grads, count);
     if (rc) return rc;
     if (!d_norm || ((uintptr_t)d_norm & 3)) return fail(HEDDLE_E_INVAL, "d_norm is NULL or misaligned");
-    rc = check_parts(ws, bytes, tables_of(grads, count));
+    rc = check_parts(ws, bytes);
     if (rc) return rc;
     int parts = 0;
     rc = launch_squares(grads, count, (double *)ws, &parts, stream);
@@ -314,7 +280,7 @@ extern "C" int heddle_clip_grad_norm(const heddle_grad_desc *grads, int32_t coun
     if (!d_norm || ((uintptr_t)d_norm & 3)) return fail(HEDDLE_E_INVAL, "d_norm is NULL or misaligned");
     rc = check_max_norm(max_norm);
     if (rc) return rc;
-    rc = check_parts(ws, bytes, tables_of(grads, count));
+    rc = check_parts(ws, bytes);
     if (rc) return rc;
     int parts = 0;
     rc = launch_squares(grads, count, (double *)ws, &parts, stream);

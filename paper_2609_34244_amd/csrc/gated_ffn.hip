@@ -80,7 +80,7 @@ template <typename T> static int forward(const heddle_gated_ffn_desc *d, Scratch
     if (rc == HEDDLE_OK) rc = copy_rows(wo, d->d, d->f, groups, s, run, stream);
     if (rc) return rc;
     EpiGated<T> e = {};
-    e.ldh = up8(d->f), e.h = (T *)s.take((size_t)d->t * e.ldh * 2), e.wide_h = 8;
+    e.ldh = scratch_ld(d->f), e.h = (T *)s.take((size_t)d->t * e.ldh * 2), e.wide_h = 8;
     e.pre = (T *)d->preact, e.ldp = d->ldp, e.wide_p = width_of(d->preact, d->ldp, d->f);
     e.act = d->act, e.N = (int)d->f;
     rc = hidden<T, EpiGated<T>, false>(x, wi, d->t, d->f, d->d, groups, d->d_offsets, e, s, run, stream);
@@ -105,7 +105,7 @@ template <typename T> static int backward(const heddle_gated_ffn_desc *d, Scratc
         if (rc) return rc;
     }
     EpiGatedGrad<T> e = {};
-    e.ldd = up8(2 * d->f), e.ldh = up8(d->f);
+    e.ldd = scratch_ld(2 * d->f), e.ldh = scratch_ld(d->f);
     e.dp = (T *)s.take((size_t)d->t * e.ldd * 2), e.wide_d = width_of(nullptr, e.ldd, d->f);
     e.h = (T *)s.take((size_t)d->t * e.ldh * 2), e.wide_h = 8;
     e.pre = (const T *)d->preact, e.ldp = d->ldp, e.wide_p = width_of(d->preact, d->ldp, d->f);

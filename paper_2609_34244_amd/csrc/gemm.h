@@ -8,7 +8,7 @@
 // to LDS, 16 bytes a lane, through a buffer resource whose size is the
 // operand's remaining bytes: what lies past the end arrives as zero, so no
 // address needs a test. Rows tiles are [row][64] with the 16-byte pieces of a
-// row exchanged by row & 7; a lane reads its 8 k with one 16-byte read.
+// row exchanged by 3 bits of the row; a lane reads its 8 k with one 16-byte read.
 // Columns tiles are [64][column] with the 32-byte pieces exchanged by 3 bits of
 // k; the transposing LDS read hands each lane 4 k of its column. Either way a
 // quarter-wave's reads touch every bank once.
@@ -295,8 +295,9 @@ __device__ inline __amdgpu_buffer_rsrc_t resource(const char *base, int64_t byte
     return __builtin_amdgcn_make_buffer_rsrc((void *)base, 0, (int)(uint32_t)(n > 0xFFFFFFFCll ? 0xFFFFFFFCll : n), 0x00020000);
 }
 
-// columns tiles: the exchange of a row's 32-byte pieces
-template <int ROWS> __device__ inline int swz(int k) { return ((k & 3) | ((k >> 3 & 1) << 2)) & (ROWS / 16 - 1); }
+// the exchange of a rows tile's 16-byte and of a columns tile's 32-byte pieces
+__device__ inline int row_swz(int r) { return (r >> 1) & 7; }
+template <int ROWS> __device__ inline int col_swz(int k) { return ((k & 3) | ((k >> 3 & 1) << 2)) & (ROWS / 16 - 1); }
 
 // One operand's tile of ROWS x 64, loaded by NW wavefronts. COLS: the operand
 // is "columns". PAIR: 16-row blocks alternate between gate and up rows.
@@ -312,11 +313,11 @@ template <int ROWS, int NW, bool COLS, bool PAIR> struct Loader {
             const int c = (i * NW + wave) * 64 + lane;
             if (COLS) {
                 const int k = c / (ROWS / 8), pos = c % (ROWS / 8);
-                voff[i] = (int)(k * ld * 2) + (pos ^ (swz<ROWS>(k) << 1)) * 16;
+                voff[i] = (int)(k * ld * 2) + (pos ^ (col_swz<ROWS>(k) << 1)) * 16;
             } else {
                 const int r = c / 8, pos = c % 8;
                 const int src = PAIR ? (r / 32) * 16 + r % 16 : r;
-                voff[i] = (int)(src * ld * 2) + (pos ^ (r & 7)) * 16;
+                voff[i] = (int)(src * ld * 2) + (pos ^ row_swz(r)) * 16;
             }
         }
     }
@@ -341,7 +342,7 @@ template <int ROWS, int NW, bool COLS, bool PAIR> struct Loader {
     {
         for (int c = threadIdx.x; c < ROWS * kBK; c += NW * 64) {
             const int r = c / kBK, k = c % kBK;
-            if (k >= valid) *(short *)(lds + r * 128 + (((k / 8) ^ (r & 7)) * 16) + (k % 8) * 2) = 0;
+            if (k >= valid) *(short *)(lds + r * 128 + (((k / 8) ^ row_swz(r)) * 16) + (k % 8) * 2) = 0;
         }
     }
 };
@@ -352,7 +353,7 @@ __device__ inline typename pack8<T>::type fragment(const char *lds, int rb, int 
 {
     const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
     if (COLS) {
-        const int q = i >> 2, f = swz<ROWS>(g * 8 + q);
+        const int q = i >> 2, f = col_swz<ROWS>(g * 8 + q);
         const char *p = lds + (s * 32 + g * 8 + q) * (ROWS * 2) + ((rb ^ f) << 5) + (i & 3) * 8;
         typedef __attribute__((address_space(3))) s16x4 *rd;
         const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((rd)p);
@@ -360,7 +361,27 @@ __device__ inline typename pack8<T>::type fragment(const char *lds, int rb, int 
         const s16x8 z = __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
         return __builtin_bit_cast(typename pack8<T>::type, z);
     }
-    return *(const typename pack8<T>::type *)(lds + (rb * 16 + i) * 128 + (((s * 4 + g) ^ (i & 7)) << 4));
+    return *(const typename pack8<T>::type *)(lds + (rb * 16 + i) * 128 + (((s * 4 + g) ^ row_swz(i)) << 4));
+}
+
+// every wavefront's loads have landed and its reads of LDS are done
+__device__ inline void arrive()
+{
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0);
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+// the order of a half step's instructions: one LDS read to every other product, so that the
+// reads of the next fragments run beside the products of these
+template <int READS, int PRODUCTS, bool COLS> __device__ inline void interleave()
+{
+#pragma unroll
+    for (int i = 0; i < READS; i++) {
+        __builtin_amdgcn_sched_group_barrier(0x100, COLS ? 2 : 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x008, PRODUCTS / READS, 0);
+    }
 }
 
 // Workgroup order: consecutive workgroups go to the 8 XCDs in turn, so each
@@ -385,7 +406,7 @@ __global__ void __launch_bounds__(WM * WN * 64) gemm_kernel(Args x, Epi epi)
 {
 #ifdef __HIP_DEVICE_COMPILE__   // the host pass has no buffer resources
     constexpr int NW = WM * WN, TM = BM / WM / 16, TN = BN / WN / 16, kOut = BN / WN;
-    constexpr bool PAIR = Epi::gated;
+    constexpr bool PAIR = Epi::gated, PIPED = BM * BN >= 256 * 256;   // one workgroup on a CU
     typedef Loader<BM, NW, ACOL, false> LA;
     typedef Loader<BN, NW, BCOL, PAIR> LB;
     constexpr int kStage = LA::kBytes + LB::kBytes;
@@ -448,35 +469,68 @@ __global__ void __launch_bounds__(WM * WN * 64) gemm_kernel(Args x, Epi epi)
 #pragma unroll
         for (int j = 0; j < TN; j++) acc[i][j] = f32x4{0, 0, 0, 0};
 
-    if (tiles) {
-        la.load(pa, na, 0, smem, wave);
-        lb.load(pb, nb, up, smem + LA::kBytes, wave);
-    }
-    for (int kt = 0; kt < tiles; kt++) {
-        char *cur = smem + (kt & 1) * kStage, *nxt = smem + (~kt & 1) * kStage;
-        __builtin_amdgcn_s_waitcnt(0);
-        __syncthreads();
-        if (kt + 1 < tiles) {
+    typedef typename pack8<T>::type frag;
+    frag fa[2][TM], fb[2][TN];
+    auto read = [&](const char *tile, int s, frag *a, frag *b) {
+#pragma unroll
+        for (int j = 0; j < TN; j++) b[j] = fragment<BN, BCOL, T>(tile + LA::kBytes, wn * TN + j, s);
+#pragma unroll
+        for (int i = 0; i < TM; i++) a[i] = fragment<BM, ACOL, T>(tile, wm * TM + i, s);
+    };
+    auto multiply = [&](const frag *a, const frag *b) {
+#pragma unroll
+        for (int i = 0; i < TM; i++)
+#pragma unroll
+            for (int j = 0; j < TN; j++) acc[i][j] = mfma(b[j], a[i], acc[i][j]);
+    };
+    int loaded = 0;                                         // k-tiles asked for
+    auto load = [&](char *tile) {
+        if (loaded < tiles) {
+            la.load(pa, na, 0, tile, wave);
+            lb.load(pb, nb, up, tile + LA::kBytes, wave);
             pa += step_a, na -= step_a, pb += step_b, nb -= step_b;
-            la.load(pa, na, 0, nxt, wave);
-            lb.load(pb, nb, up, nxt + LA::kBytes, wave);
-        } else if ((!ACOL || !BCOL) && (k_last - k_first) % kBK && k_last == k_hi) {
-            const int valid = (k_last - k_first) % kBK;
-            if (!ACOL) LA::clear_tail(cur, valid);
-            if (!BCOL) LB::clear_tail(cur + LA::kBytes, valid);
+        }
+        loaded++;
+    };
+    const int valid = (k_last - k_first) % kBK;             // k of a last, partial tile
+    auto landed = [&](char *tile, int kt) {
+        arrive();
+        if ((!ACOL || !BCOL) && valid && kt == tiles - 1 && k_last == k_hi) {
+            if (!ACOL) LA::clear_tail(tile, valid);
+            if (!BCOL) LB::clear_tail(tile + LA::kBytes, valid);
             __syncthreads();
         }
+    };
+    if (PIPED && tiles) {
+        // Half a k-tile's fragments are read while the other half's are multiplied. A tile's
+        // buffer is free, and the next tile must be there, at the middle of the tile.
+        load(smem);
+        landed(smem, 0);
+        load(smem + kStage);
+        read(smem, 0, fa[0], fb[0]);
+        for (int kt = 0; kt < tiles; kt++) {
+            char *cur = smem + (kt & 1) * kStage, *nxt = smem + (~kt & 1) * kStage;
+            read(cur, 1, fa[1], fb[1]);
+            multiply(fa[0], fb[0]);
+            interleave<TM + TN, TM * TN, ACOL || BCOL>();
+            landed(nxt, kt + 1);
+            load(cur);
+            read(nxt, 0, fa[0], fb[0]);
+            multiply(fa[1], fb[1]);
+            interleave<TM + TN, TM * TN, ACOL || BCOL>();
+        }
+    } else if (tiles) {
+        // several workgroups on a CU hide each other's reads
+        load(smem);
+        for (int kt = 0; kt < tiles; kt++) {
+            char *cur = smem + (kt & 1) * kStage;
+            landed(cur, kt);
+            load(smem + (~kt & 1) * kStage);
 #pragma unroll
-        for (int s = 0; s < kBK / 32; s++) {
-            typename pack8<T>::type fa[TM], fb[TN];
-#pragma unroll
-            for (int i = 0; i < TM; i++) fa[i] = fragment<BM, ACOL, T>(cur, wm * TM + i, s);
-#pragma unroll
-            for (int j = 0; j < TN; j++) fb[j] = fragment<BN, BCOL, T>(cur + LA::kBytes, wn * TN + j, s);
-#pragma unroll
-            for (int i = 0; i < TM; i++)
-#pragma unroll
-                for (int j = 0; j < TN; j++) acc[i][j] = mfma(fb[j], fa[i], acc[i][j]);
+            for (int s = 0; s < kBK / 32; s++) {
+                read(cur, s, fa[0], fb[0]);
+                multiply(fa[0], fb[0]);
+            }
         }
     }
     __syncthreads();

