@@ -585,7 +585,7 @@ int heddle_profile_info_get(const heddle_profile *p, heddle_profile_info *info);
 #define HEDDLE_A_SILU      4   /* z / (1 + exp(-z)) */
 
 #define HEDDLE_MAX_LD      (1 << 22)
-#define HEDDLE_MAX_GROUPS  65536
+#define HEDDLE_MAX_GROUPS  65535
 
 /* Y = act(Z) + R with Z = X W^T + b, and its gradients. */
 typedef struct heddle_linear_desc {

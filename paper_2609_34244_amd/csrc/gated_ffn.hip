@@ -58,15 +58,18 @@ template <typename T, typename Epi, bool BCOL>
 static int hidden(const Operand &a, const Operand &b, int64_t t, int64_t f, int64_t k, int groups, const int32_t *offsets,
                   const Epi &epi, Scratch &s, bool run, hipStream_t stream)
 {
+    const bool skinny = !BCOL && is_skinny(t, offsets ? groups : 1);
     const Shape sh = shape_of(t, f, k, offsets ? groups : 1, Epi::gated, false);
     Args x = {};
-    x.partial = (float *)s.take(partial_bytes(sh, t, f, Epi::gated));
+    if (!skinny) x.partial = (float *)s.take(partial_bytes(sh, t, f, Epi::gated));
     if (!run || t == 0) return HEDDLE_OK;
     x.a = a.p, x.lda = a.ld;
     x.b = b.p, x.ldb = b.ld, x.stride_b = b.stride;
     x.M = (int)t, x.N = (int)f, x.K = (int)k, x.F = (int)f;
     x.offsets = offsets;
     x.groups = offsets ? groups : 1;
+    if constexpr (!BCOL)
+        if (skinny) return launch_skinny<T>(x, epi, stream);
     return launch_gemm<false, BCOL, kGroupRows, T>(x, sh, epi, stream);
 }
 
@@ -75,9 +78,12 @@ template <typename T> static int forward(const heddle_gated_ffn_desc *d, Scratch
     const int groups = d->d_offsets ? d->groups : 1;
     if (d->t == 0) return HEDDLE_OK;
     Operand x = {d->x, d->ldx, 0}, wi = {d->w_in, d->ldw_in, d->stride_in}, wo = {d->w_out, d->ldw_out, d->stride_out};
-    int rc = copy_rows(x, d->t, d->d, 1, s, run, stream);
-    if (rc == HEDDLE_OK) rc = copy_rows(wi, 2 * d->f, d->d, groups, s, run, stream);
-    if (rc == HEDDLE_OK) rc = copy_rows(wo, d->d, d->f, groups, s, run, stream);
+    int rc = HEDDLE_OK;
+    if (!is_skinny(d->t, groups)) {
+        rc = copy_rows(x, d->t, d->d, 1, s, run, stream);
+        if (rc == HEDDLE_OK) rc = copy_rows(wi, 2 * d->f, d->d, groups, s, run, stream);
+        if (rc == HEDDLE_OK) rc = copy_rows(wo, d->d, d->f, groups, s, run, stream);
+    }
     if (rc) return rc;
     EpiGated<T> e = {};
     e.ldh = scratch_ld(d->f), e.h = (T *)s.take((size_t)d->t * e.ldh * 2), e.wide_h = 8;

@@ -3,6 +3,7 @@
 #pragma once
 
 #include "gemm.h"
+#include "skinny.h"
 
 namespace heddle {
 namespace mm {

@@ -171,15 +171,17 @@ template <typename T>
 int product(bool cols_b, const Operand &a, const Operand &b, int64_t m, int64_t n, int64_t k, int groups,
             const int32_t *offsets, EpiLinear<T> epi, Scratch &s, bool run, hipStream_t stream)
 {
+    const bool skinny = !cols_b && is_skinny(m, offsets ? groups : 1);
     const Shape sh = shape_of(m, n, k, offsets ? groups : 1, false, false);
     Args x = {};
-    x.partial = (float *)s.take(partial_bytes(sh, m, n, false));
+    if (!skinny) x.partial = (float *)s.take(partial_bytes(sh, m, n, false));
     if (!run || m == 0) return HEDDLE_OK;
     x.a = a.p, x.lda = a.ld;
     x.b = b.p, x.ldb = b.ld, x.stride_b = b.stride;
     x.M = (int)m, x.N = (int)n, x.K = (int)k;
     x.offsets = offsets;
     x.groups = offsets ? groups : 1;
+    if (skinny) return launch_skinny<T>(x, epi, stream);
     return cols_b ? launch_gemm<false, true, kGroupRows, T>(x, sh, epi, stream)
                   : launch_gemm<false, false, kGroupRows, T>(x, sh, epi, stream);
 }
@@ -254,8 +256,9 @@ template <typename T> static int forward(const heddle_linear_desc *d, Scratch &s
 {
     const int groups = d->d_offsets ? d->groups : 1;
     Operand x = {d->x, d->ldx, 0}, w = {d->w, d->ldw, d->stride_w};
-    int rc = copy_rows(x, d->m, d->k, 1, s, run, stream);
-    if (rc == HEDDLE_OK && d->m > 0) rc = copy_rows(w, d->n, d->k, groups, s, run, stream);
+    int rc = HEDDLE_OK;
+    if (!is_skinny(d->m, groups)) rc = copy_rows(x, d->m, d->k, 1, s, run, stream);
+    if (rc == HEDDLE_OK && !is_skinny(d->m, groups)) rc = copy_rows(w, d->n, d->k, groups, s, run, stream);
     if (rc) return rc;
     EpiLinear<T> e = plain_output<T>(d->y, d->ldy, d->n);
     e.pre = (T *)d->preact, e.ldp = d->ldp, e.wide_p = width_of(d->preact, d->ldp);

@@ -1,0 +1,167 @@
+// Products with few rows of X (single tokens): Y[m][n] = sum over k of X[m][k] W[n][k].
+//
+// Bound by reading W once. A workgroup of eight wavefronts takes 16 rows of W
+// (gated: 16 gate and 16 up rows) and every row of X, at most 16 kBlocks at a time; each
+// wavefront takes an eighth of k. W goes from memory straight to the registers that the
+// matrix instruction reads (16 rows x 32 k, lane = row, 16 bytes of k), U pieces of W in
+// flight per lane, and X, which the caches hold, beside it. The eight sums meet in LDS in a
+// fixed order. Loads need only the alignment of a value, so no operand is copied.
+//
+// Groups: a workgroup takes the j-th group that has rows; there are at most as many as rows.
+#pragma once
+
+#include "gemm.h"
+
+namespace heddle {
+namespace mm {
+
+__device__ inline f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+__device__ inline f32x4 mfma16(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+
+// group j of those with rows; false past the last one
+__device__ inline bool find_group(const int32_t *offsets, int groups, int total, int j, int &g, int &lo, int &hi)
+{
+    const int lane = threadIdx.x & 63;
+    for (int g0 = 0; g0 < groups; g0 += 64) {
+        int a = 0, b = 0;
+        if (g0 + lane < groups) group_range(offsets, g0 + lane, total, a, b);
+        uint64_t has = __ballot(b > a);
+        const int n = __popcll(has);
+        if (j < n) {
+            for (; j > 0; j--) has &= has - 1;
+            const int l = __builtin_ctzll(has);
+            g = __builtin_amdgcn_readfirstlane(g0 + l);
+            lo = __builtin_amdgcn_readfirstlane(__shfl(a, l));
+            hi = __builtin_amdgcn_readfirstlane(__shfl(b, l));
+            return true;
+        }
+        j -= n;
+    }
+    return false;
+}
+
+template <typename T> __device__ inline typename pack8<T>::type load_any(const T *p)
+{
+    typename pack8<T>::type v;
+    __builtin_memcpy(&v, p, 16);
+    return v;
+}
+// the values with index below count; the others are zero and not read
+template <typename T> __device__ inline typename pack8<T>::type load_some(const T *p, int count)
+{
+    typename pack8<T>::type v;
+#pragma unroll
+    for (int i = 0; i < 8; i++) v[i] = i < count ? p[i] : (T)0.0f;
+    return v;
+}
+
+constexpr int kSkinnyWaves = 8;
+
+template <int MB, typename T, typename Epi> __global__ void __launch_bounds__(kSkinnyWaves * 64) skinny_kernel(Args x, Epi epi)
+{
+    constexpr bool PAIR = Epi::gated;
+    constexpr int P = PAIR ? 2 : 1, U = MB * P > 2 ? 4 : 8;
+    typedef typename pack8<T>::type frag;
+    __shared__ float part[kSkinnyWaves][P * MB * 256], sum[P * MB * 256];
+    const int lane = threadIdx.x & 63, i = lane & 15, kg = (lane >> 4) * 8;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    int g = 0, lo = 0, hi = x.M;
+    if (x.offsets && !find_group(x.offsets, x.groups, x.M, blockIdx.y, g, lo, hi)) return;
+    const int n0 = blockIdx.x * 16;
+    const T *w = (const T *)x.b + (int64_t)g * x.stride_b + (int64_t)(n0 + min(i, x.N - 1 - n0)) * x.ldb;
+    const int64_t up = PAIR ? (int64_t)x.F * x.ldb : 0;
+    // whole 32-k steps of this wavefront, and the last, partial one
+    const int steps = x.K / 32, each = (steps + kSkinnyWaves - 1) / kSkinnyWaves;
+    const int first = min(wave * each, steps), last = min(first + each, steps);
+    for (int m0 = lo; m0 < hi; m0 += 16 * MB) {
+        const T *xr[MB];
+#pragma unroll
+        for (int b = 0; b < MB; b++) xr[b] = (const T *)x.a + (int64_t)min(m0 + b * 16 + i, hi - 1) * x.lda;
+        f32x4 acc[P][MB];
+#pragma unroll
+        for (int p = 0; p < P; p++)
+#pragma unroll
+            for (int b = 0; b < MB; b++) acc[p][b] = f32x4{0, 0, 0, 0};
+        int s = first;
+        for (; s + U <= last; s += U) {
+            frag fw[P][U], fx[MB][U];
+#pragma unroll
+            for (int u = 0; u < U; u++) {
+                const int k = (s + u) * 32 + kg;
+#pragma unroll
+                for (int p = 0; p < P; p++) fw[p][u] = load_any(w + p * up + k);
+#pragma unroll
+                for (int b = 0; b < MB; b++) fx[b][u] = load_any(xr[b] + k);
+            }
+#pragma unroll
+            for (int u = 0; u < U; u++)
+#pragma unroll
+                for (int p = 0; p < P; p++)
+#pragma unroll
+                    for (int b = 0; b < MB; b++) acc[p][b] = mfma16(fw[p][u], fx[b][u], acc[p][b]);
+        }
+        for (; s < last; s++) {
+            const int k = s * 32 + kg;
+#pragma unroll
+            for (int p = 0; p < P; p++) {
+                const frag fw = load_any(w + p * up + k);
+#pragma unroll
+                for (int b = 0; b < MB; b++) acc[p][b] = mfma16(fw, load_any(xr[b] + k), acc[p][b]);
+            }
+        }
+        if (wave == kSkinnyWaves - 1 && x.K % 32) {
+            const int k = steps * 32 + kg, count = x.K - k;
+#pragma unroll
+            for (int p = 0; p < P; p++) {
+                const frag fw = load_some(w + p * up + k, count);
+#pragma unroll
+                for (int b = 0; b < MB; b++) acc[p][b] = mfma16(fw, load_some(xr[b] + k, count), acc[p][b]);
+            }
+        }
+        // a lane holds row i of X and rows 4 (lane / 16) .. + 3 of W: [p][b][row of X][row of W]
+#pragma unroll
+        for (int p = 0; p < P; p++)
+#pragma unroll
+            for (int b = 0; b < MB; b++) *(f32x4 *)&part[wave][((p * MB + b) * 16 + i) * 16 + (lane >> 4) * 4] = acc[p][b];
+        __syncthreads();
+        for (int c = threadIdx.x; c < P * MB * 256; c += kSkinnyWaves * 64) {
+            float v = 0;
+#pragma unroll
+            for (int q = 0; q < kSkinnyWaves; q++) v += part[q][c];
+            sum[c] = v;
+        }
+        __syncthreads();
+        if (threadIdx.x < MB * 32) {
+            const int r = threadIdx.x >> 1, n = n0 + (threadIdx.x & 1) * 8, m = m0 + r;
+            if (m < hi && n < x.N) {
+                float v[8], u[8];
+#pragma unroll
+                for (int q = 0; q < 8; q++) {
+                    v[q] = sum[r * 16 + (threadIdx.x & 1) * 8 + q];
+                    if (PAIR) u[q] = sum[MB * 256 + r * 16 + (threadIdx.x & 1) * 8 + q];
+                }
+                if constexpr (PAIR) epi(m, n, g, v, u);
+                else epi(m, n, g, v);
+            }
+        }
+    }
+}
+
+// few enough rows for it: its time is W's, while the tiles' grows with what they leave empty
+inline bool is_skinny(int64_t m, int groups) { return groups > 1 ? m <= 8 * (int64_t)groups : m <= 32; }
+
+template <typename T, typename Epi> inline int launch_skinny(const Args &x, const Epi &epi, hipStream_t stream)
+{
+    const unsigned blocks = (unsigned)((x.N + 15) / 16);
+    const unsigned groups = x.offsets ? (unsigned)(x.groups < x.M ? x.groups : x.M) : 1;
+    const bool one = x.offsets || x.M <= 16;
+    if (one)
+        hipLaunchKernelGGL((skinny_kernel<1, T, Epi>), dim3(blocks, groups), dim3(kSkinnyWaves * 64), 0, stream, x, epi);
+    else
+        hipLaunchKernelGGL((skinny_kernel<2, T, Epi>), dim3(blocks, groups), dim3(kSkinnyWaves * 64), 0, stream, x, epi);
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess ? HEDDLE_OK : hip_fail(e, "skinny_kernel");
+}
+
+}  // namespace mm
+}  // namespace heddle
