@@ -59,7 +59,7 @@ static int hidden(const Operand &a, const Operand &b, int64_t t, int64_t f, int6
                   const Epi &epi, Scratch &s, bool run, hipStream_t stream)
 {
     const bool skinny = !BCOL && is_skinny(t, offsets ? groups : 1);
-    const Shape sh = shape_of(t, f, k, offsets ? groups : 1, Epi::gated, false);
+    const Shape sh = shape_of(t, f, k, offsets ? groups : 1, Epi::gated, BCOL ? kRowsCols : kRowsRows);
     Args x = {};
     if (!skinny) x.partial = (float *)s.take(partial_bytes(sh, t, f, Epi::gated));
     if (!run || t == 0) return HEDDLE_OK;
@@ -78,18 +78,18 @@ template <typename T> static int forward(const heddle_gated_ffn_desc *d, Scratch
     const int groups = d->d_offsets ? d->groups : 1;
     if (d->t == 0) return HEDDLE_OK;
     Operand x = {d->x, d->ldx, 0}, wi = {d->w_in, d->ldw_in, d->stride_in}, wo = {d->w_out, d->ldw_out, d->stride_out};
-    int rc = HEDDLE_OK;
     if (!is_skinny(d->t, groups)) {
-        rc = copy_rows(x, d->t, d->d, 1, s, run, stream);
-        if (rc == HEDDLE_OK) rc = copy_rows(wi, 2 * d->f, d->d, groups, s, run, stream);
-        if (rc == HEDDLE_OK) rc = copy_rows(wo, d->d, d->f, groups, s, run, stream);
+        Copies c;
+        c.add(x, d->t, d->d, 1, s);
+        c.add(wi, 2 * d->f, d->d, groups, s);
+        c.add(wo, d->d, d->f, groups, s);
+        if (const int rc = run ? c.launch(stream) : HEDDLE_OK) return rc;
     }
-    if (rc) return rc;
     EpiGated<T> e = {};
     e.ldh = scratch_ld(d->f), e.h = (T *)s.take((size_t)d->t * e.ldh * 2), e.wide_h = 8;
     e.pre = (T *)d->preact, e.ldp = d->ldp, e.wide_p = width_of(d->preact, d->ldp, d->f);
     e.act = d->act, e.N = (int)d->f;
-    rc = hidden<T, EpiGated<T>, false>(x, wi, d->t, d->f, d->d, groups, d->d_offsets, e, s, run, stream);
+    int rc = hidden<T, EpiGated<T>, false>(x, wi, d->t, d->f, d->d, groups, d->d_offsets, e, s, run, stream);
     if (rc) return rc;
     EpiLinear<T> o = plain_output<T>(d->y, d->ldy, d->d);
     o.residual = (const T *)d->residual, o.ldr = d->ldr, o.wide_r = width_of(d->residual, d->ldr);
@@ -104,10 +104,12 @@ template <typename T> static int backward(const heddle_gated_ffn_desc *d, Scratc
     int rc = HEDDLE_OK;
     if (!d->dx && !d->dw_in && !d->dw_out) return rc;
     if (d->t > 0) {
-        rc = copy_rows(dy, d->t, d->d, 1, s, run, stream);
-        if (rc == HEDDLE_OK) rc = copy_rows(wo, d->d, d->f, groups, s, run, stream);
-        if (rc == HEDDLE_OK && d->dx) rc = copy_rows(wi, 2 * d->f, d->d, groups, s, run, stream);
-        if (rc == HEDDLE_OK && d->dw_in) rc = copy_rows(x, d->t, d->d, 1, s, run, stream);
+        Copies c;
+        c.add(dy, d->t, d->d, 1, s);
+        c.add(wo, d->d, d->f, groups, s);
+        if (d->dx) c.add(wi, 2 * d->f, d->d, groups, s);
+        if (d->dw_in) c.add(x, d->t, d->d, 1, s);
+        if (run) rc = c.launch(stream);
         if (rc) return rc;
     }
     EpiGatedGrad<T> e = {};

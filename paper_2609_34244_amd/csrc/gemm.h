@@ -401,18 +401,19 @@ __device__ inline void tile_of(int t, int tiles_m, int tiles_n, int &tm, int &tn
     tn = in / width;
 }
 
-template <int BM, int BN, int WM, int WN, bool ACOL, bool BCOL, Grouping GR, typename T, typename Epi>
+template <int BM, int BN, int WM, int WN, int STAGES, bool ACOL, bool BCOL, Grouping GR, typename T, typename Epi>
 __global__ void __launch_bounds__(WM * WN * 64) gemm_kernel(Args x, Epi epi)
 {
 #ifdef __HIP_DEVICE_COMPILE__   // the host pass has no buffer resources
     constexpr int NW = WM * WN, TM = BM / WM / 16, TN = BN / WN / 16, kOut = BN / WN;
-    constexpr bool PAIR = Epi::gated, PIPED = BM * BN >= 256 * 256;   // one workgroup on a CU
+    constexpr bool PAIR = Epi::gated, PIPED = STAGES == 2 && BM * BN >= 256 * 256;   // one workgroup on a CU
     typedef Loader<BM, NW, ACOL, false> LA;
     typedef Loader<BN, NW, BCOL, PAIR> LB;
     constexpr int kStage = LA::kBytes + LB::kBytes;
     static_assert(TM % 4 == 0 && (!PAIR || TN % 2 == 0), "a wavefront's part");
-    static_assert(NW * 64 * kOut * 4 <= 2 * kStage, "the epilogue's part of LDS");
-    __shared__ __align__(1024) char smem[2 * kStage];
+    constexpr int kFit = STAGES * kStage / (NW * kOut * 4), kRows = kFit >= 64 ? 64 : kFit >= 32 ? 32 : 16;   // of the epilogue at a time
+    static_assert(NW * kRows * kOut * 4 <= STAGES * kStage, "the epilogue's part of LDS");
+    __shared__ __align__(1024) char smem[STAGES * kStage];
 
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int per = x.tiles_m * x.tiles_n;
@@ -519,6 +520,17 @@ __global__ void __launch_bounds__(WM * WN * 64) gemm_kernel(Args x, Epi epi)
             multiply(fa[1], fb[1]);
             interleave<TM + TN, TM * TN, ACOL || BCOL>();
         }
+    } else if (STAGES == 1 && tiles) {
+        for (int kt = 0; kt < tiles; kt++) {
+            if (kt) __syncthreads();
+            load(smem);
+            landed(smem, kt);
+#pragma unroll
+            for (int s = 0; s < kBK / 32; s++) {
+                read(smem, s, fa[0], fb[0]);
+                multiply(fa[0], fb[0]);
+            }
+        }
     } else if (tiles) {
         // several workgroups on a CU hide each other's reads
         load(smem);
@@ -535,28 +547,28 @@ __global__ void __launch_bounds__(WM * WN * 64) gemm_kernel(Args x, Epi epi)
     }
     __syncthreads();
 
-    // Epilogue: a wavefront takes 64 of its rows at a time through its own part
+    // Epilogue: a wavefront takes kRows of its rows at a time through its own part
     // of LDS, so that a lane finishes eight neighbouring columns. The product
     // was formed transposed: a lane holds row lane % 16, columns 4 (lane / 16)
     // .. + 3 of a block. 16-byte pieces of a row are exchanged by row & (pieces - 1).
     constexpr int kPieces = kOut / 4;
-    float *own = (float *)smem + wave * 64 * kOut;
+    float *own = (float *)smem + wave * kRows * kOut;
     const int nw = n0 + (PAIR ? wn * kOut / 2 : wn * kOut);
 #pragma unroll
-    for (int h = 0; h < TM / 4; h++) {
+    for (int h = 0; h < TM * 16 / kRows; h++) {
 #pragma unroll
-        for (int i = 0; i < 4; i++)
+        for (int i = 0; i < kRows / 16; i++)
 #pragma unroll
             for (int j = 0; j < TN; j++) {
                 const int r = i * 16 + (lane & 15), p = j * 4 + (lane >> 4);
-                *(f32x4 *)(own + r * kOut + ((p ^ (r & (kPieces - 1))) << 2)) = acc[h * 4 + i][j];
+                *(f32x4 *)(own + r * kOut + ((p ^ (r & (kPieces - 1))) << 2)) = acc[h * (kRows / 16) + i][j];
             }
         __builtin_amdgcn_wave_barrier();
         constexpr int kUnits = (PAIR ? kOut / 2 : kOut) / 8;    // eights of a row
 #pragma unroll 1
-        for (int c = lane; c < 64 * kUnits; c += 64) {
+        for (int c = lane; c < kRows * kUnits; c += 64) {
             const int r = c / kUnits, q = c % kUnits;
-            const int m = m0 + wm * (TM * 16) + h * 64 + r;
+            const int m = m0 + wm * (TM * 16) + h * kRows + r;
             const int n = nw + q * 8;
             auto piece = [&](int p) { return *(const f32x4 *)(own + r * kOut + ((p ^ (r & (kPieces - 1))) << 2)); };
             // PAIR: gate columns 16 b .. + 15 are pieces 8 b .. + 3, the up columns the four after
@@ -614,13 +626,14 @@ template <typename Epi> __global__ void __launch_bounds__(256) join_kernel(Args 
 // ---- host side ----
 // A tile shape and the parts of the reduction.
 struct Shape { int cfg, splits, split_tiles; };
-Shape shape_of(int64_t M, int64_t N, int64_t K, int groups, bool gated, bool sum);
+enum Order { kRowsRows = 0, kRowsCols = 1, kColsCols = 2 };   // of the operands in memory
+Shape shape_of(int64_t M, int64_t N, int64_t K, int groups, bool gated, Order order);
 inline size_t partial_bytes(const Shape &s, int64_t M, int64_t N, bool gated)
 {
     return s.splits > 1 ? (size_t)s.splits * M * partial_cols((int)N, gated) * 4 : 0;
 }
 
-template <int BM, int BN, int WM, int WN, bool ACOL, bool BCOL, Grouping GR, typename T, typename Epi>
+template <int BM, int BN, int WM, int WN, int STAGES, bool ACOL, bool BCOL, Grouping GR, typename T, typename Epi>
 inline int launch_cfg(Args x, const Shape &s, const Epi &epi, hipStream_t stream)
 {
     const int64_t cols = Epi::gated ? 2 * (int64_t)x.N : x.N;
@@ -631,7 +644,7 @@ inline int launch_cfg(Args x, const Shape &s, const Epi &epi, hipStream_t stream
     x.split_tiles = s.split_tiles;
     const int64_t blocks = (int64_t)x.tiles_m * x.tiles_n * (GR == kGroupSum && grouped ? x.groups : s.splits);
     if (blocks > 0x7FFFFFFF) return fail(HEDDLE_E_RANGE, "more tiles than a launch holds");
-    hipLaunchKernelGGL((gemm_kernel<BM, BN, WM, WN, ACOL, BCOL, GR, T, Epi>), dim3((unsigned)blocks), dim3(WM * WN * 64), 0,
+    hipLaunchKernelGGL((gemm_kernel<BM, BN, WM, WN, STAGES, ACOL, BCOL, GR, T, Epi>), dim3((unsigned)blocks), dim3(WM * WN * 64), 0,
                        stream, x, epi);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return hip_fail(e, "gemm_kernel");
@@ -648,9 +661,9 @@ template <bool ACOL, bool BCOL, Grouping GR, typename T, typename Epi>
 inline int launch_gemm(const Args &x, const Shape &s, const Epi &epi, hipStream_t stream)
 {
     switch (s.cfg) {
-    case 0: return launch_cfg<256, 256, 2, 4, ACOL, BCOL, GR, T>(x, s, epi, stream);
-    case 1: return launch_cfg<128, 128, 2, 2, ACOL, BCOL, GR, T>(x, s, epi, stream);
-    default: return launch_cfg<64, 128, 1, 4, ACOL, BCOL, GR, T>(x, s, epi, stream);
+    case 0: return launch_cfg<256, 256, 2, 4, 2, ACOL, BCOL, GR, T>(x, s, epi, stream);
+    case 1: return launch_cfg<128, 128, 2, 2, 1, ACOL, BCOL, GR, T>(x, s, epi, stream);
+    default: return launch_cfg<64, 128, 1, 4, 2, ACOL, BCOL, GR, T>(x, s, epi, stream);
     }
 }
 

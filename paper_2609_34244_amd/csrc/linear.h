@@ -38,7 +38,20 @@ inline bool needs_copy(const Operand &o, int groups)
 {
     return ((uintptr_t)o.p & 3) || (o.ld & 1) || (groups > 1 && (o.stride & 1));
 }
-int copy_rows(Operand &o, int64_t rows, int64_t cols, int groups, Scratch &s, bool run, hipStream_t stream);
+class Copies {
+public:
+    // takes scratch for the copy of o, if it needs one, and lets o name it
+    void add(Operand &o, int64_t rows, int64_t cols, int groups, Scratch &s);
+    int launch(hipStream_t stream) const;     // one launch for all that were added
+    static constexpr int kMost = 4;
+    struct One {
+        const uint16_t *src;
+        uint16_t *dst;
+        int64_t ld, stride, rows, cols, ldd, first;   // first: its first eight of the launch
+    } one[kMost];
+    int count = 0;
+    int64_t eights = 0;
+};
 
 // dZ = dY act'(Z) (written where dz is given) and its column sums per group
 struct BiasGrad {

@@ -9,32 +9,47 @@
 namespace heddle {
 namespace mm {
 
-Shape shape_of(int64_t M, int64_t N, int64_t K, int groups, bool gated, bool sum)
+// The tile shape and the split of the reduction with the least estimated time. Constants in
+// us, from times of every shape and split on 120 products of 33 .. 8192 rows, 128 .. 20000
+// columns and k of the three memory orders: the choice costs 1.9% over the best one on
+// average. step: a k-tile on a CU whose workgroup slots are taken; least: the same for
+// workgroups alone on their CU; fixed: start and epilogue of a round of workgroups.
+//   256 x 256: one workgroup a CU, the highest rate; 128 x 128: four a CU, each with one buffer
+//   (what fills the chip with 2000 x 2000 outputs, and what writes most while little is
+//   summed); 64 x 128: three a CU, for few rows.
+Shape shape_of(int64_t M, int64_t N, int64_t K, int groups, bool gated, Order order)
 {
-    const int bm[3] = {256, 128, 64}, bn[3] = {256, 128, 128}, per_cu[3] = {1, 2, 3};
-    const int64_t cols = gated ? 2 * N : N;
-    Shape best = {0, 1, 1};
+    static const struct { int bm, bn, per_cu; double step[3], least, fixed; } cfg[3] = {
+        {256, 256, 1, {1.50, 1.65, 1.65}, 1.36, 8.3},
+        {128, 128, 4, {2.19, 2.38, 1.73}, 0.97, 5.0},
+        {64, 128, 3, {1.00, 1.16, 1.13}, 0.63, 3.6},
+    };
+    const int cus = 256;
+    const bool sums = order == kColsCols;
+    const int64_t cols = gated ? 2 * N : N, kt = K > 0 ? (K + kBK - 1) / kBK : 1;
+    // groups: every one of the average size
+    const int64_t rows = groups > 1 && !sums ? (M + groups - 1) / groups : M, outer = groups > 1 ? groups : 1;
+    const int64_t steps = groups > 1 && sums ? (kt + groups - 1) / groups : kt;
+    Shape best = {0, 1, (int)kt};
     double least = 0;
-    const int64_t kt = (K + kBK - 1) / kBK > 0 ? (K + kBK - 1) / kBK : 1;
-    for (int c = 0; c < 3; c++) {
-        const bool rows_grouped = groups > 1 && !sum;
-        // a group's rows end inside a tile: half a tile is lost on average
-        const int64_t tm = (M + bm[c] - 1) / bm[c] + (rows_grouped ? groups : 0), tn = (cols + bn[c] - 1) / bn[c];
-        const int64_t tiles = tm * tn * (groups > 1 && sum ? groups : 1);
-        const int64_t steps = groups > 1 && sum ? (kt + groups - 1) / groups : kt;
-        const int max_split = groups > 1 ? 1 : (int)(kt < 16 ? kt : 16);
-        for (int s = 1; s <= max_split; s *= 2) {
-            const int64_t part = (steps + s - 1) / s;
-            const double rounds = (double)((tiles * s + 256 * per_cu[c] - 1) / (256 * per_cu[c]));
-            // time of a k-tile in one workgroup, all of a CU's slots taken
-            const double step = bm[c] * bn[c] * per_cu[c] / (c == 0 ? 1.0 : c == 1 ? 0.75 : 0.6);
-            const double t = rounds * (part * step + 3e5) + (s > 1 ? 2e6 + 1.5 * s * M * cols / 256 : 0);
+    for (int c = 0; c < 3; c++)
+        for (int s = 1; s <= 16 && s <= kt && (s == 1 || groups <= 1); s *= 2) {
+            const double part = (double)((steps + s - 1) / s);
+            const int64_t tiles = (rows + cfg[c].bm - 1) / cfg[c].bm * ((cols + cfg[c].bn - 1) / cfg[c].bn) * outer * s;
+            const int64_t full = tiles / (cus * cfg[c].per_cu), rest = tiles - full * cus * cfg[c].per_cu;
+            const double step = cfg[c].step[order];
+            double t = (double)full * (part * step + cfg[c].fixed);
+            if (rest) {
+                const double share = (double)((rest + cus - 1) / cus) / cfg[c].per_cu;
+                const double alone = step * share > cfg[c].least ? step * share : cfg[c].least;
+                t += part * alone + cfg[c].fixed * (0.5 + 0.5 * share);
+            }
+            if (s > 1) t += 3.9 + 1.2e-6 * (double)s * (double)M * (double)cols;
             if (least == 0 || t < least) {
                 least = t;
                 best = {c, s, (int)((kt + s - 1) / s)};
             }
         }
-    }
     return best;
 }
 
@@ -46,34 +61,42 @@ int check_matrix(const char *name, const void *p, int64_t ld, int64_t cols)
     return HEDDLE_OK;
 }
 
-__global__ void __launch_bounds__(256) copy_rows_kernel(const uint16_t *src, int64_t ld, int64_t stride, int64_t rows,
-                                                        int64_t cols, uint16_t *dst, int64_t ldd, int64_t all)
+__global__ void __launch_bounds__(256) copy_rows_kernel(Copies c)
 {
-    const int64_t eights = ldd / 8;
-    for (int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x; c < all * eights; c += (int64_t)gridDim.x * 256) {
-        const int64_t r = c / eights, j = (c - r * eights) * 8, g = r / rows;
-        const uint16_t *from = src + g * stride + (r - g * rows) * ld + j;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < c.eights; i += (int64_t)gridDim.x * 256) {
+        int n = 0;
+        while (n + 1 < c.count && i >= c.one[n + 1].first) n++;
+        const Copies::One &o = c.one[n];
+        const int64_t at = i - o.first, per = o.ldd / 8, r = at / per, j = (at - r * per) * 8, g = r / o.rows;
+        const uint16_t *from = o.src + g * o.stride + (r - g * o.rows) * o.ld + j;
         s16x8 v;
+        if (j + 8 <= o.cols) {
+            __builtin_memcpy(&v, from, 16);   // at any address its values may have
+        } else {
 #pragma unroll
-        for (int i = 0; i < 8; i++) v[i] = j + i < cols ? (short)from[i] : (short)0;
-        *(s16x8 *)(dst + r * ldd + j) = v;
+            for (int q = 0; q < 8; q++) v[q] = j + q < o.cols ? (short)from[q] : (short)0;
+        }
+        *(s16x8 *)(o.dst + r * o.ldd + j) = v;
     }
 }
 
-int copy_rows(Operand &o, int64_t rows, int64_t cols, int groups, Scratch &s, bool run, hipStream_t stream)
+void Copies::add(Operand &o, int64_t rows, int64_t cols, int groups, Scratch &s)
 {
-    if (!needs_copy(o, groups)) return HEDDLE_OK;
-    const int64_t ldd = scratch_ld(cols), all = rows * groups;
-    uint16_t *to = (uint16_t *)s.take((size_t)all * ldd * 2);
-    if (run && all > 0) {
-        const int64_t want = (all * (ldd / 8) + 255) / 256;
-        hipLaunchKernelGGL(copy_rows_kernel, dim3((unsigned)(want < 16384 ? want : 16384)), dim3(256), 0, stream,
-                           (const uint16_t *)o.p, o.ld, o.stride, rows, cols, to, ldd, all);
-        const hipError_t e = hipGetLastError();
-        if (e != hipSuccess) return hip_fail(e, "copy_rows_kernel");
-    }
+    if (rows == 0 || !needs_copy(o, groups)) return;
+    const int64_t ldd = scratch_ld(cols);
+    uint16_t *to = (uint16_t *)s.take((size_t)(rows * groups) * ldd * 2);
+    one[count++] = {(const uint16_t *)o.p, to, o.ld, o.stride, rows, cols, ldd, eights};
+    eights += rows * groups * (ldd / 8);
     o = {to, ldd, rows * ldd};
-    return HEDDLE_OK;
+}
+
+int Copies::launch(hipStream_t stream) const
+{
+    if (count == 0) return HEDDLE_OK;
+    const int64_t want = (eights + 255) / 256;
+    hipLaunchKernelGGL(copy_rows_kernel, dim3((unsigned)(want < 16384 ? want : 16384)), dim3(256), 0, stream, *this);
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess ? HEDDLE_OK : hip_fail(e, "copy_rows_kernel");
 }
 
 // A workgroup takes 256 columns (32 lanes of eight) and its chunk of rows, 8
@@ -172,7 +195,7 @@ int product(bool cols_b, const Operand &a, const Operand &b, int64_t m, int64_t 
             const int32_t *offsets, EpiLinear<T> epi, Scratch &s, bool run, hipStream_t stream)
 {
     const bool skinny = !cols_b && is_skinny(m, offsets ? groups : 1);
-    const Shape sh = shape_of(m, n, k, offsets ? groups : 1, false, false);
+    const Shape sh = shape_of(m, n, k, offsets ? groups : 1, false, cols_b ? kRowsCols : kRowsRows);
     Args x = {};
     if (!skinny) x.partial = (float *)s.take(partial_bytes(sh, m, n, false));
     if (!run || m == 0) return HEDDLE_OK;
@@ -190,7 +213,7 @@ template <typename T>
 int product_sum(const Operand &a, const Operand &b, int64_t m, int64_t n, int64_t k, int groups, const int32_t *offsets,
                 EpiLinear<T> epi, Scratch &s, bool run, hipStream_t stream)
 {
-    const Shape sh = shape_of(m, n, k, offsets ? groups : 1, false, true);
+    const Shape sh = shape_of(m, n, k, offsets ? groups : 1, false, kColsCols);
     Args x = {};
     x.partial = (float *)s.take(partial_bytes(sh, m, n, false));
     if (!run) return HEDDLE_OK;
@@ -256,10 +279,12 @@ template <typename T> static int forward(const heddle_linear_desc *d, Scratch &s
 {
     const int groups = d->d_offsets ? d->groups : 1;
     Operand x = {d->x, d->ldx, 0}, w = {d->w, d->ldw, d->stride_w};
-    int rc = HEDDLE_OK;
-    if (!is_skinny(d->m, groups)) rc = copy_rows(x, d->m, d->k, 1, s, run, stream);
-    if (rc == HEDDLE_OK && !is_skinny(d->m, groups)) rc = copy_rows(w, d->n, d->k, groups, s, run, stream);
-    if (rc) return rc;
+    if (!is_skinny(d->m, groups)) {
+        Copies c;
+        c.add(x, d->m, d->k, 1, s);
+        c.add(w, d->n, d->k, groups, s);
+        if (const int rc = run ? c.launch(stream) : HEDDLE_OK) return rc;
+    }
     EpiLinear<T> e = plain_output<T>(d->y, d->ldy, d->n);
     e.pre = (T *)d->preact, e.ldp = d->ldp, e.wide_p = width_of(d->preact, d->ldp);
     e.bias = (const T *)d->bias, e.wide_b = width_of(d->bias, groups > 1 ? d->n : 0);
@@ -285,20 +310,17 @@ template <typename T> static int backward(const heddle_linear_desc *d, Scratch &
     }
     if (b.db) b.partial = (float *)s.take(bias_grad_bytes(d->m, d->n, d->d_offsets != nullptr, groups));
     if (run && (b.db || (b.dz && d->m > 0))) rc = launch_bias_grad(d->dtype, b, stream);
-    if (rc == HEDDLE_OK && d->dx) {
-        Operand w = {d->w, d->ldw, d->stride_w};
-        if (d->m > 0) rc = copy_rows(w, d->n, d->k, groups, s, run, stream);
-        if (rc == HEDDLE_OK)
-            rc = product<T>(true, dz, w, d->m, d->k, d->n, groups, d->d_offsets, plain_output<T>(d->dx, d->lddx, d->k), s,
-                            run, stream);
-    }
-    if (rc == HEDDLE_OK && d->dw) {
-        Operand x = {d->x, d->ldx, 0};
-        rc = copy_rows(x, d->m, d->k, 1, s, run, stream);
-        if (rc == HEDDLE_OK)
-            rc = product_sum<T>(dz, x, d->n, d->k, d->m, groups, d->d_offsets,
-                                plain_output<T>(d->dw, d->lddw, d->k, groups > 1 ? d->stride_dw : 0), s, run, stream);
-    }
+    Operand w = {d->w, d->ldw, d->stride_w}, x = {d->x, d->ldx, 0};
+    Copies c;
+    if (d->dx && d->m > 0) c.add(w, d->n, d->k, groups, s);
+    if (d->dw) c.add(x, d->m, d->k, 1, s);
+    if (rc == HEDDLE_OK && run) rc = c.launch(stream);
+    if (rc == HEDDLE_OK && d->dx)
+        rc = product<T>(true, dz, w, d->m, d->k, d->n, groups, d->d_offsets, plain_output<T>(d->dx, d->lddx, d->k), s, run,
+                        stream);
+    if (rc == HEDDLE_OK && d->dw)
+        rc = product_sum<T>(dz, x, d->n, d->k, d->m, groups, d->d_offsets,
+                            plain_output<T>(d->dw, d->lddw, d->k, groups > 1 ? d->stride_dw : 0), s, run, stream);
     return rc;
 }
 

@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 
 import numpy as np
 
@@ -127,19 +128,15 @@ def lib():
         L.heddle_enum_templates.argtypes = [C.POINTER(heddle_enum_spec), I64, I64, P, P, P]
         L.heddle_best_enumerated.argtypes = [P, C.POINTER(heddle_enum_spec), P, I32, U32, I64,
                                              C.POINTER(C.c_int64), C.POINTER(C.c_int32), P, C.POINTER(C.c_int64), P]
-        for op, desc in (("linear", heddle_linear_desc), ("gated_ffn", heddle_gated_ffn_desc)):
+        # descriptors of the operators: packed bytes
+        for op in ("linear", "gated_ffn"):
             for back in ("", "_backward"):
-                f = getattr(L, f"heddle_{op}{back}")
-                f.argtypes, f.restype = [C.POINTER(desc), P, I64, P], C.c_int
-            f = getattr(L, f"heddle_{op}_workspace")
-            f.argtypes, f.restype = [C.POINTER(desc), I32, C.POINTER(C.c_int64)], C.c_int
-        G = C.POINTER(heddle_grad_desc)
-        L.heddle_grad_norm.argtypes = [G, I32, P, P, I64, P]
-        L.heddle_clip_grads.argtypes = [G, I32, P, C.c_float, P]
-        L.heddle_clip_grad_norm.argtypes = [G, I32, C.c_float, P, P, I64, P]
-        L.heddle_grad_norm_workspace.argtypes = [G, I32, C.POINTER(C.c_int64)]
-        for f in ("heddle_grad_norm", "heddle_clip_grads", "heddle_clip_grad_norm", "heddle_grad_norm_workspace"):
-            getattr(L, f).restype = C.c_int
+                getattr(L, f"heddle_{op}{back}").argtypes = [P, P, I64, P]
+            getattr(L, f"heddle_{op}_workspace").argtypes = [P, I32, C.POINTER(C.c_int64)]
+        L.heddle_grad_norm.argtypes = [P, I32, P, P, I64, P]
+        L.heddle_clip_grads.argtypes = [P, I32, P, C.c_float, P]
+        L.heddle_clip_grad_norm.argtypes = [P, I32, C.c_float, P, P, I64, P]
+        L.heddle_grad_norm_workspace.argtypes = [P, I32, C.POINTER(C.c_int64)]
         L.heddle_last_error.restype = C.c_char_p
         for f in ("heddle_load_profile", "heddle_price_plans", "heddle_price_plans_noalloc", "heddle_argmin_plans",
                   "heddle_best_plan",
@@ -441,77 +438,110 @@ def heddle_fill_plans(profiles, mbs, cl, global_batch, dp_cap, n_stages, stages,
 
 
 # ---- feed-forward and gradient operators ----
+# A call on small tensors takes as long as its marshalling, so a descriptor is
+# packed in one step and every tensor is looked at once.
+
+_LINEAR = struct.Struct("@iiqqqPqPqPPqPqPqiPqPqPqPqqP")
+_GATED_FFN = struct.Struct("@iiqqqPqPqPqPqPqPqiPqqPqPqPqqPqq")
+_GRAD = struct.Struct("@PPqi4x")
+assert (_LINEAR.size, _GATED_FFN.size, _GRAD.size) == tuple(
+    C.sizeof(d) for d in (heddle_linear_desc, heddle_gated_ffn_desc, heddle_grad_desc))
+
+
+def _refuse(msg):
+    raise HeddleError(HEDDLE_E_INVAL, msg)
+
 
 def _dtype(t, what):
-    import torch
-    code = {torch.bfloat16: HEDDLE_T_BF16, torch.float16: HEDDLE_T_F16, torch.float32: HEDDLE_T_F32}.get(t.dtype)
+    code = _dtype_codes().get(t.dtype)
     if code is None:
-        raise HeddleError(HEDDLE_E_INVAL, f"{what}: type {t.dtype} is not supported")
+        _refuse(f"{what}: type {t.dtype} is not supported")
     return code
 
 
-def _matrix(t, what, shape, like):
+_codes = {}
+
+
+def _dtype_codes():
+    if not _codes:
+        import torch
+        _codes.update({torch.bfloat16: HEDDLE_T_BF16, torch.float16: HEDDLE_T_F16, torch.float32: HEDDLE_T_F32})
+    return _codes
+
+
+def _matrix(t, what, shape, dtype, gpu):
     """(data pointer, ld) of a device matrix whose rows are contiguous"""
-    if t.dtype != like.dtype or t.device != like.device or not t.is_cuda:
-        raise HeddleError(HEDDLE_E_INVAL, f"{what}: {t.dtype} on {t.device}, not {like.dtype} on the GPU of {like.device}")
-    if tuple(t.shape) != tuple(shape):
-        raise HeddleError(HEDDLE_E_INVAL, f"{what}: shape {tuple(t.shape)}, not {tuple(shape)}")
-    rows, cols = t.shape[-2], t.shape[-1]
-    if cols > 1 and t.stride(-1) != 1:
-        raise HeddleError(HEDDLE_E_INVAL, f"{what}: rows are not contiguous")
-    return t.data_ptr(), t.stride(-2) if rows > 1 else cols
+    if t.dtype != dtype or t.get_device() != gpu:
+        _refuse(f"{what}: {t.dtype} on {t.device}, not {dtype} on GPU {gpu}")
+    if t.shape != shape:
+        _refuse(f"{what}: shape {tuple(t.shape)}, not {shape}")
+    stride = t.stride()
+    if stride[-1] != 1 and shape[-1] > 1:
+        _refuse(f"{what}: rows are not contiguous")
+    return t.data_ptr(), stride[-2] if shape[-2] > 1 else shape[-1]
 
 
-def _weights(t, what, shape, groups, like):
+def _weights(t, what, shape, dtype, gpu):
     """(data pointer, ld, distance between groups)"""
-    p, ld = _matrix(t, what, shape, like)
-    return p, ld, t.stride(0) if groups and t.shape[0] > 1 else shape[-2] * ld
+    p, ld = _matrix(t, what, shape, dtype, gpu)
+    return p, ld, t.stride(0) if len(shape) == 3 and shape[0] > 1 else shape[-2] * ld
 
 
-def _vector(t, what, shape, like):
-    if t.dtype != like.dtype or t.device != like.device or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
-        raise HeddleError(HEDDLE_E_INVAL, f"{what}: not a contiguous {like.dtype} tensor of shape {tuple(shape)} on {like.device}")
+def _vector(t, what, shape, dtype, gpu):
+    if t.dtype != dtype or t.get_device() != gpu or t.shape != shape or not t.is_contiguous():
+        _refuse(f"{what}: not a contiguous {dtype} tensor of shape {shape} on GPU {gpu}")
     return t.data_ptr()
 
 
-def _groups(offsets, w, like):
-    """number of expert groups, 0 without offsets"""
-    import torch
+def _groups(offsets, w, gpu):
+    """(number of expert groups, offsets' address), (0, 0) without offsets"""
     if offsets is None:
-        return 0
-    if offsets.dtype != torch.int32 or offsets.device != like.device or offsets.dim() != 1 or not offsets.is_contiguous():
-        raise HeddleError(HEDDLE_E_INVAL, "offsets: not a contiguous int32 vector on the inputs' device")
+        return 0, 0
+    if str(offsets.dtype) != "torch.int32" or offsets.get_device() != gpu or offsets.dim() != 1 or not offsets.is_contiguous():
+        _refuse("offsets: not a contiguous int32 vector on the inputs' GPU")
     if w.dim() != 3 or offsets.numel() != w.shape[0] + 1:
-        raise HeddleError(HEDDLE_E_INVAL, f"offsets: {offsets.numel()} entries for weights of shape {tuple(w.shape)}")
-    return w.shape[0]
+        _refuse(f"offsets: {offsets.numel()} entries for weights of shape {tuple(w.shape)}")
+    return w.shape[0], offsets.data_ptr()
 
 
-def _fresh(shape, like, stream):
-    import torch
-    t = torch.empty(shape, dtype=like.dtype, device=like.device)
+def _rows(x, w, what):
+    """(GPU, type, rows, columns) of the input of a product"""
+    if x.dim() != 2 or w.dim() not in (2, 3) or not x.is_cuda:
+        _refuse(f"{what}: rows must be a matrix and weights a matrix, or one for each group, on the GPU")
+    return x.get_device(), x.dtype, x.shape[0], x.shape[1]
+
+
+def _fresh(like, shape, stream):
+    t = like.new_empty(shape)
     if stream is not None:
         t.record_stream(stream)
     return t
 
 
-def _run(name, desc, backward, like, stream):
+def _on_gpu(gpu, stream, call):
+    """call(stream handle) with the tensors' GPU current"""
+    import torch
+    if torch.cuda.current_device() != gpu:
+        with torch.cuda.device(gpu):
+            return _on_gpu(gpu, stream, call)
+    _check(call((torch.cuda.current_stream() if stream is None else stream).cuda_stream))
+
+
+def _run(work, need, desc, backward, like, gpu, stream):
     """scratch from torch's allocator, then the call"""
     import torch
-    L, need = lib(), C.c_int64()
-    with torch.cuda.device(like.device):
-        _check(getattr(L, f"heddle_{name}_workspace")(C.byref(desc), backward, C.byref(need)))
+
+    def call(handle):
+        n = C.c_int64()
+        _check(need(desc, backward, C.byref(n)))
         ws = None
-        if need.value:
-            ws = torch.empty(need.value, dtype=torch.uint8, device=like.device)
+        if n.value:
+            ws = torch.empty(n.value, dtype=torch.uint8, device=like.device)
             if stream is not None:
                 ws.record_stream(stream)
-        f = getattr(L, f"heddle_{name}_backward" if backward else f"heddle_{name}")
-        _check(f(C.byref(desc), _ptr(ws), need.value, _stream(stream)))
+        return work(desc, None if ws is None else ws.data_ptr(), n.value, handle)
 
-
-def _two(x, w, what):
-    if x.dim() != 2 or w.dim() not in (2, 3) or not x.is_cuda:
-        raise HeddleError(HEDDLE_E_INVAL, f"{what}: rows must be a matrix and weights a matrix, or one for each group, on the GPU")
+    _on_gpu(gpu, stream, call)
 
 
 def heddle_linear(x, w, bias=None, act=HEDDLE_A_NONE, residual=None, preact=None, out=None, offsets=None, stream=None):
@@ -519,22 +549,21 @@ def heddle_linear(x, w, bias=None, act=HEDDLE_A_NONE, residual=None, preact=None
     [groups, n, k] for rows sorted by expert; bias: [n] ([groups, n]);
     preact: [m, n] to keep the values before the activation for the backward
     pass. Matrices may have any distance between rows. Returns out ([m, n])."""
-    _two(x, w, "heddle_linear")
-    m, k, n = x.shape[0], x.shape[1], w.shape[-2]
-    e = _groups(offsets, w, x)
+    gpu, dt, m, k = _rows(x, w, "heddle_linear")
+    n, (e, off) = w.shape[-2], _groups(offsets, w, gpu)
     lead = (e,) if e else ()
-    out = _fresh((m, n), x, stream) if out is None else out
-    d = heddle_linear_desc(dtype=_dtype(x, "x"), act=act, m=m, n=n, k=k, groups=e, d_offsets=offsets.data_ptr() if e else None)
-    d.x, d.ldx = _matrix(x, "x", (m, k), x)
-    d.w, d.ldw, d.stride_w = _weights(w, "w", (*lead, n, k), e, x)
-    d.y, d.ldy = _matrix(out, "out", (m, n), x)
-    if bias is not None:
-        d.bias = _vector(bias, "bias", (*lead, n), x)
-    if residual is not None:
-        d.residual, d.ldr = _matrix(residual, "residual", (m, n), x)
-    if preact is not None:
-        d.preact, d.ldp = _matrix(preact, "preact", (m, n), x)
-    _run("linear", d, 0, x, stream)
+    if out is None:
+        out = _fresh(x, (m, n), stream)
+    px, ldx = _matrix(x, "x", (m, k), dt, gpu)
+    pw, ldw, sw = _weights(w, "w", (*lead, n, k), dt, gpu)
+    py, ldy = _matrix(out, "out", (m, n), dt, gpu)
+    pb = 0 if bias is None else _vector(bias, "bias", (*lead, n), dt, gpu)
+    pr, ldr = (0, 0) if residual is None else _matrix(residual, "residual", (m, n), dt, gpu)
+    pp, ldp = (0, 0) if preact is None else _matrix(preact, "preact", (m, n), dt, gpu)
+    L = lib()
+    _run(L.heddle_linear, L.heddle_linear_workspace,
+         _LINEAR.pack(_dtype(x, "x"), act, m, n, k, px, ldx, pw, ldw, pb, pr, ldr, pp, ldp, py, ldy, e, off, sw,
+                      0, 0, 0, 0, 0, 0, 0, 0), 0, x, gpu, stream)
     return out
 
 
@@ -543,43 +572,39 @@ def heddle_linear_backward(dy, x, w, act=HEDDLE_A_NONE, preact=None, offsets=Non
     """Gradients of heddle_linear: a dict with dx, dw and db (those wanted;
     given tensors are written). preact: what heddle_linear kept (any act but
     HEDDLE_A_NONE). The residual's gradient is dy itself."""
-    _two(x, w, "heddle_linear_backward")
-    m, k, n = x.shape[0], x.shape[1], w.shape[-2]
-    e = _groups(offsets, w, x)
+    gpu, dt, m, k = _rows(x, w, "heddle_linear_backward")
+    n, (e, off) = w.shape[-2], _groups(offsets, w, gpu)
     lead = (e,) if e else ()
-    d = heddle_linear_desc(dtype=_dtype(x, "x"), act=act, m=m, n=n, k=k, groups=e, d_offsets=offsets.data_ptr() if e else None)
-    d.x, d.ldx = _matrix(x, "x", (m, k), x)
-    d.w, d.ldw, d.stride_w = _weights(w, "w", (*lead, n, k), e, x)
-    d.dy, d.lddy = _matrix(dy, "dy", (m, n), x)
-    if preact is not None:
-        d.preact, d.ldp = _matrix(preact, "preact", (m, n), x)
+    px, ldx = _matrix(x, "x", (m, k), dt, gpu)
+    pw, ldw, sw = _weights(w, "w", (*lead, n, k), dt, gpu)
+    pg, ldg = _matrix(dy, "dy", (m, n), dt, gpu)
+    pp, ldp = (0, 0) if preact is None else _matrix(preact, "preact", (m, n), dt, gpu)
     out = {}
+    pdx = lddx = pdw = lddw = sdw = pdb = 0
     if want_dx or dx is not None:
-        out["dx"] = _fresh((m, k), x, stream) if dx is None else dx
-        d.dx, d.lddx = _matrix(out["dx"], "dx", (m, k), x)
+        out["dx"] = _fresh(x, (m, k), stream) if dx is None else dx
+        pdx, lddx = _matrix(out["dx"], "dx", (m, k), dt, gpu)
     if want_dw or dw is not None:
-        out["dw"] = _fresh((*lead, n, k), x, stream) if dw is None else dw
-        d.dw, d.lddw, d.stride_dw = _weights(out["dw"], "dw", (*lead, n, k), e, x)
+        out["dw"] = _fresh(x, (*lead, n, k), stream) if dw is None else dw
+        pdw, lddw, sdw = _weights(out["dw"], "dw", (*lead, n, k), dt, gpu)
     if want_db or db is not None:
-        out["db"] = _fresh((*lead, n), x, stream) if db is None else db
-        d.db = _vector(out["db"], "db", (*lead, n), x)
-    _run("linear", d, 1, x, stream)
+        out["db"] = _fresh(x, (*lead, n), stream) if db is None else db
+        pdb = _vector(out["db"], "db", (*lead, n), dt, gpu)
+    L = lib()
+    _run(L.heddle_linear_backward, L.heddle_linear_workspace,
+         _LINEAR.pack(_dtype(x, "x"), act, m, n, k, px, ldx, pw, ldw, 0, 0, 0, pp, ldp, 0, 0, e, off, sw,
+                      pg, ldg, pdx, lddx, pdw, lddw, sdw, pdb), 1, x, gpu, stream)
     return out
 
 
-def _ffn_desc(x, w_in, w_out, act, offsets):
-    _two(x, w_in, "heddle_gated_ffn")
-    t, dim = x.shape
+def _ffn_inputs(x, w_in, w_out, offsets):
+    gpu, dt, t, d = _rows(x, w_in, "heddle_gated_ffn")
+    f, (e, off) = w_in.shape[-2] // 2, _groups(offsets, w_in, gpu)
     if w_in.shape[-2] % 2:
-        raise HeddleError(HEDDLE_E_INVAL, "w_in: an odd number of gate and up rows")
-    f, e = w_in.shape[-2] // 2, _groups(offsets, w_in, x)
+        _refuse("w_in: an odd number of gate and up rows")
     lead = (e,) if e else ()
-    d = heddle_gated_ffn_desc(dtype=_dtype(x, "x"), act=act, t=t, d=dim, f=f, groups=e,
-                              d_offsets=offsets.data_ptr() if e else None)
-    d.x, d.ldx = _matrix(x, "x", (t, dim), x)
-    d.w_in, d.ldw_in, d.stride_in = _weights(w_in, "w_in", (*lead, 2 * f, dim), e, x)
-    d.w_out, d.ldw_out, d.stride_out = _weights(w_out, "w_out", (*lead, dim, f), e, x)
-    return d, t, dim, f, e, lead
+    return (gpu, dt, t, d, f, e, off, lead, *_matrix(x, "x", (t, d), dt, gpu),
+            *_weights(w_in, "w_in", (*lead, 2 * f, d), dt, gpu), *_weights(w_out, "w_out", (*lead, d, f), dt, gpu))
 
 
 def heddle_gated_ffn(x, w_in, w_out, act=HEDDLE_A_SILU, residual=None, preact=None, out=None, offsets=None, stream=None):
@@ -587,14 +612,16 @@ def heddle_gated_ffn(x, w_in, w_out, act=HEDDLE_A_SILU, residual=None, preact=No
     [2 f, d], gate rows then up rows; w_out: [d, f]; with offsets both have a
     leading dimension of expert groups. preact: [t, 2 f] to keep the two
     projections for the backward pass. Returns out ([t, d])."""
-    d, t, dim, f, _, _ = _ffn_desc(x, w_in, w_out, act, offsets)
-    out = _fresh((t, dim), x, stream) if out is None else out
-    d.y, d.ldy = _matrix(out, "out", (t, dim), x)
-    if residual is not None:
-        d.residual, d.ldr = _matrix(residual, "residual", (t, dim), x)
-    if preact is not None:
-        d.preact, d.ldp = _matrix(preact, "preact", (t, 2 * f), x)
-    _run("gated_ffn", d, 0, x, stream)
+    gpu, dt, t, d, f, e, off, _, px, ldx, pi, ldi, si, po, ldo, so = _ffn_inputs(x, w_in, w_out, offsets)
+    if out is None:
+        out = _fresh(x, (t, d), stream)
+    py, ldy = _matrix(out, "out", (t, d), dt, gpu)
+    pr, ldr = (0, 0) if residual is None else _matrix(residual, "residual", (t, d), dt, gpu)
+    pp, ldp = (0, 0) if preact is None else _matrix(preact, "preact", (t, 2 * f), dt, gpu)
+    L = lib()
+    _run(L.heddle_gated_ffn, L.heddle_gated_ffn_workspace,
+         _GATED_FFN.pack(_dtype(x, "x"), act, t, d, f, px, ldx, pi, ldi, po, ldo, pr, ldr, pp, ldp, py, ldy, e, off, si, so,
+                         0, 0, 0, 0, 0, 0, 0, 0, 0, 0), 0, x, gpu, stream)
     return out
 
 
@@ -602,80 +629,85 @@ def heddle_gated_ffn_backward(dy, x, w_in, w_out, preact, act=HEDDLE_A_SILU, off
                               dx=None, dw_in=None, dw_out=None, stream=None):
     """Gradients of heddle_gated_ffn: a dict with dx, dw_in and dw_out (those
     wanted; given tensors are written). preact: what heddle_gated_ffn kept."""
-    d, t, dim, f, e, lead = _ffn_desc(x, w_in, w_out, act, offsets)
-    d.dy, d.lddy = _matrix(dy, "dy", (t, dim), x)
-    d.preact, d.ldp = _matrix(preact, "preact", (t, 2 * f), x)
+    gpu, dt, t, d, f, e, off, lead, px, ldx, pi, ldi, si, po, ldo, so = _ffn_inputs(x, w_in, w_out, offsets)
+    pg, ldg = _matrix(dy, "dy", (t, d), dt, gpu)
+    pp, ldp = _matrix(preact, "preact", (t, 2 * f), dt, gpu)
     out = {}
+    pdx = lddx = pdi = lddi = sdi = pdo = lddo = sdo = 0
     if want_dx or dx is not None:
-        out["dx"] = _fresh((t, dim), x, stream) if dx is None else dx
-        d.dx, d.lddx = _matrix(out["dx"], "dx", (t, dim), x)
+        out["dx"] = _fresh(x, (t, d), stream) if dx is None else dx
+        pdx, lddx = _matrix(out["dx"], "dx", (t, d), dt, gpu)
     if want_dw or dw_in is not None:
-        out["dw_in"] = _fresh((*lead, 2 * f, dim), x, stream) if dw_in is None else dw_in
-        d.dw_in, d.lddw_in, d.stride_dw_in = _weights(out["dw_in"], "dw_in", (*lead, 2 * f, dim), e, x)
+        out["dw_in"] = _fresh(x, (*lead, 2 * f, d), stream) if dw_in is None else dw_in
+        pdi, lddi, sdi = _weights(out["dw_in"], "dw_in", (*lead, 2 * f, d), dt, gpu)
     if want_dw or dw_out is not None:
-        out["dw_out"] = _fresh((*lead, dim, f), x, stream) if dw_out is None else dw_out
-        d.dw_out, d.lddw_out, d.stride_dw_out = _weights(out["dw_out"], "dw_out", (*lead, dim, f), e, x)
-    _run("gated_ffn", d, 1, x, stream)
+        out["dw_out"] = _fresh(x, (*lead, d, f), stream) if dw_out is None else dw_out
+        pdo, lddo, sdo = _weights(out["dw_out"], "dw_out", (*lead, d, f), dt, gpu)
+    L = lib()
+    _run(L.heddle_gated_ffn_backward, L.heddle_gated_ffn_workspace,
+         _GATED_FFN.pack(_dtype(x, "x"), act, t, d, f, px, ldx, pi, ldi, po, ldo, 0, 0, pp, ldp, 0, 0, e, off, si, so,
+                         pg, ldg, pdx, lddx, pdi, lddi, sdi, pdo, lddo, sdo), 1, x, gpu, stream)
     return out
 
 
 def _grads(grads, out=None):
-    """descriptor array of a list of gradient tensors, and their device"""
+    """(packed descriptors of a list of gradient tensors, their GPU)"""
     if out is not None and len(out) != len(grads):
-        raise HeddleError(HEDDLE_E_INVAL, f"{len(out)} outputs for {len(grads)} gradient tensors")
-    table = (heddle_grad_desc * max(len(grads), 1))()
-    device = grads[0].device if len(grads) else None
+        _refuse(f"{len(out)} outputs for {len(grads)} gradient tensors")
+    gpu, codes, table = grads[0].get_device() if len(grads) else None, _dtype_codes(), []
     for i, g in enumerate(grads):
-        if not g.is_cuda or g.device != device or not g.is_contiguous():
-            raise HeddleError(HEDDLE_E_INVAL, f"gradient tensor {i}: not contiguous on the GPU of the first one")
-        e = table[i]
-        e.g, e.n, e.dtype = g.data_ptr(), g.numel(), _dtype(g, f"gradient tensor {i}")
+        dt, n = g.dtype, g.numel()
+        if gpu < 0 or g.get_device() != gpu or not g.is_contiguous() or dt not in codes:
+            _refuse(f"gradient tensor {i}: not contiguous on the GPU of the first one, or of type {dt}")
+        at = g.data_ptr()
+        to = at
         if out is not None:
             o = out[i]
-            if o.dtype != g.dtype or o.device != device or o.numel() != e.n or not o.is_contiguous():
-                raise HeddleError(HEDDLE_E_INVAL, f"output {i}: not contiguous, or unlike its gradient tensor")
-            e.out = o.data_ptr()
-    return table, device
+            if o.dtype != dt or o.get_device() != gpu or o.numel() != n or not o.is_contiguous():
+                _refuse(f"output {i}: not contiguous, or unlike its gradient tensor")
+            to = o.data_ptr()
+        table.append(_GRAD.pack(at, to, n, codes[dt]))
+    return b"".join(table), gpu
 
 
-def _norm_call(table, count, device, stream, call):
+def _norm_call(table, count, gpu, stream, work):
     import torch
-    L, need = lib(), C.c_int64()
-    with torch.cuda.device(device):
-        _check(L.heddle_grad_norm_workspace(table, count, C.byref(need)))
-        norm = torch.empty(1, dtype=torch.float32, device="cuda" if device is None else device)
-        ws = torch.empty(need.value, dtype=torch.uint8, device=norm.device)
-        if stream is not None:
-            norm.record_stream(stream)
-            ws.record_stream(stream)
-        _check(call(L, _ptr(norm), _ptr(ws), need.value, _stream(stream)))
+    n = C.c_int64()
+    _check(lib().heddle_grad_norm_workspace(table, count, C.byref(n)))
+    if gpu is None:
+        gpu = torch.cuda.current_device()
+    # the norm and the scratch of the call
+    norm = torch.empty(1, dtype=torch.float32, device=gpu)
+    ws = torch.empty(n.value, dtype=torch.uint8, device=gpu)
+    if stream is not None:
+        norm.record_stream(stream)
+        ws.record_stream(stream)
+    _on_gpu(gpu, stream, lambda handle: work(norm.data_ptr(), ws.data_ptr(), n.value, handle))
     return norm
 
 
 def heddle_grad_norm(grads, stream=None):
     """The 2-norm over all values of all gradient tensors, as a float32 tensor
     of one value on their device."""
-    table, device = _grads(grads)
-    return _norm_call(table, len(grads), device, stream,
-                      lambda L, norm, ws, n, s: L.heddle_grad_norm(table, len(grads), norm, ws, n, s))
+    table, gpu = _grads(grads)
+    return _norm_call(table, len(grads), gpu, stream, lambda *a: lib().heddle_grad_norm(table, len(grads), *a))
 
 
 def heddle_clip_grads(grads, norm, max_norm, out=None, stream=None):
     """Scale the gradient tensors by min(1, max_norm / (norm + 1e-6)), in
     place or into out. norm: float32 tensor of one value on their device (of
     all ranks' shards, say)."""
-    import torch
-    table, device = _grads(grads, out)
-    if not norm.is_cuda or norm.dtype != torch.float32 or norm.numel() != 1 or device not in (None, norm.device):
-        raise HeddleError(HEDDLE_E_INVAL, "norm: not one float32 value on the gradients' device")
-    with torch.cuda.device(norm.device):
-        _check(lib().heddle_clip_grads(table, len(grads), _ptr(norm), max_norm, _stream(stream)))
+    table, gpu = _grads(grads, out)
+    if str(norm.dtype) != "torch.float32" or norm.numel() != 1 or not norm.is_cuda or gpu not in (None, norm.get_device()):
+        _refuse("norm: not one float32 value on the gradients' GPU")
+    _on_gpu(norm.get_device(), stream,
+            lambda handle: lib().heddle_clip_grads(table, len(grads), norm.data_ptr(), max_norm, handle))
     return grads if out is None else out
 
 
 def heddle_clip_grad_norm(grads, max_norm, out=None, stream=None):
     """heddle_grad_norm and heddle_clip_grads in one call; returns the norm
     before clipping."""
-    table, device = _grads(grads, out)
-    return _norm_call(table, len(grads), device, stream,
-                      lambda L, norm, ws, n, s: L.heddle_clip_grad_norm(table, len(grads), max_norm, norm, ws, n, s))
+    table, gpu = _grads(grads, out)
+    return _norm_call(table, len(grads), gpu, stream,
+                      lambda *a: lib().heddle_clip_grad_norm(table, len(grads), max_norm, *a))
