@@ -86,13 +86,13 @@ template <typename T> static int forward(const heddle_gated_ffn_desc *d, Scratch
         if (const int rc = run ? c.launch(stream) : HEDDLE_OK) return rc;
     }
     EpiGated<T> e = {};
-    e.ldh = scratch_ld(d->f), e.h = (T *)s.take((size_t)d->t * e.ldh * 2), e.wide_h = 8;
-    e.pre = (T *)d->preact, e.ldp = d->ldp, e.wide_p = width_of(d->preact, d->ldp, d->f);
+    e.ldh = scratch_ld(d->f), e.h = (T *)s.take((size_t)d->t * e.ldh * 2);
+    e.pre = (T *)d->preact, e.ldp = d->ldp;
     e.act = d->act, e.N = (int)d->f;
     int rc = hidden<T, EpiGated<T>, false>(x, wi, d->t, d->f, d->d, groups, d->d_offsets, e, s, run, stream);
     if (rc) return rc;
     EpiLinear<T> o = plain_output<T>(d->y, d->ldy, d->d);
-    o.residual = (const T *)d->residual, o.ldr = d->ldr, o.wide_r = width_of(d->residual, d->ldr);
+    o.residual = (const T *)d->residual, o.ldr = d->ldr;
     return product<T>(false, {e.h, e.ldh, 0}, wo, d->t, d->d, d->f, groups, d->d_offsets, o, s, run, stream);
 }
 
@@ -114,9 +114,9 @@ template <typename T> static int backward(const heddle_gated_ffn_desc *d, Scratc
     }
     EpiGatedGrad<T> e = {};
     e.ldd = scratch_ld(2 * d->f), e.ldh = scratch_ld(d->f);
-    e.dp = (T *)s.take((size_t)d->t * e.ldd * 2), e.wide_d = width_of(nullptr, e.ldd, d->f);
-    e.h = (T *)s.take((size_t)d->t * e.ldh * 2), e.wide_h = 8;
-    e.pre = (const T *)d->preact, e.ldp = d->ldp, e.wide_p = width_of(d->preact, d->ldp, d->f);
+    e.dp = (T *)s.take((size_t)d->t * e.ldd * 2);
+    e.h = (T *)s.take((size_t)d->t * e.ldh * 2);
+    e.pre = (const T *)d->preact, e.ldp = d->ldp;
     e.act = d->act, e.N = (int)d->f;
     rc = hidden<T, EpiGatedGrad<T>, true>(dy, wo, d->t, d->f, d->d, groups, d->d_offsets, e, s, run, stream);
     if (rc) return rc;

@@ -109,55 +109,32 @@ __device__ inline void act_both(int act, float z, float &v, float &d)
     }
 }
 
-// ---- eight neighbouring values of a row; `width`: elements of a memory access ----
-template <typename T, int W> struct packed { typedef T type __attribute__((ext_vector_type(W))); };
-template <int W, typename T> __device__ inline void load_by(const T *p, float v[8])
+// ---- eight neighbouring values of a row: one access of 16 bytes at any address that its
+// values may have, single values at the row's end ----
+template <typename T> __device__ inline void load8(const T *p, int count, float v[8])
 {
-    typedef typename packed<T, W>::type P;
+    typename pack8<T>::type x;
+    if (count >= 8) {
+        __builtin_memcpy(&x, p, 16);
+    } else {
 #pragma unroll
-    for (int i = 0; i < 8; i += W) {
-        const P x = *(const P *)(p + i);
-#pragma unroll
-        for (int j = 0; j < W; j++) v[i + j] = (float)x[j];
+        for (int i = 0; i < 8; i++) x[i] = i < count ? p[i] : (T)0.0f;
     }
-}
-template <int W, typename T> __device__ inline void store_by(T *p, const float v[8])
-{
-    typedef typename packed<T, W>::type P;
 #pragma unroll
-    for (int i = 0; i < 8; i += W) {
-        P x;
-#pragma unroll
-        for (int j = 0; j < W; j++) x[j] = (T)v[i + j];
-        *(P *)(p + i) = x;
-    }
+    for (int i = 0; i < 8; i++) v[i] = (float)x[i];
 }
-template <typename T> __device__ inline void load8(const T *p, int count, int width, float v[8])
+template <typename T> __device__ inline void store8(T *p, int count, const float v[8])
 {
-    if (count >= 8 && width == 8) load_by<8>(p, v);
-    else if (count >= 8 && width == 4) load_by<4>(p, v);
-    else if (count >= 8 && width == 2) load_by<2>(p, v);
-    else {
+    typename pack8<T>::type x;
 #pragma unroll
-        for (int i = 0; i < 8; i++) v[i] = i < count ? (float)p[i] : 0.0f;
-    }
-}
-template <typename T> __device__ inline void store8(T *p, int count, int width, const float v[8])
-{
-    if (count >= 8 && width == 8) store_by<8>(p, v);
-    else if (count >= 8 && width == 4) store_by<4>(p, v);
-    else if (count >= 8 && width == 2) store_by<2>(p, v);
-    else {
+    for (int i = 0; i < 8; i++) x[i] = (T)v[i];
+    if (count >= 8) {
+        __builtin_memcpy(p, &x, 16);
+    } else {
 #pragma unroll
         for (int i = 0; i < 8; i++)
-            if (i < count) p[i] = (T)v[i];
+            if (i < count) p[i] = x[i];
     }
-}
-// the widest access that suits a pointer and every distance added to it (elements)
-inline uint8_t width_of(const void *p, int64_t a, int64_t b = 0, int64_t c = 0)
-{
-    const uint64_t bits = (uint64_t)(uintptr_t)p | (uint64_t)(a | b | c) * 2;
-    return bits % 16 == 0 ? 8 : bits % 8 == 0 ? 4 : bits % 4 == 0 ? 2 : 1;
 }
 
 // ---- epilogues: one call finishes eight columns n .. n+7 of row m ----
@@ -169,28 +146,27 @@ template <typename T> struct EpiLinear {
     const T *bias, *residual;
     int64_t ldy, ldp, ldr, stride_y;          // stride_y: from a group's output to the next one's (kGroupSum)
     int32_t act, N;
-    uint8_t wide_y, wide_p, wide_r, wide_b;   // width_of the output, preact, residual and bias
     __device__ inline void operator()(int64_t m, int n, int g, float v[8]) const
     {
         const int count = N - n;
         if (bias) {
             float b[8];
-            load8(bias + (int64_t)g * N + n, count, wide_b, b);
+            load8(bias + (int64_t)g * N + n, count, b);
 #pragma unroll
             for (int i = 0; i < 8; i++) v[i] += b[i];
         }
-        if (pre) store8(pre + m * ldp + n, count, wide_p, v);
+        if (pre) store8(pre + m * ldp + n, count, v);
         if (act) {
 #pragma unroll
             for (int i = 0; i < 8; i++) v[i] = act_of(act, v[i]);
         }
         if (residual) {
             float r[8];
-            load8(residual + m * ldr + n, count, wide_r, r);
+            load8(residual + m * ldr + n, count, r);
 #pragma unroll
             for (int i = 0; i < 8; i++) v[i] += r[i];
         }
-        store8(y + (int64_t)g * stride_y + m * ldy + n, count, wide_y, v);
+        store8(y + (int64_t)g * stride_y + m * ldy + n, count, v);
     }
 };
 
@@ -200,17 +176,16 @@ template <typename T> struct EpiGated {
     T *h, *pre;
     int64_t ldh, ldp;
     int32_t act, N;                           // N = F
-    uint8_t wide_h, wide_p;
     __device__ inline void operator()(int64_t m, int n, int, float gate[8], const float up[8]) const
     {
         const int count = N - n;
         if (pre) {
-            store8(pre + m * ldp + n, count, wide_p, gate);
-            store8(pre + m * ldp + N + n, count, wide_p, up);
+            store8(pre + m * ldp + n, count, gate);
+            store8(pre + m * ldp + N + n, count, up);
         }
 #pragma unroll
         for (int i = 0; i < 8; i++) gate[i] = act_of(act, gate[i]) * up[i];
-        store8(h + m * ldh + n, count, wide_h, gate);
+        store8(h + m * ldh + n, count, gate);
     }
 };
 
@@ -223,13 +198,12 @@ template <typename T> struct EpiGatedGrad {
     const T *pre;
     int64_t ldd, ldh, ldp;
     int32_t act, N;
-    uint8_t wide_d, wide_h, wide_p;
     __device__ inline void operator()(int64_t m, int n, int, float v[8]) const
     {
         const int count = N - n;
         float g[8], u[8], dg[8], hh[8];
-        load8(pre + m * ldp + n, count, wide_p, g);
-        load8(pre + m * ldp + N + n, count, wide_p, u);
+        load8(pre + m * ldp + n, count, g);
+        load8(pre + m * ldp + N + n, count, u);
 #pragma unroll
         for (int i = 0; i < 8; i++) {
             float a, d;
@@ -238,9 +212,9 @@ template <typename T> struct EpiGatedGrad {
             hh[i] = a * u[i];
             v[i] *= a;
         }
-        store8(dp + m * ldd + n, count, wide_d, dg);
-        store8(dp + m * ldd + N + n, count, wide_d, v);
-        store8(h + m * ldh + n, count, wide_h, hh);
+        store8(dp + m * ldd + n, count, dg);
+        store8(dp + m * ldd + N + n, count, v);
+        store8(h + m * ldh + n, count, hh);
     }
 };
 

@@ -83,7 +83,6 @@ template <typename T> inline EpiLinear<T> plain_output(void *y, int64_t ld, int6
     e.ldy = ld;
     e.stride_y = stride;
     e.N = (int32_t)n;
-    e.wide_y = width_of(y, ld, stride);
     return e;
 }
 

@@ -101,7 +101,7 @@ int Copies::launch(hipStream_t stream) const
 
 // A workgroup takes 256 columns (32 lanes of eight) and its chunk of rows, 8
 // rows at a time; its lanes' sums are joined in LDS in a fixed order.
-template <typename T> __global__ void __launch_bounds__(256) bias_grad_kernel(BiasGrad b, int wide_dy, int wide_p, int wide_z)
+template <typename T> __global__ void __launch_bounds__(256) bias_grad_kernel(BiasGrad b)
 {
     __shared__ float part[8][256 + 8];
     const int col = threadIdx.x & 31, row = threadIdx.x >> 5;
@@ -112,13 +112,14 @@ template <typename T> __global__ void __launch_bounds__(256) bias_grad_kernel(Bi
     const int first = lo + chunk * b.chunk_rows;
     const int last = b.offsets ? hi : min(hi, first + b.chunk_rows);
     float sum[8] = {};
-    if (count > 0)
+    if (count > 0) {
+#pragma unroll 4
         for (int m = first + row; m < last; m += 8) {
             float v[8];
-            load8((const T *)b.dy + m * b.lddy + n, count, wide_dy, v);
+            load8((const T *)b.dy + m * b.lddy + n, count, v);
             if (b.act) {
                 float z[8];
-                load8((const T *)b.pre + m * b.ldp + n, count, wide_p, z);
+                load8((const T *)b.pre + m * b.ldp + n, count, z);
 #pragma unroll
                 for (int i = 0; i < 8; i++) {
                     float a, d;
@@ -126,10 +127,11 @@ template <typename T> __global__ void __launch_bounds__(256) bias_grad_kernel(Bi
                     v[i] *= d;
                 }
             }
-            if (b.dz) store8((T *)b.dz + m * b.lddz + n, count, wide_z, v);
+            if (b.dz) store8((T *)b.dz + m * b.lddz + n, count, v);
 #pragma unroll
             for (int i = 0; i < 8; i++) sum[i] += v[i];
         }
+    }
     if (!b.db) return;
 #pragma unroll
     for (int i = 0; i < 8; i++) part[row][col * 8 + i] = sum[i];
@@ -143,19 +145,28 @@ template <typename T> __global__ void __launch_bounds__(256) bias_grad_kernel(Bi
     else ((T *)b.db)[(int64_t)g * b.n + c] = (T)v;
 }
 
+// 32 columns, 8 parts of the chunks
 template <typename T> __global__ void __launch_bounds__(256) bias_join_kernel(BiasGrad b)
 {
-    const int c = blockIdx.x * 256 + threadIdx.x;
-    if (c >= b.n) return;
+    __shared__ float part[8][32];
+    const int col = threadIdx.x & 31, row = threadIdx.x >> 5, c = blockIdx.x * 32 + col;
     float v = 0;
-    for (int i = 0; i < b.chunks; i++) v += b.partial[(int64_t)i * b.n + c];
+    if (c < b.n) {
+#pragma unroll 8
+        for (int i = row; i < b.chunks; i += 8) v += b.partial[(int64_t)i * b.n + c];
+    }
+    part[row][col] = v;
+    __syncthreads();
+    if (row || c >= b.n) return;
+#pragma unroll
+    for (int r = 1; r < 8; r++) v += part[r][col];
     ((T *)b.db)[c] = (T)v;
 }
 
-// enough chunks of rows to fill the chip, at least 16 rows in each
+// enough chunks of rows to fill the chip, at least 32 rows in each
 static void bias_chunks(int64_t m, int64_t n, bool grouped, int &chunks, int &rows)
 {
-    const int64_t blocks = (n + 255) / 256, want = grouped ? 1 : (2048 + blocks - 1) / blocks, most = (m + 15) / 16;
+    const int64_t blocks = (n + 255) / 256, want = grouped ? 1 : (2048 + blocks - 1) / blocks, most = (m + 31) / 32;
     chunks = (int)(want < most ? want : most);
     if (chunks < 1) chunks = 1;
     rows = (int)((m + chunks - 1) / chunks);
@@ -173,12 +184,11 @@ template <typename T> static int run_bias_grad(BiasGrad b, hipStream_t stream)
     bias_chunks(b.m, b.n, b.offsets != nullptr, b.chunks, b.chunk_rows);
     const int groups = b.offsets ? b.groups : 1;
     const dim3 grid((unsigned)((b.n + 255) / 256), (unsigned)(groups * b.chunks));
-    hipLaunchKernelGGL((bias_grad_kernel<T>), grid, dim3(256), 0, stream, b, (int)width_of(b.dy, b.lddy),
-                       (int)width_of(b.pre, b.ldp), (int)width_of(b.dz, b.lddz));
+    hipLaunchKernelGGL((bias_grad_kernel<T>), grid, dim3(256), 0, stream, b);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return hip_fail(e, "bias_grad_kernel");
     if (b.db && b.chunks > 1) {
-        hipLaunchKernelGGL((bias_join_kernel<T>), dim3((unsigned)((b.n + 255) / 256)), dim3(256), 0, stream, b);
+        hipLaunchKernelGGL((bias_join_kernel<T>), dim3((unsigned)((b.n + 31) / 32)), dim3(256), 0, stream, b);
         e = hipGetLastError();
         if (e != hipSuccess) return hip_fail(e, "bias_join_kernel");
     }
@@ -286,9 +296,9 @@ template <typename T> static int forward(const heddle_linear_desc *d, Scratch &s
         if (const int rc = run ? c.launch(stream) : HEDDLE_OK) return rc;
     }
     EpiLinear<T> e = plain_output<T>(d->y, d->ldy, d->n);
-    e.pre = (T *)d->preact, e.ldp = d->ldp, e.wide_p = width_of(d->preact, d->ldp);
-    e.bias = (const T *)d->bias, e.wide_b = width_of(d->bias, groups > 1 ? d->n : 0);
-    e.residual = (const T *)d->residual, e.ldr = d->ldr, e.wide_r = width_of(d->residual, d->ldr);
+    e.pre = (T *)d->preact, e.ldp = d->ldp;
+    e.bias = (const T *)d->bias;
+    e.residual = (const T *)d->residual, e.ldr = d->ldr;
     e.act = d->act;
     return product<T>(false, x, w, d->m, d->n, d->k, groups, d->d_offsets, e, s, run, stream);
 }

@@ -524,7 +524,7 @@ def _on_gpu(gpu, stream, call):
     if torch.cuda.current_device() != gpu:
         with torch.cuda.device(gpu):
             return _on_gpu(gpu, stream, call)
-    _check(call((torch.cuda.current_stream() if stream is None else stream).cuda_stream))
+    _check(call(torch._C._cuda_getCurrentRawStream(gpu) if stream is None else stream.cuda_stream))
 
 
 def _run(work, need, desc, backward, like, gpu, stream):
