@@ -260,13 +260,26 @@ __device__ inline bool find_tile(const int32_t *offsets, int groups, int total, 
 }
 
 // ---- tile loads ----
-typedef __attribute__((address_space(3))) void *lds_ptr;
+typedef int i32x4 __attribute__((ext_vector_type(4)));
 
-__device__ inline __amdgpu_buffer_rsrc_t resource(const char *base, int64_t bytes)
+// a raw buffer of the bytes from base on, in whole 4-byte words (the word of the last value
+// never crosses a page); what lies past them reads as zero
+__device__ inline i32x4 resource(const char *base, int64_t bytes)
 {
-    // whole 4-byte words: the word of the last value never crosses a page
     const int64_t n = bytes <= 0 ? 0 : (bytes + 3) & ~int64_t(3);
-    return __builtin_amdgcn_make_buffer_rsrc((void *)base, 0, (int)(uint32_t)(n > 0xFFFFFFFCll ? 0xFFFFFFFCll : n), 0x00020000);
+    const uint64_t p = (uint64_t)(uintptr_t)base;
+    return i32x4{(int)(uint32_t)p, (int)(uint32_t)(p >> 32) & 0xFFFF, (int)(uint32_t)(n > 0xFFFFFFFCll ? 0xFFFFFFFCll : n), 0x00020000};
+}
+
+// 16 bytes a lane from the buffer to LDS, at lds + 16 lane. Written out, because after the
+// builtin the compiler waits for the load before the next transposing LDS read, whichever
+// buffer that reads; arrive() has the wait. No register receives anything. The no-op covers the
+// wait states after a write of m0, and after one of the buffer's registers by a vector
+// instruction.
+__device__ inline void load_to_lds(i32x4 buffer, int offset, uint32_t lds)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+                 : : "s"(lds), "v"(offset), "s"(buffer) : "memory", "m0");
 }
 
 // the exchange of a rows tile's 16-byte and of a columns tile's 32-byte pieces
@@ -299,16 +312,12 @@ template <int ROWS, int NW, bool COLS, bool PAIR> struct Loader {
     // up: from a gate row to its up row, in bytes
     __device__ inline void load(const char *base, int64_t bytes, int64_t up, char *lds, int wave) const
     {
-        const __amdgpu_buffer_rsrc_t r = resource(base, bytes);
-        const __amdgpu_buffer_rsrc_t ru = PAIR ? resource(base + up, bytes - up) : r;
+        const i32x4 r = resource(base, bytes), ru = PAIR ? resource(base + up, bytes - up) : r;
+        const uint32_t to = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds;
 #pragma unroll
         for (int i = 0; i < kLoads; i++) {
             const int piece = i * NW + wave;              // 1024 bytes, 8 rows of a rows tile
-            lds_ptr to = (lds_ptr)(lds + piece * 1024);
-            if (PAIR && (piece / 2) % 2)
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(ru, to, 16, voff[i], 0, 0, 0);
-            else
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(r, to, 16, voff[i], 0, 0, 0);
+            load_to_lds(PAIR && (piece / 2) % 2 ? ru : r, voff[i], to + piece * 1024);
         }
     }
     // a rows tile's values with k >= valid hold the next row's: make them zero
@@ -338,7 +347,7 @@ __device__ inline typename pack8<T>::type fragment(const char *lds, int rb, int 
     return *(const typename pack8<T>::type *)(lds + (rb * 16 + i) * 128 + (((s * 4 + g) ^ row_swz(i)) << 4));
 }
 
-// every wavefront's loads have landed and its reads of LDS are done
+// every wavefront's loads to LDS have landed and its reads of LDS are done
 __device__ inline void arrive()
 {
     asm volatile("" ::: "memory");
@@ -378,7 +387,7 @@ __device__ inline void tile_of(int t, int tiles_m, int tiles_n, int &tm, int &tn
 template <int BM, int BN, int WM, int WN, int STAGES, bool ACOL, bool BCOL, Grouping GR, typename T, typename Epi>
 __global__ void __launch_bounds__(WM * WN * 64) gemm_kernel(Args x, Epi epi)
 {
-#ifdef __HIP_DEVICE_COMPILE__   // the host pass has no buffer resources
+#ifdef __HIP_DEVICE_COMPILE__   // the host pass knows no LDS loads
     constexpr int NW = WM * WN, TM = BM / WM / 16, TN = BN / WN / 16, kOut = BN / WN;
     constexpr bool PAIR = Epi::gated, PIPED = STAGES == 2 && BM * BN >= 256 * 256;   // one workgroup on a CU
     typedef Loader<BM, NW, ACOL, false> LA;
