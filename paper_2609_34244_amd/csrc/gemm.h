@@ -262,24 +262,40 @@ __device__ inline bool find_tile(const int32_t *offsets, int groups, int total, 
 // ---- tile loads ----
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 
-// a raw buffer of the bytes from base on, in whole 4-byte words (the word of the last value
-// never crosses a page); what lies past them reads as zero
-__device__ inline i32x4 resource(const char *base, int64_t bytes)
-{
-    const int64_t n = bytes <= 0 ? 0 : (bytes + 3) & ~int64_t(3);
-    const uint64_t p = (uint64_t)(uintptr_t)base;
-    return i32x4{(int)(uint32_t)p, (int)(uint32_t)(p >> 32) & 0xFFFF, (int)(uint32_t)(n > 0xFFFFFFFCll ? 0xFFFFFFFCll : n), 0x00020000};
-}
+// What is left of an operand from a tile's first value on: a raw buffer in whole 4-byte
+// words (the word of the last value never crosses a page); what lies past it reads as zero.
+// Kept as a pointer and a 64-bit count, advanced by whole tiles in scalar arithmetic.
+struct Rest {
+    const char *p;
+    int64_t bytes;
+    __device__ inline void set(const char *base, int64_t n)
+    {
+        p = base;
+        bytes = n <= 0 ? 0 : (n + 3) & ~int64_t(3);
+    }
+    __device__ inline i32x4 buffer() const
+    {
+        const int high = (int)(bytes >> 32), low = (int)bytes;
+        return i32x4{(int)(uintptr_t)p, (int)((uintptr_t)p >> 32), high > 0 ? -4 : high < 0 ? 0 : low, 0x00020000};
+    }
+    __device__ inline void advance(int64_t step) { p += step, bytes -= step; }
+};
 
-// 16 bytes a lane from the buffer to LDS, at lds + 16 lane. Written out, because after the
-// builtin the compiler waits for the load before the next transposing LDS read, whichever
-// buffer that reads; arrive() has the wait. No register receives anything. The no-op covers the
-// wait states after a write of m0, and after one of the buffer's registers by a vector
-// instruction.
+// 16 bytes a lane from the buffer to LDS, at lds + 16 lane; two of them. Written out, because
+// after the builtin the compiler waits for the load before the next transposing LDS read,
+// whichever buffer that reads; arrive() has the wait. No register receives anything. The
+// no-ops cover the wait states after a write of m0, and after one of the buffer's registers by
+// a vector instruction.
 __device__ inline void load_to_lds(i32x4 buffer, int offset, uint32_t lds)
 {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
                  : : "s"(lds), "v"(offset), "s"(buffer) : "memory", "m0");
+}
+__device__ inline void load_to_lds(i32x4 buffer, int offset0, uint32_t lds0, int offset1, uint32_t lds1)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %2, %4, 0 offen lds\n\t"
+                 "s_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %3, %4, 0 offen lds"
+                 : : "s"(lds0), "s"(lds1), "v"(offset0), "v"(offset1), "s"(buffer) : "memory", "m0");
 }
 
 // the exchange of a rows tile's 16-byte and of a columns tile's 32-byte pieces
@@ -308,17 +324,19 @@ template <int ROWS, int NW, bool COLS, bool PAIR> struct Loader {
             }
         }
     }
-    // base: the tile's first value; bytes: from there to the operand's end;
-    // up: from a gate row to its up row, in bytes
-    __device__ inline void load(const char *base, int64_t bytes, int64_t up, char *lds, int wave) const
+    // a wavefront's 8 rows lie in one 16-row block, every kLoads piece in one of the same kind
+    static __device__ inline bool takes_up(int wave) { return PAIR && (wave / 2) % 2; }
+    // piece i of the tile: 1024 bytes a wavefront, 8 rows of a rows tile
+    __device__ inline void load(int i, i32x4 buffer, uint32_t lds, int wave) const
     {
-        const i32x4 r = resource(base, bytes), ru = PAIR ? resource(base + up, bytes - up) : r;
-        const uint32_t to = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds;
+        load_to_lds(buffer, voff[i], lds + (i * NW + wave) * 1024);
+    }
+    __device__ inline void load_all(i32x4 buffer, uint32_t lds, int wave) const
+    {
+        static_assert(kLoads % 2 == 0 && NW % 4 == 0, "pieces in pairs");
 #pragma unroll
-        for (int i = 0; i < kLoads; i++) {
-            const int piece = i * NW + wave;              // 1024 bytes, 8 rows of a rows tile
-            load_to_lds(PAIR && (piece / 2) % 2 ? ru : r, voff[i], to + piece * 1024);
-        }
+        for (int i = 0; i < kLoads; i += 2)
+            load_to_lds(buffer, voff[i], lds + (i * NW + wave) * 1024, voff[i + 1], lds + ((i + 1) * NW + wave) * 1024);
     }
     // a rows tile's values with k >= valid hold the next row's: make them zero
     __device__ static inline void clear_tail(char *lds, int valid)
@@ -439,7 +457,11 @@ __global__ void __launch_bounds__(WM * WN * 64) gemm_kernel(Args x, Epi epi)
         nb = ((int64_t)(brows - n0 - 1) * x.ldb + (k_hi - k_first)) * eb;
     }
     const int64_t step_a = (ACOL ? x.lda * kBK : kBK) * eb, step_b = (BCOL ? x.ldb * kBK : kBK) * eb;
-    const int64_t up = PAIR ? (int64_t)x.F * x.ldb * eb : 0;
+    // a wavefront loads either gate or up rows
+    const int64_t up = LB::takes_up(wave) ? (int64_t)x.F * x.ldb * eb : 0;
+    Rest rest_a, rest_b;
+    rest_a.set(pa, na);
+    rest_b.set(pb + up, nb - up);
 
     LA la;
     LB lb;
@@ -467,15 +489,16 @@ __global__ void __launch_bounds__(WM * WN * 64) gemm_kernel(Args x, Epi epi)
 #pragma unroll
             for (int j = 0; j < TN; j++) acc[i][j] = mfma(b[j], a[i], acc[i][j]);
     };
-    int loaded = 0;                                         // k-tiles asked for
-    auto load = [&](char *tile) {
-        if (loaded < tiles) {
-            la.load(pa, na, 0, tile, wave);
-            lb.load(pb, nb, up, tile + LA::kBytes, wave);
-            pa += step_a, na -= step_a, pb += step_b, nb -= step_b;
-        }
-        loaded++;
+    constexpr int kLoads = LA::kLoads + LB::kLoads;
+    int asked = 0;                                          // k-tiles asked for
+    auto load = [&](uint32_t tile) {
+        if (asked++ >= tiles) return;
+        la.load_all(rest_a.buffer(), tile, wave);
+        lb.load_all(rest_b.buffer(), tile + LA::kBytes, wave);
+        rest_a.advance(step_a);
+        rest_b.advance(step_b);
     };
+    const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)smem;
     const int valid = (k_last - k_first) % kBK;             // k of a last, partial tile
     auto landed = [&](char *tile, int kt) {
         arrive();
@@ -487,10 +510,13 @@ __global__ void __launch_bounds__(WM * WN * 64) gemm_kernel(Args x, Epi epi)
     };
     if (PIPED && tiles) {
         // Half a k-tile's fragments are read while the other half's are multiplied. A tile's
-        // buffer is free, and the next tile must be there, at the middle of the tile.
-        load(smem);
+        // buffer is free, and the next tile must be there, at the middle of the tile. The loads
+        // of the one after it go out at once where the wait for them shows (a rows operand:
+        // 1225 against 1200 TFLOP/s at 2048 x 8192 x 24032), else between the products of the
+        // second half (columns of both: 1335 against 1432).
+        load(lds);
         landed(smem, 0);
-        load(smem + kStage);
+        load(lds + kStage);
         read(smem, 0, fa[0], fb[0]);
         for (int kt = 0; kt < tiles; kt++) {
             char *cur = smem + (kt & 1) * kStage, *nxt = smem + (~kt & 1) * kStage;
@@ -498,15 +524,37 @@ __global__ void __launch_bounds__(WM * WN * 64) gemm_kernel(Args x, Epi epi)
             multiply(fa[0], fb[0]);
             interleave<TM + TN, TM * TN, ACOL || BCOL>();
             landed(nxt, kt + 1);
-            load(cur);
-            read(nxt, 0, fa[0], fb[0]);
-            multiply(fa[1], fb[1]);
-            interleave<TM + TN, TM * TN, ACOL || BCOL>();
+            if constexpr (!ACOL) {
+                load(lds + (kt & 1) * kStage);
+                read(nxt, 0, fa[0], fb[0]);
+                multiply(fa[1], fb[1]);
+                interleave<TM + TN, TM * TN, ACOL || BCOL>();
+            } else {
+                const bool any = asked++ < tiles;           // past the last tile: empty buffers
+                i32x4 ra = rest_a.buffer(), rb = rest_b.buffer();
+                ra[2] = any ? ra[2] : 0, rb[2] = any ? rb[2] : 0;
+                rest_a.advance(step_a);
+                rest_b.advance(step_b);
+#pragma unroll
+                for (int i = 0; i < kLoads; i++) {
+                    if (i < LA::kLoads) la.load(i, ra, lds + (kt & 1) * kStage, wave);
+                    else lb.load(i - LA::kLoads, rb, lds + (kt & 1) * kStage + LA::kBytes, wave);
+#pragma unroll
+                    for (int f = i * (TM + TN) / kLoads; f < (i + 1) * (TM + TN) / kLoads; f++) {
+                        if (f < TN) fb[0][f] = fragment<BN, BCOL, T>(nxt + LA::kBytes, wn * TN + f, 0);
+                        else fa[0][f - TN] = fragment<BM, ACOL, T>(nxt, wm * TM + f - TN, 0);
+                    }
+#pragma unroll
+                    for (int q = i * TM * TN / kLoads; q < (i + 1) * TM * TN / kLoads; q++)
+                        acc[q / TN][q % TN] = mfma(fb[1][q % TN], fa[1][q / TN], acc[q / TN][q % TN]);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
         }
     } else if (STAGES == 1 && tiles) {
         for (int kt = 0; kt < tiles; kt++) {
             if (kt) __syncthreads();
-            load(smem);
+            load(lds);
             landed(smem, kt);
 #pragma unroll
             for (int s = 0; s < kBK / 32; s++) {
@@ -516,11 +564,11 @@ __global__ void __launch_bounds__(WM * WN * 64) gemm_kernel(Args x, Epi epi)
         }
     } else if (tiles) {
         // several workgroups on a CU hide each other's reads
-        load(smem);
+        load(lds);
         for (int kt = 0; kt < tiles; kt++) {
             char *cur = smem + (kt & 1) * kStage;
             landed(cur, kt);
-            load(smem + (~kt & 1) * kStage);
+            load(lds + (~kt & 1) * kStage);
 #pragma unroll
             for (int s = 0; s < kBK / 32; s++) {
                 read(cur, s, fa[0], fb[0]);
@@ -528,7 +576,7 @@ __global__ void __launch_bounds__(WM * WN * 64) gemm_kernel(Args x, Epi epi)
             }
         }
     }
-    __syncthreads();
+    arrive();                                               // also the loads of empty buffers
 
     // Epilogue: a wavefront takes kRows of its rows at a time through its own part
     // of LDS, so that a lane finishes eight neighbouring columns. The product

@@ -10,8 +10,8 @@ namespace heddle {
 namespace mm {
 
 // The tile shape and the split of the reduction with the least estimated time. Constants in
-// us, from times of every shape and split on 120 products of 33 .. 8192 rows, 128 .. 20000
-// columns and k of the three memory orders: the choice costs 1.9% over the best one on
+// us, from times of every shape and split on 270 products of 33 .. 8192 rows, 128 .. 20000
+// columns and k of the three memory orders: the choice costs 1.3% over the best one on
 // average. step: a k-tile on a CU whose workgroup slots are taken; least: the same for
 // workgroups alone on their CU; fixed: start and epilogue of a round of workgroups.
 //   256 x 256: one workgroup a CU, the highest rate; 128 x 128: four a CU, each with one buffer
@@ -20,9 +20,9 @@ namespace mm {
 Shape shape_of(int64_t M, int64_t N, int64_t K, int groups, bool gated, Order order)
 {
     static const struct { int bm, bn, per_cu; double step[3], least, fixed; } cfg[3] = {
-        {256, 256, 1, {1.50, 1.65, 1.65}, 1.36, 8.3},
-        {128, 128, 4, {2.19, 2.38, 1.73}, 0.97, 5.0},
-        {64, 128, 3, {1.00, 1.16, 1.13}, 0.63, 3.6},
+        {256, 256, 1, {1.53, 1.50, 1.64}, 1.20, 7.2},
+        {128, 128, 4, {2.45, 2.36, 2.29}, 0.93, 5.3},
+        {64, 128, 3, {1.13, 1.09, 1.16}, 0.52, 3.3},
     };
     const int cus = 256;
     const bool sums = order == kColsCols;
@@ -33,7 +33,7 @@ Shape shape_of(int64_t M, int64_t N, int64_t K, int groups, bool gated, Order or
     Shape best = {0, 1, (int)kt};
     double least = 0;
     for (int c = 0; c < 3; c++)
-        for (int s = 1; s <= 16 && s <= kt && (s == 1 || groups <= 1); s *= 2) {
+        for (int s = 1, log2 = 0; s == 1 || (s <= 16 && groups <= 1 && (kt + s - 1) / s >= 4); s *= 2, log2++) {
             const double part = (double)((steps + s - 1) / s);
             const int64_t tiles = (rows + cfg[c].bm - 1) / cfg[c].bm * ((cols + cfg[c].bn - 1) / cfg[c].bn) * outer * s;
             const int64_t full = tiles / (cus * cfg[c].per_cu), rest = tiles - full * cus * cfg[c].per_cu;
@@ -44,7 +44,7 @@ Shape shape_of(int64_t M, int64_t N, int64_t K, int groups, bool gated, Order or
                 const double alone = step * share > cfg[c].least ? step * share : cfg[c].least;
                 t += part * alone + cfg[c].fixed * (0.5 + 0.5 * share);
             }
-            if (s > 1) t += 3.9 + 1.2e-6 * (double)s * (double)M * (double)cols;
+            if (s > 1) t += 2.9 + 0.3 * log2 + 1.2e-6 * (double)s * (double)M * (double)cols;
             if (least == 0 || t < least) {
                 least = t;
                 best = {c, s, (int)((kt + s - 1) / s)};
