@@ -1,14 +1,16 @@
 // Products with few rows of X (single tokens): Y[m][n] = sum over k of X[m][k] W[n][k].
 //
-// Bound by reading W once. A workgroup of eight wavefronts takes 16 rows of W
-// (gated: 16 gate and 16 up rows) and every row of X, at most 16 kBlocks at a time; each
-// wavefront takes an eighth of k. W goes from memory straight to the registers that the
+// Bound by reading W once. A workgroup of WAVES wavefronts takes 16 rows of W
+// (gated: 16 gate and 16 up rows) and every row of X, 16 MB at a time; each
+// wavefront takes its part of k. W goes from memory straight to the registers that the
 // matrix instruction reads (16 rows x 32 k, lane = row, 16 bytes of k), U pieces of W in
-// flight per lane, and X, which the caches hold, beside it. The eight sums meet in LDS in a
+// flight per lane, and X, which the caches hold, beside it. The wavefronts' sums meet in LDS in a
 // fixed order. Loads need only the alignment of a value, so no operand is copied.
 //
 // Groups: a workgroup takes the j-th group that has rows; there are at most as many as rows.
 #pragma once
+
+#include <type_traits>
 
 #include "gemm.h"
 
@@ -55,14 +57,12 @@ template <typename T> __device__ inline typename pack8<T>::type load_some(const 
     return v;
 }
 
-constexpr int kSkinnyWaves = 8;
-
-template <int MB, typename T, typename Epi> __global__ void __launch_bounds__(kSkinnyWaves * 64) skinny_kernel(Args x, Epi epi)
+template <int MB, int WAVES, typename T, typename Epi> __global__ void __launch_bounds__(WAVES * 64) skinny_kernel(Args x, Epi epi)
 {
     constexpr bool PAIR = Epi::gated;
-    constexpr int P = PAIR ? 2 : 1, U = MB * P > 2 ? 4 : 8;
+    constexpr int P = PAIR ? 2 : 1, U = MB * P > 1 ? 4 : 8;
     typedef typename pack8<T>::type frag;
-    __shared__ float part[kSkinnyWaves][P * MB * 256], sum[P * MB * 256];
+    __shared__ float part[WAVES][P * MB * 256], sum[P * MB * 256];
     const int lane = threadIdx.x & 63, i = lane & 15, kg = (lane >> 4) * 8;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     int g = 0, lo = 0, hi = x.M;
@@ -71,7 +71,7 @@ template <int MB, typename T, typename Epi> __global__ void __launch_bounds__(kS
     const T *w = (const T *)x.b + (int64_t)g * x.stride_b + (int64_t)(n0 + min(i, x.N - 1 - n0)) * x.ldb;
     const int64_t up = PAIR ? (int64_t)x.F * x.ldb : 0;
     // whole 32-k steps of this wavefront, and the last, partial one
-    const int steps = x.K / 32, each = (steps + kSkinnyWaves - 1) / kSkinnyWaves;
+    const int steps = x.K / 32, each = (steps + WAVES - 1) / WAVES;
     const int first = min(wave * each, steps), last = min(first + each, steps);
     for (int m0 = lo; m0 < hi; m0 += 16 * MB) {
         const T *xr[MB];
@@ -83,10 +83,12 @@ template <int MB, typename T, typename Epi> __global__ void __launch_bounds__(kS
 #pragma unroll
             for (int b = 0; b < MB; b++) acc[p][b] = f32x4{0, 0, 0, 0};
         int s = first;
-        for (; s + U <= last; s += U) {
-            frag fw[P][U], fx[MB][U];
+        // n steps: all their loads, then their products
+        auto batch = [&](auto n) {
+            constexpr int N = decltype(n)::value;
+            frag fw[P][N], fx[MB][N];
 #pragma unroll
-            for (int u = 0; u < U; u++) {
+            for (int u = 0; u < N; u++) {
                 const int k = (s + u) * 32 + kg;
 #pragma unroll
                 for (int p = 0; p < P; p++) fw[p][u] = load_any(w + p * up + k);
@@ -94,22 +96,18 @@ template <int MB, typename T, typename Epi> __global__ void __launch_bounds__(kS
                 for (int b = 0; b < MB; b++) fx[b][u] = load_any(xr[b] + k);
             }
 #pragma unroll
-            for (int u = 0; u < U; u++)
+            for (int u = 0; u < N; u++)
 #pragma unroll
                 for (int p = 0; p < P; p++)
 #pragma unroll
                     for (int b = 0; b < MB; b++) acc[p][b] = mfma16(fw[p][u], fx[b][u], acc[p][b]);
-        }
-        for (; s < last; s++) {
-            const int k = s * 32 + kg;
-#pragma unroll
-            for (int p = 0; p < P; p++) {
-                const frag fw = load_any(w + p * up + k);
-#pragma unroll
-                for (int b = 0; b < MB; b++) acc[p][b] = mfma16(fw, load_any(xr[b] + k), acc[p][b]);
-            }
-        }
-        if (wave == kSkinnyWaves - 1 && x.K % 32) {
+            s += N;
+        };
+        while (s + U <= last) batch(std::integral_constant<int, U>());
+        if (U > 4 && s + 4 <= last) batch(std::integral_constant<int, 4>());
+        if (s + 2 <= last) batch(std::integral_constant<int, 2>());
+        if (s < last) batch(std::integral_constant<int, 1>());
+        if (wave == WAVES - 1 && x.K % 32) {
             const int k = steps * 32 + kg, count = x.K - k;
 #pragma unroll
             for (int p = 0; p < P; p++) {
@@ -124,10 +122,10 @@ template <int MB, typename T, typename Epi> __global__ void __launch_bounds__(kS
 #pragma unroll
             for (int b = 0; b < MB; b++) *(f32x4 *)&part[wave][((p * MB + b) * 16 + i) * 16 + (lane >> 4) * 4] = acc[p][b];
         __syncthreads();
-        for (int c = threadIdx.x; c < P * MB * 256; c += kSkinnyWaves * 64) {
+        for (int c = threadIdx.x; c < P * MB * 256; c += WAVES * 64) {
             float v = 0;
 #pragma unroll
-            for (int q = 0; q < kSkinnyWaves; q++) v += part[q][c];
+            for (int q = 0; q < WAVES; q++) v += part[q][c];
             sum[c] = v;
         }
         __syncthreads();
@@ -154,11 +152,26 @@ template <typename T, typename Epi> inline int launch_skinny(const Args &x, cons
 {
     const unsigned blocks = (unsigned)((x.N + 15) / 16);
     const unsigned groups = x.offsets ? (unsigned)(x.groups < x.M ? x.groups : x.M) : 1;
+    // k is divided among 16 wavefronts where each has eight pieces of W to load at once, twice
+    // over (4096 x 10816, one row: 17.0 us, 20.4 with 8), else among 8, or 4 where there are
+    // workgroups enough for the chip without (experts of 4096 x 1632: 66 us, 83 with 8). A gated
+    // workgroup has as much in flight with 8 and half the pieces (2 x 10816 x 4096: 35 us, 37
+    // with 16 wavefronts, 44 with twice the pieces and half the workgroups on a CU).
+    const int waves = Epi::gated ? 8 : x.K >= 16 * 8 * 32 ? 16 : blocks * groups >= 4 * 256 ? 4 : 8;
+#define HEDDLE_SKINNY(MB, WAVES)                                                                                       \
+    hipLaunchKernelGGL((skinny_kernel<MB, WAVES, T, Epi>), dim3(blocks, groups), dim3(WAVES * 64), 0, stream, x, epi)
     const bool one = x.offsets || x.M <= 16;
-    if (one)
-        hipLaunchKernelGGL((skinny_kernel<1, T, Epi>), dim3(blocks, groups), dim3(kSkinnyWaves * 64), 0, stream, x, epi);
-    else
-        hipLaunchKernelGGL((skinny_kernel<2, T, Epi>), dim3(blocks, groups), dim3(kSkinnyWaves * 64), 0, stream, x, epi);
+    if (waves == 16) {
+        if (one) HEDDLE_SKINNY(1, 16);
+        else HEDDLE_SKINNY(2, 16);
+    } else if (waves == 8) {
+        if (one) HEDDLE_SKINNY(1, 8);
+        else HEDDLE_SKINNY(2, 8);
+    } else {
+        if (one) HEDDLE_SKINNY(1, 4);
+        else HEDDLE_SKINNY(2, 4);
+    }
+#undef HEDDLE_SKINNY
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? HEDDLE_OK : hip_fail(e, "skinny_kernel");
 }
