@@ -4,7 +4,7 @@
 // Bound by memory: every value is read for the norm and read again, and
 // written, for the clipping. The tensors' table goes to the kernels as an
 // argument (kTensors a launch), so no copy to the device precedes them.
-// A tensor is cut into chunks of kChunk bytes at 16-byte addresses; workgroup
+// A tensor is cut into chunks at 16-byte addresses; workgroup
 // b of G takes chunks b, b + G, ... and leaves one fp64 sum. Squares are
 // summed in fp64 throughout: fp32 squares overflow from 1.9e19, and at two
 // fp64 operations a value the sums stay far below the vector units' rate. The
@@ -16,24 +16,45 @@
 
 namespace heddle {
 
-constexpr int kTensors = 128, kParts = 2048;
-constexpr int64_t kChunk = 32768;
+constexpr int kTensors = 120, kParts = 2048;
+// 16-byte pieces of a lane in a chunk: many to have their loads in flight, few where a call's
+// tensors are too small to give every CU a large chunk (9 tensors of 1e6 fp32 values in all:
+// both kernels 14.6 us with 8, 10.4 us with 2)
+constexpr int kMany = 8, kFew = 2;
+constexpr int64_t kSmallBytes = int64_t(32) << 20;
+constexpr int64_t chunk_bytes(int pieces) { return (int64_t)pieces * 16 * 256; }
 
+// one entry is half a cache line: the argument lies in host memory
+struct GradEntry {
+    const void *g;
+    void *out;
+    int64_t n;
+    int32_t first, dtype;                     // first: the tensor's first chunk in the launch
+};
 struct GradTable {
-    const void *g[kTensors];
-    void *out[kTensors];
-    int64_t n[kTensors];
-    int32_t first[kTensors + 1];              // a tensor's first chunk in the launch
-    uint8_t dtype[kTensors];
-    int32_t count;
+    int32_t count, chunks;
+    GradEntry t[kTensors];
 };
 
-// Chunk c of a tensor, one 16-byte piece a lane at a time. A whole chunk is eight
-// loads before the first use, f(values, index of the first); at a tensor's ends
-// the values come one by one, g(value, index).
-template <typename T, typename F, typename G> __device__ inline void each_of_chunk(const void *g, int64_t n, int64_t c, F f, G one)
+// the tensor that holds chunk c
+__device__ inline int tensor_of(const GradTable &t, int c)
 {
-    constexpr int V = 16 / sizeof(T), kPieces = kChunk / 16 / 256;
+    int lo = 0, hi = t.count - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) / 2;
+        if (t.t[mid].first <= c) lo = mid;
+        else hi = mid - 1;
+    }
+    return lo;
+}
+
+// Chunk c of a tensor, one 16-byte piece a lane at a time. A whole chunk's loads
+// precede the first use, f(values, index of the first); at a tensor's ends
+// the values come one by one, g(value, index).
+template <int kPieces, typename T, typename F, typename G> __device__ inline void each_of_chunk(const void *g, int64_t n, int64_t c, F f, G one)
+{
+    constexpr int V = 16 / sizeof(T);
+    constexpr int64_t kChunk = chunk_bytes(kPieces);
     typedef T piece __attribute__((ext_vector_type(V)));
     const uintptr_t p = (uintptr_t)g;
     const int64_t skew = (int64_t)(p & 15) / (int64_t)sizeof(T);        // values before g in its first piece
@@ -52,11 +73,11 @@ template <typename T, typename F, typename G> __device__ inline void each_of_chu
             if (v + j >= skew && v + j < end) one(base[v + j], v + j - skew);
 }
 
-template <typename T> __device__ inline double chunk_squares(const void *g, int64_t n, int64_t c)
+template <int PIECES, typename T> __device__ inline double chunk_squares(const void *g, int64_t n, int64_t c)
 {
     double s = 0;
     auto add = [&](float v) { s = fma((double)v, (double)v, s); };
-    each_of_chunk<T>(g, n, c, [&](auto x, int64_t) {
+    each_of_chunk<PIECES, T>(g, n, c, [&](auto x, int64_t) {
 #pragma unroll
         for (int i = 0; i < 16 / (int)sizeof(T); i++) add((float)x[i]);
     }, [&](T x, int64_t) { add((float)x); });
@@ -76,17 +97,19 @@ __device__ inline double block_sum(double s, double *lds)
 }
 
 // held: sums that earlier launches left
-__global__ void __launch_bounds__(256) grad_squares_kernel(GradTable t, double *parts, int held)
+template <int PIECES> __global__ void __launch_bounds__(256) grad_squares_kernel(GradTable t, double *parts, int held)
 {
     __shared__ double lds[4];
     double s = 0;
-    int k = 0;
-    for (int c = blockIdx.x; c < t.first[t.count]; c += gridDim.x) {
-        while (c >= t.first[k + 1]) k++;
-        const int64_t local = c - t.first[k];
-        if (t.dtype[k] == HEDDLE_T_BF16) s += chunk_squares<__bf16>(t.g[k], t.n[k], local);
-        else if (t.dtype[k] == HEDDLE_T_F16) s += chunk_squares<_Float16>(t.g[k], t.n[k], local);
-        else s += chunk_squares<float>(t.g[k], t.n[k], local);
+    int k = -1;
+    for (int c = blockIdx.x; c < t.chunks; c += gridDim.x) {
+        if (k < 0) k = tensor_of(t, c);
+        while (k + 1 < t.count && c >= t.t[k + 1].first) k++;
+        const GradEntry &e = t.t[k];
+        const int64_t local = c - e.first;
+        if (e.dtype == HEDDLE_T_BF16) s += chunk_squares<PIECES, __bf16>(e.g, e.n, local);
+        else if (e.dtype == HEDDLE_T_F16) s += chunk_squares<PIECES, _Float16>(e.g, e.n, local);
+        else s += chunk_squares<PIECES, float>(e.g, e.n, local);
     }
     s = block_sum(s, lds);
     if (threadIdx.x == 0) parts[blockIdx.x] = (int)blockIdx.x < held ? parts[blockIdx.x] + s : s;
@@ -106,10 +129,10 @@ __global__ void __launch_bounds__(256) grad_norm_kernel(const double *parts, int
     if (threadIdx.x == 0) *norm = v;
 }
 
-template <typename T>
+template <int PIECES, typename T>
 __device__ inline void clip_chunk(const void *g, void *out, int64_t n, int64_t c, float factor)
 {
-    each_of_chunk<T>(g, n, c, [&](auto x, int64_t at) {
+    each_of_chunk<PIECES, T>(g, n, c, [&](auto x, int64_t at) {
 #pragma unroll
         for (int i = 0; i < 16 / (int)sizeof(T); i++) x[i] = (T)((float)x[i] * factor);
         __builtin_memcpy((T *)out + at, &x, 16);      // out may start anywhere its values may
@@ -118,8 +141,8 @@ __device__ inline void clip_chunk(const void *g, void *out, int64_t n, int64_t c
 
 // The factor from d_norm, or from the parts (then the first workgroup of the
 // first launch writes the norm).
-__global__ void __launch_bounds__(256) clip_kernel(GradTable t, const double *parts, int count, float *norm, int write,
-                                                   float max_norm)
+template <int PIECES>
+__global__ void __launch_bounds__(256) clip_kernel(GradTable t, const double *parts, int count, float *norm, int write, float max_norm)
 {
     __shared__ double lds[4];
     float v;
@@ -133,14 +156,16 @@ __global__ void __launch_bounds__(256) clip_kernel(GradTable t, const double *pa
     if (factor >= 1.0f) factor = 1.0f;                                  // a NaN stays
     // The table runs from the last tensor to the first, and so do a tensor's chunks here: what
     // the norm read last is still in the 256 MB memory-side cache.
-    int k = 0;
-    for (int c = blockIdx.x; c < t.first[t.count]; c += gridDim.x) {
-        while (c >= t.first[k + 1]) k++;
-        if (factor == 1.0f && t.out[k] == t.g[k]) continue;
-        const int64_t local = t.first[k + 1] - 1 - c;
-        if (t.dtype[k] == HEDDLE_T_BF16) clip_chunk<__bf16>(t.g[k], t.out[k], t.n[k], local, factor);
-        else if (t.dtype[k] == HEDDLE_T_F16) clip_chunk<_Float16>(t.g[k], t.out[k], t.n[k], local, factor);
-        else clip_chunk<float>(t.g[k], t.out[k], t.n[k], local, factor);
+    int k = -1;
+    for (int c = blockIdx.x; c < t.chunks; c += gridDim.x) {
+        if (k < 0) k = tensor_of(t, c);
+        while (k + 1 < t.count && c >= t.t[k + 1].first) k++;
+        const GradEntry &e = t.t[k];
+        if (factor == 1.0f && e.out == e.g) continue;
+        const int64_t local = (k + 1 < t.count ? t.t[k + 1].first : t.chunks) - 1 - c;
+        if (e.dtype == HEDDLE_T_BF16) clip_chunk<PIECES, __bf16>(e.g, e.out, e.n, local, factor);
+        else if (e.dtype == HEDDLE_T_F16) clip_chunk<PIECES, _Float16>(e.g, e.out, e.n, local, factor);
+        else clip_chunk<PIECES, float>(e.g, e.out, e.n, local, factor);
     }
 }
 
@@ -160,32 +185,31 @@ static int check_grads(const heddle_grad_desc *g, int32_t count)
     return HEDDLE_OK;
 }
 
-static int64_t chunks_of(const heddle_grad_desc &g)
+static int64_t bytes_of(const heddle_grad_desc &g) { return g.n * (g.dtype == HEDDLE_T_F32 ? 4 : 2); }
+
+static bool is_small(const heddle_grad_desc *g, int32_t count)
 {
-    const int64_t size = g.dtype == HEDDLE_T_F32 ? 4 : 2, skew = (int64_t)((uintptr_t)g.g & 15);
-    return g.n > 0 ? (skew + g.n * size + kChunk - 1) / kChunk : 0;
+    int64_t all = 0;
+    for (int32_t i = 0; i < count; i++) all += bytes_of(g[i]);
+    return all < kSmallBytes;
 }
 
 // tables of up to kTensors tensors (and 2^30 chunks) each, from the first tensor or from
 // the last; f(table) launches
-template <typename F> static int each_table(const heddle_grad_desc *g, int32_t count, bool backward, F f)
+template <typename F> static int each_table(const heddle_grad_desc *g, int32_t count, bool small, bool backward, F f)
 {
+    const int64_t chunk = chunk_bytes(small ? kFew : kMany);
     int32_t done = 0;
     do {
         GradTable t;
-        t.count = 0;
-        t.first[0] = 0;
+        t.count = t.chunks = 0;
         for (; done < count && t.count < kTensors; done++) {
             const heddle_grad_desc &d = g[backward ? count - 1 - done : done];
-            const int64_t c = chunks_of(d);
-            if (c == 0) continue;
-            if (t.first[t.count] + c > (int64_t(1) << 30)) break;
-            const int k = t.count++;
-            t.g[k] = d.g;
-            t.out[k] = d.out ? d.out : const_cast<void *>(d.g);
-            t.n[k] = d.n;
-            t.dtype[k] = (uint8_t)d.dtype;
-            t.first[k + 1] = (int32_t)(t.first[k] + c);
+            if (d.n == 0) continue;
+            const int64_t c = ((int64_t)((uintptr_t)d.g & 15) + bytes_of(d) + chunk - 1) / chunk;
+            if (t.chunks + c > (int64_t(1) << 30)) break;
+            t.t[t.count++] = {d.g, d.out ? d.out : const_cast<void *>(d.g), d.n, t.chunks, d.dtype};
+            t.chunks += (int32_t)c;
         }
         const int rc = f(t);
         if (rc) return rc;
@@ -203,10 +227,12 @@ static int check_parts(const void *ws, int64_t bytes)
 // the sums of squares; *parts: how many
 static int launch_squares(const heddle_grad_desc *g, int32_t count, double *ws, int *parts, hipStream_t stream)
 {
+    const bool small = is_small(g, count);
     *parts = 0;
-    return each_table(g, count, false, [&](const GradTable &t) {
-        const int mine = t.first[t.count], blocks = mine < 1 ? 1 : mine < kParts ? mine : kParts;
-        hipLaunchKernelGGL(grad_squares_kernel, dim3((unsigned)blocks), dim3(256), 0, stream, t, ws, *parts);
+    return each_table(g, count, small, false, [&](const GradTable &t) {
+        const int blocks = t.chunks < 1 ? 1 : t.chunks < kParts ? t.chunks : kParts;
+        auto kernel = small ? grad_squares_kernel<kFew> : grad_squares_kernel<kMany>;
+        hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), 0, stream, t, ws, *parts);
         if (blocks > *parts) *parts = blocks;
         const hipError_t e = hipGetLastError();
         return e == hipSuccess ? HEDDLE_OK : hip_fail(e, "grad_squares_kernel");
@@ -216,11 +242,12 @@ static int launch_squares(const heddle_grad_desc *g, int32_t count, double *ws, 
 static int launch_clip(const heddle_grad_desc *g, int32_t count, const double *parts, int n_parts, float *norm, float max_norm,
                        hipStream_t stream)
 {
+    const bool small = is_small(g, count);
     int write = 1;
-    return each_table(g, count, true, [&](const GradTable &t) {
-        const int64_t mine = t.first[t.count];
-        const int64_t blocks = mine < 1 ? 1 : mine < kParts ? mine : kParts;
-        hipLaunchKernelGGL(clip_kernel, dim3((unsigned)blocks), dim3(256), 0, stream, t, parts, n_parts, norm, write, max_norm);
+    return each_table(g, count, small, true, [&](const GradTable &t) {
+        const int blocks = t.chunks < 1 ? 1 : t.chunks < kParts ? t.chunks : kParts;
+        auto kernel = small ? clip_kernel<kFew> : clip_kernel<kMany>;
+        hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), 0, stream, t, parts, n_parts, norm, write, max_norm);
         write = 0;
         const hipError_t e = hipGetLastError();
         return e == hipSuccess ? HEDDLE_OK : hip_fail(e, "clip_kernel");
