@@ -694,7 +694,10 @@ inline int launch_gemm(const Args &x, const Shape &s, const Epi &epi, hipStream_
     switch (s.cfg) {
     case 0: return launch_cfg<256, 256, 2, 4, 2, ACOL, BCOL, GR, T>(x, s, epi, stream);
     case 1: return launch_cfg<128, 128, 2, 2, 1, ACOL, BCOL, GR, T>(x, s, epi, stream);
-    default: return launch_cfg<64, 128, 1, 4, 2, ACOL, BCOL, GR, T>(x, s, epi, stream);
+    case 2: return launch_cfg<64, 128, 1, 4, 2, ACOL, BCOL, GR, T>(x, s, epi, stream);
+    default:   // groups of few rows only
+        if constexpr (GR == kGroupRows) return launch_cfg<64, 256, 1, 4, 2, ACOL, BCOL, GR, T>(x, s, epi, stream);
+        else return fail(HEDDLE_E_INVAL, "no such tile");
     }
 }
 
