@@ -59,7 +59,7 @@ static int hidden(const Operand &a, const Operand &b, int64_t t, int64_t f, int6
                   const Epi &epi, Scratch &s, bool run, hipStream_t stream)
 {
     const bool skinny = !BCOL && is_skinny(t, offsets ? groups : 1);
-    const Shape sh = shape_of(t, f, k, offsets ? groups : 1, Epi::gated, BCOL ? kRowsCols : kRowsRows);
+    const Shape sh = shape_of(t, f, k, offsets ? groups : 0, Epi::gated, BCOL ? kRowsCols : kRowsRows);
     Args x = {};
     if (!skinny) x.partial = (float *)s.take(partial_bytes(sh, t, f, Epi::gated));
     if (!run || t == 0) return HEDDLE_OK;

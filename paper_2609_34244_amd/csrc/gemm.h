@@ -658,7 +658,7 @@ template <typename Epi> __global__ void __launch_bounds__(256) join_kernel(Args 
 // A tile shape and the parts of the reduction.
 struct Shape { int cfg, splits, split_tiles; };
 enum Order { kRowsRows = 0, kRowsCols = 1, kColsCols = 2 };   // of the operands in memory
-Shape shape_of(int64_t M, int64_t N, int64_t K, int groups, bool gated, Order order);
+Shape shape_of(int64_t M, int64_t N, int64_t K, int groups, bool gated, Order order);   // groups: 0 without offsets
 inline size_t partial_bytes(const Shape &s, int64_t M, int64_t N, bool gated)
 {
     return s.splits > 1 ? (size_t)s.splits * M * partial_cols((int)N, gated) * 4 : 0;

@@ -27,16 +27,17 @@ Shape shape_of(int64_t M, int64_t N, int64_t K, int groups, bool gated, Order or
     const int cus = 256;
     const bool sums = order == kColsCols;
     const int64_t cols = gated ? 2 * N : N, kt = K > 0 ? (K + kBK - 1) / kBK : 1;
-    // groups: every one of the average size
-    const int64_t rows = groups > 1 && !sums ? (M + groups - 1) / groups : M, outer = groups > 1 ? groups : 1;
-    const int64_t steps = groups > 1 && sums ? (kt + groups - 1) / groups : kt;
+    // groups: every one of the average size; with offsets, also of one group, a reduction is not split
+    const bool grouped = groups > 0;
+    const int64_t rows = grouped && !sums ? (M + groups - 1) / groups : M, outer = grouped ? groups : 1;
+    const int64_t steps = grouped && sums ? (kt + groups - 1) / groups : kt;
     Shape best = {0, 1, (int)kt};
     // Experts of few rows: the weights' reading bounds, and tiles of 64 x 256 read 512 bytes of
     // a row of theirs (64 experts of 64 rows, 1632 of 4096 columns: 208 us, 248 with 64 x 128).
-    if (groups > 1 && !sums && rows <= 96 && cols > 128) return {3, 1, (int)kt};
+    if (grouped && !sums && rows <= 96 && cols > 128) return {3, 1, (int)kt};
     double least = 0;
     for (int c = 0; c < 3; c++)
-        for (int s = 1, log2 = 0; s == 1 || (s <= 16 && groups <= 1 && (kt + s - 1) / s >= 4); s *= 2, log2++) {
+        for (int s = 1, log2 = 0; s == 1 || (s <= 16 && !grouped && (kt + s - 1) / s >= 4); s *= 2, log2++) {
             const double part = (double)((steps + s - 1) / s);
             const int64_t tiles = (rows + cfg[c].bm - 1) / cfg[c].bm * ((cols + cfg[c].bn - 1) / cfg[c].bn) * outer * s;
             const int64_t full = tiles / (cus * cfg[c].per_cu), rest = tiles - full * cus * cfg[c].per_cu;
@@ -208,7 +209,7 @@ int product(bool cols_b, const Operand &a, const Operand &b, int64_t m, int64_t 
             const int32_t *offsets, EpiLinear<T> epi, Scratch &s, bool run, hipStream_t stream)
 {
     const bool skinny = !cols_b && is_skinny(m, offsets ? groups : 1);
-    const Shape sh = shape_of(m, n, k, offsets ? groups : 1, false, cols_b ? kRowsCols : kRowsRows);
+    const Shape sh = shape_of(m, n, k, offsets ? groups : 0, false, cols_b ? kRowsCols : kRowsRows);
     Args x = {};
     if (!skinny) x.partial = (float *)s.take(partial_bytes(sh, m, n, false));
     if (!run || m == 0) return HEDDLE_OK;
@@ -226,7 +227,7 @@ template <typename T>
 int product_sum(const Operand &a, const Operand &b, int64_t m, int64_t n, int64_t k, int groups, const int32_t *offsets,
                 EpiLinear<T> epi, Scratch &s, bool run, hipStream_t stream)
 {
-    const Shape sh = shape_of(m, n, k, offsets ? groups : 1, false, kColsCols);
+    const Shape sh = shape_of(m, n, k, offsets ? groups : 0, false, kColsCols);
     Args x = {};
     x.partial = (float *)s.take(partial_bytes(sh, m, n, false));
     if (!run) return HEDDLE_OK;

@@ -187,6 +187,19 @@ def test_linear_groups(H, kind, rows, groups, k, n, gap, shift):
     mk.untouched()
 
 
+@pytest.mark.parametrize("rows,k,n", [(1500, 72, 40), (100, 2048, 72), (20, 4096, 24)])
+def test_linear_one_group(H, rows, k, n):
+    """one expert's rows: the same as without offsets, also where that product's reduction is divided"""
+    mk = Maker(rows, torch.bfloat16)
+    x, w, dy = mk.part((rows, k), 0, 0, 1.0), mk.part((n, k), 0, 0, k ** -0.5), mk.part((rows, n), 0, 0, 1.0)
+    off = torch.tensor([0, rows], dtype=torch.int32, device="cuda")
+    y, by, _, _ = R.linear(x, w, None, "none", None, torch.bfloat16)
+    near(H.heddle_linear(x, w[None], offsets=off), y, by, "y")
+    got = H.heddle_linear_backward(dy, x, w[None], offsets=off, want_db=True)
+    for key, (c, e) in R.linear_backward(dy, x, w, "none", None, torch.bfloat16).items():
+        near(got[key].view(c.shape), c, e, key)
+
+
 def run_ffn(H, seed, t, d, f, act, residual, dtype, off=None, gap=0, shift=0):
     print(f"ffn {t} {d} {f} {act} residual={residual} {dtype} groups={off and len(off) - 1} gap={gap} shift={shift}", flush=True)
     mk = Maker(seed, dtype)
