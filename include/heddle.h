@@ -586,11 +586,13 @@ int heddle_profile_info_get(const heddle_profile *p, heddle_profile_info *info);
 
 #define HEDDLE_MAX_LD      (1 << 22)
 #define HEDDLE_MAX_GROUPS  65535
+#define HEDDLE_MAX_ROWS    (1 << 30)
 
 /* Y = act(Z) + R with Z = X W^T + b, and its gradients. */
 typedef struct heddle_linear_desc {
     int32_t dtype, act;
-    int64_t m, n, k;                                  /* rows of X; columns of Y and of X; m >= 0, n, k >= 1 */
+    int64_t m, n, k;                                  /* rows of X, 0 .. HEDDLE_MAX_ROWS; columns of Y and of X,
+                                                         1 .. HEDDLE_MAX_LD */
     const void *x; int64_t ldx;                       /* [m][k] */
     const void *w; int64_t ldw;                       /* [n][k]; grouped: [groups][n][k] */
     const void *bias;                                 /* [n] ([groups][n]) or NULL */
@@ -627,7 +629,8 @@ int heddle_linear_workspace(const heddle_linear_desc *d, int32_t backward, int64
  */
 typedef struct heddle_gated_ffn_desc {
     int32_t dtype, act;
-    int64_t t, d, f;                                  /* rows, model width, hidden units; t >= 0, d, f >= 1 */
+    int64_t t, d, f;                                  /* rows, 0 .. HEDDLE_MAX_ROWS; model width and hidden units,
+                                                         d and 2 f 1 .. HEDDLE_MAX_LD */
     const void *x; int64_t ldx;                       /* [t][d] */
     const void *w_in; int64_t ldw_in;                 /* [2 f][d]; grouped: [groups][2 f][d] */
     const void *w_out; int64_t ldw_out;               /* [d][f]; grouped: [groups][d][f] */

@@ -8,7 +8,7 @@
 namespace heddle {
 namespace mm {
 
-constexpr int64_t kMaxRows = 0x7FFFFFFF - 512;
+constexpr int64_t kMaxRows = HEDDLE_MAX_ROWS;   // sums of a row and a few tiles or chunks stay 32-bit
 
 // Distance between rows of a scratch matrix: whole 128-byte lines, an odd number of them, so
 // that the 128 bytes a tile reads of a row are one line and neighbouring rows lie in
