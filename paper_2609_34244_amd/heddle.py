@@ -440,6 +440,11 @@ def heddle_fill_plans(profiles, mbs, cl, global_batch, dp_cap, n_stages, stages,
 # ---- feed-forward and gradient operators ----
 # A call on small tensors takes as long as its marshalling, so a descriptor is
 # packed in one step and every tensor is looked at once.
+#
+# stream: a torch stream of the tensors' GPU, torch's current one without. Its
+# work precedes the call's; inputs of another stream's making must be waited
+# for by the caller. Outputs that the call allocates belong to that stream, as
+# those of torch's operators under torch.cuda.stream(stream) do.
 
 _LINEAR = struct.Struct("@iiqqqPqPqPPqPqPqiPqPqPqPqqP")
 _GATED_FFN = struct.Struct("@iiqqqPqPqPqPqPqPqiPqqPqPqPqqPqq")
@@ -512,15 +517,25 @@ def _rows(x, w, what):
 
 
 def _fresh(like, shape, stream):
-    t = like.new_empty(shape)
-    if stream is not None:
-        t.record_stream(stream)
-    return t
+    return _on_stream(stream, lambda: like.new_empty(shape))
+
+
+def _on_stream(stream, make):
+    """make() with the call's stream current: torch's allocator may hand out
+    memory that only the current stream's earlier work still uses, so memory
+    for a call must come from the stream that the call runs on"""
+    if stream is None:
+        return make()
+    import torch
+    with torch.cuda.stream(stream):
+        return make()
 
 
 def _on_gpu(gpu, stream, call):
     """call(stream handle) with the tensors' GPU current"""
     import torch
+    if stream is not None and stream.device.index != gpu:
+        _refuse(f"stream: of {stream.device}, the tensors are on GPU {gpu}")
     if torch.cuda.current_device() != gpu:
         with torch.cuda.device(gpu):
             return _on_gpu(gpu, stream, call)
@@ -536,9 +551,7 @@ def _run(work, need, desc, backward, like, gpu, stream):
         _check(need(desc, backward, C.byref(n)))
         ws = None
         if n.value:
-            ws = torch.empty(n.value, dtype=torch.uint8, device=like.device)
-            if stream is not None:
-                ws.record_stream(stream)
+            ws = _on_stream(stream, lambda: torch.empty(n.value, dtype=torch.uint8, device=like.device))
         return work(desc, None if ws is None else ws.data_ptr(), n.value, handle)
 
     _on_gpu(gpu, stream, call)
@@ -677,11 +690,8 @@ def _norm_call(table, count, gpu, stream, work):
     if gpu is None:
         gpu = torch.cuda.current_device()
     # the norm and the scratch of the call
-    norm = torch.empty(1, dtype=torch.float32, device=gpu)
-    ws = torch.empty(n.value, dtype=torch.uint8, device=gpu)
-    if stream is not None:
-        norm.record_stream(stream)
-        ws.record_stream(stream)
+    norm, ws = _on_stream(stream, lambda: (torch.empty(1, dtype=torch.float32, device=gpu),
+                                           torch.empty(n.value, dtype=torch.uint8, device=gpu)))
     _on_gpu(gpu, stream, lambda handle: work(norm.data_ptr(), ws.data_ptr(), n.value, handle))
     return norm
 
