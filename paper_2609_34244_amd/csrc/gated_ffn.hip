@@ -55,10 +55,9 @@ static int check_ffn(const heddle_gated_ffn_desc *d, bool backward)
 }
 
 template <typename T, typename Epi, bool BCOL>
-static int hidden(const Operand &a, const Operand &b, int64_t t, int64_t f, int64_t k, int groups, const int32_t *offsets,
+static int hidden(bool skinny, const Operand &a, const Operand &b, int64_t t, int64_t f, int64_t k, int groups, const int32_t *offsets,
                   const Epi &epi, Scratch &s, bool run, hipStream_t stream)
 {
-    const bool skinny = !BCOL && is_skinny(t, offsets ? groups : 1);
     const Shape sh = shape_of(t, f, k, offsets ? groups : 0, Epi::gated, BCOL ? kRowsCols : kRowsRows);
     Args x = {};
     if (!skinny) x.partial = (float *)s.take(partial_bytes(sh, t, f, Epi::gated));
@@ -78,22 +77,25 @@ template <typename T> static int forward(const heddle_gated_ffn_desc *d, Scratch
     const int groups = d->d_offsets ? d->groups : 1;
     if (d->t == 0) return HEDDLE_OK;
     Operand x = {d->x, d->ldx, 0}, wi = {d->w_in, d->ldw_in, d->stride_in}, wo = {d->w_out, d->ldw_out, d->stride_out};
-    if (!is_skinny(d->t, groups)) {
-        Copies c;
+    const int used = d->d_offsets ? groups : 0;
+    const bool skinny_in = is_skinny(d->t, 2 * d->f, d->d, used, needs_copy(x, 1) || needs_copy(wi, groups));
+    const bool skinny_out = is_skinny(d->t, d->d, d->f, used, needs_copy(wo, groups));
+    Copies c;
+    if (!skinny_in) {
         c.add(x, d->t, d->d, 1, s);
         c.add(wi, 2 * d->f, d->d, groups, s);
-        c.add(wo, d->d, d->f, groups, s);
-        if (const int rc = run ? c.launch(stream) : HEDDLE_OK) return rc;
     }
+    if (!skinny_out) c.add(wo, d->d, d->f, groups, s);
+    if (const int rc = run ? c.launch(stream) : HEDDLE_OK) return rc;
     EpiGated<T> e = {};
     e.ldh = scratch_ld(d->f), e.h = (T *)s.take((size_t)d->t * e.ldh * 2);
     e.pre = (T *)d->preact, e.ldp = d->ldp;
     e.act = d->act, e.N = (int)d->f;
-    int rc = hidden<T, EpiGated<T>, false>(x, wi, d->t, d->f, d->d, groups, d->d_offsets, e, s, run, stream);
+    int rc = hidden<T, EpiGated<T>, false>(skinny_in, x, wi, d->t, d->f, d->d, groups, d->d_offsets, e, s, run, stream);
     if (rc) return rc;
     EpiLinear<T> o = plain_output<T>(d->y, d->ldy, d->d);
     o.residual = (const T *)d->residual, o.ldr = d->ldr;
-    return product<T>(false, {e.h, e.ldh, 0}, wo, d->t, d->d, d->f, groups, d->d_offsets, o, s, run, stream);
+    return product<T>(false, skinny_out, {e.h, e.ldh, 0}, wo, d->t, d->d, d->f, groups, d->d_offsets, o, s, run, stream);
 }
 
 template <typename T> static int backward(const heddle_gated_ffn_desc *d, Scratch &s, bool run, hipStream_t stream)
@@ -118,11 +120,11 @@ template <typename T> static int backward(const heddle_gated_ffn_desc *d, Scratc
     e.h = (T *)s.take((size_t)d->t * e.ldh * 2);
     e.pre = (const T *)d->preact, e.ldp = d->ldp;
     e.act = d->act, e.N = (int)d->f;
-    rc = hidden<T, EpiGatedGrad<T>, true>(dy, wo, d->t, d->f, d->d, groups, d->d_offsets, e, s, run, stream);
+    rc = hidden<T, EpiGatedGrad<T>, true>(false, dy, wo, d->t, d->f, d->d, groups, d->d_offsets, e, s, run, stream);
     if (rc) return rc;
     const Operand dp = {e.dp, e.ldd, 0}, h = {e.h, e.ldh, 0};
     if (d->dx)
-        rc = product<T>(true, dp, wi, d->t, d->d, 2 * d->f, groups, d->d_offsets, plain_output<T>(d->dx, d->lddx, d->d), s,
+        rc = product<T>(true, false, dp, wi, d->t, d->d, 2 * d->f, groups, d->d_offsets, plain_output<T>(d->dx, d->lddx, d->d), s,
                         run, stream);
     if (rc == HEDDLE_OK && d->dw_in)
         rc = product_sum<T>(dp, x, 2 * d->f, d->d, d->t, groups, d->d_offsets,

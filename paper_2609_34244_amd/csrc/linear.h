@@ -68,9 +68,10 @@ int launch_bias_grad(int dtype, BiasGrad b, hipStream_t stream);
 
 int check_matrix(const char *name, const void *p, int64_t ld, int64_t cols);
 
-// C = A B^T of plain row-major outputs with EpiLinear; sum: C = A^T B over rows
+// C = A B^T of plain row-major outputs with EpiLinear (skinny: by is_skinny, with operands as
+// they are); sum: C = A^T B over rows
 template <typename T>
-int product(bool cols_b, const Operand &a, const Operand &b, int64_t m, int64_t n, int64_t k, int groups,
+int product(bool cols_b, bool skinny, const Operand &a, const Operand &b, int64_t m, int64_t n, int64_t k, int groups,
             const int32_t *offsets, EpiLinear<T> epi, Scratch &s, bool run, hipStream_t stream);
 template <typename T>
 int product_sum(const Operand &a, const Operand &b, int64_t m, int64_t n, int64_t k, int groups, const int32_t *offsets,

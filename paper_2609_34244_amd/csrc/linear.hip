@@ -205,10 +205,9 @@ int launch_bias_grad(int dtype, BiasGrad b, hipStream_t stream)
 }
 
 template <typename T>
-int product(bool cols_b, const Operand &a, const Operand &b, int64_t m, int64_t n, int64_t k, int groups,
+int product(bool cols_b, bool skinny, const Operand &a, const Operand &b, int64_t m, int64_t n, int64_t k, int groups,
             const int32_t *offsets, EpiLinear<T> epi, Scratch &s, bool run, hipStream_t stream)
 {
-    const bool skinny = !cols_b && is_skinny(m, offsets ? groups : 1);
     const Shape sh = shape_of(m, n, k, offsets ? groups : 0, false, cols_b ? kRowsCols : kRowsRows);
     Args x = {};
     if (!skinny) x.partial = (float *)s.take(partial_bytes(sh, m, n, false));
@@ -240,7 +239,7 @@ int product_sum(const Operand &a, const Operand &b, int64_t m, int64_t n, int64_
 }
 
 #define HEDDLE_PRODUCTS(T)                                                                                             \
-    template int product<T>(bool, const Operand &, const Operand &, int64_t, int64_t, int64_t, int, const int32_t *,   \
+    template int product<T>(bool, bool, const Operand &, const Operand &, int64_t, int64_t, int64_t, int, const int32_t *,   \
                             EpiLinear<T>, Scratch &, bool, hipStream_t);                                               \
     template int product_sum<T>(const Operand &, const Operand &, int64_t, int64_t, int64_t, int, const int32_t *,     \
                                 EpiLinear<T>, Scratch &, bool, hipStream_t);
@@ -293,7 +292,8 @@ template <typename T> static int forward(const heddle_linear_desc *d, Scratch &s
 {
     const int groups = d->d_offsets ? d->groups : 1;
     Operand x = {d->x, d->ldx, 0}, w = {d->w, d->ldw, d->stride_w};
-    if (!is_skinny(d->m, groups)) {
+    const bool skinny = is_skinny(d->m, d->n, d->k, d->d_offsets ? groups : 0, needs_copy(x, 1) || needs_copy(w, groups));
+    if (!skinny) {
         Copies c;
         c.add(x, d->m, d->k, 1, s);
         c.add(w, d->n, d->k, groups, s);
@@ -304,7 +304,7 @@ template <typename T> static int forward(const heddle_linear_desc *d, Scratch &s
     e.bias = (const T *)d->bias;
     e.residual = (const T *)d->residual, e.ldr = d->ldr;
     e.act = d->act;
-    return product<T>(false, x, w, d->m, d->n, d->k, groups, d->d_offsets, e, s, run, stream);
+    return product<T>(false, skinny, x, w, d->m, d->n, d->k, groups, d->d_offsets, e, s, run, stream);
 }
 
 template <typename T> static int backward(const heddle_linear_desc *d, Scratch &s, bool run, hipStream_t stream)
@@ -330,7 +330,7 @@ template <typename T> static int backward(const heddle_linear_desc *d, Scratch &
     if (d->dw) c.add(x, d->m, d->k, 1, s);
     if (rc == HEDDLE_OK && run) rc = c.launch(stream);
     if (rc == HEDDLE_OK && d->dx)
-        rc = product<T>(true, dz, w, d->m, d->k, d->n, groups, d->d_offsets, plain_output<T>(d->dx, d->lddx, d->k), s, run,
+        rc = product<T>(true, false, dz, w, d->m, d->k, d->n, groups, d->d_offsets, plain_output<T>(d->dx, d->lddx, d->k), s, run,
                         stream);
     if (rc == HEDDLE_OK && d->dw)
         rc = product_sum<T>(dz, x, d->n, d->k, d->m, groups, d->d_offsets,

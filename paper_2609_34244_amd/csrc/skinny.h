@@ -42,10 +42,23 @@ __device__ inline bool find_group(const int32_t *offsets, int groups, int total,
     return false;
 }
 
-template <typename T> __device__ inline typename pack8<T>::type load_any(const T *p)
+// eight values at any address that values may have. ODD: by whole words, as loads of 16 bytes
+// at addresses that are odd multiples of 2 run at half the rate (20000 x 4096, one row: 73 us
+// against 42); no word without one of the values is read.
+template <bool ODD, typename T> __device__ inline typename pack8<T>::type load_any(const T *p)
 {
     typename pack8<T>::type v;
-    __builtin_memcpy(&v, p, 16);
+    if (!ODD) {
+        __builtin_memcpy(&v, p, 16);
+        return v;
+    }
+    const uint32_t *words = (const uint32_t *)((uintptr_t)p & ~(uintptr_t)3), skew = (uint32_t)((uintptr_t)p & 2);
+    uint32_t w[5];
+    __builtin_memcpy(w, words, 16);
+    w[4] = words[3 + skew / 2];
+#pragma unroll
+    for (int i = 0; i < 4; i++) w[i] = __builtin_amdgcn_alignbyte(w[i + 1], w[i], skew);
+    __builtin_memcpy(&v, w, 16);
     return v;
 }
 // the values with index below count; the others are zero and not read
@@ -57,7 +70,8 @@ template <typename T> __device__ inline typename pack8<T>::type load_some(const 
     return v;
 }
 
-template <int MB, int WAVES, typename T, typename Epi> __global__ void __launch_bounds__(WAVES * 64) skinny_kernel(Args x, Epi epi)
+template <int MB, int WAVES, bool ODD, typename T, typename Epi>
+__global__ void __launch_bounds__(WAVES * 64) skinny_kernel(Args x, Epi epi)
 {
     constexpr bool PAIR = Epi::gated;
     constexpr int P = PAIR ? 2 : 1, U = MB * P > 1 ? 4 : 8;
@@ -68,7 +82,7 @@ template <int MB, int WAVES, typename T, typename Epi> __global__ void __launch_
     int g = 0, lo = 0, hi = x.M;
     if (x.offsets && !find_group(x.offsets, x.groups, x.M, blockIdx.y, g, lo, hi)) return;
     const int n0 = blockIdx.x * 16;
-    const T *w = (const T *)x.b + (int64_t)g * x.stride_b + (int64_t)(n0 + min(i, x.N - 1 - n0)) * x.ldb;
+    const T *w = (const T *)x.b + (int64_t)g * x.stride_b + (int64_t)min(n0 + i, x.N - 1) * x.ldb;
     const int64_t up = PAIR ? (int64_t)x.F * x.ldb : 0;
     // whole 32-k steps of this wavefront, and the last, partial one
     const int steps = x.K / 32, each = (steps + WAVES - 1) / WAVES;
@@ -91,9 +105,9 @@ template <int MB, int WAVES, typename T, typename Epi> __global__ void __launch_
             for (int u = 0; u < N; u++) {
                 const int k = (s + u) * 32 + kg;
 #pragma unroll
-                for (int p = 0; p < P; p++) fw[p][u] = load_any(w + p * up + k);
+                for (int p = 0; p < P; p++) fw[p][u] = load_any<ODD>(w + p * up + k);
 #pragma unroll
-                for (int b = 0; b < MB; b++) fx[b][u] = load_any(xr[b] + k);
+                for (int b = 0; b < MB; b++) fx[b][u] = load_any<ODD>(xr[b] + k);
             }
 #pragma unroll
             for (int u = 0; u < N; u++)
@@ -105,15 +119,18 @@ template <int MB, int WAVES, typename T, typename Epi> __global__ void __launch_
         };
         while (s + U <= last) batch(std::integral_constant<int, U>());
         if (U > 4 && s + 4 <= last) batch(std::integral_constant<int, 4>());
-        if (s + 2 <= last) batch(std::integral_constant<int, 2>());
+        if (U > 2 && s + 2 <= last) batch(std::integral_constant<int, 2>());
         if (s < last) batch(std::integral_constant<int, 1>());
         if (wave == WAVES - 1 && x.K % 32) {
             const int k = steps * 32 + kg, count = x.K - k;
+            frag fx[MB];
+#pragma unroll
+            for (int b = 0; b < MB; b++) fx[b] = load_some(xr[b] + k, count);
 #pragma unroll
             for (int p = 0; p < P; p++) {
                 const frag fw = load_some(w + p * up + k, count);
 #pragma unroll
-                for (int b = 0; b < MB; b++) acc[p][b] = mfma16(fw, load_some(xr[b] + k, count), acc[p][b]);
+                for (int b = 0; b < MB; b++) acc[p][b] = mfma16(fw, fx[b], acc[p][b]);
             }
         }
         // a lane holds row i of X and rows 4 (lane / 16) .. + 3 of W: [p][b][row of X][row of W]
@@ -132,11 +149,12 @@ template <int MB, int WAVES, typename T, typename Epi> __global__ void __launch_
         if (threadIdx.x < MB * 32) {
             const int r = threadIdx.x >> 1, n = n0 + (threadIdx.x & 1) * 8, m = m0 + r;
             if (m < hi && n < x.N) {
+                const float *at = sum + r * 16 + (threadIdx.x & 1) * 8;
                 float v[8], u[8];
 #pragma unroll
                 for (int q = 0; q < 8; q++) {
-                    v[q] = sum[r * 16 + (threadIdx.x & 1) * 8 + q];
-                    if (PAIR) u[q] = sum[MB * 256 + r * 16 + (threadIdx.x & 1) * 8 + q];
+                    v[q] = at[q];
+                    if (PAIR) u[q] = at[MB * 256 + q];
                 }
                 if constexpr (PAIR) epi(m, n, g, v, u);
                 else epi(m, n, g, v);
@@ -145,8 +163,28 @@ template <int MB, int WAVES, typename T, typename Epi> __global__ void __launch_
     }
 }
 
-// few enough rows for it: its time is W's, while the tiles' grows with what they leave empty
-inline bool is_skinny(int64_t m, int groups) { return groups > 1 ? m <= 8 * (int64_t)groups : m <= 32; }
+// Whether it is the faster way. A row costs it what X's loads add to those of W, which tiles of
+// 64 rows do not have; they need a second launch, that joins parts of k, and where an operand's
+// rows are not on 4-byte boundaries a copy of it. us with it / with tiles:
+//   4096 x 4096: 1 row 10.7 / 15.1, 32 rows 14.0 / 14.2;  8192 x 8192: 1 row 30.4 / 30.7, 8 rows
+//   35.9 / 31.1;  4096 x 10816: 4 rows 23.0 / 21.2.
+// Groups: tiles go through k without parts, so that they are slow where there are few.
+//   64 blocks of 4096 x 1632: 2 rows a group 341 / 376, 4: 426 / 425, 8: 585 / 459;
+//   32 of 4096 x 204: 8 rows a group 77 / 93, 12: 102 / 97;  16 of 2048 x 408: 12: 40 / 44.
+inline bool is_skinny(int64_t m, int64_t n, int64_t k, int groups, bool copied)
+{
+    if (groups) return m <= 4 * (int64_t)groups || (m <= 10 * (int64_t)groups && (copied || groups * n * k <= 1 << 26));
+    return m <= 32 && (copied || m * n * k <= 1 << 28);
+}
+
+template <int MB, int WAVES, typename T, typename Epi>
+inline void launch_skinny_cfg(const Args &x, const Epi &epi, unsigned groups, hipStream_t stream)
+{
+    const bool odd = (((uintptr_t)x.a | (uintptr_t)x.b) & 2) || ((x.lda | x.ldb | x.stride_b) & 1);
+    const dim3 grid((unsigned)((x.N + 15) / 16), groups);
+    if (odd) hipLaunchKernelGGL((skinny_kernel<MB, WAVES, true, T, Epi>), grid, dim3(WAVES * 64), 0, stream, x, epi);
+    else hipLaunchKernelGGL((skinny_kernel<MB, WAVES, false, T, Epi>), grid, dim3(WAVES * 64), 0, stream, x, epi);
+}
 
 template <typename T, typename Epi> inline int launch_skinny(const Args &x, const Epi &epi, hipStream_t stream)
 {
@@ -157,21 +195,18 @@ template <typename T, typename Epi> inline int launch_skinny(const Args &x, cons
     // workgroups enough for the chip without (experts of 4096 x 1632: 66 us, 83 with 8). A gated
     // workgroup has as much in flight with 8 and half the pieces (2 x 10816 x 4096: 35 us, 37
     // with 16 wavefronts, 44 with twice the pieces and half the workgroups on a CU).
-    const int waves = Epi::gated ? 8 : x.K >= 16 * 8 * 32 ? 16 : blocks * groups >= 4 * 256 ? 4 : 8;
-#define HEDDLE_SKINNY(MB, WAVES)                                                                                       \
-    hipLaunchKernelGGL((skinny_kernel<MB, WAVES, T, Epi>), dim3(blocks, groups), dim3(WAVES * 64), 0, stream, x, epi)
     const bool one = x.offsets || x.M <= 16;
-    if (waves == 16) {
-        if (one) HEDDLE_SKINNY(1, 16);
-        else HEDDLE_SKINNY(2, 16);
-    } else if (waves == 8) {
-        if (one) HEDDLE_SKINNY(1, 8);
-        else HEDDLE_SKINNY(2, 8);
-    } else {
-        if (one) HEDDLE_SKINNY(1, 4);
-        else HEDDLE_SKINNY(2, 4);
+    const int waves = Epi::gated ? 8 : x.K >= 16 * 8 * 32 ? 16 : blocks * groups >= 4 * 256 ? 4 : 8;
+    auto run = [&](auto w) {
+        constexpr int WAVES = decltype(w)::value;
+        if (one) launch_skinny_cfg<1, WAVES, T>(x, epi, groups, stream);
+        else launch_skinny_cfg<2, WAVES, T>(x, epi, groups, stream);
+    };
+    if (waves == 8) run(std::integral_constant<int, 8>());
+    if constexpr (!Epi::gated) {
+        if (waves == 16) run(std::integral_constant<int, 16>());
+        if (waves == 4) run(std::integral_constant<int, 4>());
     }
-#undef HEDDLE_SKINNY
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? HEDDLE_OK : hip_fail(e, "skinny_kernel");
 }
