@@ -50,8 +50,8 @@ __device__ inline int tensor_of(const GradTable &t, int c)
 
 // Chunk c of a tensor, one 16-byte piece a lane at a time. A whole chunk's loads
 // precede the first use, f(values, index of the first); at a tensor's ends
-// the values come one by one, g(value, index).
-template <int kPieces, typename T, typename F, typename G> __device__ inline void each_of_chunk(const void *g, int64_t n, int64_t c, F f, G one)
+// the values come one by one, g(value, index). LAST: nothing reads the values again.
+template <int kPieces, bool LAST, typename T, typename F, typename G> __device__ inline void each_of_chunk(const void *g, int64_t n, int64_t c, F f, G one)
 {
     constexpr int V = 16 / sizeof(T);
     constexpr int64_t kChunk = chunk_bytes(kPieces);
@@ -63,7 +63,10 @@ template <int kPieces, typename T, typename F, typename G> __device__ inline voi
     if ((c > 0 || skew == 0) && (c + 1) * (kChunk / (int64_t)sizeof(T)) <= end) {
         piece x[kPieces];
 #pragma unroll
-        for (int i = 0; i < kPieces; i++) x[i] = *(const piece *)(base + v0 + i * 256 * V);
+        for (int i = 0; i < kPieces; i++) {
+            const piece *at = (const piece *)(base + v0 + i * 256 * V);
+            x[i] = LAST ? __builtin_nontemporal_load(at) : *at;
+        }
 #pragma unroll
         for (int i = 0; i < kPieces; i++) f(x[i], v0 + i * 256 * V - skew);
         return;
@@ -77,7 +80,7 @@ template <int PIECES, typename T> __device__ inline double chunk_squares(const v
 {
     double s = 0;
     auto add = [&](float v) { s = fma((double)v, (double)v, s); };
-    each_of_chunk<PIECES, T>(g, n, c, [&](auto x, int64_t) {
+    each_of_chunk<PIECES, false, T>(g, n, c, [&](auto x, int64_t) {
 #pragma unroll
         for (int i = 0; i < 16 / (int)sizeof(T); i++) add((float)x[i]);
     }, [&](T x, int64_t) { add((float)x); });
@@ -132,10 +135,11 @@ __global__ void __launch_bounds__(256) grad_norm_kernel(const double *parts, int
 template <int PIECES, typename T>
 __device__ inline void clip_chunk(const void *g, void *out, int64_t n, int64_t c, float factor)
 {
-    each_of_chunk<PIECES, T>(g, n, c, [&](auto x, int64_t at) {
+    typedef T aligned __attribute__((ext_vector_type(16 / sizeof(T)), aligned(sizeof(T))));   // out may start anywhere its values may
+    each_of_chunk<PIECES, true, T>(g, n, c, [&](auto x, int64_t at) {
 #pragma unroll
         for (int i = 0; i < 16 / (int)sizeof(T); i++) x[i] = (T)((float)x[i] * factor);
-        __builtin_memcpy((T *)out + at, &x, 16);      // out may start anywhere its values may
+        __builtin_nontemporal_store(x, (aligned *)((T *)out + at));
     }, [&](T x, int64_t at) { ((T *)out)[at] = (T)((float)x * factor); });
 }
 
