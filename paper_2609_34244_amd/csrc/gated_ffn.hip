@@ -93,9 +93,9 @@ template <typename T> static int forward(const heddle_gated_ffn_desc *d, Scratch
     e.act = d->act, e.N = (int)d->f;
     int rc = hidden<T, EpiGated<T>, false>(skinny_in, x, wi, d->t, d->f, d->d, groups, d->d_offsets, e, s, run, stream);
     if (rc) return rc;
-    EpiLinear<T> o = plain_output<T>(d->y, d->ldy, d->d);
+    EpiLinear<T> o = linear_output<T>(d->y, d->ldy, d->d);
     o.residual = (const T *)d->residual, o.ldr = d->ldr;
-    return product<T>(false, skinny_out, {e.h, e.ldh, 0}, wo, d->t, d->d, d->f, groups, d->d_offsets, o, s, run, stream);
+    return product<T>(skinny_out, {e.h, e.ldh, 0}, wo, d->t, d->d, d->f, groups, d->d_offsets, o, s, run, stream);
 }
 
 template <typename T> static int backward(const heddle_gated_ffn_desc *d, Scratch &s, bool run, hipStream_t stream)
@@ -124,8 +124,8 @@ template <typename T> static int backward(const heddle_gated_ffn_desc *d, Scratc
     if (rc) return rc;
     const Operand dp = {e.dp, e.ldd, 0}, h = {e.h, e.ldh, 0};
     if (d->dx)
-        rc = product<T>(true, false, dp, wi, d->t, d->d, 2 * d->f, groups, d->d_offsets, plain_output<T>(d->dx, d->lddx, d->d), s,
-                        run, stream);
+        rc = product_cols<T>(dp, wi, d->t, d->d, 2 * d->f, groups, d->d_offsets, plain_output<T>(d->dx, d->lddx, d->d), s,
+                             run, stream);
     if (rc == HEDDLE_OK && d->dw_in)
         rc = product_sum<T>(dp, x, 2 * d->f, d->d, d->t, groups, d->d_offsets,
                             plain_output<T>(d->dw_in, d->lddw_in, d->d, groups > 1 ? d->stride_dw_in : 0), s, run, stream);

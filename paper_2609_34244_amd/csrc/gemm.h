@@ -141,14 +141,15 @@ template <typename T> __device__ inline void store8(T *p, int count, const float
     }
 }
 
-// ---- epilogues: one call finishes eight columns n .. n+7 of row m ----
+// ---- epilogues: one call finishes eight columns n .. n+7 of row m; unroll: of the loop of calls ----
 // y = act(z + bias) + residual, z rounded once where it is kept for the
 // backward pass (`pre`), the outputs once.
 template <typename T> struct EpiLinear {
     static constexpr bool gated = false;
+    static constexpr int unroll = 1;
     T *y, *pre;
     const T *bias, *residual;
-    int64_t ldy, ldp, ldr, stride_y;          // stride_y: from a group's output to the next one's (kGroupSum)
+    int64_t ldy, ldp, ldr;
     int32_t act, N;
     __device__ inline void operator()(int64_t m, int n, int g, float v[8]) const
     {
@@ -170,13 +171,29 @@ template <typename T> struct EpiLinear {
 #pragma unroll
             for (int i = 0; i < 8; i++) v[i] += r[i];
         }
-        store8(y + (int64_t)g * stride_y + m * ldy + n, count, v);
+        store8(y + m * ldy + n, count, v);
+    }
+};
+
+// A gradient: the sums, rounded once. Apart from EpiLinear, whose tests and registers show where
+// little is summed for each output (64 experts of 64 rows, both weights' gradients: the training
+// step 2.11 ms, 2.18 with it).
+template <typename T> struct EpiPlain {
+    static constexpr bool gated = false;
+    static constexpr int unroll = 8;          // short enough for its LDS reads and stores to overlap
+    T *y;
+    int64_t ldy, stride_y;
+    int32_t N;
+    __device__ inline void operator()(int64_t m, int n, int g, const float v[8]) const
+    {
+        store8(y + (int64_t)g * stride_y + m * ldy + n, N - n, v);
     }
 };
 
 // h = act(gate) * up, with both kept for the backward pass where `pre` is given
 template <typename T> struct EpiGated {
     static constexpr bool gated = true;
+    static constexpr int unroll = 1;
     T *h, *pre;
     int64_t ldh, ldp;
     int32_t act, N;                           // N = F
@@ -198,6 +215,7 @@ template <typename T> struct EpiGated {
 // the operands' type here because the next products read them as operands.
 template <typename T> struct EpiGatedGrad {
     static constexpr bool gated = false;
+    static constexpr int unroll = 1;
     T *dp, *h;
     const T *pre;
     int64_t ldd, ldh, ldp;
@@ -622,7 +640,7 @@ __global__ void __launch_bounds__(WM * WN * 64) gemm_kernel(Args x, Epi epi)
             }
         __builtin_amdgcn_wave_barrier();
         constexpr int kUnits = (PAIR ? kOut / 2 : kOut) / 8;    // eights of a row
-#pragma unroll 1
+#pragma unroll Epi::unroll
         for (int c = lane; c < kRows * kUnits; c += 64) {
             const int r = c / kUnits, q = c % kUnits;
             const int m = m0 + wm * (TM * 16) + h * kRows + r;

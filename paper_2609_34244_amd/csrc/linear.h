@@ -68,21 +68,27 @@ int launch_bias_grad(int dtype, BiasGrad b, hipStream_t stream);
 
 int check_matrix(const char *name, const void *p, int64_t ld, int64_t cols);
 
-// C = A B^T of plain row-major outputs with EpiLinear (skinny: by is_skinny, with operands as
-// they are); sum: C = A^T B over rows
+// C = A B^T with EpiLinear, all in rows (skinny: by is_skinny, with operands as they are); cols:
+// B in columns (dX = dZ W); sum: C = A^T B over rows
 template <typename T>
-int product(bool cols_b, bool skinny, const Operand &a, const Operand &b, int64_t m, int64_t n, int64_t k, int groups,
+int product(bool skinny, const Operand &a, const Operand &b, int64_t m, int64_t n, int64_t k, int groups,
             const int32_t *offsets, EpiLinear<T> epi, Scratch &s, bool run, hipStream_t stream);
 template <typename T>
+int product_cols(const Operand &a, const Operand &b, int64_t m, int64_t n, int64_t k, int groups, const int32_t *offsets,
+                 EpiPlain<T> epi, Scratch &s, bool run, hipStream_t stream);
+template <typename T>
 int product_sum(const Operand &a, const Operand &b, int64_t m, int64_t n, int64_t k, int groups, const int32_t *offsets,
-                EpiLinear<T> epi, Scratch &s, bool run, hipStream_t stream);
+                EpiPlain<T> epi, Scratch &s, bool run, hipStream_t stream);
 
-template <typename T> inline EpiLinear<T> plain_output(void *y, int64_t ld, int64_t n, int64_t stride = 0)
+template <typename T> inline EpiPlain<T> plain_output(void *y, int64_t ld, int64_t n, int64_t stride = 0)
+{
+    return {(T *)y, ld, stride, (int32_t)n};
+}
+template <typename T> inline EpiLinear<T> linear_output(void *y, int64_t ld, int64_t n)
 {
     EpiLinear<T> e = {};
     e.y = (T *)y;
     e.ldy = ld;
-    e.stride_y = stride;
     e.N = (int32_t)n;
     return e;
 }

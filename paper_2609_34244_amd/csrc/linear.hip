@@ -204,45 +204,58 @@ int launch_bias_grad(int dtype, BiasGrad b, hipStream_t stream)
     return dtype == HEDDLE_T_BF16 ? run_bias_grad<__bf16>(b, stream) : run_bias_grad<_Float16>(b, stream);
 }
 
-template <typename T>
-int product(bool cols_b, bool skinny, const Operand &a, const Operand &b, int64_t m, int64_t n, int64_t k, int groups,
-            const int32_t *offsets, EpiLinear<T> epi, Scratch &s, bool run, hipStream_t stream)
+static Args rows_args(const Operand &a, const Operand &b, int64_t m, int64_t n, int64_t k, int groups, const int32_t *offsets)
 {
-    const Shape sh = shape_of(m, n, k, offsets ? groups : 0, false, cols_b ? kRowsCols : kRowsRows);
     Args x = {};
-    if (!skinny) x.partial = (float *)s.take(partial_bytes(sh, m, n, false));
-    if (!run || m == 0) return HEDDLE_OK;
     x.a = a.p, x.lda = a.ld;
     x.b = b.p, x.ldb = b.ld, x.stride_b = b.stride;
     x.M = (int)m, x.N = (int)n, x.K = (int)k;
     x.offsets = offsets;
     x.groups = offsets ? groups : 1;
+    return x;
+}
+
+template <typename T>
+int product(bool skinny, const Operand &a, const Operand &b, int64_t m, int64_t n, int64_t k, int groups,
+            const int32_t *offsets, EpiLinear<T> epi, Scratch &s, bool run, hipStream_t stream)
+{
+    const Shape sh = shape_of(m, n, k, offsets ? groups : 0, false, kRowsRows);
+    Args x = rows_args(a, b, m, n, k, groups, offsets);
+    if (!skinny) x.partial = (float *)s.take(partial_bytes(sh, m, n, false));
+    if (!run || m == 0) return HEDDLE_OK;
     if (skinny) return launch_skinny<T>(x, epi, stream);
-    return cols_b ? launch_gemm<false, true, kGroupRows, T>(x, sh, epi, stream)
-                  : launch_gemm<false, false, kGroupRows, T>(x, sh, epi, stream);
+    return launch_gemm<false, false, kGroupRows, T>(x, sh, epi, stream);
+}
+
+template <typename T>
+int product_cols(const Operand &a, const Operand &b, int64_t m, int64_t n, int64_t k, int groups, const int32_t *offsets,
+                 EpiPlain<T> epi, Scratch &s, bool run, hipStream_t stream)
+{
+    const Shape sh = shape_of(m, n, k, offsets ? groups : 0, false, kRowsCols);
+    Args x = rows_args(a, b, m, n, k, groups, offsets);
+    x.partial = (float *)s.take(partial_bytes(sh, m, n, false));
+    if (!run || m == 0) return HEDDLE_OK;
+    return launch_gemm<false, true, kGroupRows, T>(x, sh, epi, stream);
 }
 
 template <typename T>
 int product_sum(const Operand &a, const Operand &b, int64_t m, int64_t n, int64_t k, int groups, const int32_t *offsets,
-                EpiLinear<T> epi, Scratch &s, bool run, hipStream_t stream)
+                EpiPlain<T> epi, Scratch &s, bool run, hipStream_t stream)
 {
     const Shape sh = shape_of(m, n, k, offsets ? groups : 0, false, kColsCols);
-    Args x = {};
+    Args x = rows_args(a, b, m, n, k, groups, offsets);
     x.partial = (float *)s.take(partial_bytes(sh, m, n, false));
     if (!run) return HEDDLE_OK;
-    x.a = a.p, x.lda = a.ld;
-    x.b = b.p, x.ldb = b.ld;
-    x.M = (int)m, x.N = (int)n, x.K = (int)k;
-    x.offsets = offsets;
-    x.groups = offsets ? groups : 1;
     return launch_gemm<true, true, kGroupSum, T>(x, sh, epi, stream);
 }
 
 #define HEDDLE_PRODUCTS(T)                                                                                             \
-    template int product<T>(bool, bool, const Operand &, const Operand &, int64_t, int64_t, int64_t, int, const int32_t *,   \
+    template int product<T>(bool, const Operand &, const Operand &, int64_t, int64_t, int64_t, int, const int32_t *,   \
                             EpiLinear<T>, Scratch &, bool, hipStream_t);                                               \
+    template int product_cols<T>(const Operand &, const Operand &, int64_t, int64_t, int64_t, int, const int32_t *,    \
+                                 EpiPlain<T>, Scratch &, bool, hipStream_t);                                           \
     template int product_sum<T>(const Operand &, const Operand &, int64_t, int64_t, int64_t, int, const int32_t *,     \
-                                EpiLinear<T>, Scratch &, bool, hipStream_t);
+                                EpiPlain<T>, Scratch &, bool, hipStream_t);
 HEDDLE_PRODUCTS(__bf16)
 HEDDLE_PRODUCTS(_Float16)
 
@@ -299,12 +312,12 @@ template <typename T> static int forward(const heddle_linear_desc *d, Scratch &s
         c.add(w, d->n, d->k, groups, s);
         if (const int rc = run ? c.launch(stream) : HEDDLE_OK) return rc;
     }
-    EpiLinear<T> e = plain_output<T>(d->y, d->ldy, d->n);
+    EpiLinear<T> e = linear_output<T>(d->y, d->ldy, d->n);
     e.pre = (T *)d->preact, e.ldp = d->ldp;
     e.bias = (const T *)d->bias;
     e.residual = (const T *)d->residual, e.ldr = d->ldr;
     e.act = d->act;
-    return product<T>(false, skinny, x, w, d->m, d->n, d->k, groups, d->d_offsets, e, s, run, stream);
+    return product<T>(skinny, x, w, d->m, d->n, d->k, groups, d->d_offsets, e, s, run, stream);
 }
 
 template <typename T> static int backward(const heddle_linear_desc *d, Scratch &s, bool run, hipStream_t stream)
@@ -330,8 +343,8 @@ template <typename T> static int backward(const heddle_linear_desc *d, Scratch &
     if (d->dw) c.add(x, d->m, d->k, 1, s);
     if (rc == HEDDLE_OK && run) rc = c.launch(stream);
     if (rc == HEDDLE_OK && d->dx)
-        rc = product<T>(true, false, dz, w, d->m, d->k, d->n, groups, d->d_offsets, plain_output<T>(d->dx, d->lddx, d->k), s, run,
-                        stream);
+        rc = product_cols<T>(dz, w, d->m, d->k, d->n, groups, d->d_offsets, plain_output<T>(d->dx, d->lddx, d->k), s, run,
+                             stream);
     if (rc == HEDDLE_OK && d->dw)
         rc = product_sum<T>(dz, x, d->n, d->k, d->m, groups, d->d_offsets,
                             plain_output<T>(d->dw, d->lddw, d->k, groups > 1 ? d->stride_dw : 0), s, run, stream);

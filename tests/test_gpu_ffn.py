@@ -200,6 +200,24 @@ def test_linear_one_group(H, rows, k, n):
         near(got[key].view(c.shape), c, e, key)
 
 
+@pytest.mark.parametrize("groups,rows,k,n", [(70, 900, 2600, 1030), (40, 300, 1000, 1100)])
+def test_linear_groups_wide(H, groups, rows, k, n):
+    """weights of many tiles for few rows: several of a group's tiles go through one workgroup"""
+    dtype = torch.bfloat16
+    mk = Maker(groups, dtype)
+    off = group_offsets("uneven", rows, groups, torch.Generator().manual_seed(groups))
+    offsets = torch.tensor(off, dtype=torch.int32, device="cuda")
+    x, w, dy = mk.part((rows, k), 0, 0, 1.0), mk.part((groups, n, k), 0, 0, k ** -0.5), mk.part((rows, n), 2, 2, 1.0)
+    got = H.heddle_linear_backward(dy, x, w, offsets=offsets, dx=mk.part((rows, k)), dw=mk.part((groups, n, k), 2, 2))
+    for e in range(groups):
+        s = slice(off[e], off[e + 1])
+        want = R.linear_backward(dy[s], x[s], w[e], "none", None, dtype)
+        near(got["dx"][s], *want["dx"], f"dx of group {e}")
+        near(got["dw"][e], *want["dw"], f"dw of group {e}")
+    torch.cuda.synchronize()
+    mk.untouched()
+
+
 def run_ffn(H, seed, t, d, f, act, residual, dtype, off=None, gap=0, shift=0):
     print(f"ffn {t} {d} {f} {act} residual={residual} {dtype} groups={off and len(off) - 1} gap={gap} shift={shift}", flush=True)
     mk = Maker(seed, dtype)
