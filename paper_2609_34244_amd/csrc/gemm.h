@@ -410,6 +410,16 @@ __device__ inline void arrive()
     asm volatile("" ::: "memory");
 }
 
+// the same, but for each wavefront's `later` newest loads
+template <int later> __device__ inline void arrive_but()
+{
+    static_assert(later < 64, "vmcnt");
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt((later & 15) | 7 << 4 | (later >> 4) << 14);
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
 // the order of a half step's instructions: one LDS read to every other product, so that the
 // reads of the next fragments run beside the products of these
 template <int READS, int PRODUCTS, bool COLS> __device__ inline void interleave()
@@ -542,10 +552,21 @@ __global__ void __launch_bounds__(WM * WN * 64) gemm_kernel(Args x, Epi epi)
         rest_a.advance(step_a);
         rest_b.advance(step_b);
     };
+    // the same, where a wait counts loads: past the last tile from empty buffers
+    auto load_counted = [&](uint32_t tile) {
+        const bool any = asked++ < tiles;
+        i32x4 ra = rest_a.buffer(), rb = rest_b.buffer();
+        ra[2] = any ? ra[2] : 0, rb[2] = any ? rb[2] : 0;
+        la.load_all(ra, tile, wave);
+        lb.load_all(rb, tile + LA::kBytes, wave);
+        rest_a.advance(step_a);
+        rest_b.advance(step_b);
+    };
     const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)smem;
     const int valid = (k_last - k_first) % kBK;             // k of a last, partial tile
     auto landed = [&](char *tile, int kt) {
-        arrive();
+        if constexpr (STAGES > 2) arrive_but<(STAGES - 2) * kLoads>();
+        else arrive();
         if ((!ACOL || !BCOL) && valid && kt == tiles - 1 && k_last == k_hi) {
             if (!ACOL) LA::clear_tail(tile, valid);
             if (!BCOL) LB::clear_tail(tile + LA::kBytes, valid);
@@ -603,6 +624,21 @@ __global__ void __launch_bounds__(WM * WN * 64) gemm_kernel(Args x, Epi epi)
 #pragma unroll
             for (int s = 0; s < kBK / 32; s++) {
                 read(smem, s, fa[0], fb[0]);
+                multiply(fa[0], fb[0]);
+            }
+        }
+    } else if (STAGES > 2 && tiles) {
+        // STAGES - 1 tiles on their way; the wait is for the oldest one's loads
+#pragma unroll
+        for (int i = 0; i < STAGES - 1; i++) load_counted(lds + i * kStage);
+        for (int kt = 0, at = 0; kt < tiles; kt++) {
+            char *cur = smem + at * kStage;
+            landed(cur, kt);
+            load_counted(lds + (at ? at - 1 : STAGES - 1) * kStage);
+            at = at + 1 == STAGES ? 0 : at + 1;
+#pragma unroll
+            for (int s = 0; s < kBK / 32; s++) {
+                read(cur, s, fa[0], fb[0]);
                 multiply(fa[0], fb[0]);
             }
         }
@@ -738,7 +774,16 @@ inline int launch_gemm(const Args &x, const Shape &s, const Epi &epi, hipStream_
     switch (s.cfg) {
     case 0: return launch_cfg<256, 256, 2, 4, 2, ACOL, BCOL, GR, T>(x, s, epi, stream);
     case 1: return launch_cfg<128, 128, 2, 2, 1, ACOL, BCOL, GR, T>(x, s, epi, stream);
-    case 2: return launch_cfg<64, 128, 1, 4, 2, ACOL, BCOL, GR, T>(x, s, epi, stream);
+    case 2: {
+        // A workgroup alone on its CU keeps two tiles on their way, not one (64 x 10816 x 4096:
+        // 27.5 -> 23.1 us); where there are more, a third workgroup does more than a third buffer
+        // (64 x 4096 x 10816: 24.7 us, 26.6 with three). Groups: about half have a tile that is
+        // not full.
+        const int64_t rows = x.offsets && GR == kGroupRows ? (x.M + 63) / 64 + x.groups / 2 : (x.M + 63) / 64;
+        const int64_t tiles = rows * (((Epi::gated ? 2 : 1) * (int64_t)x.N + 127) / 128) * (x.offsets && GR == kGroupSum ? x.groups : s.splits);
+        if (tiles <= 256) return launch_cfg<64, 128, 1, 4, 3, ACOL, BCOL, GR, T>(x, s, epi, stream);
+        return launch_cfg<64, 128, 1, 4, 2, ACOL, BCOL, GR, T>(x, s, epi, stream);
+    }
     default:   // groups of few rows only
         if constexpr (GR == kGroupRows) return launch_cfg<64, 256, 1, 4, 2, ACOL, BCOL, GR, T>(x, s, epi, stream);
         else return fail(HEDDLE_E_INVAL, "no such tile");

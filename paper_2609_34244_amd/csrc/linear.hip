@@ -17,6 +17,7 @@ namespace mm {
 //   256 x 256: one workgroup a CU, the highest rate; 128 x 128: four a CU, each with one buffer
 //   (what fills the chip with 2000 x 2000 outputs, and what writes most while little is
 //   summed); 64 x 128: three a CU, for few rows.
+// (Of 64 x 128, a third buffer where a workgroup has a CU to itself is not in the estimate.)
 Shape shape_of(int64_t M, int64_t N, int64_t K, int groups, bool gated, Order order)
 {
     static const struct { int bm, bn, per_cu; double step[3], least, fixed; } cfg[3] = {
@@ -33,8 +34,10 @@ Shape shape_of(int64_t M, int64_t N, int64_t K, int groups, bool gated, Order or
     const int64_t steps = grouped && sums ? (kt + groups - 1) / groups : kt;
     Shape best = {0, 1, (int)kt};
     // Experts of few rows: the weights' reading bounds, and tiles of 64 x 256 read 512 bytes of
-    // a row of theirs (64 experts of 64 rows, 1632 of 4096 columns: 208 us, 248 with 64 x 128).
-    if (grouped && !sums && rows <= 96 && cols > 128) return {3, 1, (int)kt};
+    // a row of theirs (training step over 64 experts of 4096 x 1632, 24 rows each: 1.68 ms, 1.71
+    // with 64 x 128), where they fill the chip (16 of 2048 x 408, 24 rows each, forward: 52 us,
+    // 33 with 64 x 128).
+    if (grouped && !sums && rows <= 96 && (cols + 255) / 256 * groups > 2 * cus) return {3, 1, (int)kt};
     double least = 0;
     for (int c = 0; c < 3; c++)
         for (int s = 1, log2 = 0; s == 1 || (s <= 16 && !grouped && (kt + s - 1) / s >= 4); s *= 2, log2++) {

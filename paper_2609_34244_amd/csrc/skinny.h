@@ -43,8 +43,8 @@ __device__ inline bool find_group(const int32_t *offsets, int groups, int total,
 }
 
 // eight values at any address that values may have. ODD: by whole words, as loads of 16 bytes
-// at addresses that are odd multiples of 2 run at half the rate (20000 x 4096, one row: 73 us
-// against 42); no word without one of the values is read.
+// at odd multiples of 2 run at half the rate (20000 x 4096, one row: 73 us, 59 by words, 42 at
+// multiples of 4); no word without one of the values is read.
 template <bool ODD, typename T> __device__ inline typename pack8<T>::type load_any(const T *p)
 {
     typename pack8<T>::type v;
@@ -167,14 +167,14 @@ __global__ void __launch_bounds__(WAVES * 64) skinny_kernel(Args x, Epi epi)
 // 64 rows do not have; they need a second launch, that joins parts of k, and where an operand's
 // rows are not on 4-byte boundaries a copy of it. us with it / with tiles:
 //   4096 x 4096: 1 row 10.7 / 15.1, 32 rows 14.0 / 14.2;  8192 x 8192: 1 row 30.4 / 30.7, 8 rows
-//   35.9 / 31.1;  4096 x 10816: 4 rows 23.0 / 21.2.
-// Groups: tiles go through k without parts, so that they are slow where there are few.
-//   64 blocks of 4096 x 1632: 2 rows a group 341 / 376, 4: 426 / 425, 8: 585 / 459;
-//   32 of 4096 x 204: 8 rows a group 77 / 93, 12: 102 / 97;  16 of 2048 x 408: 12: 40 / 44.
+//   35.9 / 31.1;  4096 x 10816: 4 rows 23.0 / 21.2;  20000 x 4096 with odd rows: 8 rows 73 / about
+//   105, 32 rows 119 / about 107.
+// Groups, forward pass of the block: 64 of 4096 x 1632: 2 rows each 349 / 379, 4: 435 / 427, 8:
+//   595 / 460;  8 of 4096 x 816: 2: 33 / 49, 4: 56 / 52;  32 of 4096 x 204: 2: 37 / 48, 6: 71 / 60.
 inline bool is_skinny(int64_t m, int64_t n, int64_t k, int groups, bool copied)
 {
-    if (groups) return m <= 4 * (int64_t)groups || (m <= 10 * (int64_t)groups && (copied || groups * n * k <= 1 << 26));
-    return m <= 32 && (copied || m * n * k <= 1 << 28);
+    if (groups) return m <= (copied ? 10 : 3) * (int64_t)groups;
+    return copied ? m <= 16 : m <= 32 && m * n * k <= 1 << 28;
 }
 
 template <int MB, int WAVES, typename T, typename Epi>
