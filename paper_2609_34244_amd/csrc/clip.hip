@@ -9,7 +9,8 @@
 // summed in fp64 throughout: fp32 squares overflow from 1.9e19, and at two
 // fp64 operations a value the sums stay far below the vector units' rate. The
 // clipping's workgroups each add up the at most kParts sums by themselves, in
-// one order, which saves a launch between the two passes.
+// one order, which saves a launch between the two passes. 2e8 bf16 values: 72 + 138 us (5.6 and
+// 5.8 TB/s); 1.6e9 values of 320 tensors: 1.97 ms (4.9 TB/s); 1e6 fp32 values: 4.3 + 6.0 us.
 #include <cmath>
 
 #include "heddle_internal.h"
@@ -159,7 +160,9 @@ __global__ void __launch_bounds__(256) clip_kernel(GradTable t, const double *pa
     float factor = max_norm / (v + 1e-6f);
     if (factor >= 1.0f) factor = 1.0f;                                  // a NaN stays
     // The table runs from the last tensor to the first, and so do a tensor's chunks here: what
-    // the norm read last is still in the 256 MB memory-side cache.
+    // the norm read last is still in the 256 MB memory-side cache. It keeps what is still to be
+    // read, as this pass reads and writes past the caches (2e8 bf16 values, both passes: 249 us
+    // without, 210 us; 1.6e9: 2003 and 1970 us).
     int k = -1;
     for (int c = blockIdx.x; c < t.chunks; c += gridDim.x) {
         if (k < 0) k = tensor_of(t, c);

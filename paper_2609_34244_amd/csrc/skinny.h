@@ -5,7 +5,9 @@
 // wavefront takes its part of k. W goes from memory straight to the registers that the
 // matrix instruction reads (16 rows x 32 k, lane = row, 16 bytes of k), U pieces of W in
 // flight per lane, and X, which the caches hold, beside it. The wavefronts' sums meet in LDS in a
-// fixed order. Loads need only the alignment of a value, so no operand is copied.
+// fixed order. Loads need only the alignment of a value, so no operand is copied. One row of
+// 4096 x 4096: 8.4 us, 4.0 TB/s of W; of 2 x 10816 x 4096, gated: 35.8 us, 4.95 TB/s (a large copy
+// moves 4.8).
 //
 // Groups: a workgroup takes the j-th group that has rows; there are at most as many as rows.
 #pragma once
@@ -42,24 +44,22 @@ __device__ inline bool find_group(const int32_t *offsets, int groups, int total,
     return false;
 }
 
-// eight values at any address that values may have. ODD: by whole words, as loads of 16 bytes
-// at odd multiples of 2 run at half the rate (20000 x 4096, one row: 73 us, 59 by words, 42 at
-// multiples of 4); no word without one of the values is read.
-template <bool ODD, typename T> __device__ inline typename pack8<T>::type load_any(const T *p)
+// 8 H values at any address that values may have. H = 2: by whole words, as loads of 16 bytes
+// at odd multiples of 2 run at half the rate (20000 x 4096, one row: 73 us; 59 by words for
+// each eight, 53 for sixteen; 42 at multiples of 4); no word without one of the values is read.
+template <int H, typename T> __device__ inline void load_any(const T *p, typename pack8<T>::type *v)
 {
-    typename pack8<T>::type v;
-    if (!ODD) {
-        __builtin_memcpy(&v, p, 16);
-        return v;
+    if (H == 1) {
+        __builtin_memcpy(v, p, 16);
+        return;
     }
     const uint32_t *words = (const uint32_t *)((uintptr_t)p & ~(uintptr_t)3), skew = (uint32_t)((uintptr_t)p & 2);
-    uint32_t w[5];
-    __builtin_memcpy(w, words, 16);
-    w[4] = words[3 + skew / 2];
+    uint32_t w[4 * H + 1];
+    __builtin_memcpy(w, words, 16 * H);
+    w[4 * H] = words[4 * H - 1 + skew / 2];
 #pragma unroll
-    for (int i = 0; i < 4; i++) w[i] = __builtin_amdgcn_alignbyte(w[i + 1], w[i], skew);
-    __builtin_memcpy(&v, w, 16);
-    return v;
+    for (int i = 0; i < 4 * H; i++) w[i] = __builtin_amdgcn_alignbyte(w[i + 1], w[i], skew);
+    __builtin_memcpy(v, w, 16 * H);
 }
 // the values with index below count; the others are zero and not read
 template <typename T> __device__ inline typename pack8<T>::type load_some(const T *p, int count)
@@ -74,18 +74,18 @@ template <int MB, int WAVES, bool ODD, typename T, typename Epi>
 __global__ void __launch_bounds__(WAVES * 64) skinny_kernel(Args x, Epi epi)
 {
     constexpr bool PAIR = Epi::gated;
-    constexpr int P = PAIR ? 2 : 1, U = MB * P > 1 ? 4 : 8;
+    constexpr int P = PAIR ? 2 : 1, H = ODD ? 2 : 1, U = (MB * P > 1 ? 4 : 8) / H;   // H eights of k a lane and step
     typedef typename pack8<T>::type frag;
     __shared__ float part[WAVES][P * MB * 256], sum[P * MB * 256];
-    const int lane = threadIdx.x & 63, i = lane & 15, kg = (lane >> 4) * 8;
+    const int lane = threadIdx.x & 63, i = lane & 15, kg = (lane >> 4) * 8 * H;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     int g = 0, lo = 0, hi = x.M;
     if (x.offsets && !find_group(x.offsets, x.groups, x.M, blockIdx.y, g, lo, hi)) return;
     const int n0 = blockIdx.x * 16;
     const T *w = (const T *)x.b + (int64_t)g * x.stride_b + (int64_t)min(n0 + i, x.N - 1) * x.ldb;
     const int64_t up = PAIR ? (int64_t)x.F * x.ldb : 0;
-    // whole 32-k steps of this wavefront, and the last, partial one
-    const int steps = x.K / 32, each = (steps + WAVES - 1) / WAVES;
+    // whole steps (32 k, 64 for ODD) of this wavefront, and the last, partial one
+    const int steps = x.K / (32 * H), each = (steps + WAVES - 1) / WAVES;
     const int first = min(wave * each, steps), last = min(first + each, steps);
     for (int m0 = lo; m0 < hi; m0 += 16 * MB) {
         const T *xr[MB];
@@ -100,37 +100,40 @@ __global__ void __launch_bounds__(WAVES * 64) skinny_kernel(Args x, Epi epi)
         // n steps: all their loads, then their products
         auto batch = [&](auto n) {
             constexpr int N = decltype(n)::value;
-            frag fw[P][N], fx[MB][N];
+            frag fw[P][N][H], fx[MB][N][H];
 #pragma unroll
             for (int u = 0; u < N; u++) {
-                const int k = (s + u) * 32 + kg;
+                const int k = (s + u) * 32 * H + kg;
 #pragma unroll
-                for (int p = 0; p < P; p++) fw[p][u] = load_any<ODD>(w + p * up + k);
+                for (int p = 0; p < P; p++) load_any<H>(w + p * up + k, fw[p][u]);
 #pragma unroll
-                for (int b = 0; b < MB; b++) fx[b][u] = load_any<ODD>(xr[b] + k);
+                for (int b = 0; b < MB; b++) load_any<H>(xr[b] + k, fx[b][u]);
             }
 #pragma unroll
-            for (int u = 0; u < N; u++)
+            for (int u = 0; u < N * H; u++)
 #pragma unroll
                 for (int p = 0; p < P; p++)
 #pragma unroll
-                    for (int b = 0; b < MB; b++) acc[p][b] = mfma16(fw[p][u], fx[b][u], acc[p][b]);
+                    for (int b = 0; b < MB; b++) acc[p][b] = mfma16(fw[p][u / H][u % H], fx[b][u / H][u % H], acc[p][b]);
             s += N;
         };
         while (s + U <= last) batch(std::integral_constant<int, U>());
         if (U > 4 && s + 4 <= last) batch(std::integral_constant<int, 4>());
         if (U > 2 && s + 2 <= last) batch(std::integral_constant<int, 2>());
         if (s < last) batch(std::integral_constant<int, 1>());
-        if (wave == WAVES - 1 && x.K % 32) {
-            const int k = steps * 32 + kg, count = x.K - k;
-            frag fx[MB];
+        if (wave == WAVES - 1 && x.K % (32 * H)) {
 #pragma unroll
-            for (int b = 0; b < MB; b++) fx[b] = load_some(xr[b] + k, count);
+            for (int h = 0; h < H; h++) {
+                const int k = steps * 32 * H + kg + h * 8, count = x.K - k;
+                frag fx[MB];
 #pragma unroll
-            for (int p = 0; p < P; p++) {
-                const frag fw = load_some(w + p * up + k, count);
+                for (int b = 0; b < MB; b++) fx[b] = load_some(xr[b] + k, count);
 #pragma unroll
-                for (int b = 0; b < MB; b++) acc[p][b] = mfma16(fw, fx[b], acc[p][b]);
+                for (int p = 0; p < P; p++) {
+                    const frag fw = load_some(w + p * up + k, count);
+#pragma unroll
+                    for (int b = 0; b < MB; b++) acc[p][b] = mfma16(fw, fx[b], acc[p][b]);
+                }
             }
         }
         // a lane holds row i of X and rows 4 (lane / 16) .. + 3 of W: [p][b][row of X][row of W]
@@ -167,7 +170,7 @@ __global__ void __launch_bounds__(WAVES * 64) skinny_kernel(Args x, Epi epi)
 // 64 rows do not have; they need a second launch, that joins parts of k, and where an operand's
 // rows are not on 4-byte boundaries a copy of it. us with it / with tiles:
 //   4096 x 4096: 1 row 10.7 / 15.1, 32 rows 14.0 / 14.2;  8192 x 8192: 1 row 30.4 / 30.7, 8 rows
-//   35.9 / 31.1;  4096 x 10816: 4 rows 23.0 / 21.2;  20000 x 4096 with odd rows: 8 rows 73 / about
+//   35.9 / 31.1;  4096 x 10816: 4 rows 23.0 / 21.2;  20000 x 4096 with odd rows: 8 rows 63 / about
 //   105, 32 rows 119 / about 107.
 // Groups, forward pass of the block: 64 of 4096 x 1632: 2 rows each 349 / 379, 4: 435 / 427, 8:
 //   595 / 460;  8 of 4096 x 816: 2: 33 / 49, 4: 56 / 52;  32 of 4096 x 204: 2: 37 / 48, 6: 71 / 60.
