@@ -59,7 +59,9 @@ __host__ __device__ inline int64_t partial_cols(int n, bool gated) { return (int
 constexpr int64_t kMaxLd = int64_t(1) << 22;  // 256 rows stay below 2^31 bytes
 
 // ---- activations (fp32) ----
-__device__ inline float sigmoid(float z) { return 1.0f / (1.0f + __expf(-z)); }
+// the reciprocal of one instruction, off by 1 ulp: a division is ten, and the activations bound
+// the pass that forms dZ (4096 x 10816, gelu_tanh: 79 us with a division, 75 without)
+__device__ inline float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.0f + __expf(-z)); }
 __device__ inline float act_of(int act, float z)
 {
     switch (act) {

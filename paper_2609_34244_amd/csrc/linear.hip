@@ -5,8 +5,8 @@
 // Backward: dZ = dY act'(Z) is formed once, in the pass that sums db (without
 // an activation dZ is dY itself), then dX = dZ W and dW = dZ^T X.
 // Bound by the matrix cores from some 500 rows on: 4096 rows of 4096 x 10816 with bias and
-// gelu_tanh 392 us forward (925 TFLOP/s), dZ and db 79 us (266 MB, 3.4 TB/s), dX 303 us and dW
-// 338 us (1200 and 1075 TFLOP/s); 8192^3 alone 795 us (1383 TFLOP/s).
+// gelu_tanh 384 us forward (945 TFLOP/s), dZ and db 75 us (266 MB, 3.5 TB/s), dX 304 us and dW
+// 339 us (1195 and 1070 TFLOP/s); 8192^3 alone 795 us (1383 TFLOP/s).
 #include "linear.h"
 
 namespace heddle {
