@@ -559,9 +559,9 @@ int heddle_profile_info_get(const heddle_profile *p, heddle_profile_info *info);
  * from 0 to the row count) rows d_offsets[e] .. d_offsets[e+1] - 1 use the
  * weights of expert e, which lie stride elements apart. A group may be
  * empty; the gradients of its weights are zero. The values are read on the
- * device only. Values out of order or range are clamped: no access leaves
- * the tensors, but rows that then belong to no group are not written and
- * those in two groups hold the product of either.
+ * device only. One outside 0 .. row count counts as the nearer of the two,
+ * one below an earlier one as that one: no access leaves the tensors, no row
+ * is in two groups, and rows in none are not written.
  *
  * Scratch is the caller's: the *_workspace call tells how many bytes the call
  * with the same descriptor needs (0 often; d_workspace may then be NULL). It

@@ -243,36 +243,77 @@ template <typename T> struct EpiGatedGrad {
 };
 
 // ---- groups ----
-// rows of group g, inside 0 .. total whatever the offsets hold
-__device__ inline void group_range(const int32_t *offsets, int g, int total, int &lo, int &hi)
+// Group g's rows are c[g] .. c[g + 1] - 1, c[i] the largest of offsets[0 .. i], inside 0 .. total:
+// the offsets themselves where they are in order, and whatever they hold no row is in two groups,
+// so that a grid sized for the rows and groups has a workgroup for every tile. Offsets in order,
+// which a ballot shows, cost no scan. All lanes of a wavefront call these.
+
+// the first 64 offsets, one a lane: a kernel asks for them before it knows its group
+__device__ inline int first_offsets(const int32_t *offsets, int groups) { return offsets[min((int)(threadIdx.x & 63), groups)]; }
+
+// rows of group g; head: first_offsets()
+__device__ inline void group_range(const int32_t *offsets, int head, int g, int total, int &lo, int &hi)
 {
-    lo = min(max(offsets[g], 0), total);
-    hi = min(max(offsets[g + 1], lo), total);
+    const int lane = threadIdx.x & 63;
+    int before = lane < g ? head : 0, next;
+    if (g < 63) {
+        lo = __builtin_amdgcn_readlane(head, g);
+        next = __builtin_amdgcn_readlane(head, g + 1);
+    } else {
+#pragma unroll 4
+        for (int i = 64 + lane; i < g; i += 64) before = max(before, offsets[i]);
+        lo = offsets[g];
+        next = offsets[g + 1];
+    }
+    lo = min(max(lo, 0), total);
+    if (__ballot(before > lo)) {
+#pragma unroll
+        for (int d = 32; d; d /= 2) before = max(before, __shfl_xor(before, d));
+        lo = min(max(lo, __builtin_amdgcn_readfirstlane(before)), total);
+    }
+    hi = min(max(next, lo), total);
+}
+
+// rows of group g0 + lane, none past the last group; carry: c[g0]
+__device__ inline void group_ranges(const int32_t *offsets, int groups, int total, int g0, int carry, int &lo, int &hi)
+{
+    const int lane = threadIdx.x & 63;
+    const bool any = g0 + lane < groups;
+    lo = hi = 0;
+    if (any) {
+        lo = min(max(offsets[g0 + lane], 0), total);
+        hi = min(max(offsets[g0 + lane + 1], 0), total);
+    }
+    if (!__ballot(any && (lo < carry || hi < lo))) return;
+    lo = max(lo, carry);
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) lo = max(lo, __shfl_up(lo, d));   // (a lane without one d below has its own)
+    hi = max(hi, lo);
 }
 
 // tiles of bm rows of all groups together
 __device__ inline int count_tiles(const int32_t *offsets, int groups, int total, int bm)
 {
-    int sum = 0;
-    for (int g = threadIdx.x & 63; g < groups; g += 64) {
+    int sum = 0, carry = 0;
+    for (int g0 = 0; g0 < groups; g0 += 64) {
         int lo, hi;
-        group_range(offsets, g, total, lo, hi);
+        group_ranges(offsets, groups, total, g0, carry, lo, hi);
         sum += (hi - lo + bm - 1) / bm;
+        carry = __builtin_amdgcn_readlane(hi, 63);
     }
 #pragma unroll
     for (int d = 32; d; d /= 2) sum += __shfl_xor(sum, d);
     return __builtin_amdgcn_readfirstlane(sum);
 }
 
-// the group and first row of tile t of BM rows; false past the last tile.
-// All lanes of a wavefront call it; 64 groups are summed at a time.
+// the group and first row of tile t of BM rows; false past the last tile
 __device__ inline bool find_tile(const int32_t *offsets, int groups, int total, int bm, int t, int &g, int &row, int &end)
 {
     const int lane = threadIdx.x & 63;
-    int before = 0;
+    int before = 0, carry = 0;
     for (int g0 = 0; g0 < groups; g0 += 64) {
-        int lo = 0, hi = 0;
-        if (g0 + lane < groups) group_range(offsets, g0 + lane, total, lo, hi);
+        int lo, hi;
+        group_ranges(offsets, groups, total, g0, carry, lo, hi);
         const int mine = (hi - lo + bm - 1) / bm;
         int sum = mine;
 #pragma unroll
@@ -293,6 +334,7 @@ __device__ inline bool find_tile(const int32_t *offsets, int groups, int total, 
             return true;
         }
         before += __shfl(sum, 63);
+        carry = __builtin_amdgcn_readlane(hi, 63);
     }
     return false;
 }
@@ -465,11 +507,13 @@ __global__ void __launch_bounds__(WM * WN * 64) gemm_kernel(Args x, Epi epi)
     __shared__ __align__(1024) char smem[STAGES * kStage];
 
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const bool grouped_sum = GR == kGroupSum && x.offsets;
+    const int head = grouped_sum ? first_offsets(x.offsets, x.groups) : 0;
     // The grid of grouped rows holds the most tiles that the groups may have. Those that they do
     // have are shared out among the XCDs (shared out by the grid, the last XCDs had none).
     int tiles_m = x.tiles_m, ids = gridDim.x;
     if (GR == kGroupRows && x.offsets) {
-        tiles_m = min(tiles_m, count_tiles(x.offsets, x.groups, x.M, BM));
+        tiles_m = count_tiles(x.offsets, x.groups, x.M, BM);
         ids = tiles_m * x.tiles_n;
         if ((int)blockIdx.x >= ids) return;
     }
@@ -482,10 +526,9 @@ __global__ void __launch_bounds__(WM * WN * 64) gemm_kernel(Args x, Epi epi)
 
     int g = 0, m0 = tm * BM, m_end = x.M, k_lo = 0, k_hi = x.K;
     if (GR == kGroupRows && x.offsets && !find_tile(x.offsets, x.groups, x.M, BM, tm, g, m0, m_end)) return;
-    const bool grouped_sum = GR == kGroupSum && x.offsets;
     if (grouped_sum) {
         g = __builtin_amdgcn_readfirstlane(outer);
-        group_range(x.offsets, g, x.K, k_lo, k_hi);
+        group_range(x.offsets, head, g, x.K, k_lo, k_hi);
     }
     const int split = grouped_sum ? 0 : outer;              // a grouped product is not split
     const int k_first = k_lo + split * x.split_tiles * kBK;

@@ -118,7 +118,7 @@ template <typename T> __global__ void __launch_bounds__(256) bias_grad_kernel(Bi
     const int n = blockIdx.x * 256 + col * 8, count = b.n - n;
     const int g = blockIdx.y / b.chunks, chunk = blockIdx.y - g * b.chunks;
     int lo = 0, hi = b.m;
-    if (b.offsets) group_range(b.offsets, g, b.m, lo, hi);
+    if (b.offsets) group_range(b.offsets, first_offsets(b.offsets, b.groups), g, b.m, lo, hi);
     const int first = lo + chunk * b.chunk_rows;
     const int last = b.offsets ? hi : min(hi, first + b.chunk_rows);
     float sum[8] = {};

@@ -25,10 +25,10 @@ __device__ inline f32x4 mfma16(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amd
 // group j of those with rows; false past the last one
 __device__ inline bool find_group(const int32_t *offsets, int groups, int total, int j, int &g, int &lo, int &hi)
 {
-    const int lane = threadIdx.x & 63;
+    int carry = 0;
     for (int g0 = 0; g0 < groups; g0 += 64) {
-        int a = 0, b = 0;
-        if (g0 + lane < groups) group_range(offsets, g0 + lane, total, a, b);
+        int a, b;
+        group_ranges(offsets, groups, total, g0, carry, a, b);
         uint64_t has = __ballot(b > a);
         const int n = __popcll(has);
         if (j < n) {
@@ -40,6 +40,7 @@ __device__ inline bool find_group(const int32_t *offsets, int groups, int total,
             return true;
         }
         j -= n;
+        carry = __builtin_amdgcn_readlane(b, 63);
     }
     return false;
 }
