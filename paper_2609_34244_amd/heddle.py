@@ -445,6 +445,9 @@ def heddle_fill_plans(profiles, mbs, cl, global_batch, dp_cap, n_stages, stages,
 # work precedes the call's; inputs of another stream's making must be waited
 # for by the caller. Outputs that the call allocates belong to that stream, as
 # those of torch's operators under torch.cuda.stream(stream) do.
+#
+# Autograd records none of the calls: gradients come from the *_backward ones. The
+# products refuse tensors that require a gradient unless it is off (torch.no_grad()).
 
 _LINEAR = struct.Struct("@iiqqqPqPqPPqPqPqiPqPqPqPqqP")
 _GATED_FFN = struct.Struct("@iiqqqPqPqPqPqPqPqiPqqPqPqPqqPqq")
@@ -474,8 +477,17 @@ def _dtype_codes():
     return _codes
 
 
+def _unrecorded(what):
+    import torch
+    if torch.is_grad_enabled():
+        _refuse(f"{what}: requires a gradient, and autograd records nothing of this call; use torch.no_grad() and the "
+                "operator's backward call")
+
+
 def _matrix(t, what, shape, dtype, gpu):
     """(data pointer, ld) of a device matrix whose rows are contiguous"""
+    if t.requires_grad:
+        _unrecorded(what)
     if t.dtype != dtype or t.get_device() != gpu:
         _refuse(f"{what}: {t.dtype} on {t.device}, not {dtype} on GPU {gpu}")
     if t.shape != shape:
@@ -493,6 +505,8 @@ def _weights(t, what, shape, dtype, gpu):
 
 
 def _vector(t, what, shape, dtype, gpu):
+    if t.requires_grad:
+        _unrecorded(what)
     if t.dtype != dtype or t.get_device() != gpu or t.shape != shape or not t.is_contiguous():
         _refuse(f"{what}: not a contiguous {dtype} tensor of shape {shape} on GPU {gpu}")
     return t.data_ptr()
