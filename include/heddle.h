@@ -553,7 +553,10 @@ int heddle_profile_info_get(const heddle_profile *p, heddle_profile_info *info);
  * any address and any ld will do: sums run at full speed for rows that start
  * on 4-byte boundaries, others are copied to scratch first). Sums are fp32;
  * every output is rounded once, to nearest even. Inputs and outputs must not
- * overlap, except that residual may be the output itself.
+ * overlap, except that residual may be the output itself. A call that would
+ * read what it has overwritten, or write one output over another, is refused
+ * where the descriptor shows it (matrices with different distances between
+ * rows may overlap unseen).
  *
  * Expert groups: with d_offsets (DEVICE [groups + 1] int32, non-decreasing,
  * from 0 to the row count) rows d_offsets[e] .. d_offsets[e+1] - 1 use the
@@ -570,9 +573,9 @@ int heddle_profile_info_get(const heddle_profile *p, heddle_profile_info *info);
  * and allocate nothing, so they can be captured into a graph.
  *
  * Errors: HEDDLE_E_INVAL (null pointer, a size, type, activation or ld out of
- * range, misaligned pointer or too little workspace), HEDDLE_E_RANGE (more
- * tiles than a launch holds) or HEDDLE_E_DEVICE; with the first nothing is
- * enqueued.
+ * range, misaligned pointer, an output over an input or too little workspace),
+ * HEDDLE_E_RANGE (more tiles than a launch holds) or HEDDLE_E_DEVICE; with the
+ * first nothing is enqueued.
  * ====================================================================== */
 #define HEDDLE_T_BF16 0
 #define HEDDLE_T_F16  1
@@ -665,7 +668,7 @@ int heddle_gated_ffn_workspace(const heddle_gated_ffn_desc *d, int32_t backward,
 /* A gradient tensor: n contiguous values, aligned to their own size. */
 typedef struct heddle_grad_desc {
     const void *g;
-    void *out;                                        /* clipped values; NULL or g: in place */
+    void *out;                                        /* clipped values; NULL or g: in place; else apart from every g */
     int64_t n;                                        /* >= 0 */
     int32_t dtype;                                    /* HEDDLE_T_* */
 } heddle_grad_desc;

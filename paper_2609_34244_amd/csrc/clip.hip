@@ -176,6 +176,8 @@ __global__ void __launch_bounds__(256) clip_kernel(GradTable t, const double *pa
     }
 }
 
+static int64_t bytes_of(const heddle_grad_desc &g) { return g.n * (g.dtype == HEDDLE_T_F32 ? 4 : 2); }
+
 static int check_grads(const heddle_grad_desc *g, int32_t count)
 {
     if (count < 0) return fail(HEDDLE_E_INVAL, "count < 0");
@@ -188,11 +190,12 @@ static int check_grads(const heddle_grad_desc *g, int32_t count)
         if (g[i].n > 0 && !g[i].g) return fail(HEDDLE_E_INVAL, "a gradient tensor is NULL");
         if (((uintptr_t)g[i].g | (uintptr_t)g[i].out) & mask)
             return fail(HEDDLE_E_INVAL, "a gradient tensor is not aligned to its values");
+        const uintptr_t from = (uintptr_t)g[i].g, to = (uintptr_t)g[i].out, bytes = (uintptr_t)bytes_of(g[i]);
+        if (to && to != from && (to > from ? to - from : from - to) < bytes)
+            return fail(HEDDLE_E_INVAL, "a gradient tensor's output overlaps it");
     }
     return HEDDLE_OK;
 }
-
-static int64_t bytes_of(const heddle_grad_desc &g) { return g.n * (g.dtype == HEDDLE_T_F32 ? 4 : 2); }
 
 static bool is_small(const heddle_grad_desc *g, int32_t count)
 {

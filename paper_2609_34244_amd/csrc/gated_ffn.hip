@@ -59,6 +59,29 @@ static int check_ffn(const heddle_gated_ffn_desc *d, bool backward)
     return rc;
 }
 
+// Whether an output lies on what the call reads when it writes it, or later, or on another output.
+static int check_overlaps(const heddle_gated_ffn_desc *d, bool backward)
+{
+    const int groups = d->d_offsets ? d->groups : 1;
+    const Region x = {"x", d->x, d->t, d->d, d->ldx}, wi = {"w_in", d->w_in, 2 * d->f, d->d, d->ldw_in, groups, d->stride_in};
+    const Region wo = {"w_out", d->w_out, d->d, d->f, d->ldw_out, groups, d->stride_out}, pre = {"preact", d->preact, d->t, 2 * d->f, d->ldp};
+    int rc;
+    if (!backward) {
+        // the first product has read x when the second one writes y
+        const Region y = {"y", d->y, d->t, d->d, d->ldy}, r = {"residual", d->residual, d->t, d->d, d->ldr};
+        const bool own = r.p == y.p && (r.ld == y.ld || d->t == 1);       // y may be the residual itself
+        rc = check_apart(y, {&wo, &pre, own ? nullptr : &r});
+        return rc ? rc : check_apart(pre, {&x, &wi, &wo, &r});
+    }
+    const Region dy = {"dy", d->dy, d->t, d->d, d->lddy}, dx = {"dx", d->dx, d->t, d->d, d->lddx};
+    const Region di = {"dw_in", d->dw_in, 2 * d->f, d->d, d->lddw_in, groups, d->stride_dw_in};
+    const Region dout = {"dw_out", d->dw_out, d->d, d->f, d->lddw_out, groups, d->stride_dw_out};
+    // in this order, after dP and H, which are the last to read preact and w_out
+    rc = check_apart(dx, {&wi, &di, &dout, d->dw_in ? &x : nullptr, d->dw_out ? &dy : nullptr});
+    if (rc == HEDDLE_OK) rc = check_apart(di, {&x, &dout, d->dw_out ? &dy : nullptr});
+    return rc ? rc : check_apart(dout, {&dy});
+}
+
 template <typename T, typename Epi, bool BCOL>
 static int hidden(bool skinny, const Operand &a, const Operand &b, int64_t t, int64_t f, int64_t k, int groups, const int32_t *offsets,
                   const Epi &epi, Scratch &s, bool run, hipStream_t stream)
@@ -155,6 +178,7 @@ static int gated_ffn(const heddle_gated_ffn_desc *d, bool back, void *ws, int64_
             if (need) *need = (int64_t)s.used;
             if (!run) return HEDDLE_OK;
             rc = check_scratch(s.used, ws, bytes);
+            if (rc == HEDDLE_OK) rc = check_overlaps(d, back);
             if (rc) return rc;
         }
     }

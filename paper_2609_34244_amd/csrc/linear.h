@@ -2,6 +2,8 @@
 // want them, scratch layout, and the launches the entry points are made of.
 #pragma once
 
+#include <initializer_list>
+
 #include "gemm.h"
 #include "skinny.h"
 
@@ -67,6 +69,18 @@ int64_t bias_grad_bytes(int64_t m, int64_t n, bool grouped, int groups);
 int launch_bias_grad(int dtype, BiasGrad b, hipStream_t stream);
 
 int check_matrix(const char *name, const void *p, int64_t ld, int64_t cols);
+
+// What a descriptor's pointer stands for: rows of cols values, ld apart, groups stride apart.
+struct Region {
+    const char *name;
+    const void *p;                            // NULL: not given
+    int64_t rows, cols, ld;
+    int groups = 1;
+    int64_t stride = 0;
+};
+// An output and what must not lie in it (NULL: nothing). Exact where both have one distance between rows or one
+// of them is a single run of values; else an overlap is seen if the first value of one is in the other.
+int check_apart(const Region &out, std::initializer_list<const Region *> others);
 
 // C = A B^T with EpiLinear, all in rows (skinny: by is_skinny, with operands as they are); cols:
 // B in columns (dX = dZ W); sum: C = A^T B over rows

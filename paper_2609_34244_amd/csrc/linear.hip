@@ -71,6 +71,47 @@ int check_matrix(const char *name, const void *p, int64_t ld, int64_t cols)
     return HEDDLE_OK;
 }
 
+// values from a's first to b's
+static int64_t between(const Region &a, const Region &b) { return ((intptr_t)b.p - (intptr_t)a.p) / 2; }
+
+static bool holds_first_of(const Region &a, const Region &b)
+{
+    int64_t at = between(a, b);
+    if (at < 0) return false;
+    if (a.groups > 1) {
+        const int64_t g = at / a.stride < a.groups ? at / a.stride : a.groups - 1;
+        at -= g * a.stride;
+    }
+    return at / a.ld < a.rows && at % a.ld < a.cols;
+}
+
+static bool overlap(const Region &x, const Region &y)
+{
+    // (in fp64: exact below 2^53 values, and no product of sizes overflows)
+    auto length = [](const Region &r) { return (double)(r.groups - 1) * (double)r.stride + (double)(r.rows - 1) * (double)r.ld + (double)r.cols; };
+    const int64_t d = between(x, y);
+    if (d >= 0 ? (double)d >= length(x) : (double)-d >= length(y)) return false;
+    Region a = x, b = y;
+    for (Region *r : {&a, &b}) {
+        if (r->groups > 1 && r->stride == r->rows * r->ld) r->rows *= r->groups, r->groups = 1;
+        if (r->groups == 1 && (r->ld == r->cols || r->rows == 1)) r->cols += (r->rows - 1) * r->ld, r->rows = 1;
+    }
+    if (a.groups > 1 || b.groups > 1 || (a.rows > 1 && b.rows > 1 && a.ld != b.ld)) return holds_first_of(a, b) || holds_first_of(b, a);
+    // rows i of a and j of b meet where -b.cols < d + q ld < a.cols, q = j - i
+    const int64_t ld = a.rows > 1 ? a.ld : b.ld, least = -b.cols - d;
+    int64_t q = least / ld - (least % ld < 0) + 1;
+    if (q < 1 - a.rows) q = 1 - a.rows;
+    return q <= b.rows - 1 && d + q * ld < a.cols;
+}
+
+int check_apart(const Region &out, std::initializer_list<const Region *> others)
+{
+    if (!out.p || out.rows == 0) return HEDDLE_OK;
+    for (const Region *r : others)
+        if (r && r->p && r->rows > 0 && overlap(out, *r)) return fail(HEDDLE_E_INVAL, std::string(out.name) + " overlaps " + r->name);
+    return HEDDLE_OK;
+}
+
 __global__ void __launch_bounds__(256) copy_rows_kernel(Copies c)
 {
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < c.eights; i += (int64_t)gridDim.x * 256) {
@@ -307,6 +348,30 @@ static int check_linear(const heddle_linear_desc *d, bool backward)
     return rc;
 }
 
+// Whether an output lies on what the call reads when it writes it, or later.
+static int check_overlaps(const heddle_linear_desc *d, bool backward)
+{
+    const int groups = d->d_offsets ? d->groups : 1;
+    const Region x = {"x", d->x, d->m, d->k, d->ldx}, w = {"w", d->w, d->n, d->k, d->ldw, groups, d->stride_w};
+    const Region pre = {"preact", d->preact, d->m, d->n, d->ldp};
+    int rc;
+    if (!backward) {
+        const Region y = {"y", d->y, d->m, d->n, d->ldy}, bias = {"bias", d->bias, 1, groups * d->n, groups * d->n};
+        const Region r = {"residual", d->residual, d->m, d->n, d->ldr};
+        const bool own = r.p == y.p && (r.ld == y.ld || d->m == 1);       // y may be the residual itself
+        rc = check_apart(y, {&x, &w, &bias, &pre, own ? nullptr : &r});
+        return rc ? rc : check_apart(pre, {&x, &w, &bias, &r});
+    }
+    const Region dy = {"dy", d->dy, d->m, d->n, d->lddy};
+    const Region dx = {"dx", d->dx, d->m, d->k, d->lddx}, dw = {"dw", d->dw, d->n, d->k, d->lddw, groups, d->stride_dw};
+    const Region db = {"db", d->db, 1, groups * d->n, groups * d->n};
+    // with an activation, dy and preact are read by the first pass alone, which leaves dZ and db
+    const bool act = d->act != HEDDLE_A_NONE;
+    rc = check_apart(db, {&dy, act ? &pre : nullptr, &dx, &dw, d->dx ? &w : nullptr, d->dw ? &x : nullptr});
+    if (rc == HEDDLE_OK) rc = check_apart(dx, {act ? nullptr : &dy, &w, &dw, d->dw ? &x : nullptr});
+    return rc ? rc : check_apart(dw, {act ? nullptr : &dy, &x});
+}
+
 template <typename T> static int forward(const heddle_linear_desc *d, Scratch &s, bool run, hipStream_t stream)
 {
     const int groups = d->d_offsets ? d->groups : 1;
@@ -371,6 +436,7 @@ static int linear(const heddle_linear_desc *d, bool back, void *ws, int64_t byte
             if (need) *need = (int64_t)s.used;
             if (!run) return HEDDLE_OK;
             rc = check_scratch(s.used, ws, bytes);
+            if (rc == HEDDLE_OK) rc = check_overlaps(d, back);
             if (rc) return rc;
         }
     }
