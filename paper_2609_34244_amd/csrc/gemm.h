@@ -822,7 +822,7 @@ inline int launch_cfg(Args x, const Shape &s, const Epi &epi, hipStream_t stream
     x.splits = s.splits;
     x.split_tiles = s.split_tiles;
     const int64_t blocks = (int64_t)x.tiles_m * x.tiles_n * (GR == kGroupSum && grouped ? x.groups : s.splits);
-    if (blocks > 0x7FFFFFFF) return fail(HEDDLE_E_RANGE, "more tiles than a launch holds");
+    if (blocks > 0xFFFFFFFF / (WM * WN * 64)) return fail(HEDDLE_E_RANGE, "more tiles than a launch holds");   // below 2^32 lanes
     hipLaunchKernelGGL((gemm_kernel<BM, BN, WM, WN, STAGES, ACOL, BCOL, GR, T, Epi>), dim3((unsigned)blocks), dim3(WM * WN * 64), 0,
                        stream, x, epi);
     hipError_t e = hipGetLastError();
