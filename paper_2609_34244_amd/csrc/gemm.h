@@ -807,6 +807,7 @@ template <typename Epi> __global__ void __launch_bounds__(256) join_kernel(Args 
 struct Shape { int cfg, splits, split_tiles; };
 enum Order { kRowsRows = 0, kRowsCols = 1, kColsCols = 2 };   // of the operands in memory
 Shape shape_of(int64_t M, int64_t N, int64_t K, int groups, bool gated, Order order);   // groups: 0 without offsets
+bool third_buffer(int64_t M, int64_t N, int groups, bool gated, bool sums, int splits);       // of 64 x 128 tiles
 inline size_t partial_bytes(const Shape &s, int64_t M, int64_t N, bool gated)
 {
     return s.splits > 1 ? (size_t)s.splits * M * partial_cols((int)N, gated) * 4 : 0;
@@ -842,16 +843,10 @@ inline int launch_gemm(const Args &x, const Shape &s, const Epi &epi, hipStream_
     switch (s.cfg) {
     case 0: return launch_cfg<256, 256, 2, 4, 2, ACOL, BCOL, GR, T>(x, s, epi, stream);
     case 1: return launch_cfg<128, 128, 2, 2, 1, ACOL, BCOL, GR, T>(x, s, epi, stream);
-    case 2: {
-        // A workgroup alone on its CU keeps two tiles on their way, not one (64 x 10816 x 4096:
-        // 27.5 -> 23.1 us); where there are more, a third workgroup does more than a third buffer
-        // (64 x 4096 x 10816: 24.7 us, 26.6 with three). Groups: about half have a tile that is
-        // not full.
-        const int64_t rows = x.offsets && GR == kGroupRows ? (x.M + 63) / 64 + x.groups / 2 : (x.M + 63) / 64;
-        const int64_t tiles = rows * (((Epi::gated ? 2 : 1) * (int64_t)x.N + 127) / 128) * (x.offsets && GR == kGroupSum ? x.groups : s.splits);
-        if (tiles <= 256) return launch_cfg<64, 128, 1, 4, 3, ACOL, BCOL, GR, T>(x, s, epi, stream);
+    case 2:
+        if (third_buffer(x.M, x.N, x.offsets ? x.groups : 0, Epi::gated, GR == kGroupSum, s.splits))
+            return launch_cfg<64, 128, 1, 4, 3, ACOL, BCOL, GR, T>(x, s, epi, stream);
         return launch_cfg<64, 128, 1, 4, 2, ACOL, BCOL, GR, T>(x, s, epi, stream);
-    }
     default:   // groups of few rows only
         if constexpr (GR == kGroupRows) return launch_cfg<64, 256, 1, 4, 2, ACOL, BCOL, GR, T>(x, s, epi, stream);
         else return fail(HEDDLE_E_INVAL, "no such tile");

@@ -63,6 +63,16 @@ Shape shape_of(int64_t M, int64_t N, int64_t K, int groups, bool gated, Order or
     return best;
 }
 
+// A workgroup alone on its CU keeps two tiles on their way, not one (64 x 10816 x 4096:
+// 27.5 -> 23.1 us); where there are more, a third workgroup does more than a third buffer
+// (64 x 4096 x 10816: 24.7 us, 26.6 with three). Groups: about half have a tile that is
+// not full.
+bool third_buffer(int64_t M, int64_t N, int groups, bool gated, bool sums, int splits)
+{
+    const int64_t rows = (M + 63) / 64 + (sums ? 0 : groups / 2), cols = (gated ? 2 * N : N) + 127;
+    return rows * (cols / 128) * (sums && groups ? groups : splits) <= 256;
+}
+
 int check_matrix(const char *name, const void *p, int64_t ld, int64_t cols)
 {
     if (!p) return fail(HEDDLE_E_INVAL, std::string(name) + " is NULL");
