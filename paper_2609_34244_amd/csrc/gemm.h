@@ -98,8 +98,9 @@ __device__ inline float act_of(int act, float z)
     default: return z;
     }
 }
-// value and derivative; the derivative is that at +-88 beyond, where it is 0 or 1 to fp32
-// but its factors leave the type's range
+// Value and derivative of a kept z. The derivative is that at +-88 beyond, where it is 0 or 1 to
+// fp32 but its factors leave the type's range; the value that at -88 below, where it is 0: a z below
+// float16's range was kept as -infinity, and the forward pass had 0 there.
 __device__ inline void act_both(int act, float z, float &v, float &d)
 {
     const float y = z > 88.0f ? 88.0f : z < -88.0f ? -88.0f : z;
@@ -110,21 +111,21 @@ __device__ inline void act_both(int act, float z, float &v, float &d)
         break;
     case HEDDLE_A_SILU: {
         const float s = sigmoid(z);
-        v = z * s;
+        v = fmaxf(z, y) * s;
         d = s * (1.0f + y * (1.0f - s));
         break;
     }
     case HEDDLE_A_GELU: {
         float e;
         const float c = normal_cdf(z, e);
-        v = z * c;
+        v = fmaxf(z, y) * c;
         d = c + y * 0.39894228040143268f * e;
         break;
     }
     case HEDDLE_A_GELU_TANH: {
         const float u = 0.79788456080286536f * (z + 0.044715f * z * z * z);
         const float s = sigmoid(2.0f * u);
-        v = z * s;
+        v = fmaxf(z, y) * s;
         d = s + 2.0f * y * s * (1.0f - s) * 0.79788456080286536f * (1.0f + 0.134145f * y * y);
         break;
     }
