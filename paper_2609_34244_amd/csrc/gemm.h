@@ -44,8 +44,9 @@ enum Grouping { kGroupRows = 1, kGroupSum = 2 };
 
 struct Args {
     const void *a, *b;
-    int64_t lda, ldb;                         // elements between rows in memory, even, at most kMaxLd
-    int64_t stride_a, stride_b;               // elements from a group's operand to the next one's
+    int64_t lda, ldb;                         // elements between rows in memory, even, at most HEDDLE_MAX_LD:
+                                              // 256 rows stay below 2^31 bytes
+    int64_t stride_b;                         // elements from a group's B to the next one's
     int32_t M, N, K;                          // K: the reduction (kGroupSum: of all groups together)
     int32_t F;                                // gated: rows of B from a gate row to its up row (N = F)
     const int32_t *offsets;                   // device [groups + 1], or NULL
@@ -56,7 +57,6 @@ struct Args {
 };
 // columns of a partial sum's row: whole eights; gated: the up columns after the gate ones
 __host__ __device__ inline int64_t partial_cols(int n, bool gated) { return (int64_t)((n + 7) & ~7) * (gated ? 2 : 1); }
-constexpr int64_t kMaxLd = int64_t(1) << 22;  // 256 rows stay below 2^31 bytes
 
 // ---- activations (fp32) ----
 // the reciprocal of one instruction, off by 1 ulp: a division is ten, and the activations bound

@@ -63,9 +63,9 @@ struct BiasGrad {
     const int32_t *offsets;
     int32_t groups, act, m, n;
     int32_t chunks, chunk_rows;               // parts of the rows (1 with offsets)
-    float *partial;                           // [chunks][groups][n]
+    float *partial;                           // [chunks][n] (chunks > 1)
 };
-int64_t bias_grad_bytes(int64_t m, int64_t n, bool grouped, int groups);
+int64_t bias_grad_bytes(int64_t m, int64_t n, bool grouped);
 int launch_bias_grad(int dtype, BiasGrad b, hipStream_t stream);
 
 int check_matrix(const char *name, const void *p, int64_t ld, int64_t cols);

@@ -233,7 +233,7 @@ static void bias_chunks(int64_t m, int64_t n, bool grouped, int &chunks, int &ro
     rows = (int)((m + chunks - 1) / chunks);
 }
 
-int64_t bias_grad_bytes(int64_t m, int64_t n, bool grouped, int)
+int64_t bias_grad_bytes(int64_t m, int64_t n, bool grouped)
 {
     int chunks, rows;
     bias_chunks(m, n, grouped, chunks, rows);
@@ -416,7 +416,7 @@ template <typename T> static int backward(const heddle_linear_desc *d, Scratch &
         b.dz = s.take((size_t)d->m * b.lddz * 2);
         dz = {b.dz, b.lddz, 0};
     }
-    if (b.db) b.partial = (float *)s.take(bias_grad_bytes(d->m, d->n, d->d_offsets != nullptr, groups));
+    if (b.db) b.partial = (float *)s.take(bias_grad_bytes(d->m, d->n, d->d_offsets != nullptr));
     if (run && (b.db || (b.dz && d->m > 0))) rc = launch_bias_grad(d->dtype, b, stream);
     Operand w = {d->w, d->ldw, d->stride_w}, x = {d->x, d->ldx, 0};
     Copies c;

@@ -19,9 +19,6 @@
 namespace heddle {
 namespace mm {
 
-__device__ inline f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
-__device__ inline f32x4 mfma16(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
-
 // group j of those with rows; false past the last one
 __device__ inline bool find_group(const int32_t *offsets, int groups, int total, int j, int &g, int &lo, int &hi)
 {
@@ -115,7 +112,7 @@ __global__ void __launch_bounds__(WAVES * 64) skinny_kernel(Args x, Epi epi)
 #pragma unroll
                 for (int p = 0; p < P; p++)
 #pragma unroll
-                    for (int b = 0; b < MB; b++) acc[p][b] = mfma16(fw[p][u / H][u % H], fx[b][u / H][u % H], acc[p][b]);
+                    for (int b = 0; b < MB; b++) acc[p][b] = mfma(fw[p][u / H][u % H], fx[b][u / H][u % H], acc[p][b]);
             s += N;
         };
         while (s + U <= last) batch(std::integral_constant<int, U>());
@@ -133,7 +130,7 @@ __global__ void __launch_bounds__(WAVES * 64) skinny_kernel(Args x, Epi epi)
                 for (int p = 0; p < P; p++) {
                     const frag fw = load_some(w + p * up + k, count);
 #pragma unroll
-                    for (int b = 0; b < MB; b++) acc[p][b] = mfma16(fw, fx[b], acc[p][b]);
+                    for (int b = 0; b < MB; b++) acc[p][b] = mfma(fw, fx[b], acc[p][b]);
                 }
             }
         }
