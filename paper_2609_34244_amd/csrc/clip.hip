@@ -9,8 +9,8 @@
 // summed in fp64 throughout: fp32 squares overflow from 1.9e19, and at two
 // fp64 operations a value the sums stay far below the vector units' rate. The
 // clipping's workgroups each add up the at most kParts sums by themselves, in
-// one order, which saves a launch between the two passes. 2e8 bf16 values: 72 + 138 us (5.6 and
-// 5.8 TB/s); 1.6e9 values of 320 tensors: 1.97 ms (4.9 TB/s); 1e6 fp32 values: 4.3 + 6.0 us.
+// one order, which saves a launch between the two passes. 2e8 bf16 values: 74 + 137 us (5.4 and
+// 5.9 TB/s); 1.6e9 values of 320 tensors: 1.96 ms (4.9 TB/s); 1e6 fp32 values: 4.3 + 6.2 us.
 #include <cmath>
 
 #include "heddle_internal.h"

@@ -6,11 +6,11 @@
 // Backward, 12 t d f flops: dY Wout forms dP and H again in its epilogue
 // (P is what the forward pass kept; H costs t f values less to keep), then the
 // three products over them.
-// Bound by the matrix cores for many rows: 4096 rows of 4096 x 10816, forward 660 + 292 us (1100
-// and 1244 TFLOP/s), backward 424 us with dP and H in the epilogue (856), then 566, 613 and 313 us
-// (1282, 1184, 1158). Bound by the weights for few rows a group: 64 rows for each of 64 experts
-// of 4096 x 1632, forward 399 + 248 us (4.3 and 3.5 TB/s), backward 237 + 354 us (3.6 and 4.8),
-// the weights' gradients 563 + 323 us (3.0 and 2.6 TB/s written).
+// Bound by the matrix cores for many rows: 4096 rows of 4096 x 10816, forward 657 + 289 us (1104
+// and 1258 TFLOP/s), backward 417 us with dP and H in the epilogue (871), then 558, 610 and 309 us
+// (1301, 1191, 1174). Bound by the weights for few rows a group: 64 rows for each of 64 experts
+// of 4096 x 1632, forward 398 + 250 us (4.3 and 3.4 TB/s), backward 236 + 355 us (3.6 and 4.8),
+// the weights' gradients 552 + 323 us (3.1 and 2.6 TB/s written).
 #include "linear.h"
 
 namespace heddle {

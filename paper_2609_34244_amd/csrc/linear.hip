@@ -5,8 +5,9 @@
 // Backward: dZ = dY act'(Z) is formed once, in the pass that sums db (without
 // an activation dZ is dY itself), then dX = dZ W and dW = dZ^T X.
 // Bound by the matrix cores from some 500 rows on: 4096 rows of 4096 x 10816 with bias and
-// gelu_tanh 384 us forward (945 TFLOP/s), dZ and db 75 us (266 MB, 3.5 TB/s), dX 304 us and dW
-// 339 us (1195 and 1070 TFLOP/s); 8192^3 alone 795 us (1383 TFLOP/s).
+// gelu_tanh 366 us forward (990 TFLOP/s), dZ and db 76 us (266 MB, 3.5 TB/s), dX 295 us and dW
+// 328 us (1232 and 1107 TFLOP/s); 8192^3 alone 795 us (1383 TFLOP/s). Bound by latency for small
+// odd sizes: 1001 x 1027 x 513 in 80 to 144 workgroups that walk 9 to 17 k-tiles, 10 to 18 us each.
 #include "linear.h"
 
 namespace heddle {
@@ -14,8 +15,10 @@ namespace mm {
 
 // The tile shape and the split of the reduction with the least estimated time. Constants in
 // us, from times of every shape and split on 270 products of 33 .. 8192 rows, 128 .. 20000
-// columns and k of the three memory orders: the choice costs 1.3% over the best one on
-// average. step: a k-tile on a CU whose workgroup slots are taken; least: the same for
+// columns and k of the three memory orders, before stores went past the caches, gradients had
+// an epilogue of their own and 64 x 128 a third buffer. On the kernels as they are, over 270
+// other such products: the choice is the best one for half of them, costs 1.3% over it on
+// average, 9% for one in twenty and 18% at worst (59 x 976 x 3456, 16 parts for 8). step: a k-tile on a CU whose workgroup slots are taken; least: the same for
 // workgroups alone on their CU; fixed: start and epilogue of a round of workgroups.
 //   256 x 256: one workgroup a CU, the highest rate; 128 x 128: four a CU, each with one buffer
 //   (what fills the chip with 2000 x 2000 outputs, and what writes most while little is

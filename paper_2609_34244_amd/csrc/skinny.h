@@ -6,8 +6,8 @@
 // matrix instruction reads (16 rows x 32 k, lane = row, 16 bytes of k), U pieces of W in
 // flight per lane, and X, which the caches hold, beside it. The wavefronts' sums meet in LDS in a
 // fixed order. Loads need only the alignment of a value, so no operand is copied. One row of
-// 4096 x 4096: 8.4 us, 4.0 TB/s of W; of 2 x 10816 x 4096, gated: 35.8 us, 4.95 TB/s (a large copy
-// moves 4.8).
+// 4096 x 4096: 10.4 us, 3.2 TB/s of W from memory (8.4 us from the memory-side cache); of
+// 2 x 10816 x 4096, gated: 34.5 us, 5.1 TB/s (a large copy moves 4.8).
 //
 // Groups: a workgroup takes the j-th group that has rows; there are at most as many as rows.
 #pragma once
@@ -169,7 +169,8 @@ __global__ void __launch_bounds__(WAVES * 64) skinny_kernel(Args x, Epi epi)
 // rows are not on 4-byte boundaries a copy of it. us with it / with tiles:
 //   4096 x 4096: 1 row 10.7 / 15.1, 32 rows 14.0 / 14.2;  8192 x 8192: 1 row 30.4 / 30.7, 8 rows
 //   35.9 / 31.1;  4096 x 10816: 4 rows 23.0 / 21.2;  20000 x 4096 with odd rows: 8 rows 63 / about
-//   105, 32 rows 119 / about 107.
+//   105, 32 rows 119 / about 107;  at the bound on m n k, 24032 x 8192: 1 row 80.6 / 93.2;  past it,
+//   48064 x 8192: 1 row 157 / 170, 128000 x 8192: 391 / 375, 24032 x 8192: 4 rows 89 / 95.
 // Groups, forward pass of the block: 64 of 4096 x 1632: 2 rows each 349 / 379, 4: 435 / 427, 8:
 //   595 / 460;  8 of 4096 x 816: 2: 33 / 49, 4: 56 / 52;  32 of 4096 x 204: 2: 37 / 48, 6: 71 / 60.
 inline bool is_skinny(int64_t m, int64_t n, int64_t k, int groups, bool copied)

@@ -7,7 +7,8 @@ projections is left out, its output being the values:
 
     q = x Wq^T;  [k | v] = x Wkv^T;  h = x + v Wo^T;  y = h + block(h)
 
-(q and k are formed, and their gradients taken, though they are zero then.)
+(q and k are formed, and their gradients taken, though they are zero then.) All experts are on
+this rank. A training runtime's layers take other times; these are a layer's without attention.
 :class:`Layer` runs it with ``heddle_linear`` and ``heddle_gated_ffn`` and their
 backward passes, :func:`train` a step of several layers that ends with
 ``heddle_clip_grad_norm`` and an update, and :func:`measure` puts times into the
@@ -152,7 +153,7 @@ def main():
     w = make_workload(a.config, n=a.templates)
     profile, times = measure(load_config(a.config), w.profile)
     for tp, (dense, moe) in times.items():
-        print(f"TP {tp}: dense layer {dense / 1e3:.1f} us" + (f", expert layer {moe / 1e3:.1f} us" if w.profile.is_moe.any() else ""))
+        print(f"TP {tp}, without attention: dense layer {dense / 1e3:.1f} us" + (f", expert layer {moe / 1e3:.1f} us" if w.profile.is_moe.any() else ""))
     n_stages, stages = H.to_device(w.n_stages, w.stages)
     for what, p in (("synthetic", w.profile), ("measured", profile)):
         best = H.heddle_best_plan(H.heddle_load_profile(p), n_stages, stages, [int(x) for x in w.m], 0)
