@@ -553,10 +553,10 @@ int heddle_profile_info_get(const heddle_profile *p, heddle_profile_info *info);
  * any address and any ld will do: sums run at full speed for rows that start
  * on 4-byte boundaries, others are copied to scratch first). Sums are fp32;
  * every output is rounded once, to nearest even. Inputs and outputs must not
- * overlap, except that residual may be the output itself. A call that would
- * read what it has overwritten, or write one output over another, is refused
- * where the descriptor shows it (matrices with different distances between
- * rows may overlap unseen).
+ * overlap, except that residual may be the output itself, and so may x of the
+ * gated block. A call that would read what it has overwritten, or write one
+ * output over another, is refused where the descriptor shows it (matrices with
+ * different distances between rows may overlap unseen).
  *
  * Expert groups: with d_offsets (DEVICE [groups + 1] int32, non-decreasing,
  * from 0 to the row count) rows d_offsets[e] .. d_offsets[e+1] - 1 use the

@@ -446,6 +446,9 @@ def heddle_fill_plans(profiles, mbs, cl, global_batch, dp_cap, n_stages, stages,
 # for by the caller. Outputs that the call allocates belong to that stream, as
 # those of torch's operators under torch.cuda.stream(stream) do.
 #
+# An output may be the residual itself, and of the gated block x; over what else
+# a call still reads it is refused.
+#
 # Autograd records none of the calls: gradients come from the *_backward ones. The
 # products refuse tensors that require a gradient unless it is off (torch.no_grad()).
 
