@@ -579,7 +579,7 @@ int heddle_profile_info_get(const heddle_profile *p, heddle_profile_info *info);
  * ====================================================================== */
 #define HEDDLE_T_BF16 0
 #define HEDDLE_T_F16  1
-#define HEDDLE_T_F32  2   /* gradient tensors only */
+#define HEDDLE_T_F32  2   /* gradient tensors, layer normalisation and router logits */
 
 #define HEDDLE_A_NONE      0
 #define HEDDLE_A_RELU      1
@@ -694,6 +694,137 @@ int heddle_clip_grads(const heddle_grad_desc *grads, int32_t count, const float 
 int heddle_clip_grad_norm(const heddle_grad_desc *grads, int32_t count, float max_norm, float *d_norm,
                           void *d_workspace, int64_t workspace_bytes, hipStream_t stream);
 int heddle_grad_norm_workspace(const heddle_grad_desc *grads, int32_t count, int64_t *h_bytes);
+
+/* ======================================================================
+ * What a layer does between its products: attention, layer normalisation and
+ * a router's balance, with their gradients. As above: DEVICE memory, fp32
+ * sums, outputs rounded once to nearest even, scratch of the caller's by the
+ * *_workspace call, asynchronous on `stream`, no allocation, the same errors.
+ * Integers on the device (offsets, lengths, prefixes, picks) are read there
+ * only, and whatever they hold no access leaves the tensors.
+ * ====================================================================== */
+#define HEDDLE_MAX_HEADS    1024
+#define HEDDLE_MAX_HEAD_DIM 128
+#define HEDDLE_MAX_EXPERTS  2048
+
+/*
+ * Attention. Of a sequence with lq query rows and lk key rows, query i stands
+ * at place i + lk - lq among the keys and sees key j < lk if `causal` is 0, or
+ * j <= i + lk - lq, or j < prefix. With s = scale q_i k_j, then cap tanh(s / cap)
+ * where cap > 0, then minus slope[head] |i + lk - lq - j| where slopes are given:
+ * y_i = sum_j softmax(s)_j v_j. A row that sees nothing: y = 0, lse = -infinity.
+ *
+ * Batched (packed 0): tensors are [sequences][q_len or k_len][heads][dim];
+ * d_q and d_k, where given, hold lengths [sequences] (outside 0 .. q_len or
+ * k_len: the nearer of the two), so k and v may be a cache with room left.
+ * Packed (packed 1): documents in one run of rows, tensors are
+ * [rows][heads][dim] with q_len and k_len the rows of all; rows d_q[s] ..
+ * d_q[s+1] - 1 of q and d_k[s] .. d_k[s+1] - 1 of k and v are sequence s; a
+ * document sees only itself. Offsets are non-decreasing; otherwise what the
+ * rows concerned receive is unspecified.
+ * Rows of no sequence, and past a sequence's length, are neither used nor
+ * written. Head h reads key head h / (heads / kv_heads).
+ *
+ * Values run over dim side by side; strides [3] are elements from one sequence
+ * (ignored where packed), row and head to the next; a row's at most HEDDLE_MAX_LD,
+ * one of a dimension of size 1 is not looked at. Any
+ * address and strides will do: full speed for 16-byte addresses, strides of
+ * whole eights and dim a multiple of 8 (other operands are copied to scratch).
+ * lse: [all query rows][heads] fp32, log(sum_j exp(s)). Inputs of
+ * visible rows are finite: a product of 0 and an infinity or NaN of a key that
+ * some rows do not see may reach those rows too. Outputs lie apart from inputs
+ * and from each other (seen where heads lie side by side; tensors with other
+ * orders of dimensions may overlap unseen).
+ */
+typedef struct heddle_attention_desc {
+    int32_t dtype, causal, packed, sequences;         /* HEDDLE_T_BF16 or HEDDLE_T_F16; sequences 0 .. HEDDLE_MAX_GROUPS */
+    int64_t q_len, k_len;                             /* q_len * heads, k_len 0 .. HEDDLE_MAX_ROWS */
+    int32_t heads, kv_heads, dim;                     /* heads a multiple of kv_heads; dim 1 .. HEDDLE_MAX_HEAD_DIM */
+    float scale, cap;                                 /* scale > 0; cap 0: none */
+    const int32_t *d_q, *d_k;                         /* offsets [sequences + 1], or lengths [sequences] or NULL */
+    const int32_t *d_prefix;                          /* [sequences] or NULL */
+    const float *d_slopes;                            /* [heads] or NULL */
+    const void *q; int64_t q_strides[3];
+    const void *k; int64_t k_strides[3];
+    const void *v; int64_t v_strides[3];
+    void *y; int64_t y_strides[3];                    /* output of heddle_attention, input of heddle_attention_backward */
+    float *lse;                                       /* output of heddle_attention or NULL, input of heddle_attention_backward */
+    const void *dy; int64_t dy_strides[3];
+    void *dq; int64_t dq_strides[3];                  /* or NULL */
+    void *dk; int64_t dk_strides[3];                  /* or NULL, with dv */
+    void *dv; int64_t dv_strides[3];
+} heddle_attention_desc;
+
+/*
+ * heddle_attention -- probabilities are rounded to dtype as operands of the
+ * product with v; their sum is of the values before that rounding.
+ */
+int heddle_attention(const heddle_attention_desc *d, void *d_workspace, int64_t workspace_bytes, hipStream_t stream);
+/*
+ * heddle_attention_backward -- with P = exp(s - lse), dP = dy v^T, D = sum dy y,
+ * dS = P (dP - D) (1 - tanh^2 with a cap): dq = scale dS k, dk = scale dS^T q,
+ * dv = P^T dy, the last two summed over the heads of a key head, in a fixed
+ * order. P and dS are rounded to dtype as operands. No gradient of the slopes.
+ */
+int heddle_attention_backward(const heddle_attention_desc *d, void *d_workspace, int64_t workspace_bytes, hipStream_t stream);
+int heddle_attention_workspace(const heddle_attention_desc *d, int32_t backward, int64_t *h_bytes);
+
+/* xh = (x - mean) / sqrt(mean of (x - mean)^2 + eps) by rows, y = xh w + b. */
+typedef struct heddle_layer_norm_desc {
+    int32_t dtype, wtype;                             /* HEDDLE_T_*; wtype (w, bias, dw, db): dtype or HEDDLE_T_F32 */
+    int64_t m, n;                                     /* rows 0 .. HEDDLE_MAX_ROWS, columns 1 .. HEDDLE_MAX_LD */
+    float eps;                                        /* >= 0 */
+    const void *x; int64_t ldx;                       /* [m][n] */
+    const void *w;                                    /* [n] or NULL: ones */
+    const void *bias;                                 /* [n] or NULL */
+    void *y; int64_t ldy;                             /* [m][n]; may be x */
+    float *stats;                                     /* [m][2] mean and 1 / sqrt(...): output or NULL, input of the backward call */
+    const void *dy; int64_t lddy;                     /* [m][n] */
+    const void *residual; int64_t ldr;                /* [m][n] added to dx (the gradient that reaches x past the layer), or NULL */
+    void *dx; int64_t lddx;                           /* [m][n] or NULL; may be dy or residual */
+    void *dw, *db;                                    /* [n] or NULL */
+} heddle_layer_norm_desc;
+
+int heddle_layer_norm(const heddle_layer_norm_desc *d, hipStream_t stream);
+/*
+ * heddle_layer_norm_backward -- with g = dy w:
+ * dx = (g - mean(g) - xh mean(g xh)) / sqrt(...) + residual, dw = the sum of
+ * dy xh over rows, db that of dy, in a fixed order.
+ */
+int heddle_layer_norm_backward(const heddle_layer_norm_desc *d, void *d_workspace, int64_t workspace_bytes, hipStream_t stream);
+int heddle_layer_norm_workspace(const heddle_layer_norm_desc *d, int64_t *h_bytes);
+
+/*
+ * A router's balance. p = softmax(logits) of a row; c_e: picks of expert e, C
+ * their sum, N: rows with a pick, P_e: the mean of p_e over those rows;
+ * loss = scale experts sum_e (c_e / C) P_e (0 without picks). A pick outside 0 ..
+ * experts - 1 counts nowhere; a row of nothing else (padding) adds nothing, whatever
+ * its logits. The picks' gradient is none.
+ */
+typedef struct heddle_expert_balance_desc {
+    int32_t dtype, experts, picks, pick_bytes;        /* HEDDLE_T_*; 1 .. HEDDLE_MAX_EXPERTS; picks a row, 1 .. experts; 4 or 8 */
+    int64_t t;                                        /* rows, 0 .. HEDDLE_MAX_ROWS; t picks below 2^31 */
+    float scale;
+    const void *logits; int64_t ldl;                  /* [t][experts] */
+    const void *d_picked; int64_t ldp;                /* [t][picks] int32 or int64 (ldp: picks) */
+    int32_t *d_counts;                                /* [experts] c: output, input of the backward call */
+    int32_t *d_rows;                                  /* [1] N: output or NULL, input of the backward call */
+    int32_t *d_offsets;                               /* [experts + 1] running sums of c, as the grouped products read them, or NULL */
+    float *d_mean;                                    /* [experts] P, or NULL */
+    float *d_loss;                                    /* [1] or NULL */
+    const float *d_dloss;                             /* [1] gradient of the loss; NULL: 1 */
+    const void *residual; int64_t ldr;                /* [t][experts] added to dlogits (the gradient by other ways), or NULL */
+    void *dlogits; int64_t ldd;                       /* [t][experts]; may be logits or residual */
+} heddle_expert_balance_desc;
+
+int heddle_expert_balance(const heddle_expert_balance_desc *d, void *d_workspace, int64_t workspace_bytes, hipStream_t stream);
+int heddle_expert_balance_workspace(const heddle_expert_balance_desc *d, int64_t *h_bytes);
+/*
+ * heddle_expert_balance_backward -- dlogits = dloss scale experts / (C N)
+ * p (c - sum_j p_j c_j) + residual, from counts and rows as they are given (of
+ * all ranks together, say); rows without a pick receive residual alone.
+ */
+int heddle_expert_balance_backward(const heddle_expert_balance_desc *d, hipStream_t stream);
 
 /* Message of the last negative return on this host thread ("" if none). */
 const char *heddle_last_error(void);

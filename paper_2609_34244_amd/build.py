@@ -9,7 +9,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libheddle.so")
 SOURCES = ["profile.cpp", "windows.hip", "price.hip", "search.hip", "evaluate.hip", "distribute.hip", "argmin.hip", "enumerate.hip", "tile.hip",
-           "fill.hip", "linear.hip", "gated_ffn.hip", "clip.hip"]
+           "fill.hip", "linear.hip", "gated_ffn.hip", "clip.hip", "norm.hip", "balance.hip", "attention.hip",
+           "attention_backward.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 FLAGS = [

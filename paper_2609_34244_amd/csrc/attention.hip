@@ -1,0 +1,566 @@
+// Attention on gfx950's matrix cores: y = softmax(mask(cap tanh(scale q k / cap) - slope |distance|)) v.
+//
+// One pass over the keys with a running maximum and sum. Query rows of a key head, (query, head of its
+// group) pairs in that order, are taken 32 a wavefront, so that heads that share keys share their tiles.
+// forward_kernel: 128 rows a workgroup over tiles of 64 keys, two in LDS; two workgroups a CU, so that one's
+// products run beside the other's exponentials. Bound by both: 32 keys of 32 rows are 16 products of 32
+// cycles and 16 values a lane of about 30 cycles.
+// split_kernel: 32 rows a workgroup (few queries over long caches), each wavefront with tiles of its own, the
+// keys of a row tile divided over `parts` workgroups; combine_kernel joins them. Bound by reading keys and values.
+#include <algorithm>
+#include <cmath>
+
+#include "attention.h"
+
+namespace heddle {
+namespace attn {
+
+// A lane's query row and what it sees: keys 0 .. limit - 1.
+struct Row {
+    int64_t at;                               // counted over all rows of q
+    int32_t i, head, limit, pos;
+    bool any;
+};
+__device__ inline Row row_of(const Args &a, const Sequence &q, int hk, int r)
+{
+    Row x;
+    x.any = r < q.lq * a.group;
+    x.i = r / a.group;
+    x.head = hk * a.group + (r - x.i * a.group);
+    x.at = (a.packed ? q.q0 : (int64_t)q.s * a.q_len) + x.i;
+    x.pos = x.i + (q.lk - q.lq);
+    x.limit = x.any ? max(min(q.lk, a.causal ? max(x.pos + 1, q.prefix) : q.lk), 0) : 0;
+    return x;
+}
+__device__ inline int limit_of(const Args &a, const Sequence &q, int r)
+{
+    if (r >= q.lq * a.group) return 0;
+    const int pos = r / a.group + (q.lk - q.lq);
+    return __builtin_amdgcn_readfirstlane(max(min(q.lk, a.causal ? max(pos + 1, q.prefix) : q.lk), 0));
+}
+
+// The running state of 32 rows: m in the scores' units (with a cap or slopes: times log2(e)).
+template <int DP> struct State {
+    f32x16 o[DP / 32];
+    float m, l;
+    __device__ inline void init()
+    {
+        m = -INFINITY, l = 0;
+#pragma unroll
+        for (int d = 0; d < DP / 32; d++) o[d] = f32x16{};
+    }
+};
+
+// Scores of C x 32 keys from key j0 on (of this lane's half), their probabilities and the products with the values.
+// The maximum follows only when it is 2^8 behind: p then stays below 2^8, and the sums are scaled again seldom.
+template <typename T, int DP, int C, bool MOD>
+__device__ inline void attend(const Args &a, State<DP> &st, const typename mm::pack8<T>::type *q, const char *tk, const char *tv, int j0, const Row &row,
+                              float slope2, bool masked)
+{
+    const int lane = threadIdx.x & 63, h = lane >> 5, col = lane & 31;
+    f32x16 s[C];
+#pragma unroll
+    for (int c = 0; c < C; c++) {
+        s[c] = f32x16{};
+#pragma unroll
+        for (int k = 0; k < DP / 16; k++) s[c] = mfma(row_fragment<DP, T>(tk, c * 32 + col, k, h), q[k], s[c]);
+    }
+    const int first = j0 + 4 * h;             // key of register 0 of s[0]
+    if constexpr (MOD) {
+#pragma unroll
+        for (int c = 0; c < C; c++) modify<true>(a, s[c], slope2, row.pos - first - c * 32, nullptr);
+    }
+    if (masked) {
+#pragma unroll
+        for (int c = 0; c < C; c++)
+#pragma unroll
+            for (int r = 0; r < 16; r++)
+                if (first + c * 32 + mfma_row(r, 0) >= row.limit) s[c][r] = -INFINITY;
+    }
+    float top = s[0][0];
+#pragma unroll
+    for (int c = 0; c < C; c++)
+#pragma unroll
+        for (int r = 0; r < 16; r++) top = fmaxf(top, s[c][r]);
+    top = fmaxf(top, other_half(top));
+    const float unit = MOD ? 1.0f : a.scale2;
+    if (__any(top * unit > st.m * unit + 8.0f)) {
+        const float m = fmaxf(st.m, top), f = m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((st.m - m) * unit);
+        st.m = m;
+        st.l *= f;
+#pragma unroll
+        for (int d = 0; d < DP / 32; d++)
+#pragma unroll
+            for (int r = 0; r < 16; r++) st.o[d][r] *= f;
+    }
+    const float base = st.m == -INFINITY ? 0.0f : st.m * unit;
+    float sum = 0;
+#pragma unroll
+    for (int c = 0; c < C; c++)
+#pragma unroll
+        for (int r = 0; r < 16; r++) {
+            s[c][r] = __builtin_amdgcn_exp2f(MOD ? s[c][r] - base : __builtin_fmaf(s[c][r], unit, -base));
+            sum += s[c][r];
+        }
+    st.l += sum;
+#pragma unroll
+    for (int c = 0; c < C; c++)
+#pragma unroll
+        for (int k = 0; k < 2; k++) {
+            const auto p = pack<T>(s[c], 8 * k);
+#pragma unroll
+            for (int d = 0; d < DP / 32; d++) st.o[d] = mfma(column_fragment<DP, T>(tv, c * 32 + 16 * k, d), p, st.o[d]);
+        }
+}
+
+// a lane's query row as the products' operand
+template <typename T, int DP> __device__ inline void load_query(const Args &a, const View &v, const Sequence &q, const Row &row, typename mm::pack8<T>::type *f)
+{
+    const int h = (threadIdx.x & 63) >> 5;
+    const T *p = (const T *)v.p + q.s * v.seq + (q.q0 + row.i) * v.row + row.head * v.head;
+#pragma unroll
+    for (int k = 0; k < DP / 16; k++) f[k] = global_fragment<T>(p, k * 16 + 8 * h, a.dim, row.any);
+}
+
+template <typename T, int DP, bool MOD> __global__ void __launch_bounds__(256, 2) forward_kernel(Args a, int64_t tiles)
+{
+    typedef Tile<DP, 64, 4> Tk;
+    __shared__ __align__(1024) char smem[2][2 * Tk::kBytes];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, h = lane >> 5;
+    // key heads fastest: 8 of them lie on one XCD each, whose L2 then holds its head's keys. The last tiles, which
+    // see the most keys, first.
+    const int hk = blockIdx.x % a.kv_heads;
+    const int64_t slot = gridDim.x / a.kv_heads - 1 - blockIdx.x / a.kv_heads;
+    int s;
+    int64_t tile;
+    if (a.packed) {
+        if (!find_slot(a.d_q, a.q_rows, 1, a.sequences, a.group, 128, tiles, slot, s, tile)) return;
+    } else {
+        s = (int)(slot % a.sequences), tile = slot / a.sequences;
+    }
+    const Sequence q = sequence_of(a, s);
+    if (tile * 128 >= (int64_t)q.lq * a.group) return;
+    const int r0 = (int)tile * 128, rows = q.lq * a.group;
+    const Row row = row_of(a, q, hk, r0 + wave * 32 + (lane & 31));
+    const int end = limit_of(a, q, min(r0 + 127, rows - 1)), mine = limit_of(a, q, min(r0 + wave * 32 + 31, max(rows - 1, r0 + wave * 32)));
+    const int whole = r0 + wave * 32 + 31 < rows ? limit_of(a, q, r0 + wave * 32) : 0;   // keys that all of the wavefront's rows see
+    const int count = (end + 63) / 64;
+
+    typename mm::pack8<T>::type qf[DP / 16];
+    load_query<T, DP>(a, a.q, q, row, qf);
+    const float slope2 = MOD && a.d_slopes ? a.d_slopes[row.any ? row.head : 0] * kLog2e : 0.0f;
+
+    const T *pk = (const T *)a.k.p + s * a.k.seq + q.k0 * a.k.row + hk * a.k.head;
+    const T *pv = (const T *)a.v.p + s * a.v.seq + q.k0 * a.v.row + hk * a.v.head;
+    int ok[Tk::kLoads], ov[Tk::kLoads];
+#pragma unroll
+    for (int i = 0; i < Tk::kLoads; i++) ok[i] = Tk::offset(i, wave, a.k.row, a.dim, 64), ov[i] = Tk::offset(i, wave, a.v.row, a.dim, 64);
+    const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)&smem[0][0];
+    auto load = [&](int t) {
+        const int valid = q.lk - t * 64;
+        const i32x4 bk = buffer_at(pk + (int64_t)t * 64 * a.k.row), bv = buffer_at(pv + (int64_t)t * 64 * a.v.row);
+        const uint32_t to = lds + (t & 1) * 2 * Tk::kBytes + wave * 1024;
+        if (valid >= 64) {
+#pragma unroll
+            for (int i = 0; i < Tk::kLoads; i++) {
+                mm::load_to_lds(bk, ok[i], to + i * 4096);
+                mm::load_to_lds(bv, ov[i], to + Tk::kBytes + i * 4096);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < Tk::kLoads; i++) {
+                mm::load_to_lds(bk, Tk::offset(i, wave, a.k.row, a.dim, valid), to + i * 4096);
+                mm::load_to_lds(bv, Tk::offset(i, wave, a.v.row, a.dim, valid), to + Tk::kBytes + i * 4096);
+            }
+        }
+    };
+    State<DP> st;
+    st.init();
+    if (count) load(0);
+    for (int t = 0; t < count; t++) {
+        mm::arrive();
+        if (t + 1 < count) load(t + 1);
+        if (t * 64 < mine) {
+            const char *tk = smem[t & 1];
+            attend<T, DP, 2, MOD>(a, st, qf, tk, tk + Tk::kBytes, t * 64, row, slope2, t * 64 + 64 > whole);
+        }
+    }
+    if (!row.any) return;
+    const float l = st.l + other_half(st.l), inv = l == 0 ? 0.0f : 1.0f / l;
+    T *y = (T *)a.y.p + s * a.y.seq + (q.q0 + row.i) * a.y.row + row.head * a.y.head;
+#pragma unroll
+    for (int d = 0; d < DP / 32; d++)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4)
+            store4<T>(y, d * 32 + mfma_row(r, h), a.dim, a.out_vec, st.o[d][r] * inv, st.o[d][r + 1] * inv, st.o[d][r + 2] * inv, st.o[d][r + 3] * inv);
+    if (a.lse && h == 0)
+        a.lse[row.at * a.heads + row.head] = l == 0 ? -INFINITY : (st.m * (MOD ? 1.0f : a.scale2) + __log2f(l)) * kLn2;
+}
+
+// 32 rows a workgroup. The sums of a part, where there are several: DP values, the maximum (times log2(e)) and the sum.
+template <typename T, int DP, bool MOD> __global__ void __launch_bounds__(256) split_kernel(Args a, int64_t tiles)
+{
+    typedef Tile<DP, 32, 1> Tk;
+    constexpr int kStage = 2 * Tk::kBytes, kLine = DP + 4;
+    static_assert(4 * 32 * kLine * 4 + 4 * 64 * 4 <= 8 * kStage, "the wavefronts' sums fit where the tiles were");
+    __shared__ __align__(1024) char smem[4][2][kStage];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, h = lane >> 5, col = lane & 31;
+    const int hk = blockIdx.x % a.kv_heads;
+    const int64_t rest = blockIdx.x / a.kv_heads, slot = rest / a.parts;
+    const int part = (int)(rest - slot * a.parts);
+    int s;
+    int64_t tile;
+    if (!find_slot(a.d_q, a.q_rows, a.packed, a.sequences, a.group, 32, tiles, slot, s, tile)) return;
+    const Sequence q = sequence_of(a, s);
+    if (tile * 32 >= (int64_t)q.lq * a.group) return;
+    const int r0 = (int)tile * 32, rows = q.lq * a.group;
+    const Row row = row_of(a, q, hk, r0 + col);
+    const int end = limit_of(a, q, min(r0 + 31, rows - 1)), whole = limit_of(a, q, r0);   // (no row: what is summed is not written)
+    const int all = (end + 31) / 32, per = (all + a.parts - 1) / a.parts;
+    const int first = part * per, last = min(first + per, all);
+
+    typename mm::pack8<T>::type qf[DP / 16];
+    load_query<T, DP>(a, a.q, q, row, qf);
+    const float slope2 = MOD && a.d_slopes ? a.d_slopes[row.any ? row.head : 0] * kLog2e : 0.0f;
+    const T *pk = (const T *)a.k.p + s * a.k.seq + q.k0 * a.k.row + hk * a.k.head;
+    const T *pv = (const T *)a.v.p + s * a.v.seq + q.k0 * a.v.row + hk * a.v.head;
+    const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)&smem[wave][0][0];
+    int ok[Tk::kLoads], ov[Tk::kLoads];
+#pragma unroll
+    for (int i = 0; i < Tk::kLoads; i++) ok[i] = Tk::offset(i, 0, a.k.row, a.dim, 32), ov[i] = Tk::offset(i, 0, a.v.row, a.dim, 32);
+    auto load = [&](int t, int stage) {
+        const int valid = q.lk - t * 32;
+        const i32x4 bk = buffer_at(pk + (int64_t)t * 32 * a.k.row), bv = buffer_at(pv + (int64_t)t * 32 * a.v.row);
+        const uint32_t to = lds + stage * kStage;
+#pragma unroll
+        for (int i = 0; i < Tk::kLoads; i++) mm::load_to_lds(bk, valid >= 32 ? ok[i] : Tk::offset(i, 0, a.k.row, a.dim, valid), to + i * 1024);
+#pragma unroll
+        for (int i = 0; i < Tk::kLoads; i++) mm::load_to_lds(bv, valid >= 32 ? ov[i] : Tk::offset(i, 0, a.v.row, a.dim, valid), to + Tk::kBytes + i * 1024);
+    };
+    State<DP> st;
+    st.init();
+    int stage = 0;
+    if (first + wave < last) load(first + wave, 0);
+    for (int t = first + wave; t < last; t += 4, stage ^= 1) {
+        // a wavefront's tiles are its own: it waits for its loads, and for its reads of the buffer that is filled next
+        constexpr int later = 2 * Tk::kLoads;
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        if (t + 4 < last) {
+            load(t + 4, stage ^ 1);
+            asm volatile("s_waitcnt vmcnt(%0)" :: "n"(later) : "memory");
+        } else {
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        }
+        const char *tk = smem[wave][stage];
+        attend<T, DP, 1, MOD>(a, st, qf, tk, tk + Tk::kBytes, t * 32, row, slope2, t * 32 + 32 > whole);
+    }
+    // the four wavefronts' sums
+    const float m = st.m == -INFINITY ? -INFINITY : st.m * (MOD ? 1.0f : a.scale2), l = st.l + other_half(st.l);
+    float *sums = (float *)&smem[0][0][0], *ms = sums + 4 * 32 * kLine;   // [wave][row][kLine], [wave][row] of m, then of l
+    __syncthreads();
+#pragma unroll
+    for (int d = 0; d < DP / 32; d++)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4)
+            *(mm::f32x4 *)(sums + (wave * 32 + col) * kLine + d * 32 + mfma_row(r, h)) = mm::f32x4{st.o[d][r], st.o[d][r + 1], st.o[d][r + 2], st.o[d][r + 3]};
+    if (h == 0) ms[wave * 32 + col] = m, ms[128 + wave * 32 + col] = l;
+    __syncthreads();
+    const int mine = threadIdx.x >> 3, sub = threadIdx.x & 7;
+    const Row out = row_of(a, q, hk, r0 + mine);
+    if (!out.any) return;
+    float top = ms[mine];
+#pragma unroll
+    for (int w = 1; w < 4; w++) top = fmaxf(top, ms[w * 32 + mine]);
+    float f[4], sum = 0;
+#pragma unroll
+    for (int w = 0; w < 4; w++) {
+        f[w] = ms[w * 32 + mine] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(ms[w * 32 + mine] - top);
+        sum += f[w] * ms[128 + w * 32 + mine];
+    }
+    const float inv = a.parts > 1 ? 1.0f : sum == 0 ? 0.0f : 1.0f / sum;
+    float *p = a.partial + (((slot * a.kv_heads + hk) * 32 + mine) * a.parts + part) * (DP + 2);
+    T *y = (T *)a.y.p + s * a.y.seq + (q.q0 + out.i) * a.y.row + out.head * a.y.head;
+#pragma unroll
+    for (int c = 0; c < DP / 32; c++) {
+        const int d = c * 32 + sub * 4;
+        mm::f32x4 v = {0, 0, 0, 0};
+#pragma unroll
+        for (int w = 0; w < 4; w++) v += f[w] * *(const mm::f32x4 *)(sums + (w * 32 + mine) * kLine + d);
+        if (a.parts > 1) {
+#pragma unroll
+            for (int i = 0; i < 4; i++) p[d + i] = v[i];
+        } else {
+            store4<T>(y, d, a.dim, a.out_vec, v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv);
+        }
+    }
+    if (sub) return;
+    if (a.parts > 1) p[DP] = top, p[DP + 1] = sum;
+    else if (a.lse) a.lse[out.at * a.heads + out.head] = sum == 0 ? -INFINITY : (top + __log2f(sum)) * kLn2;
+}
+
+// joins the parts of 32 rows
+template <typename T, int DP> __global__ void __launch_bounds__(256) combine_kernel(Args a, int64_t tiles)
+{
+    const int hk = blockIdx.x % a.kv_heads;
+    const int64_t slot = blockIdx.x / a.kv_heads;
+    int s;
+    int64_t tile;
+    if (!find_slot(a.d_q, a.q_rows, a.packed, a.sequences, a.group, 32, tiles, slot, s, tile)) return;
+    const Sequence q = sequence_of(a, s);
+    if (tile * 32 >= (int64_t)q.lq * a.group) return;
+    const int mine = threadIdx.x >> 3, sub = threadIdx.x & 7;
+    const Row out = row_of(a, q, hk, (int)tile * 32 + mine);
+    if (!out.any) return;
+    const float *p = a.partial + ((slot * a.kv_heads + hk) * 32 + mine) * a.parts * (DP + 2);
+    float top = -INFINITY, sum = 0;
+    for (int i = 0; i < a.parts; i++) top = fmaxf(top, p[i * (DP + 2) + DP]);
+    float v[DP / 8];
+#pragma unroll
+    for (int i = 0; i < DP / 8; i++) v[i] = 0;
+#pragma unroll 2
+    for (int i = 0; i < a.parts; i++) {
+        const float *x = p + i * (DP + 2);
+        const float f = x[DP] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(x[DP] - top);
+        sum += f * x[DP + 1];
+#pragma unroll
+        for (int c = 0; c < DP / 32; c++)
+#pragma unroll
+            for (int k = 0; k < 4; k++) v[c * 4 + k] += f * x[c * 32 + sub * 4 + k];
+    }
+    const float inv = sum == 0 ? 0.0f : 1.0f / sum;
+    T *y = (T *)a.y.p + s * a.y.seq + (q.q0 + out.i) * a.y.row + out.head * a.y.head;
+#pragma unroll
+    for (int c = 0; c < DP / 32; c++)
+        store4<T>(y, c * 32 + sub * 4, a.dim, a.out_vec, v[c * 4] * inv, v[c * 4 + 1] * inv, v[c * 4 + 2] * inv, v[c * 4 + 3] * inv);
+    if (a.lse && sub == 0) a.lse[out.at * a.heads + out.head] = sum == 0 ? -INFINITY : (top + __log2f(sum)) * kLn2;
+}
+
+// ---- operands that do not lie on 16-byte boundaries ----
+__global__ void __launch_bounds__(256) copy_kernel(Copies c)
+{
+    const Copy &o = c.one[blockIdx.y];
+    const int64_t per = o.pad / 8, all = o.rows * o.heads * per;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
+        const int64_t line = i / per, row = line / o.heads, seq = row / o.per;
+        const int col = (int)(i - line * per) * 8, head = (int)(line - row * o.heads);
+        const uint16_t *from = o.src + seq * o.seq + (row - seq * o.per) * o.row + head * o.head + col;
+        s16x8 v;
+        if (col + 8 <= o.dim) {
+            __builtin_memcpy(&v, from, 16);   // at any address its values may have
+        } else {
+#pragma unroll
+            for (int k = 0; k < 8; k++) v[k] = col + k < o.dim ? (short)from[k] : (short)0;
+        }
+        *(s16x8 *)(o.dst + line * o.pad + col) = v;
+    }
+}
+
+void Copies::add(const heddle_attention_desc *d, View &v, bool keys, mm::Scratch &s)
+{
+    if (!((uintptr_t)v.p & 15) && !((v.seq | v.row | v.head | d->dim) & 7)) return;
+    const int64_t length = keys ? d->k_len : d->q_len, rows = d->packed ? length : length * d->sequences;
+    const int32_t heads = keys ? d->kv_heads : d->heads, pad = (d->dim + 7) & ~7;
+    if (rows == 0) return;
+    uint16_t *to = (uint16_t *)s.take((size_t)(rows * heads) * pad * 2);
+    one[count++] = {(const uint16_t *)v.p, to, d->packed ? 0 : v.seq, v.row, v.head, length, rows, heads, d->dim, pad};
+    v = {to, d->packed ? 0 : length * heads * pad, (int64_t)heads * pad, pad};
+}
+
+int Copies::launch(hipStream_t stream) const
+{
+    if (count == 0) return HEDDLE_OK;
+    int64_t most = 1;
+    for (int i = 0; i < count; i++) most = std::max(most, (one[i].rows * one[i].heads * (one[i].pad / 8) + 255) / 256);
+    hipLaunchKernelGGL(copy_kernel, dim3((unsigned)std::min<int64_t>(most, 4096), (unsigned)count), dim3(256), 0, stream, *this);
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess ? HEDDLE_OK : hip_fail(e, "attention's copies");
+}
+
+// ---- host ----
+bool modified(const heddle_attention_desc *d) { return d->cap > 0 || d->d_slopes; }
+
+Args base_args(const heddle_attention_desc *d)
+{
+    Args a = {};
+    auto view = [&](const void *p, const int64_t *st) { return View{p, d->packed ? 0 : st[0], st[1], st[2]}; };
+    a.q = view(d->q, d->q_strides), a.k = view(d->k, d->k_strides), a.v = view(d->v, d->v_strides), a.y = view(d->y, d->y_strides);
+    a.dy = view(d->dy, d->dy_strides), a.dq = view(d->dq, d->dq_strides), a.dk = view(d->dk, d->dk_strides), a.dv = view(d->dv, d->dv_strides);
+    a.lse = d->lse, a.d_q = d->d_q, a.d_k = d->d_k, a.d_prefix = d->d_prefix, a.d_slopes = d->d_slopes;
+    a.q_rows = d->packed ? d->q_len : d->q_len * d->sequences, a.k_rows = d->packed ? d->k_len : d->k_len * d->sequences;
+    a.sequences = d->sequences, a.q_len = (int32_t)d->q_len, a.k_len = (int32_t)d->k_len, a.packed = d->packed;
+    a.heads = d->heads, a.kv_heads = d->kv_heads, a.group = d->heads / d->kv_heads, a.dim = d->dim, a.causal = d->causal;
+    a.scale = d->scale, a.cap = d->cap;
+    a.scale2 = d->cap > 0 ? 2 * d->scale * kLog2e / d->cap : d->scale * kLog2e;
+    a.cap2 = d->cap * kLog2e;
+    return a;
+}
+
+int check(const heddle_attention_desc *d, bool backward)
+{
+    if (!d) return fail(HEDDLE_E_INVAL, "descriptor is NULL");
+    if (d->dtype != HEDDLE_T_BF16 && d->dtype != HEDDLE_T_F16) return fail(HEDDLE_E_INVAL, "dtype is neither BF16 nor F16");
+    if (d->heads < 1 || d->kv_heads < 1 || d->heads > HEDDLE_MAX_HEADS || d->heads % d->kv_heads)
+        return fail(HEDDLE_E_INVAL, "heads out of range, or not a multiple of kv_heads");
+    if (d->dim < 1 || d->dim > HEDDLE_MAX_HEAD_DIM) return fail(HEDDLE_E_INVAL, "dim out of range");
+    if (d->sequences < 0 || d->sequences > HEDDLE_MAX_GROUPS) return fail(HEDDLE_E_INVAL, "sequences out of range");
+    if (d->q_len < 0 || d->k_len < 0 || d->q_len > HEDDLE_MAX_ROWS / d->heads || d->k_len > HEDDLE_MAX_ROWS)
+        return fail(HEDDLE_E_INVAL, "q_len or k_len out of range");
+    if (!(std::isfinite(d->scale) && d->scale > 0)) return fail(HEDDLE_E_INVAL, "scale is not finite and > 0");
+    if (!(std::isfinite(d->cap) && d->cap >= 0)) return fail(HEDDLE_E_INVAL, "cap is not finite and >= 0");
+    if (d->packed && d->sequences > 0 && (!d->d_q || !d->d_k)) return fail(HEDDLE_E_INVAL, "packed sequences without offsets");
+    if (((uintptr_t)d->d_q | (uintptr_t)d->d_k | (uintptr_t)d->d_prefix | (uintptr_t)d->d_slopes | (uintptr_t)d->lse) & 3)
+        return fail(HEDDLE_E_INVAL, "d_q, d_k, d_prefix, d_slopes or lse is misaligned");
+    const int64_t n = d->packed ? 1 : d->sequences, q_all = n * d->q_len, k_all = n * d->k_len;
+    int rc = HEDDLE_OK;
+    auto tensor = [&](const char *name, const void *p, const int64_t *st, bool keys) {
+        if (rc || (keys ? k_all : q_all) == 0) return;
+        const int64_t heads = keys ? d->kv_heads : d->heads;
+        if (!p || ((uintptr_t)p & 1)) rc = fail(HEDDLE_E_INVAL, std::string(name) + " is NULL or not aligned to its values");
+        else if (st[1] < 0 || st[1] > HEDDLE_MAX_LD || st[2] < 0 || (!d->packed && st[0] < 0) || (heads > 1 && st[2] < d->dim) ||
+                 ((keys ? d->k_len : d->q_len) > 1 && st[1] < d->dim) || (!d->packed && d->sequences > 1 && st[0] < d->dim))
+            rc = fail(HEDDLE_E_INVAL, std::string(name) + ": strides out of range");
+    };
+    tensor("q", d->q, d->q_strides, false);
+    tensor("k", d->k, d->k_strides, true);
+    tensor("v", d->v, d->v_strides, true);
+    tensor("y", d->y, d->y_strides, false);
+    if (backward) {
+        tensor("dy", d->dy, d->dy_strides, false);
+        if (rc == HEDDLE_OK && !d->lse && q_all > 0) rc = fail(HEDDLE_E_INVAL, "lse is NULL");
+        if (rc == HEDDLE_OK && !d->dk != !d->dv) rc = fail(HEDDLE_E_INVAL, "dk without dv, or dv without dk");
+        if (d->dq) tensor("dq", d->dq, d->dq_strides, false);
+        if (d->dk) tensor("dk", d->dk, d->dk_strides, true);
+        if (d->dv) tensor("dv", d->dv, d->dv_strides, true);
+    }
+    return rc;
+}
+
+// A tensor as rows of all its heads, where it can be seen as such: heads side by side, sequences as rows go on. Other
+// orders of the dimensions are compared by their first value alone.
+static mm::Region region(const heddle_attention_desc *d, const char *name, const void *p, const int64_t *st, bool keys)
+{
+    const int64_t heads = keys ? d->kv_heads : d->heads, length = keys ? d->k_len : d->q_len, n = d->packed ? 1 : d->sequences;
+    mm::Region r = {name, length * n ? p : nullptr, 1, d->dim, d->dim};
+    const bool side = heads == 1 || st[2] == d->dim;
+    if (!side) return r;
+    r.cols = heads * d->dim;
+    if (n == 1 || st[0] == length * st[1]) r.rows = length * n, r.ld = length * n > 1 ? st[1] : r.cols;
+    else if (length == 1) r.rows = n, r.ld = st[0];
+    else r.rows = length, r.ld = st[1], r.groups = (int)n, r.stride = st[0];
+    return r;
+}
+
+int check_overlaps(const heddle_attention_desc *d, bool backward)
+{
+    const mm::Region q = region(d, "q", d->q, d->q_strides, false), k = region(d, "k", d->k, d->k_strides, true), v = region(d, "v", d->v, d->v_strides, true);
+    const mm::Region y = region(d, "y", d->y, d->y_strides, false);
+    const int64_t n = d->packed ? 1 : d->sequences, words = n * d->q_len * d->heads;
+    const mm::Region lse = {"lse", words ? d->lse : nullptr, 1, 2 * words, 2 * words};
+    int rc;
+    if (!backward) {
+        rc = mm::check_apart(y, {&q, &k, &v, &lse});
+        return rc ? rc : mm::check_apart(lse, {&q, &k, &v});
+    }
+    const mm::Region dy = region(d, "dy", d->dy, d->dy_strides, false), dq = region(d, "dq", d->dq, d->dq_strides, false);
+    const mm::Region dk = region(d, "dk", d->dk, d->dk_strides, true), dv = region(d, "dv", d->dv, d->dv_strides, true);
+    rc = mm::check_apart(dq, {&q, &k, &v, &y, &dy, &lse, &dk, &dv});
+    if (rc == HEDDLE_OK) rc = mm::check_apart(dk, {&q, &k, &v, &y, &dy, &lse, &dv});
+    return rc ? rc : mm::check_apart(dv, {&q, &k, &v, &y, &dy, &lse});
+}
+
+// f(type, padded head width, modified scores) as constants
+template <typename F> static int with_kind(const heddle_attention_desc *d, F f)
+{
+    auto wide = [&](auto t) {
+        typedef decltype(t) T;
+        const bool mod = modified(d);
+        if (d->dim <= 64) return mod ? f(T(), std::integral_constant<int, 64>(), std::true_type()) : f(T(), std::integral_constant<int, 64>(), std::false_type());
+        return mod ? f(T(), std::integral_constant<int, 128>(), std::true_type()) : f(T(), std::integral_constant<int, 128>(), std::false_type());
+    };
+    return d->dtype == HEDDLE_T_BF16 ? wide((__bf16)0.0f) : wide((_Float16)0.0f);
+}
+
+static int launched(const char *what)
+{
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess ? HEDDLE_OK : hip_fail(e, what);
+}
+
+static int forward(const heddle_attention_desc *d, mm::Scratch &s, bool run, hipStream_t stream)
+{
+    Args a = base_args(d);
+    if (d->sequences == 0 || a.q_rows == 0) return HEDDLE_OK;
+    Copies c;
+    c.add(d, a.q, false, s);
+    c.add(d, a.k, true, s);
+    c.add(d, a.v, true, s);
+    a.out_vec = !((uintptr_t)d->y & 7) && !((a.y.seq | a.y.row | a.y.head | d->dim) & 3);
+    // rows of a key head in a sequence, on average
+    const int64_t rows = std::max<int64_t>(1, a.q_rows * a.group / d->sequences), keys = a.k_rows / d->sequences;
+    const bool split = rows <= 64;
+    const int T = split ? 32 : 128;
+    const int64_t slots = slots_of(d->packed, d->sequences, d->q_len, d->q_len, a.group, T), tiles = (d->q_len * a.group + T - 1) / T;
+    int64_t blocks = slots * d->kv_heads;
+    a.parts = 1;
+    if (split) {
+        const int64_t used = std::max<int64_t>(1, d->sequences * ((rows + 31) / 32) * d->kv_heads);
+        a.parts = (int32_t)std::max<int64_t>(1, std::min<int64_t>({512 / used, keys / 256, 64}));
+        if (a.parts > 1) a.partial = (float *)s.take((size_t)blocks * 32 * a.parts * ((d->dim <= 64 ? 64 : 128) + 2) * 4);
+    }
+    if (blocks * a.parts > (int64_t(1) << 24) - 1) return fail(HEDDLE_E_RANGE, "more tiles than a launch holds");
+    if (!run) return HEDDLE_OK;
+    if (const int rc = c.launch(stream)) return rc;
+    return with_kind(d, [&](auto t, auto dp, auto mod) {
+        typedef decltype(t) T;
+        if (!split) {
+            hipLaunchKernelGGL((forward_kernel<T, dp, mod>), dim3((unsigned)blocks), dim3(256), 0, stream, a, tiles);
+            return launched("attention");
+        }
+        hipLaunchKernelGGL((split_kernel<T, dp, mod>), dim3((unsigned)(blocks * a.parts)), dim3(256), 0, stream, a, tiles);
+        if (a.parts > 1) hipLaunchKernelGGL((combine_kernel<T, dp>), dim3((unsigned)blocks), dim3(256), 0, stream, a, tiles);
+        return launched("attention");
+    });
+}
+
+int run_attention(const heddle_attention_desc *d, bool back, void *ws, int64_t bytes, bool run, hipStream_t stream, int64_t *need);
+int backward(const heddle_attention_desc *d, mm::Scratch &s, bool run, hipStream_t stream);
+
+int run_attention(const heddle_attention_desc *d, bool back, void *ws, int64_t bytes, bool run, hipStream_t stream, int64_t *need)
+{
+    int rc = check(d, back);
+    if (rc) return rc;
+    for (int pass = 0; pass < 2; pass++) {
+        mm::Scratch s = {pass ? (char *)ws : nullptr, 0};
+        rc = back ? backward(d, s, pass == 1, stream) : forward(d, s, pass == 1, stream);
+        if (rc) return rc;
+        if (pass == 0) {
+            if (need) *need = (int64_t)s.used;
+            if (!run) return HEDDLE_OK;
+            rc = mm::check_scratch(s.used, ws, bytes);
+            if (rc == HEDDLE_OK) rc = check_overlaps(d, back);
+            if (rc) return rc;
+        }
+    }
+    return HEDDLE_OK;
+}
+
+}  // namespace attn
+}  // namespace heddle
+
+using namespace heddle;
+
+extern "C" int heddle_attention(const heddle_attention_desc *d, void *ws, int64_t bytes, hipStream_t stream)
+{
+    return attn::run_attention(d, false, ws, bytes, true, stream, nullptr);
+}
+
+extern "C" int heddle_attention_backward(const heddle_attention_desc *d, void *ws, int64_t bytes, hipStream_t stream)
+{
+    return attn::run_attention(d, true, ws, bytes, true, stream, nullptr);
+}
+
+extern "C" int heddle_attention_workspace(const heddle_attention_desc *d, int32_t backward, int64_t *h_bytes)
+{
+    if (!h_bytes) return fail(HEDDLE_E_INVAL, "h_bytes is NULL");
+    return attn::run_attention(d, backward != 0, nullptr, 0, false, nullptr, h_bytes);
+}

@@ -30,7 +30,10 @@ EXPORTS = ["heddle_load_profile", "heddle_free_profile", "heddle_price_plans", "
            "heddle_load_cluster", "heddle_free_cluster", "heddle_fill_dp", "heddle_fill_plans",
            "heddle_linear", "heddle_linear_backward", "heddle_linear_workspace",
            "heddle_gated_ffn", "heddle_gated_ffn_backward", "heddle_gated_ffn_workspace",
-           "heddle_grad_norm", "heddle_clip_grads", "heddle_clip_grad_norm", "heddle_grad_norm_workspace"]
+           "heddle_grad_norm", "heddle_clip_grads", "heddle_clip_grad_norm", "heddle_grad_norm_workspace",
+           "heddle_attention", "heddle_attention_backward", "heddle_attention_workspace",
+           "heddle_layer_norm", "heddle_layer_norm_backward", "heddle_layer_norm_workspace",
+           "heddle_expert_balance", "heddle_expert_balance_backward", "heddle_expert_balance_workspace"]
 
 HEDDLE_T_BF16, HEDDLE_T_F16, HEDDLE_T_F32 = 0, 1, 2
 HEDDLE_A_NONE, HEDDLE_A_RELU, HEDDLE_A_GELU, HEDDLE_A_GELU_TANH, HEDDLE_A_SILU = 0, 1, 2, 3, 4
@@ -96,6 +99,33 @@ class heddle_grad_desc(C.Structure):
     _fields_ = [("g", C.c_void_p), ("out", C.c_void_p), ("n", C.c_int64), ("dtype", C.c_int32)]
 
 
+def _tensor_fields(*names):
+    return [f for n in names for f in ((n, C.c_void_p), (f"{n}_strides", C.c_int64 * 3))]
+
+
+class heddle_attention_desc(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("causal", C.c_int32), ("packed", C.c_int32), ("sequences", C.c_int32),
+                ("q_len", C.c_int64), ("k_len", C.c_int64), ("heads", C.c_int32), ("kv_heads", C.c_int32), ("dim", C.c_int32),
+                ("scale", C.c_float), ("cap", C.c_float), ("d_q", C.c_void_p), ("d_k", C.c_void_p), ("d_prefix", C.c_void_p),
+                ("d_slopes", C.c_void_p), *_tensor_fields("q", "k", "v", "y"), ("lse", C.c_void_p),
+                *_tensor_fields("dy", "dq", "dk", "dv")]
+
+
+class heddle_layer_norm_desc(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("wtype", C.c_int32), ("m", C.c_int64), ("n", C.c_int64), ("eps", C.c_float),
+                ("x", C.c_void_p), ("ldx", C.c_int64), ("w", C.c_void_p), ("bias", C.c_void_p), ("y", C.c_void_p),
+                ("ldy", C.c_int64), ("stats", C.c_void_p), ("dy", C.c_void_p), ("lddy", C.c_int64), ("residual", C.c_void_p),
+                ("ldr", C.c_int64), ("dx", C.c_void_p), ("lddx", C.c_int64), ("dw", C.c_void_p), ("db", C.c_void_p)]
+
+
+class heddle_expert_balance_desc(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("experts", C.c_int32), ("picks", C.c_int32), ("pick_bytes", C.c_int32), ("t", C.c_int64),
+                ("scale", C.c_float), ("logits", C.c_void_p), ("ldl", C.c_int64), ("d_picked", C.c_void_p), ("ldp", C.c_int64),
+                ("d_counts", C.c_void_p), ("d_rows", C.c_void_p), ("d_offsets", C.c_void_p), ("d_mean", C.c_void_p),
+                ("d_loss", C.c_void_p), ("d_dloss", C.c_void_p), ("residual", C.c_void_p), ("ldr", C.c_int64),
+                ("dlogits", C.c_void_p), ("ldd", C.c_int64)]
+
+
 _lib = None
 
 
@@ -133,6 +163,13 @@ def lib():
             for back in ("", "_backward"):
                 getattr(L, f"heddle_{op}{back}").argtypes = [P, P, I64, P]
             getattr(L, f"heddle_{op}_workspace").argtypes = [P, I32, C.POINTER(C.c_int64)]
+        for op in ("attention", "attention_backward", "layer_norm_backward", "expert_balance"):
+            getattr(L, f"heddle_{op}").argtypes = [P, P, I64, P]
+        for op in ("layer_norm", "expert_balance_backward"):
+            getattr(L, f"heddle_{op}").argtypes = [P, P]
+        for op in ("layer_norm", "expert_balance"):
+            getattr(L, f"heddle_{op}_workspace").argtypes = [P, C.POINTER(C.c_int64)]
+        L.heddle_attention_workspace.argtypes = [P, I32, C.POINTER(C.c_int64)]
         L.heddle_grad_norm.argtypes = [P, I32, P, P, I64, P]
         L.heddle_clip_grads.argtypes = [P, I32, P, C.c_float, P]
         L.heddle_clip_grad_norm.argtypes = [P, I32, C.c_float, P, P, I64, P]
@@ -738,3 +775,240 @@ def heddle_clip_grad_norm(grads, max_norm, out=None, stream=None):
     table, gpu = _grads(grads, out)
     return _norm_call(table, len(grads), gpu, stream,
                       lambda *a: lib().heddle_clip_grad_norm(table, len(grads), max_norm, *a))
+
+
+# ---- attention, layer normalisation and a router's balance ----
+
+_ATTENTION = struct.Struct("@4i2q3i2f4P" + "Pqqq" * 4 + "P" + "Pqqq" * 4)
+_LAYER_NORM = struct.Struct("@iiqqfPqPPPqPPqPqPqPP")
+_BALANCE = struct.Struct("@iiiiqfPqPqPPPPPPPqPq")
+assert (_ATTENTION.size, _LAYER_NORM.size, _BALANCE.size) == tuple(
+    C.sizeof(d) for d in (heddle_attention_desc, heddle_layer_norm_desc, heddle_expert_balance_desc))
+_NONE = (0, 0, 0, 0)
+
+
+def _heads(t, what, shape, dtype, gpu):
+    """(data pointer, strides of sequences, rows and heads) of [sequences, rows, heads, dim] or [rows, heads, dim]"""
+    if t.requires_grad:
+        _unrecorded(what)
+    if t.dtype != dtype or t.get_device() != gpu:
+        _refuse(f"{what}: {t.dtype} on {t.device}, not {dtype} on GPU {gpu}")
+    if t.shape != shape:
+        _refuse(f"{what}: shape {tuple(t.shape)}, not {tuple(shape)}")
+    st = t.stride()
+    if st[-1] != 1 and shape[-1] > 1:
+        _refuse(f"{what}: a head's values are not contiguous")
+    head = st[-2] if shape[-2] > 1 else shape[-1]
+    row = st[-3] if shape[-3] > 1 else shape[-2] * head
+    return t.data_ptr(), st[0] if len(shape) == 4 and shape[0] > 1 else shape[-3] * row, row, head
+
+
+def _ints(t, what, n, gpu, kind="torch.int32"):
+    if t is None:
+        return 0
+    if str(t.dtype) != kind or t.get_device() != gpu or t.shape != (n,) or not t.is_contiguous():
+        _refuse(f"{what}: not a contiguous {kind} vector of {n} on the inputs' GPU")
+    return t.data_ptr()
+
+
+def _attention_inputs(q, k, v, scale, causal, cap, slopes, prefix, q_lengths, k_lengths, q_offsets, k_offsets):
+    """(GPU, packed head of the descriptor, shape of q, shape of k)"""
+    packed = q_offsets is not None or k_offsets is not None
+    if q.dim() != (3 if packed else 4) or k.dim() != q.dim() or not q.is_cuda:
+        _refuse("heddle_attention: q and k are [sequences, rows, heads, dim] on the GPU, or with offsets [rows, heads, dim]")
+    gpu, dt, qs, ks = q.get_device(), q.dtype, q.shape, k.shape
+    if packed:
+        if q_offsets is None or k_offsets is None or q_lengths is not None or k_lengths is not None:
+            _refuse("heddle_attention: packed sequences have q_offsets and k_offsets, and no lengths")
+        n = q_offsets.numel() - 1
+        if n < 0:
+            _refuse("q_offsets: empty")
+        dq, dk = _ints(q_offsets, "q_offsets", n + 1, gpu), _ints(k_offsets, "k_offsets", n + 1, gpu)
+    else:
+        n = qs[0]
+        if ks[0] != n:
+            _refuse(f"k: {ks[0]} sequences, not {n}")
+        dq, dk = _ints(q_lengths, "q_lengths", n, gpu), _ints(k_lengths, "k_lengths", n, gpu)
+    if ks[-1] != qs[-1]:
+        _refuse(f"k: heads of {ks[-1]} values, not {qs[-1]}")
+    if slopes is not None and slopes.requires_grad:
+        _unrecorded("slopes")
+    head = (_dtype(q, "q"), 1 if causal else 0, 1 if packed else 0, n, qs[-3], ks[-3], qs[-2], ks[-2], qs[-1],
+            qs[-1] ** -0.5 if scale is None else scale, cap, dq, dk, _ints(prefix, "prefix", n, gpu),
+            _ints(slopes, "slopes", qs[-2], gpu, "torch.float32"),
+            *_heads(q, "q", qs, dt, gpu), *_heads(k, "k", ks, dt, gpu), *_heads(v, "v", ks, dt, gpu))
+    return gpu, dt, head, qs, ks
+
+
+def _lse(lse, qs, gpu):
+    if str(lse.dtype) != "torch.float32" or lse.get_device() != gpu or lse.shape != qs[:-1] or not lse.is_contiguous():
+        _refuse(f"lse: not a contiguous float32 tensor of shape {tuple(qs[:-1])} on GPU {gpu}")
+    return lse.data_ptr()
+
+
+def heddle_attention(q, k, v, scale=None, causal=False, cap=0.0, slopes=None, prefix=None, q_lengths=None, k_lengths=None,
+                     q_offsets=None, k_offsets=None, lse=None, out=None, stream=None):
+    """softmax(mask(s)) @ v by heads. q: [sequences, rows, heads, dim]; k, v:
+    [sequences, rows, kv_heads, dim], heads a multiple of kv_heads; int32 q_lengths
+    and k_lengths [sequences] where rows are not all used (a cache). Or
+    documents in one run of rows: [rows, heads, dim] with int32 q_offsets and
+    k_offsets [sequences + 1]. Tensors may have any strides with a head's
+    values side by side.
+
+    s = scale q k (scale: dim ** -0.5), cap * tanh(s / cap) with a cap, minus
+    slopes[head] * distance (float32 [heads]). causal: a query sees the keys up to
+    its own place, the last query standing at the last key, and the first
+    prefix[sequence] keys (int32). lse: float32, q's shape without dim, to keep
+    for the backward pass. Returns out (q's shape); rows past the lengths, or in
+    no document, are left as they were."""
+    gpu, dt, head, qs, ks = _attention_inputs(q, k, v, scale, causal, cap, slopes, prefix, q_lengths, k_lengths, q_offsets,
+                                              k_offsets)
+    if out is None:
+        out = _fresh(q, qs, stream)
+    L = lib()
+    _run(L.heddle_attention, L.heddle_attention_workspace,
+         _ATTENTION.pack(*head, *_heads(out, "out", qs, dt, gpu), 0 if lse is None else _lse(lse, qs, gpu), *_NONE * 4),
+         0, q, gpu, stream)
+    return out
+
+
+def heddle_attention_backward(dy, q, k, v, y, lse, scale=None, causal=False, cap=0.0, slopes=None, prefix=None,
+                              q_lengths=None, k_lengths=None, q_offsets=None, k_offsets=None, want_dq=True, want_dkv=True,
+                              dq=None, dk=None, dv=None, stream=None):
+    """Gradients of heddle_attention: a dict with dq, dk and dv (those wanted;
+    given tensors are written, dk and dv together). y, lse: what
+    heddle_attention returned and kept. Rows past the lengths, or in no
+    document, are left as they were."""
+    gpu, dt, head, qs, ks = _attention_inputs(q, k, v, scale, causal, cap, slopes, prefix, q_lengths, k_lengths, q_offsets,
+                                              k_offsets)
+    if lse is None or y is None:
+        _refuse("heddle_attention_backward: y and lse are what heddle_attention returned and kept")
+    out, at = {}, {"dq": _NONE, "dk": _NONE, "dv": _NONE}
+    want_dkv = want_dkv or dk is not None or dv is not None
+    for name, t, shape, like, want in (("dq", dq, qs, q, want_dq or dq is not None), ("dk", dk, ks, k, want_dkv),
+                                       ("dv", dv, ks, k, want_dkv)):
+        if want:
+            out[name] = _fresh(like, shape, stream) if t is None else t
+            at[name] = _heads(out[name], name, shape, dt, gpu)
+    L = lib()
+    _run(L.heddle_attention_backward, L.heddle_attention_workspace,
+         _ATTENTION.pack(*head, *_heads(y, "y", qs, dt, gpu), _lse(lse, qs, gpu), *_heads(dy, "dy", qs, dt, gpu), *at["dq"],
+                         *at["dk"], *at["dv"]), 1, q, gpu, stream)
+    return out
+
+
+def _norm_weights(ts, n, x, gpu):
+    """(type code, addresses) of vectors of n, all of x's type or all float32"""
+    import torch
+    given = [t for _, t in ts if t is not None]
+    wt = given[0].dtype if given else x.dtype
+    if wt != x.dtype and wt != torch.float32:
+        _refuse(f"{next(w for w, t in ts if t is not None)}: {wt}, neither {x.dtype} nor torch.float32")
+    return _dtype_codes().get(wt, -1), [0 if t is None else _vector(t, w, (n,), wt, gpu) for w, t in ts], wt
+
+
+def _norm_rows(x, what):
+    if x.dim() != 2 or not x.is_cuda:
+        _refuse(f"{what}: rows must be a matrix on the GPU")
+    return x.get_device(), x.dtype, x.shape[0], x.shape[1]
+
+
+def _stats(stats, m, gpu):
+    if str(stats.dtype) != "torch.float32" or stats.get_device() != gpu or stats.shape != (m, 2) or not stats.is_contiguous():
+        _refuse(f"stats: not a contiguous float32 tensor of shape {(m, 2)} on GPU {gpu}")
+    return stats.data_ptr()
+
+
+def heddle_layer_norm(x, w=None, bias=None, eps=1e-5, stats=None, out=None, stream=None):
+    """(x - mean) / sqrt(variance + eps) * w + bias by rows. x: [m, n], bfloat16,
+    float16 or float32; w, bias: [n], of x's type or float32; stats: float32
+    [m, 2] to keep for the backward pass. Returns out ([m, n]; may be x)."""
+    gpu, dt, m, n = _norm_rows(x, "heddle_layer_norm")
+    if out is None:
+        out = _fresh(x, (m, n), stream)
+    wt, (pw, pb), _ = _norm_weights((("w", w), ("bias", bias)), n, x, gpu)
+    desc = _LAYER_NORM.pack(_dtype(x, "x"), wt, m, n, eps, *_matrix(x, "x", (m, n), dt, gpu), pw, pb,
+                            *_matrix(out, "out", (m, n), dt, gpu), 0 if stats is None else _stats(stats, m, gpu),
+                            0, 0, 0, 0, 0, 0, 0, 0)
+    L = lib()
+    _on_gpu(gpu, stream, lambda handle: L.heddle_layer_norm(desc, handle))
+    return out
+
+
+def heddle_layer_norm_backward(dy, x, w, stats, residual=None, want_dx=True, want_dw=True, want_db=False, dx=None, dw=None,
+                               db=None, stream=None):
+    """Gradients of heddle_layer_norm: a dict with dx, dw and db (those wanted;
+    given tensors are written; dw and db have w's type). stats: what
+    heddle_layer_norm kept. residual: [m, n] added to dx, the gradient that
+    reaches x past the layer. dx may be dy or residual."""
+    gpu, dt, m, n = _norm_rows(x, "heddle_layer_norm_backward")
+    if stats is None:
+        _refuse("stats: what heddle_layer_norm kept")
+    out, pdx = {}, (0, 0)
+    if want_dx or dx is not None:
+        out["dx"] = _fresh(x, (m, n), stream) if dx is None else dx
+        pdx = _matrix(out["dx"], "dx", (m, n), dt, gpu)
+    like = next((t for t in (w, dw, db) if t is not None), x)
+    if want_dw or dw is not None:
+        out["dw"] = _fresh(like, (n,), stream) if dw is None else dw
+    if want_db or db is not None:
+        out["db"] = _fresh(like, (n,), stream) if db is None else db
+    wt, (pw, pdw, pdb), _ = _norm_weights((("w", w), ("dw", out.get("dw")), ("db", out.get("db"))), n, x, gpu)
+    pr = (0, 0) if residual is None else _matrix(residual, "residual", (m, n), dt, gpu)
+    desc = _LAYER_NORM.pack(_dtype(x, "x"), wt, m, n, 0.0, *_matrix(x, "x", (m, n), dt, gpu), pw, 0, 0, 0,
+                            _stats(stats, m, gpu), *_matrix(dy, "dy", (m, n), dt, gpu), *pr, *pdx, pdw, pdb)
+    L = lib()
+    _run(L.heddle_layer_norm_backward, lambda d, _, n: L.heddle_layer_norm_workspace(d, n), desc, 1, x, gpu, stream)
+    return out
+
+
+def _balance_inputs(logits, picked, what):
+    if logits.dim() != 2 or picked.dim() != 2 or not logits.is_cuda:
+        _refuse(f"{what}: logits and picks must be matrices on the GPU")
+    gpu, (t, e) = logits.get_device(), logits.shape
+    size = {"torch.int32": 4, "torch.int64": 8}.get(str(picked.dtype))
+    if size is None:
+        _refuse(f"picked: {picked.dtype}, neither torch.int32 nor torch.int64")
+    k = picked.shape[1]
+    return (gpu, t, e, k, size, *_matrix(logits, "logits", (t, e), logits.dtype, gpu),
+            *_matrix(picked, "picked", (t, k), picked.dtype, gpu))
+
+
+def heddle_expert_balance(logits, picked, scale=1.0, stream=None):
+    """How a router's picks spread over the experts, and the loss
+    scale * experts * sum(counts / picks * mean probability). logits:
+    [tokens, experts], bfloat16, float16 or float32; picked: [tokens, k] int32 or
+    int64; a pick outside 0 .. experts - 1 counts nowhere, a token of nothing else
+    is padding. Returns a dict: counts (int32 [experts]), offsets (int32
+    [experts + 1], as the grouped products read them), rows (int32 [1]: tokens
+    with a pick), mean (float32 [experts]) and loss (float32 [1])."""
+    import torch
+    gpu, t, e, k, size, pl, ldl, pp, ldp = _balance_inputs(logits, picked, "heddle_expert_balance")
+    counts, offsets, rows, mean, loss = _on_stream(stream, lambda: (
+        *(torch.empty(n, dtype=torch.int32, device=logits.device) for n in (e, e + 1, 1)),
+        *(torch.empty(n, dtype=torch.float32, device=logits.device) for n in (e, 1))))
+    desc = _BALANCE.pack(_dtype(logits, "logits"), e, k, size, t, scale, pl, ldl, pp, ldp, counts.data_ptr(), rows.data_ptr(),
+                         offsets.data_ptr(), mean.data_ptr(), loss.data_ptr(), 0, 0, 0, 0, 0)
+    L = lib()
+    _run(L.heddle_expert_balance, lambda d, _, n: L.heddle_expert_balance_workspace(d, n), desc, 0, logits, gpu, stream)
+    return {"counts": counts, "offsets": offsets, "rows": rows, "mean": mean, "loss": loss}
+
+
+def heddle_expert_balance_backward(logits, picked, counts, rows, dloss=None, scale=1.0, residual=None, out=None, stream=None):
+    """Gradient of heddle_expert_balance's loss by the logits, plus residual
+    ([tokens, experts], what reaches the logits by other ways). counts, rows:
+    what heddle_expert_balance returned, or their sums over ranks; dloss: float32
+    of one value, 1 without. Returns out ([tokens, experts]; may be logits or
+    residual)."""
+    gpu, t, e, k, size, pl, ldl, pp, ldp = _balance_inputs(logits, picked, "heddle_expert_balance_backward")
+    if out is None:
+        out = _fresh(logits, (t, e), stream)
+    pr = (0, 0) if residual is None else _matrix(residual, "residual", (t, e), logits.dtype, gpu)
+    if dloss is not None and (dloss.numel() != 1 or str(dloss.dtype) != "torch.float32" or dloss.get_device() != gpu):
+        _refuse("dloss: not one float32 value on the logits' GPU")
+    desc = _BALANCE.pack(_dtype(logits, "logits"), e, k, size, t, scale, pl, ldl, pp, ldp, _ints(counts, "counts", e, gpu),
+                         _ints(rows, "rows", 1, gpu), 0, 0, 0, 0 if dloss is None else dloss.data_ptr(), *pr,
+                         *_matrix(out, "out", (t, e), logits.dtype, gpu))
+    L = lib()
+    _on_gpu(gpu, stream, lambda handle: L.heddle_expert_balance_backward(desc, handle))
+    return out
