@@ -8,17 +8,41 @@
 // the lanes hold them: 4 h + 0..3, 8 + 4 h + 0..3 for a lane of half h. The transposing LDS read
 // brings the other operand (V^T, K^T, Q^T, dY^T) in that order.
 //
-// Tiles lie in LDS as [row][DP] of 16-bit values, DP = 64 or 128, the 16-byte pieces of a row
-// exchanged by 4 bits of the row (3 and its parity for DP = 64): 16 lanes that read the same
-// piece of 16 rows, and 32 lanes of a transposing read (4 rows, 64 bytes), touch every bank once.
-// They are filled straight from global memory through a buffer resource; rows past a sequence's
-// end and columns past the head's width arrive as zeros.
+// Tiles lie in LDS by blocks of 16 rows, in a block by 16-byte pieces of the rows: piece p of row r at
+// 256 p + 16 (r ^ 4 (p % 4)) bytes. 16 lanes that read the same piece of 16 rows, and 32 lanes of a transposing
+// read (4 rows, 64 bytes of each), touch every bank once, and all of a lane's addresses are two
+// registers plus constants (with the pieces of a row side by side, exchanged by bits of the row, a sixth of the
+// forward pass's vector instructions formed addresses).
+// They are filled straight from global memory through a buffer resource, 64 bytes of 16 rows an instruction; rows
+// past a sequence's end and columns past the head's width arrive as zeros.
 #pragma once
+
+#include <utility>
 
 #include "linear.h"
 
 namespace heddle {
 namespace attn {
+
+// a call would pass the sums through memory
+#define HEDDLE_INLINE __device__ __attribute__((always_inline)) inline
+
+// f(0) .. f(N - 1), each index a constant from the start: vectors that are passed by reference and indexed
+// in loops stayed in memory where many of them were unrolled late
+template <typename F, int... I> HEDDLE_INLINE void each_of(F f, std::integer_sequence<int, I...>) { (f(I), ...); }
+template <int N, typename F> HEDDLE_INLINE void each(F f) { each_of(f, std::make_integer_sequence<int, N>()); }
+
+// A value that is formed here, between the products before and after, and not where it is used: the compiler would
+// gather what the vector units can do beside products behind them.
+template <typename V> HEDDLE_INLINE void here(V &v)
+{
+#ifdef __HIP_DEVICE_COMPILE__
+    asm volatile("" : "+v"(v));
+#endif
+}
+template <typename T> struct Pair;
+template <> struct Pair<__bf16> { typedef __bf16 type __attribute__((ext_vector_type(2))); };
+template <> struct Pair<_Float16> { typedef _Float16 type __attribute__((ext_vector_type(2))); };
 
 using mm::i32x4;
 using mm::s16x4;
@@ -49,7 +73,7 @@ struct Args {
     int32_t heads, kv_heads, group, dim;
     int32_t causal, parts;
     int32_t q_vec, out_vec, grads;            // 16-byte rows of q, k, v (dy); 8-byte rows of outputs; which gradients
-    float scale, scale2, cap, cap2;           // scale2 = scale log2(e); with a cap: 2 scale log2(e) / cap and cap log2(e)
+    float scale, scale2, cap, cap2, unscale;  // scale2 = scale log2(e); with a cap: 2 scale log2(e) / cap and cap log2(e); -1 / scale2
 };
 
 // A sequence's rows: first row of its queries and of its keys, counted over all sequences where packed, else in the sequence.
@@ -86,7 +110,7 @@ __device__ inline bool find_slot(const int32_t *offsets, int64_t rows, int packe
                                  int &s, int64_t &tile)
 {
     if (!packed) {
-        s = (int)(slot / tiles);
+        s = (int)((uint32_t)slot / (uint32_t)tiles);        // (slots of a launch stay below 2^24)
         tile = slot - s * tiles;
         return s < sequences;
     }
@@ -111,23 +135,17 @@ inline int64_t slots_of(int packed, int64_t sequences, int64_t rows, int64_t len
 }
 
 // ---- tiles in LDS ----
-template <int DP> __device__ inline int swz(int row)
-{
-    return DP == 128 ? (row & 3) << 2 | (row >> 2 & 3) : (row >> 1 & 1) << 2 | (row >> 2 & 3);
-}
-
 constexpr int kNowhere = -16;                 // past any buffer's end: arrives as zeros
 
 // ROWS x DP values by NW wavefronts, 1 KB of LDS an instruction
 template <int DP, int ROWS, int NW> struct Tile {
-    static constexpr int kRowBytes = DP * 2, kBytes = ROWS * kRowBytes, kPer = 1024 / kRowBytes;   // rows of an instruction
-    static constexpr int kLoads = ROWS / (kPer * NW);
-    static_assert(kLoads * kPer * NW == ROWS, "whole instructions");
+    static constexpr int kBytes = ROWS * DP * 2, kLoads = kBytes / (1024 * NW), kGroups = DP / 32;   // groups of four pieces in a row
+    static_assert(kLoads * NW * 1024 == kBytes && ROWS % 16 == 0, "whole instructions");
     // byte offset of a lane's piece of instruction i, from the tile's first row; valid: rows that the sequence has from there
     static __device__ inline int offset(int i, int wave, int64_t ld, int dim, int valid)
     {
-        const int lane = threadIdx.x & 63, row = (i * NW + wave) * kPer + lane / (DP / 8);
-        const int col = ((lane % (DP / 8)) ^ swz<DP>(row)) * 8;
+        const int lane = threadIdx.x & 63, block = i * NW + wave, p = lane >> 4;
+        const int row = block / kGroups * 16 + ((lane & 15) ^ p << 2), col = (block % kGroups * 4 + p) * 8;
         return row < valid && col < dim ? (int)(row * ld * 2) + col * 2 : kNowhere;
     }
 };
@@ -139,21 +157,32 @@ __device__ inline i32x4 buffer_at(const void *p)
     return i32x4{__builtin_amdgcn_readfirstlane((int)v), __builtin_amdgcn_readfirstlane((int)(v >> 32) & 0xffff), 0x7fffffff, 0x00020000};
 }
 
-// 16 bytes of columns 16 step + 8 h of row `row`
-template <int DP, typename T> __device__ inline typename mm::pack8<T>::type row_fragment(const char *tile, int row, int step, int h)
+// A lane's places in a tile (bytes): for reads of its row lane % 32, even and odd steps; for transposing reads.
+struct Places {
+    int row[2], column[2];
+    template <int DP> __device__ inline void set()
+    {
+        const int lane = threadIdx.x & 63, h = lane >> 5, r = lane & 31, i = lane & 15, p = (lane >> 4 & 1) * 2 + (i >> 1 & 1);
+        for (int k = 0; k < 2; k++) {
+            row[k] = r / 16 * (DP * 32) + h * 256 + ((r & 15) ^ (2 * k + h) << 2) * 16;
+            column[k] = p * 256 + ((4 * h + 8 * k + (i >> 2)) ^ p << 2) * 16 + (i & 1) * 8;
+        }
+    }
+};
+
+// 16 bytes of columns 16 step + 8 h of row from + lane % 32; from a multiple of 32
+template <int DP, typename T> HEDDLE_INLINE typename mm::pack8<T>::type row_fragment(const char *tile, const Places &at, int from, int step)
 {
-    return *(const typename mm::pack8<T>::type *)(tile + row * (DP * 2) + (((step * 2 + h) ^ swz<DP>(row)) << 4));
+    return *(const typename mm::pack8<T>::type *)(tile + at.row[step & 1] + (from / 16 * (DP * 32) + step * 512));
 }
 
 // Column 32 dt + lane % 32 of rows base + 4 h + 0..3 and base + 8 + 4 h + 0..3; base a multiple of 16.
-template <int DP, typename T> __device__ inline typename mm::pack8<T>::type column_fragment(const char *tile, int base, int dt)
+template <int DP, typename T> HEDDLE_INLINE typename mm::pack8<T>::type column_fragment(const char *tile, const Places &at, int base, int dt)
 {
 #ifdef __HIP_DEVICE_COMPILE__
-    const int lane = threadIdx.x & 63, i = lane & 15, h = lane >> 5;
-    const int row = base + 4 * h + (i >> 2), piece = dt * 4 + (lane >> 4 & 1) * 2 + (i >> 1 & 1);
     typedef __attribute__((address_space(3))) s16x4 *rd;
-    const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((rd)(tile + row * (DP * 2) + ((piece ^ swz<DP>(row)) << 4) + (i & 1) * 8));
-    const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((rd)(tile + (row + 8) * (DP * 2) + ((piece ^ swz<DP>(row + 8)) << 4) + (i & 1) * 8));
+    const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((rd)(tile + at.column[0] + (base / 16 * (DP * 32) + dt * 1024)));
+    const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((rd)(tile + at.column[1] + (base / 16 * (DP * 32) + dt * 1024)));
     return __builtin_bit_cast(typename mm::pack8<T>::type, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
 #else
     return {};
@@ -181,35 +210,132 @@ template <typename T> __device__ inline typename mm::pack8<T>::type pack(const f
 __device__ inline int mfma_row(int r, int h) { return 8 * (r >> 2) + 4 * h + (r & 3); }
 
 __device__ inline float other_half(float v) { return __shfl_xor(v, 32); }
-
-// tanh(u / 2) for u log2(e) = z: 1 - 2 / (1 + e^u); the ends are exact
-__device__ inline float tanh_half(float z) { return 1.0f - 2.0f * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z)); }
-
-// Scores times log2(e), capped and biased; pos: the row's place among the keys, j: the key of register 0.
-// MOD: a cap or slopes. t receives the tanh where a cap is given.
-template <bool MOD> __device__ inline void modify(const Args &a, f32x16 &s, float slope2, int distance, f32x16 *t)
+// the greater of a lane's value and the other half's
+__device__ inline float max_halves(float v)
 {
-    if constexpr (!MOD) {
+#ifdef __HIP_DEVICE_COMPILE__
+    // (written out: of the builtin's two results with one operand twice the compiler keeps one)
+    float a = v, b = v;
+    asm("s_nop 1\n\tv_permlane32_swap_b32 %0, %1" : "+v"(a), "+v"(b));
+    return fmaxf(a, b);
+#else
+    return v;
+#endif
+}
+
+// What is done to the scores, fixed for a kernel: a test in the loop would keep its products and exponentials apart.
+enum Mode { kPlain = 0, kCap = 1, kSlopes = 2 };
+
+// Scores in the units of the running maximum, which unit_of() turns into powers of two. With a cap:
+// -1 / (1 + e^u), u = 2 scale q k / cap, as tanh(u / 2) = 1 - 2 / (1 + e^u) and a row's constants
+// cancel (offset_of() has them for lse). slope: in these units. distance: from register 0's key to the row's place.
+template <int MODE> HEDDLE_INLINE float unit_of(const Args &a) { return MODE & kCap ? 2 * a.cap2 : a.scale2; }
+template <int MODE> HEDDLE_INLINE float offset_of(const Args &a) { return MODE & kCap ? a.cap2 : 0.0f; }
+template <int MODE> HEDDLE_INLINE float slope_of(const Args &a, int head) { return MODE & kSlopes ? a.d_slopes[head] * kLog2e / unit_of<MODE>(a) : 0.0f; }
+template <int MODE> HEDDLE_INLINE float modify(const Args &a, float s, int r, float slope, float distance)
+{
+    if constexpr (MODE & kCap) s = __builtin_amdgcn_rcpf(-1.0f - __builtin_amdgcn_exp2f(s * a.scale2));
+    if constexpr (MODE & kSlopes) s = __builtin_fmaf(-slope, fabsf(distance - (float)(8 * (r >> 2) + (r & 3))), s);
+    return s;
+}
+
+// ---- the forward pass's steps ----
+// A lane's query row and what it sees: keys 0 .. limit - 1.
+struct Row {
+    int64_t at;                               // counted over all rows of q
+    int32_t i, head, limit, pos;
+    bool any;
+};
+__device__ inline Row row_of(const Args &a, const Sequence &q, int hk, int r)
+{
+    Row x;
+    x.any = r < q.lq * a.group;
+    x.i = r / a.group;
+    x.head = hk * a.group + (r - x.i * a.group);
+    x.at = (a.packed ? q.q0 : (int64_t)q.s * a.q_len) + x.i;
+    x.pos = x.i + (q.lk - q.lq);
+    x.limit = x.any ? max(min(q.lk, a.causal ? max(x.pos + 1, q.prefix) : q.lk), 0) : 0;
+    return x;
+}
+__device__ inline int limit_of(const Args &a, const Sequence &q, int r)
+{
+    if (r >= q.lq * a.group) return 0;
+    const int pos = r / a.group + (q.lk - q.lq);
+    return __builtin_amdgcn_readfirstlane(max(min(q.lk, a.causal ? max(pos + 1, q.prefix) : q.lk), 0));
+}
+
+// The running state of 32 rows: m in modify()'s units.
+template <int DP> struct State {
+    f32x16 o[DP / 32];
+    float m, l;
+    __device__ inline void init()
+    {
+        m = -INFINITY, l = 0;
 #pragma unroll
-        for (int r = 0; r < 16; r++) s[r] *= a.scale2;
-        return;
+        for (int d = 0; d < DP / 32; d++) o[d] = f32x16{};
     }
-    if (a.cap > 0) {
+};
+
+// a tile's 32 keys from row `from` on against the query rows
+template <typename T, int DP> HEDDLE_INLINE f32x16 score(const char *tk, const Places &at, int from, const typename mm::pack8<T>::type *q)
+{
+    f32x16 s = {};
 #pragma unroll
-        for (int r = 0; r < 16; r++) {
-            const float u = tanh_half(s[r] * a.scale2);
-            if (t) (*t)[r] = u;
-            s[r] = a.cap2 * u;
-        }
-    } else {
+    for (int k = 0; k < DP / 16; k++) s = mfma(row_fragment<DP, T>(tk, at, from, k), q[k], s);
+    return s;
+}
+
+// Probabilities of 32 keys, key `first` the lane's register 0. The maximum follows only when it is 2^8 behind: p then
+// stays below 2^8, and the sums are scaled again seldom; true: they have to be, from the maximum `was` on, before p is added.
+template <typename T, int MODE, bool MASKED>
+HEDDLE_INLINE bool soften(const Args &a, f32x16 &s, float &m, float &was, float &sum, int first, const Row &row, float slope, typename mm::pack8<T>::type p[2])
+{
+    each<16>([&](int r) { s[r] = modify<MODE>(a, s[r], r, slope, (float)(row.pos - first)); });
+    if constexpr (MASKED) each<16>([&](int r) { s[r] = first + mfma_row(r, 0) >= row.limit ? -INFINITY : s[r]; });
+    float top = s[0];
+    each<15>([&](int r) { top = fmaxf(top, s[r + 1]); });
+    top = max_halves(top);
+    const float unit = unit_of<MODE>(a);
+    const bool follow = __any((top - m) * unit > 8.0f);     // (NaN where both are -infinity)
+    was = m;
+    m = follow ? fmaxf(m, top) : m;
+    here(m);
+    const float base = m == -INFINITY ? 0.0f : m * unit;
+    sum = 0;
+    each<16>([&](int r) {
+        s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], unit, -base));
+        sum += s[r];
+    });
+    p[0] = pack<T>(s, 0), p[1] = pack<T>(s, 8);
+    return follow;
+}
+
+template <int MODE, int DP> HEDDLE_INLINE void rescale(const Args &a, State<DP> &st, float was)
+{
+    const float f = st.m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((was - st.m) * unit_of<MODE>(a));
+    st.l *= f;
 #pragma unroll
-        for (int r = 0; r < 16; r++) s[r] *= a.scale2;
-    }
-    if (a.d_slopes) {
-        const float at = (float)distance;
+    for (int d = 0; d < DP / 32; d++)
 #pragma unroll
-        for (int r = 0; r < 16; r++) s[r] -= slope2 * fabsf(at - (float)(8 * (r >> 2) + (r & 3)));
-    }
+        for (int r = 0; r < 16; r++) st.o[d][r] *= f;
+}
+
+// adds the products of 32 probabilities with a tile's values from row `from` on
+template <typename T, int DP> HEDDLE_INLINE void collect(State<DP> &st, const char *tv, const Places &at, int from, const typename mm::pack8<T>::type p[2])
+{
+#pragma unroll
+    for (int k = 0; k < 2; k++)
+#pragma unroll
+        for (int d = 0; d < DP / 32; d++) st.o[d] = mfma(column_fragment<DP, T>(tv, at, from + 16 * k, d), p[k], st.o[d]);
+}
+
+// a lane's query row as the products' operand
+template <typename T, int DP> HEDDLE_INLINE void load_query(const Args &a, const View &v, const Sequence &q, const Row &row, typename mm::pack8<T>::type *f)
+{
+    const int h = (threadIdx.x & 63) >> 5;
+    const T *p = (const T *)v.p + q.s * v.seq + (q.q0 + row.i) * v.row + row.head * v.head;
+#pragma unroll
+    for (int k = 0; k < DP / 16; k++) f[k] = global_fragment<T>(p, k * 16 + 8 * h, a.dim, row.any);
 }
 
 // four neighbouring values of an output row
@@ -228,7 +354,26 @@ template <typename T> __device__ inline void store4(T *p, int col, int dim, int 
 int check(const heddle_attention_desc *d, bool backward);
 int check_overlaps(const heddle_attention_desc *d, bool backward);
 Args base_args(const heddle_attention_desc *d);
-bool modified(const heddle_attention_desc *d);
+int mode_of(const heddle_attention_desc *d);
+// the launches; mode: of enum Mode
+void launch_forward(const heddle_attention_desc *d, const Args &a, int rows, int64_t blocks, int64_t tiles, hipStream_t stream);
+void launch_rows(const heddle_attention_desc *d, const Args &a, int64_t blocks, int64_t tiles, hipStream_t stream);
+void launch_keys(const heddle_attention_desc *d, const Args &a, int64_t blocks, int64_t tiles, hipStream_t stream);
+
+// f(type, padded head width, mode) as constants
+template <typename F> void with_kind(const heddle_attention_desc *d, F f)
+{
+    auto mode = [&](auto t, auto dp) {
+        switch (mode_of(d)) {
+        case kPlain: return f(t, dp, std::integral_constant<int, kPlain>());
+        case kCap: return f(t, dp, std::integral_constant<int, kCap>());
+        case kSlopes: return f(t, dp, std::integral_constant<int, kSlopes>());
+        default: return f(t, dp, std::integral_constant<int, kCap | kSlopes>());
+        }
+    };
+    auto wide = [&](auto t) { return d->dim <= 64 ? mode(t, std::integral_constant<int, 64>()) : mode(t, std::integral_constant<int, 128>()); };
+    d->dtype == HEDDLE_T_BF16 ? wide((__bf16)0.0f) : wide((_Float16)0.0f);
+}
 
 // operands that do not lie on 16-byte boundaries are copied to scratch
 struct Copy {

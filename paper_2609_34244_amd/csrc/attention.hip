@@ -15,199 +15,18 @@
 namespace heddle {
 namespace attn {
 
-// A lane's query row and what it sees: keys 0 .. limit - 1.
-struct Row {
-    int64_t at;                               // counted over all rows of q
-    int32_t i, head, limit, pos;
-    bool any;
-};
-__device__ inline Row row_of(const Args &a, const Sequence &q, int hk, int r)
-{
-    Row x;
-    x.any = r < q.lq * a.group;
-    x.i = r / a.group;
-    x.head = hk * a.group + (r - x.i * a.group);
-    x.at = (a.packed ? q.q0 : (int64_t)q.s * a.q_len) + x.i;
-    x.pos = x.i + (q.lk - q.lq);
-    x.limit = x.any ? max(min(q.lk, a.causal ? max(x.pos + 1, q.prefix) : q.lk), 0) : 0;
-    return x;
-}
-__device__ inline int limit_of(const Args &a, const Sequence &q, int r)
-{
-    if (r >= q.lq * a.group) return 0;
-    const int pos = r / a.group + (q.lk - q.lq);
-    return __builtin_amdgcn_readfirstlane(max(min(q.lk, a.causal ? max(pos + 1, q.prefix) : q.lk), 0));
-}
-
-// The running state of 32 rows: m in the scores' units (with a cap or slopes: times log2(e)).
-template <int DP> struct State {
-    f32x16 o[DP / 32];
-    float m, l;
-    __device__ inline void init()
-    {
-        m = -INFINITY, l = 0;
-#pragma unroll
-        for (int d = 0; d < DP / 32; d++) o[d] = f32x16{};
-    }
-};
-
-// Scores of C x 32 keys from key j0 on (of this lane's half), their probabilities and the products with the values.
-// The maximum follows only when it is 2^8 behind: p then stays below 2^8, and the sums are scaled again seldom.
-template <typename T, int DP, int C, bool MOD>
-__device__ inline void attend(const Args &a, State<DP> &st, const typename mm::pack8<T>::type *q, const char *tk, const char *tv, int j0, const Row &row,
-                              float slope2, bool masked)
-{
-    const int lane = threadIdx.x & 63, h = lane >> 5, col = lane & 31;
-    f32x16 s[C];
-#pragma unroll
-    for (int c = 0; c < C; c++) {
-        s[c] = f32x16{};
-#pragma unroll
-        for (int k = 0; k < DP / 16; k++) s[c] = mfma(row_fragment<DP, T>(tk, c * 32 + col, k, h), q[k], s[c]);
-    }
-    const int first = j0 + 4 * h;             // key of register 0 of s[0]
-    if constexpr (MOD) {
-#pragma unroll
-        for (int c = 0; c < C; c++) modify<true>(a, s[c], slope2, row.pos - first - c * 32, nullptr);
-    }
-    if (masked) {
-#pragma unroll
-        for (int c = 0; c < C; c++)
-#pragma unroll
-            for (int r = 0; r < 16; r++)
-                if (first + c * 32 + mfma_row(r, 0) >= row.limit) s[c][r] = -INFINITY;
-    }
-    float top = s[0][0];
-#pragma unroll
-    for (int c = 0; c < C; c++)
-#pragma unroll
-        for (int r = 0; r < 16; r++) top = fmaxf(top, s[c][r]);
-    top = fmaxf(top, other_half(top));
-    const float unit = MOD ? 1.0f : a.scale2;
-    if (__any(top * unit > st.m * unit + 8.0f)) {
-        const float m = fmaxf(st.m, top), f = m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((st.m - m) * unit);
-        st.m = m;
-        st.l *= f;
-#pragma unroll
-        for (int d = 0; d < DP / 32; d++)
-#pragma unroll
-            for (int r = 0; r < 16; r++) st.o[d][r] *= f;
-    }
-    const float base = st.m == -INFINITY ? 0.0f : st.m * unit;
-    float sum = 0;
-#pragma unroll
-    for (int c = 0; c < C; c++)
-#pragma unroll
-        for (int r = 0; r < 16; r++) {
-            s[c][r] = __builtin_amdgcn_exp2f(MOD ? s[c][r] - base : __builtin_fmaf(s[c][r], unit, -base));
-            sum += s[c][r];
-        }
-    st.l += sum;
-#pragma unroll
-    for (int c = 0; c < C; c++)
-#pragma unroll
-        for (int k = 0; k < 2; k++) {
-            const auto p = pack<T>(s[c], 8 * k);
-#pragma unroll
-            for (int d = 0; d < DP / 32; d++) st.o[d] = mfma(column_fragment<DP, T>(tv, c * 32 + 16 * k, d), p, st.o[d]);
-        }
-}
-
-// a lane's query row as the products' operand
-template <typename T, int DP> __device__ inline void load_query(const Args &a, const View &v, const Sequence &q, const Row &row, typename mm::pack8<T>::type *f)
-{
-    const int h = (threadIdx.x & 63) >> 5;
-    const T *p = (const T *)v.p + q.s * v.seq + (q.q0 + row.i) * v.row + row.head * v.head;
-#pragma unroll
-    for (int k = 0; k < DP / 16; k++) f[k] = global_fragment<T>(p, k * 16 + 8 * h, a.dim, row.any);
-}
-
-template <typename T, int DP, bool MOD> __global__ void __launch_bounds__(256, 2) forward_kernel(Args a, int64_t tiles)
-{
-    typedef Tile<DP, 64, 4> Tk;
-    __shared__ __align__(1024) char smem[2][2 * Tk::kBytes];
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, h = lane >> 5;
-    // key heads fastest: 8 of them lie on one XCD each, whose L2 then holds its head's keys. The last tiles, which
-    // see the most keys, first.
-    const int hk = blockIdx.x % a.kv_heads;
-    const int64_t slot = gridDim.x / a.kv_heads - 1 - blockIdx.x / a.kv_heads;
-    int s;
-    int64_t tile;
-    if (a.packed) {
-        if (!find_slot(a.d_q, a.q_rows, 1, a.sequences, a.group, 128, tiles, slot, s, tile)) return;
-    } else {
-        s = (int)(slot % a.sequences), tile = slot / a.sequences;
-    }
-    const Sequence q = sequence_of(a, s);
-    if (tile * 128 >= (int64_t)q.lq * a.group) return;
-    const int r0 = (int)tile * 128, rows = q.lq * a.group;
-    const Row row = row_of(a, q, hk, r0 + wave * 32 + (lane & 31));
-    const int end = limit_of(a, q, min(r0 + 127, rows - 1)), mine = limit_of(a, q, min(r0 + wave * 32 + 31, max(rows - 1, r0 + wave * 32)));
-    const int whole = r0 + wave * 32 + 31 < rows ? limit_of(a, q, r0 + wave * 32) : 0;   // keys that all of the wavefront's rows see
-    const int count = (end + 63) / 64;
-
-    typename mm::pack8<T>::type qf[DP / 16];
-    load_query<T, DP>(a, a.q, q, row, qf);
-    const float slope2 = MOD && a.d_slopes ? a.d_slopes[row.any ? row.head : 0] * kLog2e : 0.0f;
-
-    const T *pk = (const T *)a.k.p + s * a.k.seq + q.k0 * a.k.row + hk * a.k.head;
-    const T *pv = (const T *)a.v.p + s * a.v.seq + q.k0 * a.v.row + hk * a.v.head;
-    int ok[Tk::kLoads], ov[Tk::kLoads];
-#pragma unroll
-    for (int i = 0; i < Tk::kLoads; i++) ok[i] = Tk::offset(i, wave, a.k.row, a.dim, 64), ov[i] = Tk::offset(i, wave, a.v.row, a.dim, 64);
-    const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)&smem[0][0];
-    auto load = [&](int t) {
-        const int valid = q.lk - t * 64;
-        const i32x4 bk = buffer_at(pk + (int64_t)t * 64 * a.k.row), bv = buffer_at(pv + (int64_t)t * 64 * a.v.row);
-        const uint32_t to = lds + (t & 1) * 2 * Tk::kBytes + wave * 1024;
-        if (valid >= 64) {
-#pragma unroll
-            for (int i = 0; i < Tk::kLoads; i++) {
-                mm::load_to_lds(bk, ok[i], to + i * 4096);
-                mm::load_to_lds(bv, ov[i], to + Tk::kBytes + i * 4096);
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < Tk::kLoads; i++) {
-                mm::load_to_lds(bk, Tk::offset(i, wave, a.k.row, a.dim, valid), to + i * 4096);
-                mm::load_to_lds(bv, Tk::offset(i, wave, a.v.row, a.dim, valid), to + Tk::kBytes + i * 4096);
-            }
-        }
-    };
-    State<DP> st;
-    st.init();
-    if (count) load(0);
-    for (int t = 0; t < count; t++) {
-        mm::arrive();
-        if (t + 1 < count) load(t + 1);
-        if (t * 64 < mine) {
-            const char *tk = smem[t & 1];
-            attend<T, DP, 2, MOD>(a, st, qf, tk, tk + Tk::kBytes, t * 64, row, slope2, t * 64 + 64 > whole);
-        }
-    }
-    if (!row.any) return;
-    const float l = st.l + other_half(st.l), inv = l == 0 ? 0.0f : 1.0f / l;
-    T *y = (T *)a.y.p + s * a.y.seq + (q.q0 + row.i) * a.y.row + row.head * a.y.head;
-#pragma unroll
-    for (int d = 0; d < DP / 32; d++)
-#pragma unroll
-        for (int r = 0; r < 16; r += 4)
-            store4<T>(y, d * 32 + mfma_row(r, h), a.dim, a.out_vec, st.o[d][r] * inv, st.o[d][r + 1] * inv, st.o[d][r + 2] * inv, st.o[d][r + 3] * inv);
-    if (a.lse && h == 0)
-        a.lse[row.at * a.heads + row.head] = l == 0 ? -INFINITY : (st.m * (MOD ? 1.0f : a.scale2) + __log2f(l)) * kLn2;
-}
-
 // 32 rows a workgroup. The sums of a part, where there are several: DP values, the maximum (times log2(e)) and the sum.
-template <typename T, int DP, bool MOD> __global__ void __launch_bounds__(256) split_kernel(Args a, int64_t tiles)
+template <typename T, int DP, int MODE> __global__ void __launch_bounds__(256) split_kernel(Args a, int64_t tiles)
 {
     typedef Tile<DP, 32, 1> Tk;
     constexpr int kStage = 2 * Tk::kBytes, kLine = DP + 4;
     static_assert(4 * 32 * kLine * 4 + 4 * 64 * 4 <= 8 * kStage, "the wavefronts' sums fit where the tiles were");
     __shared__ __align__(1024) char smem[4][2][kStage];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, h = lane >> 5, col = lane & 31;
-    const int hk = blockIdx.x % a.kv_heads;
-    const int64_t rest = blockIdx.x / a.kv_heads, slot = rest / a.parts;
-    const int part = (int)(rest - slot * a.parts);
+    const uint32_t rest = blockIdx.x / (uint32_t)a.kv_heads;
+    const int hk = blockIdx.x - rest * a.kv_heads;
+    const int64_t slot = rest / (uint32_t)a.parts;
+    const int part = (int)(rest - (uint32_t)slot * a.parts);
     int s;
     int64_t tile;
     if (!find_slot(a.d_q, a.q_rows, a.packed, a.sequences, a.group, 32, tiles, slot, s, tile)) return;
@@ -219,9 +38,6 @@ template <typename T, int DP, bool MOD> __global__ void __launch_bounds__(256) s
     const int all = (end + 31) / 32, per = (all + a.parts - 1) / a.parts;
     const int first = part * per, last = min(first + per, all);
 
-    typename mm::pack8<T>::type qf[DP / 16];
-    load_query<T, DP>(a, a.q, q, row, qf);
-    const float slope2 = MOD && a.d_slopes ? a.d_slopes[row.any ? row.head : 0] * kLog2e : 0.0f;
     const T *pk = (const T *)a.k.p + s * a.k.seq + q.k0 * a.k.row + hk * a.k.head;
     const T *pv = (const T *)a.v.p + s * a.v.seq + q.k0 * a.v.row + hk * a.v.head;
     const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)&smem[wave][0][0];
@@ -239,10 +55,15 @@ template <typename T, int DP, bool MOD> __global__ void __launch_bounds__(256) s
     };
     State<DP> st;
     st.init();
-    int stage = 0;
-    if (first + wave < last) load(first + wave, 0);
-    for (int t = first + wave; t < last; t += 4, stage ^= 1) {
-        // a wavefront's tiles are its own: it waits for its loads, and for its reads of the buffer that is filled next
+    Places at;
+    at.set<DP>();
+    typename mm::pack8<T>::type qf[DP / 16];
+    load_query<T, DP>(a, a.q, q, row, qf);
+    const float slope = slope_of<MODE>(a, row.any ? row.head : 0);
+    int stage = 0, t = first + wave;
+    if (t < last) load(t, 0);
+    // a wavefront's tiles are its own: it waits for its loads, and for its reads of the buffer that is filled next
+    auto next = [&]() __attribute__((always_inline)) {
         constexpr int later = 2 * Tk::kLoads;
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         if (t + 4 < last) {
@@ -251,11 +72,27 @@ template <typename T, int DP, bool MOD> __global__ void __launch_bounds__(256) s
         } else {
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         }
+    };
+    auto attend = [&](auto masked) __attribute__((always_inline)) {
         const char *tk = smem[wave][stage];
-        attend<T, DP, 1, MOD>(a, st, qf, tk, tk + Tk::kBytes, t * 32, row, slope2, t * 32 + 32 > whole);
+        f32x16 x = score<T, DP>(tk, at, 0, qf);
+        typename mm::pack8<T>::type p[2];
+        float was, sum;
+        if (soften<T, MODE, decltype(masked)::value>(a, x, st.m, was, sum, t * 32 + 4 * h, row, slope, p)) rescale<MODE>(a, st, was);
+        st.l += sum;
+        collect<T, DP>(st, tk + Tk::kBytes, at, 0, p);
+    };
+    const int open = min(whole / 32, last);
+    for (; t < open; t += 4, stage ^= 1) {
+        next();
+        attend(std::false_type());
+    }
+    for (; t < last; t += 4, stage ^= 1) {
+        next();
+        attend(std::true_type());
     }
     // the four wavefronts' sums
-    const float m = st.m == -INFINITY ? -INFINITY : st.m * (MOD ? 1.0f : a.scale2), l = st.l + other_half(st.l);
+    const float m = st.m == -INFINITY ? -INFINITY : st.m * unit_of<MODE>(a) + offset_of<MODE>(a), l = st.l + other_half(st.l);
     float *sums = (float *)&smem[0][0][0], *ms = sums + 4 * 32 * kLine;   // [wave][row][kLine], [wave][row] of m, then of l
     __syncthreads();
 #pragma unroll
@@ -301,8 +138,8 @@ template <typename T, int DP, bool MOD> __global__ void __launch_bounds__(256) s
 // joins the parts of 32 rows
 template <typename T, int DP> __global__ void __launch_bounds__(256) combine_kernel(Args a, int64_t tiles)
 {
-    const int hk = blockIdx.x % a.kv_heads;
-    const int64_t slot = blockIdx.x / a.kv_heads;
+    const int hk = blockIdx.x % (uint32_t)a.kv_heads;
+    const int64_t slot = blockIdx.x / (uint32_t)a.kv_heads;
     int s;
     int64_t tile;
     if (!find_slot(a.d_q, a.q_rows, a.packed, a.sequences, a.group, 32, tiles, slot, s, tile)) return;
@@ -377,7 +214,7 @@ int Copies::launch(hipStream_t stream) const
 }
 
 // ---- host ----
-bool modified(const heddle_attention_desc *d) { return d->cap > 0 || d->d_slopes; }
+int mode_of(const heddle_attention_desc *d) { return (d->cap > 0 ? kCap : 0) | (d->d_slopes ? kSlopes : 0); }
 
 Args base_args(const heddle_attention_desc *d)
 {
@@ -392,6 +229,7 @@ Args base_args(const heddle_attention_desc *d)
     a.scale = d->scale, a.cap = d->cap;
     a.scale2 = d->cap > 0 ? 2 * d->scale * kLog2e / d->cap : d->scale * kLog2e;
     a.cap2 = d->cap * kLog2e;
+    a.unscale = -1.0f / a.scale2;
     return a;
 }
 
@@ -468,22 +306,20 @@ int check_overlaps(const heddle_attention_desc *d, bool backward)
     return rc ? rc : mm::check_apart(dv, {&q, &k, &v, &y, &dy, &lse});
 }
 
-// f(type, padded head width, modified scores) as constants
-template <typename F> static int with_kind(const heddle_attention_desc *d, F f)
-{
-    auto wide = [&](auto t) {
-        typedef decltype(t) T;
-        const bool mod = modified(d);
-        if (d->dim <= 64) return mod ? f(T(), std::integral_constant<int, 64>(), std::true_type()) : f(T(), std::integral_constant<int, 64>(), std::false_type());
-        return mod ? f(T(), std::integral_constant<int, 128>(), std::true_type()) : f(T(), std::integral_constant<int, 128>(), std::false_type());
-    };
-    return d->dtype == HEDDLE_T_BF16 ? wide((__bf16)0.0f) : wide((_Float16)0.0f);
-}
-
 static int launched(const char *what)
 {
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? HEDDLE_OK : hip_fail(e, what);
+}
+
+static void launch_combine(const heddle_attention_desc *d, const Args &a, int64_t blocks, int64_t tiles, hipStream_t stream)
+{
+    auto go = [&](auto t) {
+        typedef decltype(t) T;
+        if (d->dim <= 64) hipLaunchKernelGGL((combine_kernel<T, 64>), dim3((unsigned)blocks), dim3(256), 0, stream, a, tiles);
+        else hipLaunchKernelGGL((combine_kernel<T, 128>), dim3((unsigned)blocks), dim3(256), 0, stream, a, tiles);
+    };
+    d->dtype == HEDDLE_T_BF16 ? go((__bf16)0.0f) : go((_Float16)0.0f);
 }
 
 static int forward(const heddle_attention_desc *d, mm::Scratch &s, bool run, hipStream_t stream)
@@ -498,7 +334,7 @@ static int forward(const heddle_attention_desc *d, mm::Scratch &s, bool run, hip
     // rows of a key head in a sequence, on average
     const int64_t rows = std::max<int64_t>(1, a.q_rows * a.group / d->sequences), keys = a.k_rows / d->sequences;
     const bool split = rows <= 64;
-    const int T = split ? 32 : 128;
+    const int T = split ? 32 : rows >= 1024 ? 256 : 128;
     const int64_t slots = slots_of(d->packed, d->sequences, d->q_len, d->q_len, a.group, T), tiles = (d->q_len * a.group + T - 1) / T;
     int64_t blocks = slots * d->kv_heads;
     a.parts = 1;
@@ -510,16 +346,16 @@ static int forward(const heddle_attention_desc *d, mm::Scratch &s, bool run, hip
     if (blocks * a.parts > (int64_t(1) << 24) - 1) return fail(HEDDLE_E_RANGE, "more tiles than a launch holds");
     if (!run) return HEDDLE_OK;
     if (const int rc = c.launch(stream)) return rc;
-    return with_kind(d, [&](auto t, auto dp, auto mod) {
-        typedef decltype(t) T;
-        if (!split) {
-            hipLaunchKernelGGL((forward_kernel<T, dp, mod>), dim3((unsigned)blocks), dim3(256), 0, stream, a, tiles);
-            return launched("attention");
-        }
-        hipLaunchKernelGGL((split_kernel<T, dp, mod>), dim3((unsigned)(blocks * a.parts)), dim3(256), 0, stream, a, tiles);
-        if (a.parts > 1) hipLaunchKernelGGL((combine_kernel<T, dp>), dim3((unsigned)blocks), dim3(256), 0, stream, a, tiles);
-        return launched("attention");
-    });
+    if (!split) {
+        launch_forward(d, a, T, blocks, tiles, stream);
+    } else {
+        with_kind(d, [&](auto t, auto dp, auto mode) {
+            typedef decltype(t) T;
+            hipLaunchKernelGGL((split_kernel<T, dp, mode>), dim3((unsigned)(blocks * a.parts)), dim3(256), 0, stream, a, tiles);
+        });
+        if (a.parts > 1) launch_combine(d, a, blocks, tiles, stream);
+    }
+    return launched("attention");
 }
 
 int run_attention(const heddle_attention_desc *d, bool back, void *ws, int64_t bytes, bool run, hipStream_t stream, int64_t *need);

@@ -15,43 +15,71 @@
 namespace heddle {
 namespace attn {
 
-// P and dS of 32 x 32 scores. at: distance from register 0's key or row (the sign does not matter);
-// seen(r): whether register r's pair is visible; lse2 and delta by register.
-template <bool MOD, typename Seen, typename Lse, typename Delta>
-__device__ inline void weigh(const Args &a, f32x16 &s, f32x16 &dp, float slope2, int at, bool masked, Seen seen, Lse lse2, Delta delta)
+// sixteen floats of a 32 x 32 product's rows: by fours, eight apart
+HEDDLE_INLINE f32x16 four(const float *p)
 {
-    f32x16 t;
-    modify<MOD>(a, s, slope2, at, &t);
-#pragma unroll
-    for (int r = 0; r < 16; r++) s[r] = __builtin_amdgcn_exp2f(s[r] - lse2(r));
-    if (masked) {
-#pragma unroll
-        for (int r = 0; r < 16; r++) s[r] = seen(r) ? s[r] : 0.0f;
-    }
-#pragma unroll
-    for (int r = 0; r < 16; r++) dp[r] = s[r] * (dp[r] - delta(r));
-    if constexpr (MOD) {
-        if (a.cap > 0) {
-#pragma unroll
-            for (int r = 0; r < 16; r++) dp[r] *= 1.0f - t[r] * t[r];
-        }
-    }
+    const mm::f32x4 a = *(const mm::f32x4 *)p, b = *(const mm::f32x4 *)(p + 8), c = *(const mm::f32x4 *)(p + 16), d = *(const mm::f32x4 *)(p + 24);
+    const auto x = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7), y = __builtin_shufflevector(c, d, 0, 1, 2, 3, 4, 5, 6, 7);
+    return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7, 8, 9, 10, 11, 12, 13, 14, 15);
 }
 
-template <typename T, int DP, bool MOD> __global__ void __launch_bounds__(256, 2) rows_kernel(Args a, int64_t tiles)
+// P and dS of 32 x 32 scores. INIT: the products' sums started from -delta and, without a cap or slopes, from
+// -lse / scale. at: distance from register 0's key or row (the sign does not matter); seen(r): whether register r's
+// pair is visible; start of four registers: cap log2(e) - lse log2(e); delta by register.
+// The cap's derivative is 1 - tanh^2 = 4 (r - r^2), r = 1 / (1 + e^u); kLift of the 4 is taken here, the rest by scale_of().
+template <typename T> constexpr float kLift = sizeof(T) == 2 && __is_same(T, _Float16) ? 4.0f : 1.0f;   // float16 has no range to spare
+template <typename T, int MODE> __device__ inline float scale_of(const Args &a) { return MODE & kCap ? a.scale * (4.0f / kLift<T>) : a.scale; }
+
+template <typename T, int MODE, bool INIT, bool MASKED, typename Seen, typename Start, typename Delta>
+HEDDLE_INLINE void weigh(const Args &a, f32x16 &s, f32x16 &dp, float slope2, int at, Seen seen, Start start, Delta delta)
+{
+    if constexpr (!INIT) each<16>([&](int r) { dp[r] -= delta(r); });
+    if constexpr (MODE == kPlain) {
+        each<4>([&](int q) {
+            mm::f32x4 l = {};
+            if constexpr (!INIT) l = start(q);
+            each<4>([&](int n) { s[4 * q + n] = __builtin_amdgcn_exp2f(INIT ? s[4 * q + n] * a.scale2 : __builtin_fmaf(s[4 * q + n], a.scale2, l[n])); });
+        });
+    } else {
+        if constexpr (MODE & kCap) {
+            each<4>([&](int q) {
+                const mm::f32x4 l = start(q);
+                each<4>([&](int n) {
+                    const float x = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(s[4 * q + n] * a.scale2));
+                    s[4 * q + n] = __builtin_fmaf(-2.0f * a.cap2, x, l[n]);
+                    dp[4 * q + n] *= kLift<T> * __builtin_fmaf(-x, x, x);
+                });
+            });
+        } else {
+            each<4>([&](int q) {
+                const mm::f32x4 l = start(q);
+                each<4>([&](int n) { s[4 * q + n] = __builtin_fmaf(s[4 * q + n], a.scale2, l[n]); });
+            });
+        }
+        if constexpr (MODE & kSlopes) {
+            const float from = (float)at;
+            each<16>([&](int r) { s[r] = __builtin_fmaf(-slope2, fabsf(from - (float)(8 * (r >> 2) + (r & 3))), s[r]); });
+        }
+        each<16>([&](int r) { s[r] = __builtin_amdgcn_exp2f(s[r]); });
+    }
+    if constexpr (MASKED) each<16>([&](int r) { s[r] = seen(r) ? s[r] : 0.0f; });
+    each<16>([&](int r) { dp[r] *= s[r]; });
+}
+
+template <typename T, int DP, int MODE> __global__ void __launch_bounds__(256, 2) rows_kernel(Args a, int64_t tiles)
 {
     typedef Tile<DP, 64, 4> Tk;
     typedef typename mm::pack8<T>::type frag;
     __shared__ __align__(1024) char smem[2][2 * Tk::kBytes];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, h = lane >> 5, col = lane & 31;
-    const int hk = blockIdx.x % a.kv_heads;
-    const int64_t slot = gridDim.x / a.kv_heads - 1 - blockIdx.x / a.kv_heads;
+    const int hk = blockIdx.x % (uint32_t)a.kv_heads;
+    const int64_t slot = gridDim.x / (uint32_t)a.kv_heads - 1 - blockIdx.x / (uint32_t)a.kv_heads;
     int s;
     int64_t tile;
     if (a.packed) {
         if (!find_slot(a.d_q, a.q_rows, 1, a.sequences, a.group, 128, tiles, slot, s, tile)) return;
     } else {
-        s = (int)(slot % a.sequences), tile = slot / a.sequences;
+        s = (int)((uint32_t)slot % (uint32_t)a.sequences), tile = (uint32_t)slot / (uint32_t)a.sequences;
     }
     const Sequence q = sequence_of(a, s);
     if (tile * 128 >= (int64_t)q.lq * a.group) return;
@@ -105,60 +133,81 @@ template <typename T, int DP, bool MOD> __global__ void __launch_bounds__(256, 2
         if (h == 0) a.rows[(int64_t)head * a.q_rows + at] = {lse2, delta};
     }
     if (!(a.grads & 1)) return;
-    const float slope2 = MOD && a.d_slopes ? a.d_slopes[head] * kLog2e : 0.0f;
+    const float slope2 = MODE & kSlopes ? a.d_slopes[head] * kLog2e : 0.0f, base = a.cap2 - lse2;
 
+    Places places;
+    places.set<DP>();
     f32x16 dq[DP / 32];
 #pragma unroll
     for (int d = 0; d < DP / 32; d++) dq[d] = f32x16{};
-    for (int t = 0; t < count; t++) {
+    auto next = [&](int t) __attribute__((always_inline)) {
         mm::arrive();
         if (t + 1 < count) load(t + 1);
+    };
+    auto add = [&](int t, auto masked) __attribute__((always_inline)) {
         const char *tk = smem[t & 1], *tv = tk + Tk::kBytes;
 #pragma unroll
         for (int c = 0; c < 2; c++) {
-            const int j0 = t * 64 + c * 32;
-            if (j0 >= mine) break;
             f32x16 p = {}, ds = {};
 #pragma unroll
-            for (int k = 0; k < DP / 16; k++) p = mfma(row_fragment<DP, T>(tk, c * 32 + col, k, h), qf[k], p);
+            for (int k = 0; k < DP / 16; k++) p = mfma(row_fragment<DP, T>(tk, places, c * 32, k), qf[k], p);
 #pragma unroll
-            for (int k = 0; k < DP / 16; k++) ds = mfma(row_fragment<DP, T>(tv, c * 32 + col, k, h), gf[k], ds);
-            const int first = j0 + 4 * h;
-            weigh<MOD>(a, p, ds, slope2, i + shift - first, j0 + 32 > whole, [&](int n) { return first + mfma_row(n, 0) < limit; },
-                       [&](int) { return lse2; }, [&](int) { return delta; });
+            for (int k = 0; k < DP / 16; k++) ds = mfma(row_fragment<DP, T>(tv, places, c * 32, k), gf[k], ds);
+            const int first = t * 64 + c * 32 + 4 * h;
+            weigh<T, MODE, false, decltype(masked)::value>(a, p, ds, slope2, i + shift - first, [&](int n) { return first + mfma_row(n, 0) < limit; },
+                                                          [&](int) { return mm::f32x4{base, base, base, base}; }, [&](int) { return delta; });
 #pragma unroll
             for (int k = 0; k < 2; k++) {
                 const frag b = pack<T>(ds, 8 * k);
 #pragma unroll
-                for (int d = 0; d < DP / 32; d++) dq[d] = mfma(column_fragment<DP, T>(tk, c * 32 + 16 * k, d), b, dq[d]);
+                for (int d = 0; d < DP / 32; d++) dq[d] = mfma(column_fragment<DP, T>(tk, places, c * 32 + 16 * k, d), b, dq[d]);
             }
         }
+    };
+    // tiles seen whole, in part, and by other wavefronts alone: see the forward pass
+    const int open = min(whole / 64, count), some = min((mine + 63) / 64, count);
+    int t = 0;
+    for (; t < open; t++) {
+        next(t);
+        add(t, std::false_type());
     }
+    for (; t < some; t++) {
+        next(t);
+        add(t, std::true_type());
+    }
+    for (; t < count; t++) next(t);
     if (!any) return;
+    const float sc = scale_of<T, MODE>(a);
     T *out = (T *)a.dq.p + s * a.dq.seq + (q.q0 + i) * a.dq.row + head * a.dq.head;
 #pragma unroll
     for (int d = 0; d < DP / 32; d++)
 #pragma unroll
         for (int n = 0; n < 16; n += 4)
-            store4<T>(out, d * 32 + mfma_row(n, h), a.dim, a.out_vec, dq[d][n] * a.scale, dq[d][n + 1] * a.scale, dq[d][n + 2] * a.scale, dq[d][n + 3] * a.scale);
+            store4<T>(out, d * 32 + mfma_row(n, h), a.dim, a.out_vec, dq[d][n] * sc, dq[d][n + 1] * sc, dq[d][n + 2] * sc, dq[d][n + 3] * sc);
 }
 
-template <typename T, int DP, bool MOD> __global__ void __launch_bounds__(256) keys_kernel(Args a, int64_t tiles)
+template <typename T, int DP, int MODE> __global__ void __launch_bounds__(256, 2) keys_kernel(Args a, int64_t tiles)
 {
-    constexpr int kRows = 64;
+    constexpr int kRows = 32;
     typedef Tile<DP, kRows, 4> Tk;
     typedef typename mm::pack8<T>::type frag;
     __shared__ __align__(1024) char smem[2][2 * Tk::kBytes];
-    __shared__ __align__(16) float stats[2][2][kRows];      // lse log2(e), delta
+    typedef Tile<DP, 128, 4> Tv;
+    __shared__ __align__(1024) char values[Tv::kBytes];
+    __shared__ __align__(16) float stats[2][2][kRows];      // what the exponents, or the scores' sums, start from; -delta
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, h = lane >> 5, col = lane & 31;
-    const int hk = blockIdx.x % a.kv_heads;
-    const int64_t slot = blockIdx.x / a.kv_heads;           // the first tiles, which the most rows see, first
+    const int hk = blockIdx.x % (uint32_t)a.kv_heads;
+    // The first tiles, which the most rows see, first. Where all workgroups find a place at once, two a CU, the second
+    // half in reverse: a CU's two then have as much to do as another's (4 sequences of 2048, 64 heads on 8: 1118 us without).
+    int64_t slot = blockIdx.x / (uint32_t)a.kv_heads;
+    const int64_t slots = gridDim.x / (uint32_t)a.kv_heads, half = 256 / (uint32_t)a.kv_heads;
+    if (slots <= 2 * half && slot >= half) slot = half + (slots - 1 - slot);
     int s;
     int64_t tile;
     if (a.packed) {
         if (!find_slot(a.d_k, a.k_rows, 1, a.sequences, 1, 128, tiles, slot, s, tile)) return;
     } else {
-        s = (int)(slot % a.sequences), tile = slot / a.sequences;
+        s = (int)((uint32_t)slot % (uint32_t)a.sequences), tile = (uint32_t)slot / (uint32_t)a.sequences;
     }
     const Sequence q = sequence_of(a, s);
     if (tile * 128 >= q.lk) return;
@@ -172,12 +221,15 @@ template <typename T, int DP, bool MOD> __global__ void __launch_bounds__(256) k
     const int per = q.lq > start ? (q.lq - start + kRows - 1) / kRows : 0, count = per * a.group;
 
     const T *pk = (const T *)a.k.p + s * a.k.seq + (q.k0 + j) * a.k.row + hk * a.k.head;
-    const T *pv = (const T *)a.v.p + s * a.v.seq + (q.k0 + j) * a.v.row + hk * a.v.head;
-    frag kf[DP / 16], vf[DP / 16];
+    const T *pv = (const T *)a.v.p + s * a.v.seq + (q.k0 + j0) * a.v.row + hk * a.v.head;
+    frag kf[DP / 16];
 #pragma unroll
-    for (int k = 0; k < DP / 16; k++) {
-        kf[k] = global_fragment<T>(pk, k * 16 + 8 * h, a.dim, any);
-        vf[k] = global_fragment<T>(pv, k * 16 + 8 * h, a.dim, any);
+    for (int k = 0; k < DP / 16; k++) kf[k] = global_fragment<T>(pk, k * 16 + 8 * h, a.dim, any);
+    if (count) {
+        const uint32_t to = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)&values[0] + wave * 1024;
+        const i32x4 bv = buffer_at(pv);
+#pragma unroll
+        for (int n = 0; n < Tv::kLoads; n++) mm::load_to_lds(bv, Tv::offset(n, wave, a.v.row, a.dim, q.lk - j0), to + n * 4096);
     }
     int oq[Tk::kLoads], og[Tk::kLoads];
 #pragma unroll
@@ -199,68 +251,91 @@ template <typename T, int DP, bool MOD> __global__ void __launch_bounds__(256) k
         }
     };
     auto keep = [&](int n) {
-        if (threadIdx.x < kRows) stats[n & 1][0][threadIdx.x] = stat.x, stats[n & 1][1][threadIdx.x] = stat.y;
+        if (threadIdx.x < kRows) stats[n & 1][0][threadIdx.x] = MODE != kPlain ? a.cap2 - stat.x : stat.x * a.unscale, stats[n & 1][1][threadIdx.x] = -stat.y;
     };
+    Places places;
+    places.set<DP>();
+    const char *mine_values = values + wave * (32 * DP * 2);
     f32x16 dk[DP / 32], dv[DP / 32];
 #pragma unroll
     for (int d = 0; d < DP / 32; d++) dk[d] = f32x16{}, dv[d] = f32x16{};
     if (count) load(0, 0, start), keep(0);
-    int g = 0, i0 = start;
-    for (int n = 0; n < count; n++) {
-        const int head = hk * a.group + g, i = i0;
-        i0 += kRows;
-        if (i0 >= q.lq) i0 = start, g++;
+    int n = 0, slot_of = 0;                                 // tiles so far; the current one's buffer
+    // the tile at row i of head g has arrived, the one after it is on its way
+    auto next = [&](int g, int i) __attribute__((always_inline)) {
         mm::arrive();
-        if (n + 1 < count) load(n + 1, g, i0);
-        const char *tq = smem[n & 1], *tg = tq + Tk::kBytes;
-        const float slope2 = MOD && a.d_slopes ? a.d_slopes[head] * kLog2e : 0.0f;
+        const bool last = i + kRows >= q.lq;
+        if (n + 1 < count) load(n + 1, last ? g + 1 : g, last ? start : i + kRows);
+        slot_of = n & 1;
+    };
+    auto leave = [&]() __attribute__((always_inline)) {
+        n++;
+        if (n < count) keep(n);
+    };
+    auto add = [&](int i, float slope2, auto masked) __attribute__((always_inline)) {
+        const char *tq = smem[slot_of], *tg = tq + Tk::kBytes;
+        const float *ls = &stats[slot_of][0][4 * h], *de = &stats[slot_of][1][4 * h];
+        f32x16 p = {}, ds = four(de);
+        if constexpr (MODE == kPlain) p = four(ls);
 #pragma unroll
-        for (int u = 0; u < kRows / 32; u++) {
-            const int b = i + u * 32;
-            if (b + 31 < mine || b >= q.lq) continue;
-            f32x16 p = {}, ds = {};
+        for (int k = 0; k < DP / 16; k++) p = mfma(row_fragment<DP, T>(tq, places, 0, k), kf[k], p);
 #pragma unroll
-            for (int k = 0; k < DP / 16; k++) p = mfma(row_fragment<DP, T>(tq, u * 32 + col, k, h), kf[k], p);
+        for (int k = 0; k < DP / 16; k++) ds = mfma(row_fragment<DP, T>(tg, places, 0, k), row_fragment<DP, T>(mine_values, places, 0, k), ds);
+        const int first = i + 4 * h;
+        weigh<T, MODE, true, decltype(masked)::value>(a, p, ds, slope2, j - shift - first, [&](int r) { return first + mfma_row(r, 0) >= from; },
+                                                     [&](int q) { return *(const mm::f32x4 *)(ls + 8 * q); }, [](int) { return 0.0f; });
 #pragma unroll
-            for (int k = 0; k < DP / 16; k++) ds = mfma(row_fragment<DP, T>(tg, u * 32 + col, k, h), vf[k], ds);
-            float ls[16], de[16];
+        for (int k = 0; k < 2; k++) {
+            const frag bp = pack<T>(p, 8 * k), bs = pack<T>(ds, 8 * k);
 #pragma unroll
-            for (int r = 0; r < 16; r += 4) {
-                const mm::f32x4 x = *(const mm::f32x4 *)&stats[n & 1][0][u * 32 + mfma_row(r, h)], y = *(const mm::f32x4 *)&stats[n & 1][1][u * 32 + mfma_row(r, h)];
-#pragma unroll
-                for (int m = 0; m < 4; m++) ls[r + m] = x[m], de[r + m] = y[m];
-            }
-            const int first = b + 4 * h;
-            weigh<MOD>(a, p, ds, slope2, j - shift - first, b < whole, [&](int r) { return first + mfma_row(r, 0) >= from; },
-                       [&](int r) { return ls[r]; }, [&](int r) { return de[r]; });
-#pragma unroll
-            for (int k = 0; k < 2; k++) {
-                const frag bp = pack<T>(p, 8 * k), bs = pack<T>(ds, 8 * k);
-#pragma unroll
-                for (int d = 0; d < DP / 32; d++) {
-                    dv[d] = mfma(column_fragment<DP, T>(tg, u * 32 + 16 * k, d), bp, dv[d]);
-                    dk[d] = mfma(column_fragment<DP, T>(tq, u * 32 + 16 * k, d), bs, dk[d]);
-                }
+            for (int d = 0; d < DP / 32; d++) {
+                dv[d] = mfma(column_fragment<DP, T>(tg, places, 16 * k, d), bp, dv[d]);
+                dk[d] = mfma(column_fragment<DP, T>(tq, places, 16 * k, d), bs, dk[d]);
             }
         }
-        if (n + 1 < count) keep(n + 1);
+    };
+    if (count) {
+        for (int g = 0; g < a.group; g++) {
+            const float slope2 = MODE & kSlopes ? a.d_slopes[hk * a.group + g] * kLog2e : 0.0f;
+            int i = start;
+            // rows that see none of the wavefront's keys, some, all
+            for (; i < q.lq && i + kRows <= mine; i += kRows) next(g, i), leave();
+            for (; i < q.lq && i < whole; i += kRows) {
+                next(g, i);
+                add(i, slope2, std::true_type());
+                leave();
+            }
+            for (; i < q.lq; i += kRows) {
+                next(g, i);
+                add(i, slope2, std::false_type());
+                leave();
+            }
+        }
     }
     if (!any) return;
+    const float sc = scale_of<T, MODE>(a);
     T *ok = (T *)a.dk.p + s * a.dk.seq + (q.k0 + j) * a.dk.row + hk * a.dk.head;
     T *ov = (T *)a.dv.p + s * a.dv.seq + (q.k0 + j) * a.dv.row + hk * a.dv.head;
 #pragma unroll
     for (int d = 0; d < DP / 32; d++)
 #pragma unroll
         for (int r = 0; r < 16; r += 4) {
-            store4<T>(ok, d * 32 + mfma_row(r, h), a.dim, a.out_vec, dk[d][r] * a.scale, dk[d][r + 1] * a.scale, dk[d][r + 2] * a.scale, dk[d][r + 3] * a.scale);
+            store4<T>(ok, d * 32 + mfma_row(r, h), a.dim, a.out_vec, dk[d][r] * sc, dk[d][r + 1] * sc, dk[d][r + 2] * sc, dk[d][r + 3] * sc);
             store4<T>(ov, d * 32 + mfma_row(r, h), a.dim, a.out_vec, dv[d][r], dv[d][r + 1], dv[d][r + 2], dv[d][r + 3]);
         }
 }
 
-template <typename T, int DP, bool MOD> static void launch(const Args &a, int64_t blocks, int64_t tiles, int64_t kblocks, int64_t ktiles, hipStream_t stream)
+void launch_rows(const heddle_attention_desc *d, const Args &a, int64_t blocks, int64_t tiles, hipStream_t stream)
 {
-    if (blocks) hipLaunchKernelGGL((rows_kernel<T, DP, MOD>), dim3((unsigned)blocks), dim3(256), 0, stream, a, tiles);
-    if (kblocks) hipLaunchKernelGGL((keys_kernel<T, DP, MOD>), dim3((unsigned)kblocks), dim3(256), 0, stream, a, ktiles);
+    with_kind(d, [&](auto t, auto dp, auto mode) {
+        hipLaunchKernelGGL((rows_kernel<decltype(t), dp, mode>), dim3((unsigned)blocks), dim3(256), 0, stream, a, tiles);
+    });
+}
+void launch_keys(const heddle_attention_desc *d, const Args &a, int64_t blocks, int64_t tiles, hipStream_t stream)
+{
+    with_kind(d, [&](auto t, auto dp, auto mode) {
+        hipLaunchKernelGGL((keys_kernel<decltype(t), dp, mode>), dim3((unsigned)blocks), dim3(256), 0, stream, a, tiles);
+    });
 }
 
 int backward(const heddle_attention_desc *d, mm::Scratch &s, bool run, hipStream_t stream)
@@ -283,14 +358,8 @@ int backward(const heddle_attention_desc *d, mm::Scratch &s, bool run, hipStream
     if (std::max(blocks, kblocks) > (int64_t(1) << 24) - 1) return fail(HEDDLE_E_RANGE, "more tiles than a launch holds");
     if (!run) return HEDDLE_OK;
     if (const int rc = c.launch(stream)) return rc;
-    const bool mod = modified(d), narrow = d->dim <= 64;
-    auto call = [&](auto t) {
-        typedef decltype(t) T;
-        if (narrow) mod ? launch<T, 64, true>(a, blocks, tiles, kblocks, ktiles, stream) : launch<T, 64, false>(a, blocks, tiles, kblocks, ktiles, stream);
-        else mod ? launch<T, 128, true>(a, blocks, tiles, kblocks, ktiles, stream) : launch<T, 128, false>(a, blocks, tiles, kblocks, ktiles, stream);
-    };
-    if (d->dtype == HEDDLE_T_BF16) call((__bf16)0.0f);
-    else call((_Float16)0.0f);
+    if (blocks) launch_rows(d, a, blocks, tiles, stream);
+    if (kblocks) launch_keys(d, a, kblocks, ktiles, stream);
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? HEDDLE_OK : hip_fail(e, "attention's gradients");
 }

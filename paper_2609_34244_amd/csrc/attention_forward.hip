@@ -1,0 +1,183 @@
+// Attention's forward pass over many query rows: see attention.hip.
+#include "attention.h"
+
+namespace heddle {
+namespace attn {
+
+// soften() in sixteen parts, to be done between products: 0 to 3 four scores each, 4 the maximum, 5 to 12 two
+// probabilities each.
+template <typename T, int MODE, bool MASKED> struct Softening {
+    const Args &a;
+    f32x16 &s;
+    float &m;
+    int first, limit;
+    float distance, slope, top, was, base, sum = 0;
+    bool follow;
+    unsigned words[8];
+    HEDDLE_INLINE void part(int u)
+    {
+        const float unit = unit_of<MODE>(a);
+        if (u < 4) {
+            each<4>([&](int n) {
+                const int r = 4 * u + n;
+                s[r] = modify<MODE>(a, s[r], r, slope, distance);
+                if constexpr (MASKED) s[r] = first + mfma_row(r, 0) >= limit ? -INFINITY : s[r];
+                top = r ? fmaxf(top, s[r]) : s[r];
+            });
+        } else if (u == 4) {
+            top = max_halves(top);
+            follow = __any((top - m) * unit > 8.0f);
+            was = m;
+            m = follow ? fmaxf(m, top) : m;
+            here(m);
+            base = m == -INFINITY ? 0.0f : m * unit;
+        } else if (u < 13) {
+            const int r = 2 * (u - 5);
+            const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], unit, -base)), y = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r + 1], unit, -base));
+            sum += x + y;
+            typename Pair<T>::type v = {(T)x, (T)y};
+            unsigned word = __builtin_bit_cast(unsigned, v);
+            here(word);
+            here(sum);
+            words[r >> 1] = word;
+        }
+    }
+    HEDDLE_INLINE typename mm::pack8<T>::type half(int k) const
+    {
+        typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+        return __builtin_bit_cast(typename mm::pack8<T>::type, u32x4{words[4 * k], words[4 * k + 1], words[4 * k + 2], words[4 * k + 3]});
+    }
+};
+
+template <typename T, int DP, int MODE, int NW> __global__ void __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2))) forward_kernel(Args a, int64_t tiles)
+{
+    typedef Tile<DP, 64, NW> Tk;
+    constexpr int kRows = NW * 32;
+    typedef typename mm::pack8<T>::type frag;
+    __shared__ __align__(1024) char smem[2][2][Tk::kBytes]; // keys, values
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, h = lane >> 5;
+    // key heads fastest: 8 of them lie on one XCD each, whose L2 then holds its head's keys. The last tiles, which
+    // see the most keys, first.
+    const int hk = blockIdx.x % (uint32_t)a.kv_heads;
+    const int64_t slot = gridDim.x / (uint32_t)a.kv_heads - 1 - blockIdx.x / (uint32_t)a.kv_heads;
+    int s;
+    int64_t tile;
+    if (a.packed) {
+        if (!find_slot(a.d_q, a.q_rows, 1, a.sequences, a.group, kRows, tiles, slot, s, tile)) return;
+    } else {
+        s = (int)((uint32_t)slot % (uint32_t)a.sequences), tile = (uint32_t)slot / (uint32_t)a.sequences;
+    }
+    const Sequence q = sequence_of(a, s);
+    if (tile * kRows >= (int64_t)q.lq * a.group) return;
+    const int r0 = (int)tile * kRows, rows = q.lq * a.group;
+    const Row row = row_of(a, q, hk, r0 + wave * 32 + (lane & 31));
+    const int end = limit_of(a, q, min(r0 + kRows - 1, rows - 1)), mine = limit_of(a, q, min(r0 + wave * 32 + 31, max(rows - 1, r0 + wave * 32)));
+    const int whole = r0 + wave * 32 + 31 < rows ? limit_of(a, q, r0 + wave * 32) : 0;   // keys that all of the wavefront's rows see
+    const int count = (end + 63) / 64;
+
+    const T *pk = (const T *)a.k.p + s * a.k.seq + q.k0 * a.k.row + hk * a.k.head;
+    const T *pv = (const T *)a.v.p + s * a.v.seq + q.k0 * a.v.row + hk * a.v.head;
+    int ok[Tk::kLoads], ov[Tk::kLoads];
+#pragma unroll
+    for (int i = 0; i < Tk::kLoads; i++) ok[i] = Tk::offset(i, wave, a.k.row, a.dim, 64), ov[i] = Tk::offset(i, wave, a.v.row, a.dim, 64);
+    const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)&smem[0][0][0];
+    // one half of a tile of 64 rows each: keys and values go their own ways
+    auto load = [&](int t, const T *p, int64_t ld, const int *offsets, uint32_t to) __attribute__((always_inline)) {
+        if (t >= count) return;
+        const int row = (count - 1 - t) * 64, valid = q.lk - row;
+        const i32x4 b = buffer_at(p + row * ld);
+        to += (t & 1) * Tk::kBytes + wave * 1024;
+        if (valid >= 64) {
+#pragma unroll
+            for (int i = 0; i < Tk::kLoads; i++) mm::load_to_lds(b, offsets[i], to + i * (NW * 1024));
+        } else {
+#pragma unroll
+            for (int i = 0; i < Tk::kLoads; i++) mm::load_to_lds(b, Tk::offset(i, wave, ld, a.dim, valid), to + i * (NW * 1024));
+        }
+    };
+    auto load_keys = [&](int t) __attribute__((always_inline)) { load(t, pk, a.k.row, ok, lds); };
+    auto load_values = [&](int t) __attribute__((always_inline)) { load(t, pv, a.v.row, ov, lds + 2 * Tk::kBytes); };
+    State<DP> st;
+    st.init();
+    Places at;
+    at.set<DP>();
+    load_keys(0);
+    load_values(0);
+    load_keys(1);
+    frag qf[DP / 16];
+    load_query<T, DP>(a, a.q, q, row, qf);
+    const float slope = slope_of<MODE>(a, row.any ? row.head : 0);
+
+    // Steps of 32 keys, from the last ones to the first: a bias by distance then has each row's maximum first, and
+    // the sums are hardly scaled again. A step's probabilities are formed while the products of the next step's keys and
+    // of the previous step's values run: the two are independent, and a wavefront's instructions of both kinds alternate.
+    // Tile t's keys are used by the steps 2 t - 1 and 2 t, its values by 2 t + 1 and 2 t + 2, so that one barrier a tile,
+    // between its two steps, frees a buffer of each.
+    const int open = whole / 64, some = (mine + 63) / 64;   // tiles that all of the wavefront's rows see whole; that some see
+    f32x16 now, then;
+    frag was_p[2] = {};                                     // (of no keys before the first ones)
+    auto turn = [&](int t) __attribute__((always_inline)) {
+        mm::arrive();
+        load_keys(t + 2);
+        load_values(t + 1);
+    };
+    auto step = [&](f32x16 &s, f32x16 &next, const char *keys, int from, const char *values, int back, int j0, auto masked) __attribute__((always_inline)) {
+        // even products: the next step's scores; odd ones: the previous step's values. Their operands are read kAhead ahead.
+        constexpr int N = DP / 8, kAhead = 5;
+        const int first = j0 + 4 * h;
+        Softening<T, MODE, decltype(masked)::value> v = {a, s, st.m, first, row.limit, (float)(row.pos - first), slope};
+        frag f[kAhead];
+        auto fetch = [&](int i) __attribute__((always_inline)) {
+            const int n = i >> 1;
+            f[i % kAhead] = i & 1 ? column_fragment<DP, T>(values, at, back + n / (DP / 32) * 16, n % (DP / 32)) : row_fragment<DP, T>(keys, at, from, n);
+        };
+        next = f32x16{};
+        each<kAhead - 1>([&](int i) __attribute__((always_inline)) { fetch(i); });
+        each<N>([&](int i) __attribute__((always_inline)) {
+            each<16 / N>([&](int n) __attribute__((always_inline)) { v.part(i * (16 / N) + n); });
+            if (i + kAhead - 1 < N) fetch(i + kAhead - 1);
+            const int n = i >> 1;
+            if (i & 1) st.o[n % (DP / 32)] = mfma(f[i % kAhead], was_p[n / (DP / 32)], st.o[n % (DP / 32)]);
+            else next = mfma(f[i % kAhead], qf[n], next);
+            __builtin_amdgcn_sched_barrier(0);
+        });
+        if (v.follow) rescale<MODE>(a, st, v.was);
+        st.l += v.sum;
+        was_p[0] = v.half(0), was_p[1] = v.half(1);
+    };
+    auto tile_of = [&](int t, auto masked) __attribute__((always_inline)) {
+        const int j0 = (count - 1 - t) * 64;
+        const char *values = smem[1][t & 1];
+        step(now, then, smem[0][t & 1], 0, t ? smem[1][~t & 1] : values, 0, j0 + 32, masked);
+        turn(t);
+        step(then, now, smem[0][~t & 1], 32, values, 32, j0, masked);
+    };
+    mm::arrive();
+    int t = 0;
+    for (; t < count - some; t++) turn(t);
+    if (some) now = score<T, DP>(smem[0][t & 1], at, 32, qf);
+    for (; t < count - open; t++) tile_of(t, std::true_type());
+    for (; t < count; t++) tile_of(t, std::false_type());
+    if (some) collect<T, DP>(st, smem[1][(count - 1) & 1], at, 0, was_p);
+    if (!row.any) return;
+    const float l = st.l + other_half(st.l), inv = l == 0 ? 0.0f : 1.0f / l;
+    T *y = (T *)a.y.p + s * a.y.seq + (q.q0 + row.i) * a.y.row + row.head * a.y.head;
+#pragma unroll
+    for (int d = 0; d < DP / 32; d++)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4)
+            store4<T>(y, d * 32 + mfma_row(r, h), a.dim, a.out_vec, st.o[d][r] * inv, st.o[d][r + 1] * inv, st.o[d][r + 2] * inv, st.o[d][r + 3] * inv);
+    if (a.lse && h == 0)
+        a.lse[row.at * a.heads + row.head] = l == 0 ? -INFINITY : (st.m * unit_of<MODE>(a) + offset_of<MODE>(a) + __log2f(l)) * kLn2;
+}
+
+void launch_forward(const heddle_attention_desc *d, const Args &a, int rows, int64_t blocks, int64_t tiles, hipStream_t stream)
+{
+    with_kind(d, [&](auto t, auto dp, auto mode) {
+        if (rows == 128) hipLaunchKernelGGL((forward_kernel<decltype(t), dp, mode, 4>), dim3((unsigned)blocks), dim3(256), 0, stream, a, tiles);
+        else hipLaunchKernelGGL((forward_kernel<decltype(t), dp, mode, 8>), dim3((unsigned)blocks), dim3(512), 0, stream, a, tiles);
+    });
+}
+
+}  // namespace attn
+}  // namespace heddle

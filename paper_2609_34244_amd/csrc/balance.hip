@@ -5,8 +5,8 @@
 // P_e = sum of p_e over those rows / N, loss = scale E sum_e (c_e / C) P_e;
 // dlogits = dloss scale E / (C N) p (c_e - sum_j p_j c_j) + r.
 // Bound by memory: the logits are read once, and once more for the gradient (p is formed again
-// rather than kept). G lanes to a row, K values a lane, so that a wavefront reads 64 / G rows
-// side by side. A workgroup counts picks in LDS with integer atomics, whose order changes nothing;
+// rather than kept). G lanes to a row, K neighbouring values a lane, so that a wavefront reads 64 / G
+// rows side by side, kAhead of them before the first is used. A workgroup counts picks in LDS with integer atomics, whose order changes nothing;
 // probabilities are summed in fp32 registers, then over workgroups, in one order.
 #include <algorithm>
 #include <cmath>
@@ -36,12 +36,27 @@ __device__ inline int64_t pick_at(const Args &a, int64_t r, int i)
     return a.wide_picks ? ((const int64_t *)a.picked)[r * a.ldp + i] : (int64_t)((const int32_t *)a.picked)[r * a.ldp + i];
 }
 
-// K values of a row, one every G; what is not there is -infinity
-template <typename T, int G, int K> __device__ inline void load_row(const T *row, int experts, bool any, float z[K])
+// K neighbouring values of a row; past its end other
+template <typename T, int K> struct Some {
+    typedef T loose __attribute__((ext_vector_type(K), aligned(sizeof(T))));   // at any address its values may have
+};
+template <typename T, int K> __device__ inline void load_row(const T *row, int e, int experts, float other, float z[K])
 {
-    const int lane = threadIdx.x % G;
+    if (e + K <= experts) {
+        const typename Some<T, K>::loose v = *(const typename Some<T, K>::loose *)(row + e);
 #pragma unroll
-    for (int k = 0; k < K; k++) z[k] = any && k * G + lane < experts ? (float)row[k * G + lane] : -INFINITY;
+        for (int k = 0; k < K; k++) z[k] = (float)v[k];
+        return;
+    }
+    if (e >= experts) {
+#pragma unroll
+        for (int k = 0; k < K; k++) z[k] = other;
+        return;
+    }
+#pragma unroll
+    for (int k = 0; k < K; k++) z[k] = (float)row[min(e + k, experts - 1)];
+#pragma unroll
+    for (int k = 1; k < K; k++) z[k] = e + k < experts ? z[k] : other;
 }
 
 // softmax over G lanes' K values; a row of -infinity alone has no probabilities: zeros
@@ -62,8 +77,8 @@ template <int G, int K> __device__ inline void softmax(float z[K])
     for (int k = 0; k < K; k++) z[k] *= inv;
 }
 
-// adds up a workgroup's picks of rows first .. last - 1 in LDS, and how many of the rows have one
-__device__ inline bool row_counts(const Args &a, int64_t r)
+// whether a row has a pick at all
+__device__ inline bool has_pick(const Args &a, int64_t r)
 {
     bool some = false;
     for (int i = 0; i < a.picks; i++) {
@@ -75,7 +90,7 @@ __device__ inline bool row_counts(const Args &a, int64_t r)
 
 template <typename T, int G, int K> __global__ void __launch_bounds__(256) forward_kernel(Args a)
 {
-    constexpr int kRows = 256 / G;
+    constexpr int kRows = 256 / G, kAhead = K <= 4 ? 4 : K <= 8 ? 2 : 1;
     __shared__ int count[G * K + 1];
     __shared__ float part[kRows > 1 ? kRows : 1][G * K];
     for (int i = threadIdx.x; i <= G * K; i += 256) count[i] = 0;
@@ -87,31 +102,41 @@ template <typename T, int G, int K> __global__ void __launch_bounds__(256) forwa
     int with = 0;
     const int64_t step = (int64_t)gridDim.x * kRows;
     // whole rows of lanes: every lane of a row takes the same turns
-    for (int64_t r = (int64_t)blockIdx.x * kRows + threadIdx.x / G; r < a.t; r += step) {
-        float z[K];
-        load_row<T, G, K>((const T *)a.logits + r * a.ldl, a.experts, true, z);
-        bool some = false;
-        for (int i = lane; i < a.picks; i += G) {
-            const int64_t e = pick_at(a, r, i);
-            if (e >= 0 && e < a.experts) {
-                atomicAdd(&count[e], 1);
-                some = true;
-            }
+    for (int64_t r0 = (int64_t)blockIdx.x * kRows + threadIdx.x / G; r0 < a.t; r0 += step * kAhead) {
+        float z[kAhead][K];
+        int64_t pick[kAhead];
+#pragma unroll
+        for (int n = 0; n < kAhead; n++) {
+            const int64_t r = min(r0 + n * step, a.t - 1);
+            load_row<T, K>((const T *)a.logits + r * a.ldl, lane * K, a.experts, -INFINITY, z[n]);
+            pick[n] = pick_at(a, r, min(lane, a.picks - 1));
         }
-        // a row's lanes: any of them with a pick
-        int has = some;
 #pragma unroll
-        for (int d = G / 2; d; d /= 2) has |= __shfl_xor(has, d);
-        softmax<G, K>(z);
-        if (has) {
-            with += lane == 0;
+        for (int n = 0; n < kAhead; n++) {
+            const int64_t r = r0 + n * step;
+            if (r >= a.t) break;
+            int has = 0;
+            for (int i = lane; i < a.picks; i += G) {
+                const int64_t e = i < G ? pick[n] : pick_at(a, r, i);
+                if (e >= 0 && e < a.experts) {
+                    atomicAdd(&count[e], 1);
+                    has = 1;
+                }
+            }
+            // a row's lanes: any of them with a pick
 #pragma unroll
-            for (int k = 0; k < K; k++) sum[k] += z[k];
+            for (int d = G / 2; d; d /= 2) has |= __shfl_xor(has, d);
+            softmax<G, K>(z[n]);
+            if (has) {
+                with += lane == 0;
+#pragma unroll
+                for (int k = 0; k < K; k++) sum[k] += z[n][k];
+            }
         }
     }
     if (with) atomicAdd(&count[G * K], with);
 #pragma unroll
-    for (int k = 0; k < K; k++) part[threadIdx.x / G][k * G + lane] = sum[k];
+    for (int k = 0; k < K; k++) part[threadIdx.x / G][lane * K + k] = sum[k];
     __syncthreads();
     for (int e = threadIdx.x; e < a.experts; e += 256) {
         float s = 0;
@@ -123,41 +148,65 @@ template <typename T, int G, int K> __global__ void __launch_bounds__(256) forwa
     if (threadIdx.x == 0) a.parts[(int64_t)blockIdx.x * (a.experts + 1) + a.experts] = count[G * K];
 }
 
-// many workgroups' sums become few: workgroup b of `to` adds up every to-th from b on
-__global__ void __launch_bounds__(256) fold_kernel(Args a, int from, float *sums, int32_t *parts)
+// the workgroups' sums become one row: 32 columns by 32 shares
+__global__ void __launch_bounds__(1024) fold_kernel(Args a, int blocks, float *sums, int32_t *parts)
 {
-    const int e = blockIdx.x * 256 + threadIdx.x;
-    if (e > a.experts) return;
+    __shared__ float fs[32][33];
+    __shared__ int fc[32][33];
+    const int col = threadIdx.x & 31, share = threadIdx.x >> 5, e = blockIdx.x * 32 + col;
     float s = 0;
     int c = 0;
+    if (e <= a.experts)
 #pragma unroll 4
-    for (int b = blockIdx.y; b < from; b += gridDim.y) {
-        if (e < a.experts) s += a.sums[(int64_t)b * a.experts + e];
-        c += a.parts[(int64_t)b * (a.experts + 1) + e];
-    }
-    if (e < a.experts) sums[(int64_t)blockIdx.y * a.experts + e] = s;
-    parts[(int64_t)blockIdx.y * (a.experts + 1) + e] = c;
+        for (int b = share; b < blocks; b += 32) {
+            if (e < a.experts) s += a.sums[(int64_t)b * a.experts + e];
+            c += a.parts[(int64_t)b * (a.experts + 1) + e];
+        }
+    fs[share][col] = s, fc[share][col] = c;
+    __syncthreads();
+    if (share || e > a.experts) return;
+    s = 0, c = 0;
+#pragma unroll
+    for (int i = 0; i < 32; i++) s += fs[i][col], c += fc[i][col];
+    if (e < a.experts) sums[e] = s;
+    parts[e] = c;
 }
 
-// one workgroup: the counts, their running sums, the mean probabilities and the loss
-__global__ void __launch_bounds__(1024) finish_kernel(Args a, int blocks)
+// One workgroup: the counts, their running sums, the mean probabilities and the loss. W columns by 1024 / W shares of
+// the workgroups' sums at a time.
+template <int W> __global__ void __launch_bounds__(1024) finish_kernel(Args a, int blocks)
 {
-    __shared__ int scan[16], carry_of;
+    constexpr int kShares = 1024 / W;
+    __shared__ float fs[kShares > 1 ? kShares : 1][W];
+    __shared__ int fc[kShares > 1 ? kShares : 1][W], fr[16], scan[16], carry_of;
     __shared__ double weight[16];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = threadIdx.x % W, share = threadIdx.x / W;
     int rows = 0;
-    for (int b = 0; b < blocks; b++) rows += a.parts[(int64_t)b * (a.experts + 1) + a.experts];
+    for (int b = threadIdx.x; b < blocks; b += 1024) rows += a.parts[(int64_t)b * (a.experts + 1) + a.experts];
+#pragma unroll
+    for (int d = 32; d; d /= 2) rows += __shfl_xor(rows, d);
+    if (lane == 0) fr[wave] = rows;
     int carry = 0;
     double dot = 0;
-    for (int e0 = 0; e0 < a.experts; e0 += 1024) {
-        const int e = e0 + threadIdx.x;
+    for (int e0 = 0; e0 < a.experts; e0 += W) {
+        const int e = e0 + col;
         int c = 0;
         float s = 0;
         if (e < a.experts)
-            for (int b = 0; b < blocks; b++) {
+#pragma unroll 8
+            for (int b = share; b < blocks; b += kShares) {
                 c += a.parts[(int64_t)b * (a.experts + 1) + e];
                 s += a.sums[(int64_t)b * a.experts + e];
             }
+        fs[share][col] = s, fc[share][col] = c;
+        __syncthreads();
+        s = 0, c = 0, rows = 0;
+#pragma unroll
+        for (int i = 0; i < 16; i++) rows += fr[i];
+        if (share == 0) {
+#pragma unroll
+            for (int i = 0; i < kShares; i++) s += fs[i][col], c += fc[i][col];
+        }
         int run = c;
 #pragma unroll
         for (int d = 1; d < 64; d *= 2) {
@@ -168,8 +217,8 @@ __global__ void __launch_bounds__(1024) finish_kernel(Args a, int blocks)
         __syncthreads();
         int before = carry;
         for (int i = 0; i < wave; i++) before += scan[i];
-        if (threadIdx.x == 1023) carry_of = before + run;
-        if (e < a.experts) {
+        if (threadIdx.x == W - 1) carry_of = before + run;
+        if (share == 0 && e < a.experts) {
             a.counts[e] = c;
             const float mean = rows ? s / (float)rows : 0.0f;
             if (a.mean) a.mean[e] = mean;
@@ -194,7 +243,7 @@ __global__ void __launch_bounds__(1024) finish_kernel(Args a, int blocks)
 // Every workgroup forms C from the counts by itself.
 template <typename T, int G, int K> __global__ void __launch_bounds__(256) backward_kernel(Args a)
 {
-    constexpr int kRows = 256 / G;
+    constexpr int kRows = 256 / G, kAhead = K <= 4 ? 4 : K <= 8 ? 2 : 1;
     __shared__ double all[4];
     const int lane = threadIdx.x % G;
     double total = 0;
@@ -208,25 +257,42 @@ template <typename T, int G, int K> __global__ void __launch_bounds__(256) backw
     const float factor = total > 0 && rows > 0 ? (float)((double)a.scale * (a.dloss ? (double)*a.dloss : 1.0) * a.experts / (total * rows)) : 0.0f;
     float c[K];
 #pragma unroll
-    for (int k = 0; k < K; k++) c[k] = k * G + lane < a.experts ? (float)a.counts[k * G + lane] : 0.0f;
+    for (int k = 0; k < K; k++) c[k] = lane * K + k < a.experts ? (float)a.counts[lane * K + k] : 0.0f;
     const int64_t step = (int64_t)gridDim.x * kRows;
-    for (int64_t r = (int64_t)blockIdx.x * kRows + threadIdx.x / G; r < a.t; r += step) {
-        float z[K], add[K];
-        load_row<T, G, K>((const T *)a.logits + r * a.ldl, a.experts, true, z);
+    for (int64_t r0 = (int64_t)blockIdx.x * kRows + threadIdx.x / G; r0 < a.t; r0 += step * kAhead) {
+        float z[kAhead][K], add[kAhead][K];
+        bool some[kAhead];
 #pragma unroll
-        for (int k = 0; k < K; k++)
-            add[k] = a.residual && k * G + lane < a.experts ? (float)((const T *)a.residual)[r * a.ldr + k * G + lane] : 0.0f;
-        const bool some = row_counts(a, r);
-        softmax<G, K>(z);
-        float dot = 0;
+        for (int n = 0; n < kAhead; n++) {
+            const int64_t r = min(r0 + n * step, a.t - 1);
+            load_row<T, K>((const T *)a.logits + r * a.ldl, lane * K, a.experts, -INFINITY, z[n]);
 #pragma unroll
-        for (int k = 0; k < K; k++) dot += z[k] * c[k];
+            for (int k = 0; k < K; k++) add[n][k] = 0;
+            if (a.residual) load_row<T, K>((const T *)a.residual + r * a.ldr, lane * K, a.experts, 0.0f, add[n]);
+            some[n] = has_pick(a, r);
+        }
 #pragma unroll
-        for (int d = G / 2; d; d /= 2) dot += __shfl_xor(dot, d);
-        T *out = (T *)a.dlogits + r * a.ldd;
+        for (int n = 0; n < kAhead; n++) {
+            const int64_t r = r0 + n * step;
+            if (r >= a.t) break;
+            softmax<G, K>(z[n]);
+            float dot = 0;
 #pragma unroll
-        for (int k = 0; k < K; k++)
-            if (k * G + lane < a.experts) out[k * G + lane] = (T)((some ? factor * z[k] * (c[k] - dot) : 0.0f) + add[k]);
+            for (int k = 0; k < K; k++) dot += z[n][k] * c[k];
+#pragma unroll
+            for (int d = G / 2; d; d /= 2) dot += __shfl_xor(dot, d);
+            T *out = (T *)a.dlogits + r * a.ldd + lane * K;
+            typename Some<T, K>::loose v;
+#pragma unroll
+            for (int k = 0; k < K; k++) v[k] = (T)((some[n] ? factor * z[n][k] * (c[k] - dot) : 0.0f) + add[n][k]);
+            if (lane * K + K <= a.experts) {
+                *(typename Some<T, K>::loose *)out = v;
+            } else {
+#pragma unroll
+                for (int k = 0; k < K; k++)
+                    if (lane * K + k < a.experts) out[k] = v[k];
+            }
+        }
     }
 }
 
@@ -253,13 +319,15 @@ static int launched(const char *what)
     return e == hipSuccess ? HEDDLE_OK : hip_fail(e, what);
 }
 
-constexpr int kFew = 8;                       // workgroups' sums that the last kernel adds up itself
+// Experts up to which the last kernel adds up the workgroups' sums itself, 16 shares a column: past that
+// one workgroup would read for longer than another launch takes.
+constexpr int kNarrow = 64;
 
 static int64_t blocks_of(int experts, int64_t t)
 {
     int64_t rows = 1;
     with_shape(experts, [&](auto g, auto) { rows = 256 / g; });
-    return std::max<int64_t>(1, std::min<int64_t>((t + rows - 1) / rows, 1024));
+    return std::max<int64_t>(1, std::min<int64_t>((t + rows - 1) / rows, 512));
 }
 
 template <typename T> static int forward(Args a, Scratch &s, bool run, hipStream_t stream)
@@ -267,21 +335,23 @@ template <typename T> static int forward(Args a, Scratch &s, bool run, hipStream
     const int64_t blocks = blocks_of(a.experts, a.t);
     a.sums = (float *)s.take((size_t)blocks * a.experts * 4);
     a.parts = (int32_t *)s.take((size_t)blocks * (a.experts + 1) * 4);
-    float *few_sums = nullptr;
-    int32_t *few_parts = nullptr;
-    if (blocks > kFew) {
-        few_sums = (float *)s.take((size_t)kFew * a.experts * 4);
-        few_parts = (int32_t *)s.take((size_t)kFew * (a.experts + 1) * 4);
+    const bool fold = a.experts > kNarrow && blocks > 1;
+    float *sums = nullptr;
+    int32_t *parts = nullptr;
+    if (fold) {
+        sums = (float *)s.take((size_t)a.experts * 4);
+        parts = (int32_t *)s.take((size_t)(a.experts + 1) * 4);
     }
     if (!run) return HEDDLE_OK;
     with_shape(a.experts, [&](auto g, auto k) {
         hipLaunchKernelGGL((forward_kernel<T, g, k>), dim3((unsigned)blocks), dim3(256), 0, stream, a);
     });
-    if (blocks > kFew) {
-        hipLaunchKernelGGL(fold_kernel, dim3((unsigned)(a.experts / 256 + 1), kFew), dim3(256), 0, stream, a, (int)blocks, few_sums, few_parts);
-        a.sums = few_sums, a.parts = few_parts;
+    if (fold) {
+        hipLaunchKernelGGL(fold_kernel, dim3((unsigned)(a.experts / 32 + 1)), dim3(1024), 0, stream, a, (int)blocks, sums, parts);
+        a.sums = sums, a.parts = parts;
     }
-    hipLaunchKernelGGL(finish_kernel, dim3(1), dim3(1024), 0, stream, a, (int)std::min<int64_t>(blocks, kFew));
+    if (a.experts <= kNarrow) hipLaunchKernelGGL(finish_kernel<kNarrow>, dim3(1), dim3(1024), 0, stream, a, (int)blocks);
+    else hipLaunchKernelGGL(finish_kernel<1024>, dim3(1), dim3(1024), 0, stream, a, 1);
     return launched("expert balance");
 }
 

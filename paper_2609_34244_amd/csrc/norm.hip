@@ -39,10 +39,14 @@ template <typename T> struct Piece {
 // the values from column c on, those past the row's end 0
 template <typename T> __device__ inline typename Piece<T>::type load(const T *row, int c, int n)
 {
-    typename Piece<T>::type v;
+    typename Piece<T>::type v = {};
     if (c + Piece<T>::V <= n) return *(const typename Piece<T>::loose *)(row + c);
+    if (c >= n) return v;
+    // a row's end: loads of which none waits for a test
 #pragma unroll
-    for (int i = 0; i < Piece<T>::V; i++) v[i] = c + i < n ? row[c + i] : (T)0.0f;
+    for (int i = 0; i < Piece<T>::V; i++) v[i] = row[min(c + i, n - 1)];
+#pragma unroll
+    for (int i = 1; i < Piece<T>::V; i++) v[i] = c + i < n ? v[i] : (T)0.0f;
     return v;
 }
 template <typename T> __device__ inline void store(T *row, int c, int n, typename Piece<T>::type v)
