@@ -206,6 +206,22 @@ template <typename T> __device__ inline typename mm::pack8<T>::type pack(const f
     return x;
 }
 
+// sixteen values as the next product's operands, two a word, each formed where it is set
+template <typename T> struct Words {
+    unsigned word[8];
+    HEDDLE_INLINE void set(int i, float x, float y)
+    {
+        const typename Pair<T>::type v = {(T)x, (T)y};
+        word[i] = __builtin_bit_cast(unsigned, v);
+        here(word[i]);
+    }
+    HEDDLE_INLINE typename mm::pack8<T>::type half(int k) const
+    {
+        typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+        return __builtin_bit_cast(typename mm::pack8<T>::type, u32x4{word[4 * k], word[4 * k + 1], word[4 * k + 2], word[4 * k + 3]});
+    }
+};
+
 // row of a 32 x 32 product's register r
 __device__ inline int mfma_row(int r, int h) { return 8 * (r >> 2) + 4 * h + (r & 3); }
 
@@ -358,7 +374,7 @@ int mode_of(const heddle_attention_desc *d);
 // the launches; mode: of enum Mode
 void launch_forward(const heddle_attention_desc *d, const Args &a, int rows, int64_t blocks, int64_t tiles, hipStream_t stream);
 void launch_rows(const heddle_attention_desc *d, const Args &a, int64_t blocks, int64_t tiles, hipStream_t stream);
-void launch_keys(const heddle_attention_desc *d, const Args &a, int64_t blocks, int64_t tiles, hipStream_t stream);
+void launch_keys(const heddle_attention_desc *d, const Args &a, bool pairs, int64_t blocks, int64_t tiles, hipStream_t stream);
 
 // f(type, padded head width, mode) as constants
 template <typename F> void with_kind(const heddle_attention_desc *d, F f)

@@ -23,47 +23,31 @@ HEDDLE_INLINE f32x16 four(const float *p)
     return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7, 8, 9, 10, 11, 12, 13, 14, 15);
 }
 
-// P and dS of 32 x 32 scores. INIT: the products' sums started from -delta and, without a cap or slopes, from
-// -lse / scale. at: distance from register 0's key or row (the sign does not matter); seen(r): whether register r's
-// pair is visible; start of four registers: cap log2(e) - lse log2(e); delta by register.
-// The cap's derivative is 1 - tanh^2 = 4 (r - r^2), r = 1 / (1 + e^u); kLift of the 4 is taken here, the rest by scale_of().
-template <typename T> constexpr float kLift = sizeof(T) == 2 && __is_same(T, _Float16) ? 4.0f : 1.0f;   // float16 has no range to spare
+// The cap's derivative is 1 - tanh^2 = 4 (x - x^2), x = 1 / (1 + e^u); kLift of the 4 is taken here, the rest by scale_of().
+template <typename T> constexpr float kLift = __is_same(T, _Float16) ? 4.0f : 1.0f;   // float16 has no range to spare
 template <typename T, int MODE> __device__ inline float scale_of(const Args &a) { return MODE & kCap ? a.scale * (4.0f / kLift<T>) : a.scale; }
 
-template <typename T, int MODE, bool INIT, bool MASKED, typename Seen, typename Start, typename Delta>
-HEDDLE_INLINE void weigh(const Args &a, f32x16 &s, f32x16 &dp, float slope2, int at, Seen seen, Start start, Delta delta)
+// A probability from a score, and P times the cap's derivative where there is one. start: what
+// the exponent starts from, cap log2(e) - lse log2(e) (READY: the score's sum started from -lse / scale instead).
+// distance: from register 0's key or row (the sign does not matter).
+template <typename T, int MODE, bool READY> HEDDLE_INLINE float2 weigh(const Args &a, float s, int r, float start, float slope2, float distance, bool seen)
 {
-    if constexpr (!INIT) each<16>([&](int r) { dp[r] -= delta(r); });
+    float w = 1;
     if constexpr (MODE == kPlain) {
-        each<4>([&](int q) {
-            mm::f32x4 l = {};
-            if constexpr (!INIT) l = start(q);
-            each<4>([&](int n) { s[4 * q + n] = __builtin_amdgcn_exp2f(INIT ? s[4 * q + n] * a.scale2 : __builtin_fmaf(s[4 * q + n], a.scale2, l[n])); });
-        });
+        s = READY ? s * a.scale2 : __builtin_fmaf(s, a.scale2, start);
+    } else if constexpr (MODE & kCap) {
+        const float x = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(s * a.scale2));
+        s = __builtin_fmaf(-2.0f * a.cap2, x, start);
+        w = __builtin_fmaf(-x, x, x);
     } else {
-        if constexpr (MODE & kCap) {
-            each<4>([&](int q) {
-                const mm::f32x4 l = start(q);
-                each<4>([&](int n) {
-                    const float x = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(s[4 * q + n] * a.scale2));
-                    s[4 * q + n] = __builtin_fmaf(-2.0f * a.cap2, x, l[n]);
-                    dp[4 * q + n] *= kLift<T> * __builtin_fmaf(-x, x, x);
-                });
-            });
-        } else {
-            each<4>([&](int q) {
-                const mm::f32x4 l = start(q);
-                each<4>([&](int n) { s[4 * q + n] = __builtin_fmaf(s[4 * q + n], a.scale2, l[n]); });
-            });
-        }
-        if constexpr (MODE & kSlopes) {
-            const float from = (float)at;
-            each<16>([&](int r) { s[r] = __builtin_fmaf(-slope2, fabsf(from - (float)(8 * (r >> 2) + (r & 3))), s[r]); });
-        }
-        each<16>([&](int r) { s[r] = __builtin_amdgcn_exp2f(s[r]); });
+        s = __builtin_fmaf(s, a.scale2, start);
     }
-    if constexpr (MASKED) each<16>([&](int r) { s[r] = seen(r) ? s[r] : 0.0f; });
-    each<16>([&](int r) { dp[r] *= s[r]; });
+    if constexpr (MODE & kSlopes) s = __builtin_fmaf(-slope2, fabsf(distance - (float)(8 * (r >> 2) + (r & 3))), s);
+    float p = __builtin_amdgcn_exp2f(s);
+    p = seen ? p : 0.0f;
+    float pw = MODE & kCap ? p * (kLift<T> * w) : p;
+    here(pw);
+    return {p, pw};
 }
 
 template <typename T, int DP, int MODE> __global__ void __launch_bounds__(256, 2) rows_kernel(Args a, int64_t tiles)
@@ -144,25 +128,37 @@ template <typename T, int DP, int MODE> __global__ void __launch_bounds__(256, 2
         mm::arrive();
         if (t + 1 < count) load(t + 1);
     };
+    // Products of 32 keys, in this order: scores, dP, dq. Probabilities are formed between dP's; operands are read ahead.
     auto add = [&](int t, auto masked) __attribute__((always_inline)) {
         const char *tk = smem[t & 1], *tv = tk + Tk::kBytes;
-#pragma unroll
-        for (int c = 0; c < 2; c++) {
-            f32x16 p = {}, ds = {};
-#pragma unroll
-            for (int k = 0; k < DP / 16; k++) p = mfma(row_fragment<DP, T>(tk, places, c * 32, k), qf[k], p);
-#pragma unroll
-            for (int k = 0; k < DP / 16; k++) ds = mfma(row_fragment<DP, T>(tv, places, c * 32, k), gf[k], ds);
+        constexpr int N = DP / 16, kAhead = 4, M = 16 / N;      // N products each; M scores to a product
+        each<2>([&](int c) __attribute__((always_inline)) {
             const int first = t * 64 + c * 32 + 4 * h;
-            weigh<T, MODE, false, decltype(masked)::value>(a, p, ds, slope2, i + shift - first, [&](int n) { return first + mfma_row(n, 0) < limit; },
-                                                          [&](int) { return mm::f32x4{base, base, base, base}; }, [&](int) { return delta; });
-#pragma unroll
-            for (int k = 0; k < 2; k++) {
-                const frag b = pack<T>(ds, 8 * k);
-#pragma unroll
-                for (int d = 0; d < DP / 32; d++) dq[d] = mfma(column_fragment<DP, T>(tk, places, c * 32 + 16 * k, d), b, dq[d]);
-            }
-        }
+            const float distance = (float)(i + shift - first);
+            f32x16 p = {}, ds = {};
+            Words<T> w;
+            frag f[kAhead];
+            auto fetch = [&](int n) __attribute__((always_inline)) {
+                f[n % kAhead] = n < N ? row_fragment<DP, T>(tk, places, c * 32, n) : n < 2 * N ? row_fragment<DP, T>(tv, places, c * 32, n - N) :
+                                column_fragment<DP, T>(tk, places, c * 32 + 16 * ((n - 2 * N) / (DP / 32)), (n - 2 * N) % (DP / 32));
+            };
+            each<kAhead - 1>([&](int n) __attribute__((always_inline)) { fetch(n); });
+            each<3 * N>([&](int n) __attribute__((always_inline)) {
+                if (n + kAhead - 1 < 3 * N) fetch(n + kAhead - 1);
+                if (n < N) p = mfma(f[n % kAhead], qf[n], p);
+                else if (n < 2 * N) {
+                    ds = mfma(f[n % kAhead], gf[n - N], ds);
+                    each<M>([&](int m) __attribute__((always_inline)) {
+                        const int r = (n - N) * M + m;
+                        p[r] = weigh<T, MODE, false>(a, p[r], r, base, slope2, distance, !decltype(masked)::value || first + mfma_row(r, 0) < limit).y;
+                    });
+                } else {
+                    if (n == 2 * N) each<8>([&](int m) __attribute__((always_inline)) { w.set(m, p[2 * m] * (ds[2 * m] - delta), p[2 * m + 1] * (ds[2 * m + 1] - delta)); });
+                    dq[(n - 2 * N) % (DP / 32)] = mfma(f[n % kAhead], w.half((n - 2 * N) / (DP / 32)), dq[(n - 2 * N) % (DP / 32)]);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            });
+        });
     };
     // tiles seen whole, in part, and by other wavefronts alone: see the forward pass
     const int open = min(whole / 64, count), some = min((mine + 63) / 64, count);
@@ -186,38 +182,36 @@ template <typename T, int DP, int MODE> __global__ void __launch_bounds__(256, 2
             store4<T>(out, d * 32 + mfma_row(n, h), a.dim, a.out_vec, dq[d][n] * sc, dq[d][n + 1] * sc, dq[d][n + 2] * sc, dq[d][n + 3] * sc);
 }
 
-template <typename T, int DP, int MODE> __global__ void __launch_bounds__(256, 2) keys_kernel(Args a, int64_t tiles)
+// NW 8: two tiles of 128 keys a workgroup, the sequence's p-th and p-th from the end, which together see as many rows as
+// any other such pair, and share the rows' tiles.
+template <typename T, int DP, int MODE, int NW> __global__ void __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2))) keys_kernel(Args a, int64_t tiles)
 {
-    constexpr int kRows = 32;
-    typedef Tile<DP, kRows, 4> Tk;
+    constexpr int kRows = DP == 64 && NW == 8 ? 64 : 32;
+    typedef Tile<DP, kRows, NW> Tk;
     typedef typename mm::pack8<T>::type frag;
     __shared__ __align__(1024) char smem[2][2 * Tk::kBytes];
     typedef Tile<DP, 128, 4> Tv;
-    __shared__ __align__(1024) char values[Tv::kBytes];
+    __shared__ __align__(1024) char values[NW / 4][Tv::kBytes];
     __shared__ __align__(16) float stats[2][2][kRows];      // what the exponents, or the scores' sums, start from; -delta
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, h = lane >> 5, col = lane & 31;
     const int hk = blockIdx.x % (uint32_t)a.kv_heads;
-    // The first tiles, which the most rows see, first. Where all workgroups find a place at once, two a CU, the second
-    // half in reverse: a CU's two then have as much to do as another's (4 sequences of 2048, 64 heads on 8: 1118 us without).
-    int64_t slot = blockIdx.x / (uint32_t)a.kv_heads;
-    const int64_t slots = gridDim.x / (uint32_t)a.kv_heads, half = 256 / (uint32_t)a.kv_heads;
-    if (slots <= 2 * half && slot >= half) slot = half + (slots - 1 - slot);
+    const int64_t slot = blockIdx.x / (uint32_t)a.kv_heads; // the first tiles, which the most rows see, first
     int s;
     int64_t tile;
     if (a.packed) {
-        if (!find_slot(a.d_k, a.k_rows, 1, a.sequences, 1, 128, tiles, slot, s, tile)) return;
+        if (!find_slot(a.d_k, a.k_rows, 1, a.sequences, 1, 32 * NW, tiles, slot, s, tile)) return;
     } else {
         s = (int)((uint32_t)slot % (uint32_t)a.sequences), tile = (uint32_t)slot / (uint32_t)a.sequences;
     }
     const Sequence q = sequence_of(a, s);
-    if (tile * 128 >= q.lk) return;
-    const int j0 = (int)tile * 128, j = j0 + wave * 32 + col, shift = q.lk - q.lq;
-    const bool any = j < q.lk;
+    if (tile * (32 * NW) >= q.lk) return;
+    const int team = wave >> 2, last_tile = (q.lk + 127) / 128 - 1, own = team ? last_tile - (int)tile : (int)tile;
+    const int j0 = own * 128, w0 = j0 + (wave & 3) * 32, j = w0 + col, shift = q.lk - q.lq;   // the wavefront's keys: w0 on
+    const bool busy = w0 < q.lk && (team == 0 || own > (int)tile), any = busy && j < q.lk;
     // the first row of a head that sees a key
     auto first_of = [&](int key) { return a.causal && key >= q.prefix ? max(key - shift, 0) : 0; };
-    const int from = first_of(j), start = first_of(j0) / kRows * kRows;
-    const int w0 = j0 + wave * 32;                          // the wavefront's keys: all seen from row `whole` on
-    const int whole = __builtin_amdgcn_readfirstlane(first_of(w0 + 31)), mine = w0 < q.lk ? __builtin_amdgcn_readfirstlane(first_of(w0)) : INT32_MAX;
+    const int from = first_of(j), start = first_of((int)tile * 128) / kRows * kRows;
+    const int whole = __builtin_amdgcn_readfirstlane(first_of(w0 + 31)), mine = busy ? __builtin_amdgcn_readfirstlane(first_of(w0)) : INT32_MAX;
     const int per = q.lq > start ? (q.lq - start + kRows - 1) / kRows : 0, count = per * a.group;
 
     const T *pk = (const T *)a.k.p + s * a.k.seq + (q.k0 + j) * a.k.row + hk * a.k.head;
@@ -226,10 +220,10 @@ template <typename T, int DP, int MODE> __global__ void __launch_bounds__(256, 2
 #pragma unroll
     for (int k = 0; k < DP / 16; k++) kf[k] = global_fragment<T>(pk, k * 16 + 8 * h, a.dim, any);
     if (count) {
-        const uint32_t to = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)&values[0] + wave * 1024;
+        const uint32_t to = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)&values[team][0] + (wave & 3) * 1024;
         const i32x4 bv = buffer_at(pv);
 #pragma unroll
-        for (int n = 0; n < Tv::kLoads; n++) mm::load_to_lds(bv, Tv::offset(n, wave, a.v.row, a.dim, q.lk - j0), to + n * 4096);
+        for (int n = 0; n < Tv::kLoads; n++) mm::load_to_lds(bv, Tv::offset(n, wave & 3, a.v.row, a.dim, q.lk - j0), to + n * 4096);
     }
     int oq[Tk::kLoads], og[Tk::kLoads];
 #pragma unroll
@@ -246,8 +240,8 @@ template <typename T, int DP, int MODE> __global__ void __launch_bounds__(256, 2
         if ((int)threadIdx.x < min(valid, kRows)) stat = a.rows[(int64_t)head * a.q_rows + row0 + i0 + threadIdx.x];
 #pragma unroll
         for (int m = 0; m < Tk::kLoads; m++) {
-            mm::load_to_lds(bq, valid >= kRows ? oq[m] : Tk::offset(m, wave, a.q.row, a.dim, valid), to + m * 4096);
-            mm::load_to_lds(bg, valid >= kRows ? og[m] : Tk::offset(m, wave, a.dy.row, a.dim, valid), to + Tk::kBytes + m * 4096);
+            mm::load_to_lds(bq, valid >= kRows ? oq[m] : Tk::offset(m, wave, a.q.row, a.dim, valid), to + m * (NW * 1024));
+            mm::load_to_lds(bg, valid >= kRows ? og[m] : Tk::offset(m, wave, a.dy.row, a.dim, valid), to + Tk::kBytes + m * (NW * 1024));
         }
     };
     auto keep = [&](int n) {
@@ -255,7 +249,7 @@ template <typename T, int DP, int MODE> __global__ void __launch_bounds__(256, 2
     };
     Places places;
     places.set<DP>();
-    const char *mine_values = values + wave * (32 * DP * 2);
+    const char *mine_values = values[team] + (wave & 3) * (32 * DP * 2);
     f32x16 dk[DP / 32], dv[DP / 32];
 #pragma unroll
     for (int d = 0; d < DP / 32; d++) dk[d] = f32x16{}, dv[d] = f32x16{};
@@ -272,27 +266,55 @@ template <typename T, int DP, int MODE> __global__ void __launch_bounds__(256, 2
         n++;
         if (n < count) keep(n);
     };
+    // Products of 32 rows, in this order: scores, dP, dv, dk. Probabilities are formed between dP's, dS between dv's;
+    // operands are read ahead.
     auto add = [&](int i, float slope2, auto masked) __attribute__((always_inline)) {
         const char *tq = smem[slot_of], *tg = tq + Tk::kBytes;
-        const float *ls = &stats[slot_of][0][4 * h], *de = &stats[slot_of][1][4 * h];
-        f32x16 p = {}, ds = four(de);
-        if constexpr (MODE == kPlain) p = four(ls);
-#pragma unroll
-        for (int k = 0; k < DP / 16; k++) p = mfma(row_fragment<DP, T>(tq, places, 0, k), kf[k], p);
-#pragma unroll
-        for (int k = 0; k < DP / 16; k++) ds = mfma(row_fragment<DP, T>(tg, places, 0, k), row_fragment<DP, T>(mine_values, places, 0, k), ds);
-        const int first = i + 4 * h;
-        weigh<T, MODE, true, decltype(masked)::value>(a, p, ds, slope2, j - shift - first, [&](int r) { return first + mfma_row(r, 0) >= from; },
-                                                     [&](int q) { return *(const mm::f32x4 *)(ls + 8 * q); }, [](int) { return 0.0f; });
-#pragma unroll
-        for (int k = 0; k < 2; k++) {
-            const frag bp = pack<T>(p, 8 * k), bs = pack<T>(ds, 8 * k);
-#pragma unroll
-            for (int d = 0; d < DP / 32; d++) {
-                dv[d] = mfma(column_fragment<DP, T>(tg, places, 16 * k, d), bp, dv[d]);
-                dk[d] = mfma(column_fragment<DP, T>(tq, places, 16 * k, d), bs, dk[d]);
-            }
-        }
+        constexpr int N = DP / 16, kAhead = 3, M = 16 / N;      // N products each; M scores to a product
+        each<kRows / 32>([&](int c) __attribute__((always_inline)) {
+            const float *ls = &stats[slot_of][0][c * 32 + 4 * h], *de = &stats[slot_of][1][c * 32 + 4 * h];
+            const int first = i + c * 32 + 4 * h;
+            const float distance = (float)(j - shift - first);
+            f32x16 p = {}, ds;
+            if constexpr (MODE == kPlain) p = four(ls);
+            mm::f32x4 l = {};
+            Words<T> wp, ws;
+            frag f[kAhead], v[kAhead];
+            auto fetch = [&](int n) __attribute__((always_inline)) {
+                const int k = (n - 2 * N) % N / (DP / 32) * 16, d = (n - 2 * N) % (DP / 32);
+                f[n % kAhead] = n < N ? row_fragment<DP, T>(tq, places, c * 32, n) : n < 2 * N ? row_fragment<DP, T>(tg, places, c * 32, n - N) :
+                                column_fragment<DP, T>(n < 3 * N ? tg : tq, places, c * 32 + k, d);
+                if (n >= N && n < 2 * N) v[n % kAhead] = row_fragment<DP, T>(mine_values, places, 0, n - N);
+            };
+            each<kAhead - 1>([&](int n) __attribute__((always_inline)) { fetch(n); });
+            each<4 * N>([&](int n) __attribute__((always_inline)) {
+                if (n + kAhead - 1 < 4 * N) fetch(n + kAhead - 1);
+                const int k = (n - 2 * N) % N / (DP / 32), d = (n - 2 * N) % (DP / 32);
+                if (n < N) {
+                    p = mfma(f[n % kAhead], kf[n], p);
+                    if (n == N - 1) ds = four(de);
+                } else if (n < 2 * N) {
+                    ds = mfma(f[n % kAhead], v[n % kAhead], ds);
+                    each<M / 2>([&](int m) __attribute__((always_inline)) {
+                        const int r = (n - N) * M + 2 * m;
+                        if (MODE != kPlain && (r & 3) == 0) l = *(const mm::f32x4 *)(ls + 2 * r);
+                        const float2 x = weigh<T, MODE, true>(a, p[r], r, l[r & 3], slope2, distance, !decltype(masked)::value || first + mfma_row(r, 0) >= from);
+                        const float2 y = weigh<T, MODE, true>(a, p[r + 1], r + 1, l[(r + 1) & 3], slope2, distance, !decltype(masked)::value || first + mfma_row(r + 1, 0) >= from);
+                        wp.set(r / 2, x.x, y.x);
+                        p[r] = x.y, p[r + 1] = y.y;
+                    });
+                } else if (n < 3 * N) {
+                    dv[d] = mfma(f[n % kAhead], wp.half(k), dv[d]);
+                    each<M / 2>([&](int m) __attribute__((always_inline)) {
+                        const int r = (n - 2 * N) * M + 2 * m;
+                        ws.set(r / 2, p[r] * ds[r], p[r + 1] * ds[r + 1]);
+                    });
+                } else {
+                    dk[d] = mfma(f[n % kAhead], ws.half(k), dk[d]);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            });
+        });
     };
     if (count) {
         for (int g = 0; g < a.group; g++) {
@@ -331,10 +353,11 @@ void launch_rows(const heddle_attention_desc *d, const Args &a, int64_t blocks, 
         hipLaunchKernelGGL((rows_kernel<decltype(t), dp, mode>), dim3((unsigned)blocks), dim3(256), 0, stream, a, tiles);
     });
 }
-void launch_keys(const heddle_attention_desc *d, const Args &a, int64_t blocks, int64_t tiles, hipStream_t stream)
+void launch_keys(const heddle_attention_desc *d, const Args &a, bool pairs, int64_t blocks, int64_t tiles, hipStream_t stream)
 {
     with_kind(d, [&](auto t, auto dp, auto mode) {
-        hipLaunchKernelGGL((keys_kernel<decltype(t), dp, mode>), dim3((unsigned)blocks), dim3(256), 0, stream, a, tiles);
+        if (pairs) hipLaunchKernelGGL((keys_kernel<decltype(t), dp, mode, 8>), dim3((unsigned)blocks), dim3(512), 0, stream, a, tiles);
+        else hipLaunchKernelGGL((keys_kernel<decltype(t), dp, mode, 4>), dim3((unsigned)blocks), dim3(256), 0, stream, a, tiles);
     });
 }
 
@@ -353,13 +376,14 @@ int backward(const heddle_attention_desc *d, mm::Scratch &s, bool run, hipStream
     auto aligned = [&](const void *p, const View &v) { return !((uintptr_t)p & 7) && !((v.seq | v.row | v.head | d->dim) & 3); };
     a.out_vec = (!d->dq || aligned(d->dq, a.dq)) && (!d->dk || (aligned(d->dk, a.dk) && aligned(d->dv, a.dv)));
     const int64_t blocks = a.q_rows ? slots_of(d->packed, d->sequences, d->q_len, d->q_len, a.group, 128) * d->kv_heads : 0;
-    const int64_t tiles = (d->q_len * a.group + 127) / 128, ktiles = (d->k_len + 127) / 128;
-    const int64_t kblocks = d->dk && a.k_rows ? slots_of(d->packed, d->sequences, d->k_len, d->k_len, 1, 128) * d->kv_heads : 0;
+    const bool pairs = a.k_rows / d->sequences >= 512;
+    const int64_t tiles = (d->q_len * a.group + 127) / 128, span = pairs ? 256 : 128, ktiles = (d->k_len + span - 1) / span;
+    const int64_t kblocks = d->dk && a.k_rows ? slots_of(d->packed, d->sequences, d->k_len, d->k_len, 1, span) * d->kv_heads : 0;
     if (std::max(blocks, kblocks) > (int64_t(1) << 24) - 1) return fail(HEDDLE_E_RANGE, "more tiles than a launch holds");
     if (!run) return HEDDLE_OK;
     if (const int rc = c.launch(stream)) return rc;
     if (blocks) launch_rows(d, a, blocks, tiles, stream);
-    if (kblocks) launch_keys(d, a, kblocks, ktiles, stream);
+    if (kblocks) launch_keys(d, a, pairs, kblocks, ktiles, stream);
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? HEDDLE_OK : hip_fail(e, "attention's gradients");
 }

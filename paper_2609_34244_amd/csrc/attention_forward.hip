@@ -13,7 +13,7 @@ template <typename T, int MODE, bool MASKED> struct Softening {
     int first, limit;
     float distance, slope, top, was, base, sum = 0;
     bool follow;
-    unsigned words[8];
+    Words<T> words;
     HEDDLE_INLINE void part(int u)
     {
         const float unit = unit_of<MODE>(a);
@@ -35,17 +35,9 @@ template <typename T, int MODE, bool MASKED> struct Softening {
             const int r = 2 * (u - 5);
             const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], unit, -base)), y = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r + 1], unit, -base));
             sum += x + y;
-            typename Pair<T>::type v = {(T)x, (T)y};
-            unsigned word = __builtin_bit_cast(unsigned, v);
-            here(word);
+            words.set(r >> 1, x, y);
             here(sum);
-            words[r >> 1] = word;
         }
-    }
-    HEDDLE_INLINE typename mm::pack8<T>::type half(int k) const
-    {
-        typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
-        return __builtin_bit_cast(typename mm::pack8<T>::type, u32x4{words[4 * k], words[4 * k + 1], words[4 * k + 2], words[4 * k + 3]});
     }
 };
 
@@ -143,7 +135,7 @@ template <typename T, int DP, int MODE, int NW> __global__ void __launch_bounds_
         });
         if (v.follow) rescale<MODE>(a, st, v.was);
         st.l += v.sum;
-        was_p[0] = v.half(0), was_p[1] = v.half(1);
+        was_p[0] = v.words.half(0), was_p[1] = v.words.half(1);
     };
     auto tile_of = [&](int t, auto masked) __attribute__((always_inline)) {
         const int j0 = (count - 1 - t) * 64;
