@@ -367,6 +367,35 @@ template <typename T> __device__ inline void store4(T *p, int col, int dim, int 
         if (col + i < dim) p[col + i] = v[i];
 }
 
+// A row of 32 x 32 products, factor times the lane's sums: lane l and l + 32 hold fours of the row's values in turn; they
+// exchange half of them, so that each has eight side by side.
+template <typename T, int DP> HEDDLE_INLINE void store_row(T *p, const f32x16 *o, float factor, int dim, int vec)
+{
+    const int h = (threadIdx.x & 63) >> 5;
+#pragma unroll
+    for (int d = 0; d < DP / 32; d++)
+#pragma unroll
+        for (int q = 0; q < 4; q += 2) {
+            unsigned w[4];
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                const typename Pair<T>::type v = {(T)(o[d][4 * q + 2 * i] * factor), (T)(o[d][4 * q + 2 * i + 1] * factor)};
+                w[i] = __builtin_bit_cast(unsigned, v);
+            }
+#ifdef __HIP_DEVICE_COMPILE__
+            asm("s_nop 1\n\tv_permlane32_swap_b32 %0, %1\n\tv_permlane32_swap_b32 %2, %3" : "+v"(w[0]), "+v"(w[2]), "+v"(w[1]), "+v"(w[3]));
+#endif
+            const int col = d * 32 + q * 8 + 8 * h;
+            if (vec) {
+                if (col < dim) __builtin_memcpy(__builtin_assume_aligned(p + col, 16), w, 16);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; i++)
+                    if (col + i < dim) p[col + i] = __builtin_bit_cast(T, (uint16_t)(w[i >> 1] >> (i & 1) * 16));
+            }
+        }
+}
+
 int check(const heddle_attention_desc *d, bool backward);
 int check_overlaps(const heddle_attention_desc *d, bool backward);
 Args base_args(const heddle_attention_desc *d);
@@ -374,7 +403,7 @@ int mode_of(const heddle_attention_desc *d);
 // the launches; mode: of enum Mode
 void launch_forward(const heddle_attention_desc *d, const Args &a, int rows, int64_t blocks, int64_t tiles, hipStream_t stream);
 void launch_rows(const heddle_attention_desc *d, const Args &a, int64_t blocks, int64_t tiles, hipStream_t stream);
-void launch_keys(const heddle_attention_desc *d, const Args &a, bool pairs, int64_t blocks, int64_t tiles, hipStream_t stream);
+void launch_keys(const heddle_attention_desc *d, const Args &a, int span, int64_t blocks, int64_t tiles, hipStream_t stream);
 
 // f(type, padded head width, mode) as constants
 template <typename F> void with_kind(const heddle_attention_desc *d, F f)

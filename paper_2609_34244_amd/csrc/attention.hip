@@ -135,41 +135,50 @@ template <typename T, int DP, int MODE> __global__ void __launch_bounds__(256) s
     else if (a.lse) a.lse[out.at * a.heads + out.head] = sum == 0 ? -INFINITY : (top + __log2f(sum)) * kLn2;
 }
 
-// joins the parts of 32 rows
+// Joins the parts of a row, one wavefront a row: a lane has a part's maximum and sum (parts <= 64), then DP / 64
+// of the row's values, whose loads do not wait for each other (64 parts: 30 us when eight lanes took them in turn).
 template <typename T, int DP> __global__ void __launch_bounds__(256) combine_kernel(Args a, int64_t tiles)
 {
-    const int hk = blockIdx.x % (uint32_t)a.kv_heads;
-    const int64_t slot = blockIdx.x / (uint32_t)a.kv_heads;
+    constexpr int kValues = DP / 64;
+    typedef float vec __attribute__((ext_vector_type(kValues)));
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const uint32_t tile_id = blockIdx.x >> 3, slot = tile_id / (uint32_t)a.kv_heads;      // eight workgroups for 32 rows
+    const int mine = (blockIdx.x & 7) * 4 + wave, hk = tile_id - slot * a.kv_heads;
     int s;
     int64_t tile;
     if (!find_slot(a.d_q, a.q_rows, a.packed, a.sequences, a.group, 32, tiles, slot, s, tile)) return;
     const Sequence q = sequence_of(a, s);
-    if (tile * 32 >= (int64_t)q.lq * a.group) return;
-    const int mine = threadIdx.x >> 3, sub = threadIdx.x & 7;
+    if (tile * 32 + mine >= (int64_t)q.lq * a.group) return;
     const Row out = row_of(a, q, hk, (int)tile * 32 + mine);
-    if (!out.any) return;
-    const float *p = a.partial + ((slot * a.kv_heads + hk) * 32 + mine) * a.parts * (DP + 2);
-    float top = -INFINITY, sum = 0;
-    for (int i = 0; i < a.parts; i++) top = fmaxf(top, p[i * (DP + 2) + DP]);
-    float v[DP / 8];
+    const float *p = a.partial + (((int64_t)slot * a.kv_heads + hk) * 32 + mine) * a.parts * (DP + 2);
+    const bool any = lane < a.parts;
+    const float m = any ? p[lane * (DP + 2) + DP] : -INFINITY, l = any ? p[lane * (DP + 2) + DP + 1] : 0.0f;
+    constexpr int kAhead = 8;
+    vec x[kAhead], v = {};
+    auto fetch = [&](int from) __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < DP / 8; i++) v[i] = 0;
-#pragma unroll 2
-    for (int i = 0; i < a.parts; i++) {
-        const float *x = p + i * (DP + 2);
-        const float f = x[DP] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(x[DP] - top);
-        sum += f * x[DP + 1];
+        for (int i = 0; i < kAhead; i++) x[i] = *(const vec *)(p + min(from + i, a.parts - 1) * (DP + 2) + lane * kValues);
+    };
+    fetch(0);
+    float top = m;
 #pragma unroll
-        for (int c = 0; c < DP / 32; c++)
+    for (int d = 32; d; d /= 2) top = fmaxf(top, __shfl_xor(top, d));
+    const float f = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - top);
+    float sum = f * l;
 #pragma unroll
-            for (int k = 0; k < 4; k++) v[c * 4 + k] += f * x[c * 32 + sub * 4 + k];
+    for (int d = 32; d; d /= 2) sum += __shfl_xor(sum, d);
+    for (int from = 0; from < a.parts; from += kAhead) {
+        if (from) fetch(from);
+#pragma unroll
+        for (int i = 0; i < kAhead; i++)                    // (past the last part: a factor of zero; a part of no keys: zeros)
+            v += __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, f), min(from + i, 63))) * (from + i < a.parts ? x[i] : vec{});
     }
     const float inv = sum == 0 ? 0.0f : 1.0f / sum;
     T *y = (T *)a.y.p + s * a.y.seq + (q.q0 + out.i) * a.y.row + out.head * a.y.head;
 #pragma unroll
-    for (int c = 0; c < DP / 32; c++)
-        store4<T>(y, c * 32 + sub * 4, a.dim, a.out_vec, v[c * 4] * inv, v[c * 4 + 1] * inv, v[c * 4 + 2] * inv, v[c * 4 + 3] * inv);
-    if (a.lse && sub == 0) a.lse[out.at * a.heads + out.head] = sum == 0 ? -INFINITY : (top + __log2f(sum)) * kLn2;
+    for (int i = 0; i < kValues; i++)
+        if (lane * kValues + i < a.dim) y[lane * kValues + i] = (T)(v[i] * inv);
+    if (a.lse && lane == 0) a.lse[out.at * a.heads + out.head] = sum == 0 ? -INFINITY : (top + __log2f(sum)) * kLn2;
 }
 
 // ---- operands that do not lie on 16-byte boundaries ----
@@ -219,9 +228,12 @@ int mode_of(const heddle_attention_desc *d) { return (d->cap > 0 ? kCap : 0) | (
 Args base_args(const heddle_attention_desc *d)
 {
     Args a = {};
-    auto view = [&](const void *p, const int64_t *st) { return View{p, d->packed ? 0 : st[0], st[1], st[2]}; };
-    a.q = view(d->q, d->q_strides), a.k = view(d->k, d->k_strides), a.v = view(d->v, d->v_strides), a.y = view(d->y, d->y_strides);
-    a.dy = view(d->dy, d->dy_strides), a.dq = view(d->dq, d->dq_strides), a.dk = view(d->dk, d->dk_strides), a.dv = view(d->dv, d->dv_strides);
+    auto view = [&](const void *p, const int64_t *st, bool keys) {
+        return View{p, d->packed || d->sequences <= 1 ? 0 : st[0], (keys ? d->k_len : d->q_len) <= 1 ? 0 : st[1], (keys ? d->kv_heads : d->heads) == 1 ? 0 : st[2]};
+    };
+    a.q = view(d->q, d->q_strides, false), a.k = view(d->k, d->k_strides, true), a.v = view(d->v, d->v_strides, true);
+    a.y = view(d->y, d->y_strides, false), a.dy = view(d->dy, d->dy_strides, false), a.dq = view(d->dq, d->dq_strides, false);
+    a.dk = view(d->dk, d->dk_strides, true), a.dv = view(d->dv, d->dv_strides, true);
     a.lse = d->lse, a.d_q = d->d_q, a.d_k = d->d_k, a.d_prefix = d->d_prefix, a.d_slopes = d->d_slopes;
     a.q_rows = d->packed ? d->q_len : d->q_len * d->sequences, a.k_rows = d->packed ? d->k_len : d->k_len * d->sequences;
     a.sequences = d->sequences, a.q_len = (int32_t)d->q_len, a.k_len = (int32_t)d->k_len, a.packed = d->packed;
@@ -254,8 +266,8 @@ int check(const heddle_attention_desc *d, bool backward)
         if (rc || (keys ? k_all : q_all) == 0) return;
         const int64_t heads = keys ? d->kv_heads : d->heads;
         if (!p || ((uintptr_t)p & 1)) rc = fail(HEDDLE_E_INVAL, std::string(name) + " is NULL or not aligned to its values");
-        else if (st[1] < 0 || st[1] > HEDDLE_MAX_LD || st[2] < 0 || (!d->packed && st[0] < 0) || (heads > 1 && st[2] < d->dim) ||
-                 ((keys ? d->k_len : d->q_len) > 1 && st[1] < d->dim) || (!d->packed && d->sequences > 1 && st[0] < d->dim))
+        else if ((heads > 1 && st[2] < d->dim) || ((keys ? d->k_len : d->q_len) > 1 && (st[1] < d->dim || st[1] > HEDDLE_MAX_LD)) ||
+                 (!d->packed && d->sequences > 1 && st[0] < d->dim))
             rc = fail(HEDDLE_E_INVAL, std::string(name) + ": strides out of range");
     };
     tensor("q", d->q, d->q_strides, false);
@@ -312,12 +324,13 @@ static int launched(const char *what)
     return e == hipSuccess ? HEDDLE_OK : hip_fail(e, what);
 }
 
+// (the partial sums' rows lie on 8-byte boundaries: DP + 2 is even)
 static void launch_combine(const heddle_attention_desc *d, const Args &a, int64_t blocks, int64_t tiles, hipStream_t stream)
 {
     auto go = [&](auto t) {
         typedef decltype(t) T;
-        if (d->dim <= 64) hipLaunchKernelGGL((combine_kernel<T, 64>), dim3((unsigned)blocks), dim3(256), 0, stream, a, tiles);
-        else hipLaunchKernelGGL((combine_kernel<T, 128>), dim3((unsigned)blocks), dim3(256), 0, stream, a, tiles);
+        if (d->dim <= 64) hipLaunchKernelGGL((combine_kernel<T, 64>), dim3((unsigned)(blocks * 8)), dim3(256), 0, stream, a, tiles);
+        else hipLaunchKernelGGL((combine_kernel<T, 128>), dim3((unsigned)(blocks * 8)), dim3(256), 0, stream, a, tiles);
     };
     d->dtype == HEDDLE_T_BF16 ? go((__bf16)0.0f) : go((_Float16)0.0f);
 }
@@ -330,7 +343,7 @@ static int forward(const heddle_attention_desc *d, mm::Scratch &s, bool run, hip
     c.add(d, a.q, false, s);
     c.add(d, a.k, true, s);
     c.add(d, a.v, true, s);
-    a.out_vec = !((uintptr_t)d->y & 7) && !((a.y.seq | a.y.row | a.y.head | d->dim) & 3);
+    a.out_vec = !((uintptr_t)d->y & 15) && !((a.y.seq | a.y.row | a.y.head | d->dim) & 7);
     // rows of a key head in a sequence, on average
     const int64_t rows = std::max<int64_t>(1, a.q_rows * a.group / d->sequences), keys = a.k_rows / d->sequences;
     const bool split = rows <= 64;
@@ -340,10 +353,12 @@ static int forward(const heddle_attention_desc *d, mm::Scratch &s, bool run, hip
     a.parts = 1;
     if (split) {
         const int64_t used = std::max<int64_t>(1, d->sequences * ((rows + 31) / 32) * d->kv_heads);
-        a.parts = (int32_t)std::max<int64_t>(1, std::min<int64_t>({512 / used, keys / 256, 64}));
+        // One workgroup a CU at a time. Two rounds of them where there are many anyway: the sequences' lengths differ (32 of up
+        // to 8192 keys, 8 key heads: 126 us, 142 with one part each); one round else (8 of up to 4000: 23.5 us, 26.5 with twice the parts).
+        a.parts = (int32_t)std::max<int64_t>(1, std::min<int64_t>({(used >= 128 ? 512 : 256) / used, keys / 128, 64}));
         if (a.parts > 1) a.partial = (float *)s.take((size_t)blocks * 32 * a.parts * ((d->dim <= 64 ? 64 : 128) + 2) * 4);
     }
-    if (blocks * a.parts > (int64_t(1) << 24) - 1) return fail(HEDDLE_E_RANGE, "more tiles than a launch holds");
+    if (blocks * std::max(a.parts, 8) > (int64_t(1) << 24) - 1) return fail(HEDDLE_E_RANGE, "more tiles than a launch holds");
     if (!run) return HEDDLE_OK;
     if (const int rc = c.launch(stream)) return rc;
     if (!split) {

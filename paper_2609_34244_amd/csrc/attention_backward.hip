@@ -175,11 +175,58 @@ template <typename T, int DP, int MODE> __global__ void __launch_bounds__(256, 2
     if (!any) return;
     const float sc = scale_of<T, MODE>(a);
     T *out = (T *)a.dq.p + s * a.dq.seq + (q.q0 + i) * a.dq.row + head * a.dq.head;
-#pragma unroll
-    for (int d = 0; d < DP / 32; d++)
-#pragma unroll
-        for (int n = 0; n < 16; n += 4)
-            store4<T>(out, d * 32 + mfma_row(n, h), a.dim, a.out_vec, dq[d][n] * sc, dq[d][n + 1] * sc, dq[d][n + 2] * sc, dq[d][n + 3] * sc);
+    store_row<T, DP>(out, dq, sc, a.dim, a.out_vec);
+}
+
+// Adds 32 rows of a tile (from its row `sub` on) to the gradients of 32 keys and values. Products in this order: scores,
+// dP, dv, dk. Probabilities are formed between dP's, dS between dv's; operands are read ahead. ls, de: what the
+// exponents or the scores' sums start from, and -delta, of the lane's rows; first: its first row; from: the first row that sees its key.
+template <typename T, int DP, int MODE, bool MASKED, typename Value>
+HEDDLE_INLINE void gather(const Args &a, f32x16 *dk, f32x16 *dv, const char *tq, const char *tg, int sub, const float *ls, const float *de,
+                          const typename mm::pack8<T>::type *kf, Value value, const Places &places, int first, int from, int place, float slope2)
+{
+    constexpr int N = DP / 16, kAhead = 3, M = 16 / N;          // N products each; M scores to a product
+    typedef typename mm::pack8<T>::type frag;
+    const float distance = (float)(place - first);
+    f32x16 p = {}, ds;
+    if constexpr (MODE == kPlain) p = four(ls);
+    mm::f32x4 l = {};
+    Words<T> wp, ws;
+    frag f[kAhead], v[kAhead];
+    auto fetch = [&](int n) __attribute__((always_inline)) {
+        const int k = (n - 2 * N) % N / (DP / 32) * 16, d = (n - 2 * N) % (DP / 32);
+        f[n % kAhead] = n < N ? row_fragment<DP, T>(tq, places, sub, n) : n < 2 * N ? row_fragment<DP, T>(tg, places, sub, n - N) :
+                        column_fragment<DP, T>(n < 3 * N ? tg : tq, places, sub + k, d);
+        if (n >= N && n < 2 * N) v[n % kAhead] = value(n - N);
+    };
+    each<kAhead - 1>([&](int n) __attribute__((always_inline)) { fetch(n); });
+    each<4 * N>([&](int n) __attribute__((always_inline)) {
+        if (n + kAhead - 1 < 4 * N) fetch(n + kAhead - 1);
+        const int k = (n - 2 * N) % N / (DP / 32), d = (n - 2 * N) % (DP / 32);
+        if (n < N) {
+            p = mfma(f[n % kAhead], kf[n], p);
+            if (n == N - 1) ds = four(de);
+        } else if (n < 2 * N) {
+            ds = mfma(f[n % kAhead], v[n % kAhead], ds);
+            each<M / 2>([&](int m) __attribute__((always_inline)) {
+                const int r = (n - N) * M + 2 * m;
+                if (MODE != kPlain && (r & 3) == 0) l = *(const mm::f32x4 *)(ls + 2 * r);
+                const float2 x = weigh<T, MODE, true>(a, p[r], r, l[r & 3], slope2, distance, !MASKED || first + mfma_row(r, 0) >= from);
+                const float2 y = weigh<T, MODE, true>(a, p[r + 1], r + 1, l[(r + 1) & 3], slope2, distance, !MASKED || first + mfma_row(r + 1, 0) >= from);
+                wp.set(r / 2, x.x, y.x);
+                p[r] = x.y, p[r + 1] = y.y;
+            });
+        } else if (n < 3 * N) {
+            dv[d] = mfma(f[n % kAhead], wp.half(k), dv[d]);
+            each<M / 2>([&](int m) __attribute__((always_inline)) {
+                const int r = (n - 2 * N) * M + 2 * m;
+                ws.set(r / 2, p[r] * ds[r], p[r + 1] * ds[r + 1]);
+            });
+        } else {
+            dk[d] = mfma(f[n % kAhead], ws.half(k), dk[d]);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    });
 }
 
 // NW 8: two tiles of 128 keys a workgroup, the sequence's p-th and p-th from the end, which together see as many rows as
@@ -266,54 +313,12 @@ template <typename T, int DP, int MODE, int NW> __global__ void __launch_bounds_
         n++;
         if (n < count) keep(n);
     };
-    // Products of 32 rows, in this order: scores, dP, dv, dk. Probabilities are formed between dP's, dS between dv's;
-    // operands are read ahead.
     auto add = [&](int i, float slope2, auto masked) __attribute__((always_inline)) {
         const char *tq = smem[slot_of], *tg = tq + Tk::kBytes;
-        constexpr int N = DP / 16, kAhead = 3, M = 16 / N;      // N products each; M scores to a product
         each<kRows / 32>([&](int c) __attribute__((always_inline)) {
-            const float *ls = &stats[slot_of][0][c * 32 + 4 * h], *de = &stats[slot_of][1][c * 32 + 4 * h];
-            const int first = i + c * 32 + 4 * h;
-            const float distance = (float)(j - shift - first);
-            f32x16 p = {}, ds;
-            if constexpr (MODE == kPlain) p = four(ls);
-            mm::f32x4 l = {};
-            Words<T> wp, ws;
-            frag f[kAhead], v[kAhead];
-            auto fetch = [&](int n) __attribute__((always_inline)) {
-                const int k = (n - 2 * N) % N / (DP / 32) * 16, d = (n - 2 * N) % (DP / 32);
-                f[n % kAhead] = n < N ? row_fragment<DP, T>(tq, places, c * 32, n) : n < 2 * N ? row_fragment<DP, T>(tg, places, c * 32, n - N) :
-                                column_fragment<DP, T>(n < 3 * N ? tg : tq, places, c * 32 + k, d);
-                if (n >= N && n < 2 * N) v[n % kAhead] = row_fragment<DP, T>(mine_values, places, 0, n - N);
-            };
-            each<kAhead - 1>([&](int n) __attribute__((always_inline)) { fetch(n); });
-            each<4 * N>([&](int n) __attribute__((always_inline)) {
-                if (n + kAhead - 1 < 4 * N) fetch(n + kAhead - 1);
-                const int k = (n - 2 * N) % N / (DP / 32), d = (n - 2 * N) % (DP / 32);
-                if (n < N) {
-                    p = mfma(f[n % kAhead], kf[n], p);
-                    if (n == N - 1) ds = four(de);
-                } else if (n < 2 * N) {
-                    ds = mfma(f[n % kAhead], v[n % kAhead], ds);
-                    each<M / 2>([&](int m) __attribute__((always_inline)) {
-                        const int r = (n - N) * M + 2 * m;
-                        if (MODE != kPlain && (r & 3) == 0) l = *(const mm::f32x4 *)(ls + 2 * r);
-                        const float2 x = weigh<T, MODE, true>(a, p[r], r, l[r & 3], slope2, distance, !decltype(masked)::value || first + mfma_row(r, 0) >= from);
-                        const float2 y = weigh<T, MODE, true>(a, p[r + 1], r + 1, l[(r + 1) & 3], slope2, distance, !decltype(masked)::value || first + mfma_row(r + 1, 0) >= from);
-                        wp.set(r / 2, x.x, y.x);
-                        p[r] = x.y, p[r + 1] = y.y;
-                    });
-                } else if (n < 3 * N) {
-                    dv[d] = mfma(f[n % kAhead], wp.half(k), dv[d]);
-                    each<M / 2>([&](int m) __attribute__((always_inline)) {
-                        const int r = (n - 2 * N) * M + 2 * m;
-                        ws.set(r / 2, p[r] * ds[r], p[r + 1] * ds[r + 1]);
-                    });
-                } else {
-                    dk[d] = mfma(f[n % kAhead], ws.half(k), dk[d]);
-                }
-                __builtin_amdgcn_sched_barrier(0);
-            });
+            gather<T, DP, MODE, decltype(masked)::value>(a, dk, dv, tq, tg, c * 32, &stats[slot_of][0][c * 32 + 4 * h], &stats[slot_of][1][c * 32 + 4 * h], kf,
+                                                         [&](int n) __attribute__((always_inline)) { return row_fragment<DP, T>(mine_values, places, 0, n); }, places,
+                                                         i + c * 32 + 4 * h, from, j - shift, slope2);
         });
     };
     if (count) {
@@ -338,13 +343,121 @@ template <typename T, int DP, int MODE, int NW> __global__ void __launch_bounds_
     const float sc = scale_of<T, MODE>(a);
     T *ok = (T *)a.dk.p + s * a.dk.seq + (q.k0 + j) * a.dk.row + hk * a.dk.head;
     T *ov = (T *)a.dv.p + s * a.dv.seq + (q.k0 + j) * a.dv.row + hk * a.dv.head;
+    store_row<T, DP>(ok, dk, sc, a.dim, a.out_vec);
+    store_row<T, DP>(ov, dv, 1.0f, a.dim, a.out_vec);
+}
+
+// Few keys: 32 a workgroup, whose four wavefronts take tiles of rows in turn, each with tiles and sums of its own;
+// the sums are added up at the end (3 sequences of 333, 12 heads on 4: 41 us with 128 keys a workgroup, which leaves most CUs without one).
+template <typename T, int DP, int MODE> __global__ void __launch_bounds__(256) few_keys_kernel(Args a, int64_t tiles)
+{
+    typedef Tile<DP, 32, 1> Tk;
+    typedef typename mm::pack8<T>::type frag;
+    constexpr int kStage = 2 * Tk::kBytes, kLine = DP + 4;
+    static_assert(4 * 32 * kLine * 4 <= 8 * kStage, "the wavefronts' sums fit where the tiles were");
+    __shared__ __align__(1024) char smem[4][2][kStage];
+    __shared__ __align__(16) float stats[4][2][2][32];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, h = lane >> 5, col = lane & 31;
+    const uint32_t slot = blockIdx.x / (uint32_t)a.kv_heads;
+    const int hk = blockIdx.x - slot * a.kv_heads;
+    int s;
+    int64_t tile;
+    if (!find_slot(a.d_k, a.k_rows, a.packed, a.sequences, 1, 32, tiles, slot, s, tile)) return;
+    const Sequence q = sequence_of(a, s);
+    if (tile * 32 >= q.lk) return;
+    const int j0 = (int)tile * 32, j = j0 + col, shift = q.lk - q.lq;
+    const bool any = j < q.lk;
+    auto first_of = [&](int key) { return a.causal && key >= q.prefix ? max(key - shift, 0) : 0; };
+    const int from = first_of(j), start = first_of(j0) / 32 * 32, whole = __builtin_amdgcn_readfirstlane(first_of(j0 + 31));
+    const int per = q.lq > start ? (q.lq - start + 31) / 32 : 0, count = per * a.group;
+
+    const T *pk = (const T *)a.k.p + s * a.k.seq + (q.k0 + j) * a.k.row + hk * a.k.head;
+    const T *pv = (const T *)a.v.p + s * a.v.seq + (q.k0 + j) * a.v.row + hk * a.v.head;
+    frag kf[DP / 16], vf[DP / 16];
 #pragma unroll
-    for (int d = 0; d < DP / 32; d++)
+    for (int k = 0; k < DP / 16; k++) {
+        kf[k] = global_fragment<T>(pk, k * 16 + 8 * h, a.dim, any);
+        vf[k] = global_fragment<T>(pv, k * 16 + 8 * h, a.dim, any);
+    }
+    const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)&smem[wave][0][0];
+    const T *pq = (const T *)a.q.p + s * a.q.seq + q.q0 * a.q.row, *pg = (const T *)a.dy.p + s * a.dy.seq + q.q0 * a.dy.row;
+    const int64_t row0 = a.packed ? q.q0 : (int64_t)s * a.q_len;
+    int oq[Tk::kLoads], og[Tk::kLoads];
 #pragma unroll
-        for (int r = 0; r < 16; r += 4) {
-            store4<T>(ok, d * 32 + mfma_row(r, h), a.dim, a.out_vec, dk[d][r] * sc, dk[d][r + 1] * sc, dk[d][r + 2] * sc, dk[d][r + 3] * sc);
-            store4<T>(ov, d * 32 + mfma_row(r, h), a.dim, a.out_vec, dv[d][r], dv[d][r + 1], dv[d][r + 2], dv[d][r + 3]);
+    for (int m = 0; m < Tk::kLoads; m++) oq[m] = Tk::offset(m, 0, a.q.row, a.dim, 32), og[m] = Tk::offset(m, 0, a.dy.row, a.dim, 32);
+    float2 stat;
+    auto load = [&](int n, int stage) __attribute__((always_inline)) {
+        const int g = n / per, i0 = start + (n - g * per) * 32, head = hk * a.group + g, valid = q.lq - i0;
+        const i32x4 bq = buffer_at(pq + (int64_t)i0 * a.q.row + head * a.q.head), bg = buffer_at(pg + (int64_t)i0 * a.dy.row + head * a.dy.head);
+        stat = {INFINITY, 0};                               // past the last row: P = 0
+        if (lane < min(valid, 32)) stat = a.rows[(int64_t)head * a.q_rows + row0 + i0 + lane];
+        const uint32_t to = lds + stage * kStage;
+        if (valid >= 32) {
+#pragma unroll
+            for (int m = 0; m < Tk::kLoads; m += 2) {
+                mm::load_to_lds(bq, oq[m], to + m * 1024, oq[m + 1], to + m * 1024 + 1024);
+                mm::load_to_lds(bg, og[m], to + Tk::kBytes + m * 1024, og[m + 1], to + Tk::kBytes + m * 1024 + 1024);
+            }
+        } else {
+#pragma unroll
+            for (int m = 0; m < Tk::kLoads; m++) {
+                mm::load_to_lds(bq, Tk::offset(m, 0, a.q.row, a.dim, valid), to + m * 1024);
+                mm::load_to_lds(bg, Tk::offset(m, 0, a.dy.row, a.dim, valid), to + Tk::kBytes + m * 1024);
+            }
         }
+    };
+    auto keep = [&](int stage) __attribute__((always_inline)) {
+        if (lane < 32) stats[wave][stage][0][lane] = MODE != kPlain ? a.cap2 - stat.x : stat.x * a.unscale, stats[wave][stage][1][lane] = -stat.y;
+    };
+    Places places;
+    places.set<DP>();
+    f32x16 dk[DP / 32], dv[DP / 32];
+#pragma unroll
+    for (int d = 0; d < DP / 32; d++) dk[d] = f32x16{}, dv[d] = f32x16{};
+    int stage = 0;
+    if (wave < count) load(wave, 0), keep(0);
+    for (int n = wave; n < count; n += 4, stage ^= 1) {
+        // a wavefront's tiles are its own: it waits for its loads, and for its reads of the buffer that is filled next
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        if (n + 4 < count) load(n + 4, stage ^ 1);
+        const int g = n / per, i = start + (n - g * per) * 32;
+        const float slope2 = MODE & kSlopes ? a.d_slopes[hk * a.group + g] * kLog2e : 0.0f;
+        const char *tq = smem[wave][stage];
+        auto add = [&](auto masked) __attribute__((always_inline)) {
+            gather<T, DP, MODE, decltype(masked)::value>(a, dk, dv, tq, tq + Tk::kBytes, 0, &stats[wave][stage][0][4 * h], &stats[wave][stage][1][4 * h], kf,
+                                                         [&](int k) __attribute__((always_inline)) { return vf[k]; }, places, i + 4 * h, from, j - shift, slope2);
+        };
+        if (i < whole) add(std::true_type());
+        else add(std::false_type());
+        if (n + 4 < count) keep(stage ^ 1);
+    }
+    // the four wavefronts' sums, of keys, then of values
+    float *sums = (float *)&smem[0][0][0];
+    const int mine = threadIdx.x >> 3, sub = threadIdx.x & 7;
+    const float sc = scale_of<T, MODE>(a);
+    each<2>([&](int which) __attribute__((always_inline)) {
+        __syncthreads();
+#pragma unroll
+        for (int d = 0; d < DP / 32; d++)
+#pragma unroll
+            for (int r = 0; r < 16; r += 4) {
+                const f32x16 &x = which ? dv[d] : dk[d];
+                *(mm::f32x4 *)(sums + (wave * 32 + col) * kLine + d * 32 + mfma_row(r, h)) = mm::f32x4{x[r], x[r + 1], x[r + 2], x[r + 3]};
+            }
+        __syncthreads();
+        if (j0 + mine >= q.lk) return;
+        const View &o = which ? a.dv : a.dk;
+        T *out = (T *)o.p + s * o.seq + (q.k0 + j0 + mine) * o.row + hk * o.head;
+        const float f = which ? 1.0f : sc;
+#pragma unroll
+        for (int c = 0; c < DP / 32; c++) {
+            const int d = c * 32 + sub * 4;
+            mm::f32x4 v = {0, 0, 0, 0};
+#pragma unroll
+            for (int w = 0; w < 4; w++) v += *(const mm::f32x4 *)(sums + (w * 32 + mine) * kLine + d);
+            store4<T>(out, d, a.dim, a.out_vec, v[0] * f, v[1] * f, v[2] * f, v[3] * f);
+        }
+    });
 }
 
 void launch_rows(const heddle_attention_desc *d, const Args &a, int64_t blocks, int64_t tiles, hipStream_t stream)
@@ -353,10 +466,11 @@ void launch_rows(const heddle_attention_desc *d, const Args &a, int64_t blocks, 
         hipLaunchKernelGGL((rows_kernel<decltype(t), dp, mode>), dim3((unsigned)blocks), dim3(256), 0, stream, a, tiles);
     });
 }
-void launch_keys(const heddle_attention_desc *d, const Args &a, bool pairs, int64_t blocks, int64_t tiles, hipStream_t stream)
+void launch_keys(const heddle_attention_desc *d, const Args &a, int span, int64_t blocks, int64_t tiles, hipStream_t stream)
 {
     with_kind(d, [&](auto t, auto dp, auto mode) {
-        if (pairs) hipLaunchKernelGGL((keys_kernel<decltype(t), dp, mode, 8>), dim3((unsigned)blocks), dim3(512), 0, stream, a, tiles);
+        if (span == 32) hipLaunchKernelGGL((few_keys_kernel<decltype(t), dp, mode>), dim3((unsigned)blocks), dim3(256), 0, stream, a, tiles);
+        else if (span == 256) hipLaunchKernelGGL((keys_kernel<decltype(t), dp, mode, 8>), dim3((unsigned)blocks), dim3(512), 0, stream, a, tiles);
         else hipLaunchKernelGGL((keys_kernel<decltype(t), dp, mode, 4>), dim3((unsigned)blocks), dim3(256), 0, stream, a, tiles);
     });
 }
@@ -373,17 +487,18 @@ int backward(const heddle_attention_desc *d, mm::Scratch &s, bool run, hipStream
     if (a.k_rows) c.add(d, a.k, true, s);
     if (a.k_rows) c.add(d, a.v, true, s);
     a.rows = (float2 *)s.take((size_t)a.q_rows * d->heads * 8);
-    auto aligned = [&](const void *p, const View &v) { return !((uintptr_t)p & 7) && !((v.seq | v.row | v.head | d->dim) & 3); };
+    auto aligned = [&](const void *p, const View &v) { return !((uintptr_t)p & 15) && !((v.seq | v.row | v.head | d->dim) & 7); };
     a.out_vec = (!d->dq || aligned(d->dq, a.dq)) && (!d->dk || (aligned(d->dk, a.dk) && aligned(d->dv, a.dv)));
     const int64_t blocks = a.q_rows ? slots_of(d->packed, d->sequences, d->q_len, d->q_len, a.group, 128) * d->kv_heads : 0;
-    const bool pairs = a.k_rows / d->sequences >= 512;
-    const int64_t tiles = (d->q_len * a.group + 127) / 128, span = pairs ? 256 : 128, ktiles = (d->k_len + span - 1) / span;
+    // keys a workgroup takes: 32 where there would not be one of 128 keys for every CU, pairs of 128 where most sequences have several
+    const int64_t keys = std::max<int64_t>(1, a.k_rows / d->sequences), span = d->sequences * ((keys + 127) / 128) * d->kv_heads < 256 ? 32 : keys >= 512 ? 256 : 128;
+    const int64_t tiles = (d->q_len * a.group + 127) / 128, ktiles = (d->k_len + span - 1) / span;
     const int64_t kblocks = d->dk && a.k_rows ? slots_of(d->packed, d->sequences, d->k_len, d->k_len, 1, span) * d->kv_heads : 0;
     if (std::max(blocks, kblocks) > (int64_t(1) << 24) - 1) return fail(HEDDLE_E_RANGE, "more tiles than a launch holds");
     if (!run) return HEDDLE_OK;
     if (const int rc = c.launch(stream)) return rc;
     if (blocks) launch_rows(d, a, blocks, tiles, stream);
-    if (kblocks) launch_keys(d, a, pairs, kblocks, ktiles, stream);
+    if (kblocks) launch_keys(d, a, (int)span, kblocks, ktiles, stream);
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? HEDDLE_OK : hip_fail(e, "attention's gradients");
 }

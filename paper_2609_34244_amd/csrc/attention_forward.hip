@@ -151,14 +151,10 @@ template <typename T, int DP, int MODE, int NW> __global__ void __launch_bounds_
     for (; t < count - open; t++) tile_of(t, std::true_type());
     for (; t < count; t++) tile_of(t, std::false_type());
     if (some) collect<T, DP>(st, smem[1][(count - 1) & 1], at, 0, was_p);
-    if (!row.any) return;
     const float l = st.l + other_half(st.l), inv = l == 0 ? 0.0f : 1.0f / l;
     T *y = (T *)a.y.p + s * a.y.seq + (q.q0 + row.i) * a.y.row + row.head * a.y.head;
-#pragma unroll
-    for (int d = 0; d < DP / 32; d++)
-#pragma unroll
-        for (int r = 0; r < 16; r += 4)
-            store4<T>(y, d * 32 + mfma_row(r, h), a.dim, a.out_vec, st.o[d][r] * inv, st.o[d][r + 1] * inv, st.o[d][r + 2] * inv, st.o[d][r + 3] * inv);
+    if (!row.any) return;                                   // (both of a row's lanes)
+    store_row<T, DP>(y, st.o, inv, a.dim, a.out_vec);
     if (a.lse && h == 0)
         a.lse[row.at * a.heads + row.head] = l == 0 ? -INFINITY : (st.m * unit_of<MODE>(a) + offset_of<MODE>(a) + __log2f(l)) * kLn2;
 }

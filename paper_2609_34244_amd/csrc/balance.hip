@@ -59,19 +59,35 @@ template <typename T, int K> __device__ inline void load_row(const T *row, int e
     for (int k = 1; k < K; k++) z[k] = e + k < experts ? z[k] : other;
 }
 
+// op over G neighbouring lanes, in all of them: within 16 by moves of the vector units (the cross-lane
+// exchange through LDS is as slow as a read of it, and a row takes three such sums)
+template <int CTRL> __device__ inline float moved(float v)
+{
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true));
+}
+template <int G, typename Op> __device__ inline float over(float v, Op op)
+{
+    v = op(v, moved<0xb1>(v));                              // the neighbour of a pair
+    v = op(v, moved<0x4e>(v));                              // the other pair of four
+    v = op(v, moved<0x141>(v));                             // eight in reverse
+    if constexpr (G >= 16) v = op(v, moved<0x140>(v));      // sixteen in reverse
+    if constexpr (G >= 32) v = op(v, __shfl_xor(v, 16));
+    if constexpr (G >= 64) v = op(v, __shfl_xor(v, 32));
+    return v;
+}
+template <int G> __device__ inline float sum_over(float v) { return over<G>(v, [](float a, float b) { return a + b; }); }
+
 // softmax over G lanes' K values; a row of -infinity alone has no probabilities: zeros
 template <int G, int K> __device__ inline void softmax(float z[K])
 {
     float top = z[0], sum = 0;
 #pragma unroll
     for (int k = 1; k < K; k++) top = fmaxf(top, z[k]);
-#pragma unroll
-    for (int d = G / 2; d; d /= 2) top = fmaxf(top, __shfl_xor(top, d));
+    top = over<G>(top, [](float a, float b) { return fmaxf(a, b); });
     const float base = top == -INFINITY ? 0.0f : top;
 #pragma unroll
     for (int k = 0; k < K; k++) z[k] = __expf(z[k] - base), sum += z[k];
-#pragma unroll
-    for (int d = G / 2; d; d /= 2) sum += __shfl_xor(sum, d);
+    sum = sum_over<G>(sum);
     const float inv = sum == 0 ? 0.0f : 1.0f / sum;
 #pragma unroll
     for (int k = 0; k < K; k++) z[k] *= inv;
@@ -124,8 +140,7 @@ template <typename T, int G, int K> __global__ void __launch_bounds__(256) forwa
                 }
             }
             // a row's lanes: any of them with a pick
-#pragma unroll
-            for (int d = G / 2; d; d /= 2) has |= __shfl_xor(has, d);
+            has = (__ballot(has) >> ((threadIdx.x & 63) / G * G) & (G == 64 ? ~0ull : (1ull << (G & 63)) - 1)) != 0;
             softmax<G, K>(z[n]);
             if (has) {
                 with += lane == 0;
@@ -279,8 +294,7 @@ template <typename T, int G, int K> __global__ void __launch_bounds__(256) backw
             float dot = 0;
 #pragma unroll
             for (int k = 0; k < K; k++) dot += z[n][k] * c[k];
-#pragma unroll
-            for (int d = G / 2; d; d /= 2) dot += __shfl_xor(dot, d);
+            dot = sum_over<G>(dot);
             T *out = (T *)a.dlogits + r * a.ldd + lane * K;
             typename Some<T, K>::loose v;
 #pragma unroll

@@ -985,8 +985,8 @@ def heddle_expert_balance(logits, picked, scale=1.0, stream=None):
     import torch
     gpu, t, e, k, size, pl, ldl, pp, ldp = _balance_inputs(logits, picked, "heddle_expert_balance")
     counts, offsets, rows, mean, loss = _on_stream(stream, lambda: (
-        *(torch.empty(n, dtype=torch.int32, device=logits.device) for n in (e, e + 1, 1)),
-        *(torch.empty(n, dtype=torch.float32, device=logits.device) for n in (e, 1))))
+        *torch.empty(2 * e + 2, dtype=torch.int32, device=logits.device).split_with_sizes((e, e + 1, 1)),
+        *torch.empty(e + 1, dtype=torch.float32, device=logits.device).split_with_sizes((e, 1))))
     desc = _BALANCE.pack(_dtype(logits, "logits"), e, k, size, t, scale, pl, ldl, pp, ldp, counts.data_ptr(), rows.data_ptr(),
                          offsets.data_ptr(), mean.data_ptr(), loss.data_ptr(), 0, 0, 0, 0, 0)
     L = lib()
