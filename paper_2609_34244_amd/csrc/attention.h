@@ -129,6 +129,70 @@ __device__ inline bool find_slot(const int32_t *offsets, int64_t rows, int packe
     tile = slot - ((int64_t)clamp_row(offsets[s], rows) * mul / T + s);
     return tile >= 0;
 }
+// The sum over a wavefront, in a scalar register: within 16 lanes by moves of the vector units.
+__device__ inline int wave_sum(int v)
+{
+#ifdef __HIP_DEVICE_COMPILE__
+    v += __builtin_amdgcn_update_dpp(0, v, 0xb1, 0xf, 0xf, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x4e, 0xf, 0xf, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x141, 0xf, 0xf, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x140, 0xf, 0xf, true);
+    return __builtin_amdgcn_readlane(v, 0) + __builtin_amdgcn_readlane(v, 16) + __builtin_amdgcn_readlane(v, 32) + __builtin_amdgcn_readlane(v, 48);
+#else
+    return v;
+#endif
+}
+
+// Tiles of up to 64 packed sequences by their number in their sequence, the highest first: slot `slot` of this order. The
+// last tiles of the longest documents see the most keys, and begun last they would run on alone (11 documents of 4092
+// rows, 32 heads: forward, dq, dk with dv 69, 80, 79 us in the documents' order, 62, 76, 70 so). F(t) tiles have a number of at least t.
+__device__ inline bool find_ordered(const Args &a, bool keys, int T, int slot, Sequence &q, int64_t &tile, int &tiles)
+{
+    const int lane = threadIdx.x & 63, at0 = min(lane, a.sequences), at1 = min(lane + 1, a.sequences), mul = keys ? 1 : a.group;
+    const int q0 = clamp_row(a.d_q[at0], a.q_rows), q1 = clamp_row(a.d_q[at1], a.q_rows);
+    const int k0 = clamp_row(a.d_k[at0], a.k_rows), k1 = clamp_row(a.d_k[at1], a.k_rows);
+    const int prefixes = a.d_prefix && a.sequences ? a.d_prefix[min(lane, a.sequences - 1)] : 0;
+    const int from = keys ? k0 : q0, to = keys ? k1 : q1, sequences = a.sequences;
+    const int mine = lane < sequences && to > from ? (int)(((int64_t)(to - from) * mul + T - 1) / T) : 0;
+    auto f = [&](int t) { return wave_sum(max(mine - t, 0)); };
+    const int all = f(0);
+    if (slot >= all) return false;
+    int lo = 0, hi = all, above = 0;                        // F(lo) > slot >= F(hi) = above
+    while (hi - lo > 1) {
+        const int mid = lo + (hi - lo) / 2, n = f(mid);
+        if (n > slot) lo = mid;
+        else hi = mid, above = n;
+    }
+    const uint64_t with = __ballot(mine > lo);
+    const uint64_t at = __ballot(mine > lo && __builtin_popcountll(with & ((1ull << lane) - 1)) == slot - above);
+    if (at == 0) return false;                              // (not with offsets in order)
+    q.s = __builtin_ctzll(at);
+    q.q0 = __builtin_amdgcn_readlane(q0, q.s), q.k0 = __builtin_amdgcn_readlane(k0, q.s);
+    q.lq = max(__builtin_amdgcn_readlane(q1, q.s) - (int)q.q0, 0), q.lk = max(__builtin_amdgcn_readlane(k1, q.s) - (int)q.k0, 0);
+    q.prefix = __builtin_amdgcn_readlane(prefixes, q.s);
+    tile = lo;
+    tiles = __builtin_amdgcn_readlane(mine, q.s);
+    return true;
+}
+// A workgroup's sequence and its tile of T query rows of a key head, or of T keys, those with the most work first; slots: how
+// many there may be.
+__device__ inline bool find_tile(const Args &a, bool keys, int T, uint32_t slot, uint32_t slots, Sequence &q, int64_t &tile)
+{
+    int s, tiles;
+    if (!a.packed) {
+        // the last tiles of queries see the most keys, the first tiles of keys are seen by the most queries
+        const uint32_t at = keys ? slot : slots - 1 - slot;
+        s = (int)(at % (uint32_t)a.sequences), tile = at / (uint32_t)a.sequences;
+    } else if (a.sequences <= 64) {
+        if (!find_ordered(a, keys, T, (int)slot, q, tile, tiles)) return false;
+        if (keys) tile = tiles - 1 - tile;
+        return true;
+    } else if (!find_slot(keys ? a.d_k : a.d_q, keys ? a.k_rows : a.q_rows, 1, a.sequences, keys ? 1 : a.group, T, 0, keys ? slot : slots - 1 - slot, s, tile)) {
+        return false;
+    }
+    q = sequence_of(a, s);
+    return true;
+}
 inline int64_t slots_of(int packed, int64_t sequences, int64_t rows, int64_t length, int64_t mul, int64_t T)
 {
     return packed ? rows * mul / T + sequences : sequences * ((length * mul + T - 1) / T);
@@ -146,7 +210,7 @@ template <int DP, int ROWS, int NW> struct Tile {
     {
         const int lane = threadIdx.x & 63, block = i * NW + wave, p = lane >> 4;
         const int row = block / kGroups * 16 + ((lane & 15) ^ p << 2), col = (block % kGroups * 4 + p) * 8;
-        return row < valid && col < dim ? (int)(row * ld * 2) + col * 2 : kNowhere;
+        return row < valid && col < dim ? (row * (int)ld + col) * 2 : kNowhere;
     }
 };
 
@@ -401,8 +465,8 @@ int check_overlaps(const heddle_attention_desc *d, bool backward);
 Args base_args(const heddle_attention_desc *d);
 int mode_of(const heddle_attention_desc *d);
 // the launches; mode: of enum Mode
-void launch_forward(const heddle_attention_desc *d, const Args &a, int rows, int64_t blocks, int64_t tiles, hipStream_t stream);
-void launch_rows(const heddle_attention_desc *d, const Args &a, int64_t blocks, int64_t tiles, hipStream_t stream);
+void launch_forward(const heddle_attention_desc *d, const Args &a, int rows, int64_t blocks, hipStream_t stream);
+void launch_rows(const heddle_attention_desc *d, const Args &a, int64_t blocks, hipStream_t stream);
 void launch_keys(const heddle_attention_desc *d, const Args &a, int span, int64_t blocks, int64_t tiles, hipStream_t stream);
 
 // f(type, padded head width, mode) as constants

@@ -362,7 +362,7 @@ static int forward(const heddle_attention_desc *d, mm::Scratch &s, bool run, hip
     if (!run) return HEDDLE_OK;
     if (const int rc = c.launch(stream)) return rc;
     if (!split) {
-        launch_forward(d, a, T, blocks, tiles, stream);
+        launch_forward(d, a, T, blocks, stream);
     } else {
         with_kind(d, [&](auto t, auto dp, auto mode) {
             typedef decltype(t) T;

@@ -50,22 +50,18 @@ template <typename T, int MODE, bool READY> HEDDLE_INLINE float2 weigh(const Arg
     return {p, pw};
 }
 
-template <typename T, int DP, int MODE> __global__ void __launch_bounds__(256, 2) rows_kernel(Args a, int64_t tiles)
+template <typename T, int DP, int MODE> __global__ void __launch_bounds__(256, 2) rows_kernel(Args a)
 {
     typedef Tile<DP, 64, 4> Tk;
     typedef typename mm::pack8<T>::type frag;
     __shared__ __align__(1024) char smem[2][2 * Tk::kBytes];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, h = lane >> 5, col = lane & 31;
-    const int hk = blockIdx.x % (uint32_t)a.kv_heads;
-    const int64_t slot = gridDim.x / (uint32_t)a.kv_heads - 1 - blockIdx.x / (uint32_t)a.kv_heads;
-    int s;
+    const uint32_t slot = blockIdx.x / (uint32_t)a.kv_heads;
+    const int hk = blockIdx.x - slot * a.kv_heads;
+    Sequence q;
     int64_t tile;
-    if (a.packed) {
-        if (!find_slot(a.d_q, a.q_rows, 1, a.sequences, a.group, 128, tiles, slot, s, tile)) return;
-    } else {
-        s = (int)((uint32_t)slot % (uint32_t)a.sequences), tile = (uint32_t)slot / (uint32_t)a.sequences;
-    }
-    const Sequence q = sequence_of(a, s);
+    if (!find_tile(a, false, 128, slot, gridDim.x / (uint32_t)a.kv_heads, q, tile)) return;
+    const int s = q.s;
     if (tile * 128 >= (int64_t)q.lq * a.group) return;
     const int rows = q.lq * a.group, r = (int)tile * 128 + wave * 32 + col;
     const bool any = r < rows;
@@ -231,7 +227,7 @@ HEDDLE_INLINE void gather(const Args &a, f32x16 *dk, f32x16 *dv, const char *tq,
 
 // NW 8: two tiles of 128 keys a workgroup, the sequence's p-th and p-th from the end, which together see as many rows as
 // any other such pair, and share the rows' tiles.
-template <typename T, int DP, int MODE, int NW> __global__ void __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2))) keys_kernel(Args a, int64_t tiles)
+template <typename T, int DP, int MODE, int NW> __global__ void __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2))) keys_kernel(Args a)
 {
     constexpr int kRows = DP == 64 && NW == 8 ? 64 : 32;
     typedef Tile<DP, kRows, NW> Tk;
@@ -241,16 +237,12 @@ template <typename T, int DP, int MODE, int NW> __global__ void __launch_bounds_
     __shared__ __align__(1024) char values[NW / 4][Tv::kBytes];
     __shared__ __align__(16) float stats[2][2][kRows];      // what the exponents, or the scores' sums, start from; -delta
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, h = lane >> 5, col = lane & 31;
-    const int hk = blockIdx.x % (uint32_t)a.kv_heads;
-    const int64_t slot = blockIdx.x / (uint32_t)a.kv_heads; // the first tiles, which the most rows see, first
-    int s;
+    const uint32_t slot = blockIdx.x / (uint32_t)a.kv_heads;
+    const int hk = blockIdx.x - slot * a.kv_heads;
+    Sequence q;
     int64_t tile;
-    if (a.packed) {
-        if (!find_slot(a.d_k, a.k_rows, 1, a.sequences, 1, 32 * NW, tiles, slot, s, tile)) return;
-    } else {
-        s = (int)((uint32_t)slot % (uint32_t)a.sequences), tile = (uint32_t)slot / (uint32_t)a.sequences;
-    }
-    const Sequence q = sequence_of(a, s);
+    if (!find_tile(a, true, 32 * NW, slot, gridDim.x / (uint32_t)a.kv_heads, q, tile)) return;
+    const int s = q.s;
     if (tile * (32 * NW) >= q.lk) return;
     const int team = wave >> 2, last_tile = (q.lk + 127) / 128 - 1, own = team ? last_tile - (int)tile : (int)tile;
     const int j0 = own * 128, w0 = j0 + (wave & 3) * 32, j = w0 + col, shift = q.lk - q.lq;   // the wavefront's keys: w0 on
@@ -347,16 +339,18 @@ template <typename T, int DP, int MODE, int NW> __global__ void __launch_bounds_
     store_row<T, DP>(ov, dv, 1.0f, a.dim, a.out_vec);
 }
 
-// Few keys: 32 a workgroup, whose four wavefronts take tiles of rows in turn, each with tiles and sums of its own;
-// the sums are added up at the end (3 sequences of 333, 12 heads on 4: 41 us with 128 keys a workgroup, which leaves most CUs without one).
-template <typename T, int DP, int MODE> __global__ void __launch_bounds__(256) few_keys_kernel(Args a, int64_t tiles)
+// Few keys: 32 a workgroup, whose eight wavefronts take tiles of 32 rows in turn, each with a tile and sums of its own; the
+// sums are added up at the end. One tile a wavefront: while it waits for the next, the other wavefront of its SIMD has
+// its products (3 sequences of 333, 12 heads on 4: 41 us with 128 keys a workgroup, which leaves most CUs without one,
+// 30 with four wavefronts of two tiles).
+template <typename T, int DP, int MODE> __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) few_keys_kernel(Args a, int64_t tiles)
 {
     typedef Tile<DP, 32, 1> Tk;
     typedef typename mm::pack8<T>::type frag;
     constexpr int kStage = 2 * Tk::kBytes, kLine = DP + 4;
-    static_assert(4 * 32 * kLine * 4 <= 8 * kStage, "the wavefronts' sums fit where the tiles were");
-    __shared__ __align__(1024) char smem[4][2][kStage];
-    __shared__ __align__(16) float stats[4][2][2][32];
+    static_assert(4 * 32 * kLine * 4 <= 8 * kStage && 4 * 2 * DP / 2 * 64 * 4 <= 8 * kStage, "the wavefronts' sums fit where the tiles were");
+    __shared__ __align__(1024) char smem[8][kStage], values[Tk::kBytes];
+    __shared__ __align__(16) float stats[8][2][32];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, h = lane >> 5, col = lane & 31;
     const uint32_t slot = blockIdx.x / (uint32_t)a.kv_heads;
     const int hk = blockIdx.x - slot * a.kv_heads;
@@ -368,75 +362,78 @@ template <typename T, int DP, int MODE> __global__ void __launch_bounds__(256) f
     const int j0 = (int)tile * 32, j = j0 + col, shift = q.lk - q.lq;
     const bool any = j < q.lk;
     auto first_of = [&](int key) { return a.causal && key >= q.prefix ? max(key - shift, 0) : 0; };
-    const int from = first_of(j), start = first_of(j0) / 32 * 32, whole = __builtin_amdgcn_readfirstlane(first_of(j0 + 31));
+    const int from = first_of(j), start = first_of(j0) / 32 * 32;
     const int per = q.lq > start ? (q.lq - start + 31) / 32 : 0, count = per * a.group;
 
     const T *pk = (const T *)a.k.p + s * a.k.seq + (q.k0 + j) * a.k.row + hk * a.k.head;
-    const T *pv = (const T *)a.v.p + s * a.v.seq + (q.k0 + j) * a.v.row + hk * a.v.head;
-    frag kf[DP / 16], vf[DP / 16];
+    const T *pv = (const T *)a.v.p + s * a.v.seq + (q.k0 + j0) * a.v.row + hk * a.v.head;
+    frag kf[DP / 16];
 #pragma unroll
-    for (int k = 0; k < DP / 16; k++) {
-        kf[k] = global_fragment<T>(pk, k * 16 + 8 * h, a.dim, any);
-        vf[k] = global_fragment<T>(pv, k * 16 + 8 * h, a.dim, any);
-    }
-    const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)&smem[wave][0][0];
+    for (int k = 0; k < DP / 16; k++) kf[k] = global_fragment<T>(pk, k * 16 + 8 * h, a.dim, any);
+    if (wave < Tk::kLoads)                                  // (one instruction a wavefront)
+        mm::load_to_lds(buffer_at(pv), Tk::offset(wave, 0, a.v.row, a.dim, q.lk - j0), (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)&values[0] + wave * 1024);
+    const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)&smem[wave][0];
     const T *pq = (const T *)a.q.p + s * a.q.seq + q.q0 * a.q.row, *pg = (const T *)a.dy.p + s * a.dy.seq + q.q0 * a.dy.row;
     const int64_t row0 = a.packed ? q.q0 : (int64_t)s * a.q_len;
-    int oq[Tk::kLoads], og[Tk::kLoads];
-#pragma unroll
-    for (int m = 0; m < Tk::kLoads; m++) oq[m] = Tk::offset(m, 0, a.q.row, a.dim, 32), og[m] = Tk::offset(m, 0, a.dy.row, a.dim, 32);
-    float2 stat;
-    auto load = [&](int n, int stage) __attribute__((always_inline)) {
+    auto load = [&](int n) __attribute__((always_inline)) {
         const int g = n / per, i0 = start + (n - g * per) * 32, head = hk * a.group + g, valid = q.lq - i0;
         const i32x4 bq = buffer_at(pq + (int64_t)i0 * a.q.row + head * a.q.head), bg = buffer_at(pg + (int64_t)i0 * a.dy.row + head * a.dy.head);
-        stat = {INFINITY, 0};                               // past the last row: P = 0
+        float2 stat = {INFINITY, 0};                        // past the last row: P = 0
         if (lane < min(valid, 32)) stat = a.rows[(int64_t)head * a.q_rows + row0 + i0 + lane];
-        const uint32_t to = lds + stage * kStage;
-        if (valid >= 32) {
 #pragma unroll
-            for (int m = 0; m < Tk::kLoads; m += 2) {
-                mm::load_to_lds(bq, oq[m], to + m * 1024, oq[m + 1], to + m * 1024 + 1024);
-                mm::load_to_lds(bg, og[m], to + Tk::kBytes + m * 1024, og[m + 1], to + Tk::kBytes + m * 1024 + 1024);
-            }
-        } else {
-#pragma unroll
-            for (int m = 0; m < Tk::kLoads; m++) {
-                mm::load_to_lds(bq, Tk::offset(m, 0, a.q.row, a.dim, valid), to + m * 1024);
-                mm::load_to_lds(bg, Tk::offset(m, 0, a.dy.row, a.dim, valid), to + Tk::kBytes + m * 1024);
-            }
+        for (int m = 0; m < Tk::kLoads; m++) {
+            mm::load_to_lds(bq, Tk::offset(m, 0, a.q.row, a.dim, valid), lds + m * 1024);
+            mm::load_to_lds(bg, Tk::offset(m, 0, a.dy.row, a.dim, valid), lds + Tk::kBytes + m * 1024);
         }
-    };
-    auto keep = [&](int stage) __attribute__((always_inline)) {
-        if (lane < 32) stats[wave][stage][0][lane] = MODE != kPlain ? a.cap2 - stat.x : stat.x * a.unscale, stats[wave][stage][1][lane] = -stat.y;
+        if (lane < 32) stats[wave][0][lane] = MODE != kPlain ? a.cap2 - stat.x : stat.x * a.unscale, stats[wave][1][lane] = -stat.y;
     };
     Places places;
     places.set<DP>();
     f32x16 dk[DP / 32], dv[DP / 32];
 #pragma unroll
     for (int d = 0; d < DP / 32; d++) dk[d] = f32x16{}, dv[d] = f32x16{};
-    int stage = 0;
-    if (wave < count) load(wave, 0), keep(0);
-    for (int n = wave; n < count; n += 4, stage ^= 1) {
-        // a wavefront's tiles are its own: it waits for its loads, and for its reads of the buffer that is filled next
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-        if (n + 4 < count) load(n + 4, stage ^ 1);
+    if (wave < count) load(wave);
+    mm::arrive();                                           // the values
+    for (int n = wave; n < count; n += 8) {
         const int g = n / per, i = start + (n - g * per) * 32;
         const float slope2 = MODE & kSlopes ? a.d_slopes[hk * a.group + g] * kLog2e : 0.0f;
-        const char *tq = smem[wave][stage];
-        auto add = [&](auto masked) __attribute__((always_inline)) {
-            gather<T, DP, MODE, decltype(masked)::value>(a, dk, dv, tq, tq + Tk::kBytes, 0, &stats[wave][stage][0][4 * h], &stats[wave][stage][1][4 * h], kf,
-                                                         [&](int k) __attribute__((always_inline)) { return vf[k]; }, places, i + 4 * h, from, j - shift, slope2);
-        };
-        if (i < whole) add(std::true_type());
-        else add(std::false_type());
-        if (n + 4 < count) keep(stage ^ 1);
+        const char *tq = smem[wave];
+        gather<T, DP, MODE, true>(a, dk, dv, tq, tq + Tk::kBytes, 0, &stats[wave][0][4 * h], &stats[wave][1][4 * h], kf,
+                                  [&](int k) __attribute__((always_inline)) { return row_fragment<DP, T>(values, places, 0, k); }, places, i + 4 * h, from, j - shift, slope2);
+        if (n + 8 >= count) break;
+        // a wavefront's tile is its own: it waits for its reads of it before it is filled again, and for its loads
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        load(n + 8);
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
     }
-    // the four wavefronts' sums, of keys, then of values
-    float *sums = (float *)&smem[0][0][0];
+    // the upper four wavefronts' sums to the lower four
+    float *sums = (float *)&smem[0][0];
+    __syncthreads();
+    if (wave >= 4) {
+#pragma unroll
+        for (int d = 0; d < DP / 32; d++)
+#pragma unroll
+            for (int r = 0; r < 16; r++) {
+                sums[((wave & 3) * DP + d * 16 + r) * 64 + lane] = dk[d][r];
+                sums[((wave & 3) * DP + DP / 2 + d * 16 + r) * 64 + lane] = dv[d][r];
+            }
+    }
+    __syncthreads();
+    if (wave < 4) {
+#pragma unroll
+        for (int d = 0; d < DP / 32; d++)
+#pragma unroll
+            for (int r = 0; r < 16; r++) {
+                dk[d][r] += sums[(wave * DP + d * 16 + r) * 64 + lane];
+                dv[d][r] += sums[(wave * DP + DP / 2 + d * 16 + r) * 64 + lane];
+            }
+    }
+    // those four's sums, of keys, then of values
     const int mine = threadIdx.x >> 3, sub = threadIdx.x & 7;
     const float sc = scale_of<T, MODE>(a);
     each<2>([&](int which) __attribute__((always_inline)) {
         __syncthreads();
+        if (wave < 4)
 #pragma unroll
         for (int d = 0; d < DP / 32; d++)
 #pragma unroll
@@ -445,7 +442,7 @@ template <typename T, int DP, int MODE> __global__ void __launch_bounds__(256) f
                 *(mm::f32x4 *)(sums + (wave * 32 + col) * kLine + d * 32 + mfma_row(r, h)) = mm::f32x4{x[r], x[r + 1], x[r + 2], x[r + 3]};
             }
         __syncthreads();
-        if (j0 + mine >= q.lk) return;
+        if (wave >= 4 || j0 + mine >= q.lk) return;
         const View &o = which ? a.dv : a.dk;
         T *out = (T *)o.p + s * o.seq + (q.k0 + j0 + mine) * o.row + hk * o.head;
         const float f = which ? 1.0f : sc;
@@ -460,18 +457,18 @@ template <typename T, int DP, int MODE> __global__ void __launch_bounds__(256) f
     });
 }
 
-void launch_rows(const heddle_attention_desc *d, const Args &a, int64_t blocks, int64_t tiles, hipStream_t stream)
+void launch_rows(const heddle_attention_desc *d, const Args &a, int64_t blocks, hipStream_t stream)
 {
     with_kind(d, [&](auto t, auto dp, auto mode) {
-        hipLaunchKernelGGL((rows_kernel<decltype(t), dp, mode>), dim3((unsigned)blocks), dim3(256), 0, stream, a, tiles);
+        hipLaunchKernelGGL((rows_kernel<decltype(t), dp, mode>), dim3((unsigned)blocks), dim3(256), 0, stream, a);
     });
 }
 void launch_keys(const heddle_attention_desc *d, const Args &a, int span, int64_t blocks, int64_t tiles, hipStream_t stream)
 {
     with_kind(d, [&](auto t, auto dp, auto mode) {
-        if (span == 32) hipLaunchKernelGGL((few_keys_kernel<decltype(t), dp, mode>), dim3((unsigned)blocks), dim3(256), 0, stream, a, tiles);
-        else if (span == 256) hipLaunchKernelGGL((keys_kernel<decltype(t), dp, mode, 8>), dim3((unsigned)blocks), dim3(512), 0, stream, a, tiles);
-        else hipLaunchKernelGGL((keys_kernel<decltype(t), dp, mode, 4>), dim3((unsigned)blocks), dim3(256), 0, stream, a, tiles);
+        if (span == 32) hipLaunchKernelGGL((few_keys_kernel<decltype(t), dp, mode>), dim3((unsigned)blocks), dim3(512), 0, stream, a, tiles);
+        else if (span == 256) hipLaunchKernelGGL((keys_kernel<decltype(t), dp, mode, 8>), dim3((unsigned)blocks), dim3(512), 0, stream, a);
+        else hipLaunchKernelGGL((keys_kernel<decltype(t), dp, mode, 4>), dim3((unsigned)blocks), dim3(256), 0, stream, a);
     });
 }
 
@@ -492,12 +489,12 @@ int backward(const heddle_attention_desc *d, mm::Scratch &s, bool run, hipStream
     const int64_t blocks = a.q_rows ? slots_of(d->packed, d->sequences, d->q_len, d->q_len, a.group, 128) * d->kv_heads : 0;
     // keys a workgroup takes: 32 where there would not be one of 128 keys for every CU, pairs of 128 where most sequences have several
     const int64_t keys = std::max<int64_t>(1, a.k_rows / d->sequences), span = d->sequences * ((keys + 127) / 128) * d->kv_heads < 256 ? 32 : keys >= 512 ? 256 : 128;
-    const int64_t tiles = (d->q_len * a.group + 127) / 128, ktiles = (d->k_len + span - 1) / span;
+    const int64_t ktiles = (d->k_len + span - 1) / span;
     const int64_t kblocks = d->dk && a.k_rows ? slots_of(d->packed, d->sequences, d->k_len, d->k_len, 1, span) * d->kv_heads : 0;
     if (std::max(blocks, kblocks) > (int64_t(1) << 24) - 1) return fail(HEDDLE_E_RANGE, "more tiles than a launch holds");
     if (!run) return HEDDLE_OK;
     if (const int rc = c.launch(stream)) return rc;
-    if (blocks) launch_rows(d, a, blocks, tiles, stream);
+    if (blocks) launch_rows(d, a, blocks, stream);
     if (kblocks) launch_keys(d, a, (int)span, kblocks, ktiles, stream);
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? HEDDLE_OK : hip_fail(e, "attention's gradients");

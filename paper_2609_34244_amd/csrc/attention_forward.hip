@@ -41,25 +41,20 @@ template <typename T, int MODE, bool MASKED> struct Softening {
     }
 };
 
-template <typename T, int DP, int MODE, int NW> __global__ void __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2))) forward_kernel(Args a, int64_t tiles)
+template <typename T, int DP, int MODE, int NW> __global__ void __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2))) forward_kernel(Args a)
 {
     typedef Tile<DP, 64, NW> Tk;
     constexpr int kRows = NW * 32;
     typedef typename mm::pack8<T>::type frag;
     __shared__ __align__(1024) char smem[2][2][Tk::kBytes]; // keys, values
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, h = lane >> 5;
-    // key heads fastest: 8 of them lie on one XCD each, whose L2 then holds its head's keys. The last tiles, which
-    // see the most keys, first.
-    const int hk = blockIdx.x % (uint32_t)a.kv_heads;
-    const int64_t slot = gridDim.x / (uint32_t)a.kv_heads - 1 - blockIdx.x / (uint32_t)a.kv_heads;
-    int s;
+    // key heads fastest: 8 of them lie on one XCD each, whose L2 then holds its head's keys
+    const uint32_t slot = blockIdx.x / (uint32_t)a.kv_heads;
+    const int hk = blockIdx.x - slot * a.kv_heads;
+    Sequence q;
     int64_t tile;
-    if (a.packed) {
-        if (!find_slot(a.d_q, a.q_rows, 1, a.sequences, a.group, kRows, tiles, slot, s, tile)) return;
-    } else {
-        s = (int)((uint32_t)slot % (uint32_t)a.sequences), tile = (uint32_t)slot / (uint32_t)a.sequences;
-    }
-    const Sequence q = sequence_of(a, s);
+    if (!find_tile(a, false, kRows, slot, gridDim.x / (uint32_t)a.kv_heads, q, tile)) return;
+    const int s = q.s;
     if (tile * kRows >= (int64_t)q.lq * a.group) return;
     const int r0 = (int)tile * kRows, rows = q.lq * a.group;
     const Row row = row_of(a, q, hk, r0 + wave * 32 + (lane & 31));
@@ -159,11 +154,11 @@ template <typename T, int DP, int MODE, int NW> __global__ void __launch_bounds_
         a.lse[row.at * a.heads + row.head] = l == 0 ? -INFINITY : (st.m * unit_of<MODE>(a) + offset_of<MODE>(a) + __log2f(l)) * kLn2;
 }
 
-void launch_forward(const heddle_attention_desc *d, const Args &a, int rows, int64_t blocks, int64_t tiles, hipStream_t stream)
+void launch_forward(const heddle_attention_desc *d, const Args &a, int rows, int64_t blocks, hipStream_t stream)
 {
     with_kind(d, [&](auto t, auto dp, auto mode) {
-        if (rows == 128) hipLaunchKernelGGL((forward_kernel<decltype(t), dp, mode, 4>), dim3((unsigned)blocks), dim3(256), 0, stream, a, tiles);
-        else hipLaunchKernelGGL((forward_kernel<decltype(t), dp, mode, 8>), dim3((unsigned)blocks), dim3(512), 0, stream, a, tiles);
+        if (rows == 128) hipLaunchKernelGGL((forward_kernel<decltype(t), dp, mode, 4>), dim3((unsigned)blocks), dim3(256), 0, stream, a);
+        else hipLaunchKernelGGL((forward_kernel<decltype(t), dp, mode, 8>), dim3((unsigned)blocks), dim3(512), 0, stream, a);
     });
 }
 
