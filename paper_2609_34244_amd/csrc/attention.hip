@@ -346,8 +346,15 @@ static int forward(const heddle_attention_desc *d, mm::Scratch &s, bool run, hip
     a.out_vec = !((uintptr_t)d->y & 15) && !((a.y.seq | a.y.row | a.y.head | d->dim) & 7);
     // rows of a key head in a sequence, on average
     const int64_t rows = std::max<int64_t>(1, a.q_rows * a.group / d->sequences), keys = a.k_rows / d->sequences;
-    const bool split = rows <= 64;
-    const int T = split ? 32 : rows >= 1024 ? 256 : 128;
+    // Whether the keys are divided over workgroups, by an estimate in us of both kernels. Measured, 8 sequences of 4000 keys, 32
+    // heads on 8: 2, 16, 32, 64 queries 27, 39, 59, 115 us divided, 83, 82, 84, 85 not; 32 of 200 keys, 16 queries: 18 and 14; one of
+    // 16000 keys, 64 queries: 72 and 312; 2 of 600, 600 queries, 8 heads: 21.5 and 19.3.
+    const double tiles128 = (double)d->sequences * ((rows + 127) / 128) * d->kv_heads, tiles32 = (double)d->sequences * ((rows + 31) / 32) * d->kv_heads;
+    const bool split = 8 + 0.0125 * keys * std::max(1.0, tiles32 / 256) < 2 + 0.0205 * keys * std::max(1.0, tiles128 / 360);
+    // 256 rows a workgroup read each tile of keys half as often as 128, but want two rounds of workgroups (2 sequences of 2048, 32
+    // heads: 88 us with 256 rows, 111 with 128; one of 2000, 8 heads: 64 and 50; 3 of 333, 12 heads: 18 and 15)
+    const bool tall = rows >= 512 && d->sequences * ((rows + 255) / 256) * d->kv_heads >= 512;
+    const int T = split ? 32 : tall ? 256 : 128;
     const int64_t slots = slots_of(d->packed, d->sequences, d->q_len, d->q_len, a.group, T), tiles = (d->q_len * a.group + T - 1) / T;
     int64_t blocks = slots * d->kv_heads;
     a.parts = 1;

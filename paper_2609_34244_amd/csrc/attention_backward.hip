@@ -487,8 +487,10 @@ int backward(const heddle_attention_desc *d, mm::Scratch &s, bool run, hipStream
     auto aligned = [&](const void *p, const View &v) { return !((uintptr_t)p & 15) && !((v.seq | v.row | v.head | d->dim) & 7); };
     a.out_vec = (!d->dq || aligned(d->dq, a.dq)) && (!d->dk || (aligned(d->dk, a.dk) && aligned(d->dv, a.dv)));
     const int64_t blocks = a.q_rows ? slots_of(d->packed, d->sequences, d->q_len, d->q_len, a.group, 128) * d->kv_heads : 0;
-    // keys a workgroup takes: 32 where there would not be one of 128 keys for every CU, pairs of 128 where most sequences have several
-    const int64_t keys = std::max<int64_t>(1, a.k_rows / d->sequences), span = d->sequences * ((keys + 127) / 128) * d->kv_heads < 256 ? 32 : keys >= 512 ? 256 : 128;
+    // Keys a workgroup takes: 32 where there would not be one of 128 keys for every CU (one sequence of 2000, 8 heads: 54 us, 66
+    // with pairs of 128); pairs of 128 where that leaves few rounds (4 of 2048, 64 heads on 8: 563 us, 603 with 128; 4 of 1000, 32 heads: 91 and 87).
+    const int64_t keys = std::max<int64_t>(1, a.k_rows / d->sequences), singles = d->sequences * ((keys + 127) / 128) * d->kv_heads;
+    const int64_t span = singles < 256 ? 32 : singles < 1024 && keys >= 512 ? 256 : 128;
     const int64_t ktiles = (d->k_len + span - 1) / span;
     const int64_t kblocks = d->dk && a.k_rows ? slots_of(d->packed, d->sequences, d->k_len, d->k_len, 1, span) * d->kv_heads : 0;
     if (std::max(blocks, kblocks) > (int64_t(1) << 24) - 1) return fail(HEDDLE_E_RANGE, "more tiles than a launch holds");

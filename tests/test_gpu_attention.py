@@ -190,7 +190,7 @@ def test_magnitudes(H, magnitude, lq):
     run(H, 52, [lq], [400], 2, 2, 64, FP16, False, 50.0, magnitude=magnitude, train=magnitude < 1)
 
 
-@pytest.mark.parametrize("lq,lk,hq,hk", [(1, 5000, 4, 1), (2, 3001, 2, 2), (1, 20000, 1, 1), (16, 2100, 4, 4)])
+@pytest.mark.parametrize("lq,lk,hq,hk", [(1, 5000, 4, 1), (2, 3001, 2, 2), (1, 20000, 1, 1), (16, 2100, 4, 4), (100, 4000, 4, 2)])
 def test_long_caches(H, lq, lk, hq, hk):
     """keys divided over workgroups"""
     run(H, 61, [lq], [lk], hq, hk, 128, BF16, True, 0.0, True, train=False)
