@@ -731,8 +731,9 @@ int heddle_grad_norm_workspace(const heddle_grad_desc *grads, int32_t count, int
  * address and strides will do: full speed for 16-byte addresses, strides of
  * whole eights and dim a multiple of 8 (other operands are copied to scratch).
  * lse: [all query rows][heads] fp32, log(sum_j exp(s)). Inputs of
- * visible rows are finite: a product of 0 and an infinity or NaN of a key that
- * some rows do not see may reach those rows too. Outputs lie apart from inputs
+ * sequences' rows are finite: a product of 0 and an infinity or NaN of a key that
+ * some rows do not see may reach those rows too, and one of a row's dy the
+ * gradients of keys that it does not see. Outputs lie apart from inputs
  * and from each other (seen where heads lie side by side; tensors with other
  * orders of dimensions may overlap unseen).
  */
@@ -740,7 +741,7 @@ typedef struct heddle_attention_desc {
     int32_t dtype, causal, packed, sequences;         /* HEDDLE_T_BF16 or HEDDLE_T_F16; sequences 0 .. HEDDLE_MAX_GROUPS */
     int64_t q_len, k_len;                             /* q_len * heads, k_len 0 .. HEDDLE_MAX_ROWS */
     int32_t heads, kv_heads, dim;                     /* heads a multiple of kv_heads; dim 1 .. HEDDLE_MAX_HEAD_DIM */
-    float scale, cap;                                 /* scale > 0; cap 0: none */
+    float scale, cap;                                 /* scale 1e-20 .. 1e20; cap 0: none, or 1e-3 .. 4096 */
     const int32_t *d_q, *d_k;                         /* offsets [sequences + 1], or lengths [sequences] or NULL */
     const int32_t *d_prefix;                          /* [sequences] or NULL */
     const float *d_slopes;                            /* [heads] or NULL */

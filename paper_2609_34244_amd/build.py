@@ -4,17 +4,19 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libheddle.so")
 SOURCES = ["profile.cpp", "windows.hip", "price.hip", "search.hip", "evaluate.hip", "distribute.hip", "argmin.hip", "enumerate.hip", "tile.hip",
            "fill.hip", "linear.hip", "gated_ffn.hip", "clip.hip", "norm.hip", "balance.hip", "attention.hip",
-           "attention_backward.hip"]
+           "attention_forward.hip", "attention_backward.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 FLAGS = [
-    "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared", "-Wall", "-Wno-unused-function",
+    "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",
     # inline asm that names m0, which the compiler keeps for no value of its own here
     "-Wno-inline-asm",
     # no packed fp32 instructions in device code
@@ -22,10 +24,8 @@ FLAGS = [
 ]
 
 
-def build(verbose=False):
-    srcs = [os.path.join(CSRC, s) for s in SOURCES]
-    tmp = LIB + ".tmp"
-    cmd = [HIPCC, *FLAGS, "-o", tmp, *srcs]
+def _hipcc(args, verbose):
+    cmd = [HIPCC, *FLAGS, *args]
     if verbose:
         print(" ".join(cmd), flush=True)
     r = subprocess.run(cmd, capture_output=True, text=True)
@@ -35,6 +35,15 @@ def build(verbose=False):
         raise RuntimeError(f"hipcc failed ({r.returncode}):\n{err}")
     if err.strip() and verbose:
         print(err, file=sys.stderr)
+
+
+def build(verbose=False):
+    """Compiles the sources, several at a time, and links them."""
+    tmp = LIB + ".tmp"
+    with tempfile.TemporaryDirectory() as d, ThreadPoolExecutor(max_workers=min(8, os.cpu_count() or 1)) as pool:
+        objects = [os.path.join(d, s + ".o") for s in SOURCES]
+        list(pool.map(lambda so: _hipcc(["-c", os.path.join(CSRC, so[0]), "-o", so[1]], verbose), zip(SOURCES, objects)))
+        _hipcc(["-shared", "-o", tmp, *objects], verbose)
     os.replace(tmp, LIB)
     return LIB
 

@@ -52,6 +52,7 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 __device__ inline f32x16 mfma(mm::bf16x8 a, mm::bf16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
 __device__ inline f32x16 mfma(mm::f16x8 a, mm::f16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
 
+constexpr int64_t kMostBlocks = (int64_t(1) << 23) - 1;   // of 512 lanes: a launch has fewer than 2^32
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 

@@ -255,8 +255,9 @@ int check(const heddle_attention_desc *d, bool backward)
     if (d->sequences < 0 || d->sequences > HEDDLE_MAX_GROUPS) return fail(HEDDLE_E_INVAL, "sequences out of range");
     if (d->q_len < 0 || d->k_len < 0 || d->q_len > HEDDLE_MAX_ROWS / d->heads || d->k_len > HEDDLE_MAX_ROWS)
         return fail(HEDDLE_E_INVAL, "q_len or k_len out of range");
-    if (!(std::isfinite(d->scale) && d->scale > 0)) return fail(HEDDLE_E_INVAL, "scale is not finite and > 0");
-    if (!(std::isfinite(d->cap) && d->cap >= 0)) return fail(HEDDLE_E_INVAL, "cap is not finite and >= 0");
+    if (!(d->scale >= 1e-20f && d->scale <= 1e20f)) return fail(HEDDLE_E_INVAL, "scale out of range");
+    // the tanh is off by a few 2^-24 of 1: by 2^-11 of a score of any size at the largest cap
+    if (!(d->cap == 0 || (d->cap >= 1e-3f && d->cap <= 4096))) return fail(HEDDLE_E_INVAL, "cap out of range");
     if (d->packed && d->sequences > 0 && (!d->d_q || !d->d_k)) return fail(HEDDLE_E_INVAL, "packed sequences without offsets");
     if (((uintptr_t)d->d_q | (uintptr_t)d->d_k | (uintptr_t)d->d_prefix | (uintptr_t)d->d_slopes | (uintptr_t)d->lse) & 3)
         return fail(HEDDLE_E_INVAL, "d_q, d_k, d_prefix, d_slopes or lse is misaligned");
@@ -365,7 +366,7 @@ static int forward(const heddle_attention_desc *d, mm::Scratch &s, bool run, hip
         a.parts = (int32_t)std::max<int64_t>(1, std::min<int64_t>({(used >= 128 ? 512 : 256) / used, keys / 128, 64}));
         if (a.parts > 1) a.partial = (float *)s.take((size_t)blocks * 32 * a.parts * ((d->dim <= 64 ? 64 : 128) + 2) * 4);
     }
-    if (blocks * std::max(a.parts, 8) > (int64_t(1) << 24) - 1) return fail(HEDDLE_E_RANGE, "more tiles than a launch holds");
+    if (blocks * (a.parts > 1 ? std::max(a.parts, 8) : 1) > kMostBlocks) return fail(HEDDLE_E_RANGE, "more tiles than a launch holds");
     if (!run) return HEDDLE_OK;
     if (const int rc = c.launch(stream)) return rc;
     if (!split) {

@@ -53,6 +53,7 @@ template <typename T, int MODE, bool READY> HEDDLE_INLINE float2 weigh(const Arg
 template <typename T, int DP, int MODE> __global__ void __launch_bounds__(256, 2) rows_kernel(Args a)
 {
     typedef Tile<DP, 64, 4> Tk;
+    constexpr int kRows = 128;
     typedef typename mm::pack8<T>::type frag;
     __shared__ __align__(1024) char smem[2][2 * Tk::kBytes];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, h = lane >> 5, col = lane & 31;
@@ -60,15 +61,15 @@ template <typename T, int DP, int MODE> __global__ void __launch_bounds__(256, 2
     const int hk = blockIdx.x - slot * a.kv_heads;
     Sequence q;
     int64_t tile;
-    if (!find_tile(a, false, 128, slot, gridDim.x / (uint32_t)a.kv_heads, q, tile)) return;
+    if (!find_tile(a, false, kRows, slot, gridDim.x / (uint32_t)a.kv_heads, q, tile)) return;
     const int s = q.s;
-    if (tile * 128 >= (int64_t)q.lq * a.group) return;
-    const int rows = q.lq * a.group, r = (int)tile * 128 + wave * 32 + col;
+    if (tile * kRows >= (int64_t)q.lq * a.group) return;
+    const int rows = q.lq * a.group, r = (int)tile * kRows + wave * 32 + col;
     const bool any = r < rows;
     const int i = r / a.group, head = hk * a.group + (any ? r - i * a.group : 0), shift = q.lk - q.lq;
     auto limit_at = [&](int x) { return x >= rows ? 0 : max(min(q.lk, a.causal ? max(x / a.group + shift + 1, q.prefix) : q.lk), 0); };
-    const int limit = limit_at(r), r0 = (int)tile * 128 + wave * 32;
-    const int end = __builtin_amdgcn_readfirstlane(limit_at(min((int)tile * 128 + 127, rows - 1)));
+    const int limit = limit_at(r), r0 = (int)tile * kRows + wave * 32;
+    const int end = __builtin_amdgcn_readfirstlane(limit_at(min((int)tile * kRows + kRows - 1, rows - 1)));
     const int mine = r0 < rows ? __builtin_amdgcn_readfirstlane(limit_at(min(r0 + 31, rows - 1))) : 0;
     const int whole = r0 + 31 < rows ? __builtin_amdgcn_readfirstlane(limit_at(r0)) : 0;
     const int count = (a.grads & 1) ? (end + 63) / 64 : 0;
@@ -493,7 +494,7 @@ int backward(const heddle_attention_desc *d, mm::Scratch &s, bool run, hipStream
     const int64_t span = singles < 256 ? 32 : singles < 1024 && keys >= 512 ? 256 : 128;
     const int64_t ktiles = (d->k_len + span - 1) / span;
     const int64_t kblocks = d->dk && a.k_rows ? slots_of(d->packed, d->sequences, d->k_len, d->k_len, 1, span) * d->kv_heads : 0;
-    if (std::max(blocks, kblocks) > (int64_t(1) << 24) - 1) return fail(HEDDLE_E_RANGE, "more tiles than a launch holds");
+    if (std::max(blocks, kblocks) > kMostBlocks) return fail(HEDDLE_E_RANGE, "more tiles than a launch holds");
     if (!run) return HEDDLE_OK;
     if (const int rc = c.launch(stream)) return rc;
     if (blocks) launch_rows(d, a, blocks, stream);

@@ -855,7 +855,7 @@ def heddle_attention(q, k, v, scale=None, causal=False, cap=0.0, slopes=None, pr
     k_offsets [sequences + 1]. Tensors may have any strides with a head's
     values side by side.
 
-    s = scale q k (scale: dim ** -0.5), cap * tanh(s / cap) with a cap, minus
+    s = scale q k (scale: dim ** -0.5), cap * tanh(s / cap) with a cap (to 4096), minus
     slopes[head] * distance (float32 [heads]). causal: a query sees the keys up to
     its own place, the last query standing at the last key, and the first
     prefix[sequence] keys (int32). lse: float32, q's shape without dim, to keep

@@ -190,6 +190,12 @@ def test_magnitudes(H, magnitude, lq):
     run(H, 52, [lq], [400], 2, 2, 64, FP16, False, 50.0, magnitude=magnitude, train=magnitude < 1)
 
 
+@pytest.mark.parametrize("cap,scale", [(0.5, None), (4096.0, 0.3), (0.0, 2.0), (0.0, 1e-6), (1e-3, 1.0)])
+def test_extremes_of_cap_and_scale(H, cap, scale):
+    run(H, 55, [40], [90], 2, 1, 64, BF16, True, cap, scale=scale)
+    run(H, 56, [1], [300], 4, 1, 64, BF16, True, cap, True, scale=scale)
+
+
 @pytest.mark.parametrize("lq,lk,hq,hk", [(1, 5000, 4, 1), (2, 3001, 2, 2), (1, 20000, 1, 1), (16, 2100, 4, 4), (100, 4000, 4, 2)])
 def test_long_caches(H, lq, lk, hq, hk):
     """keys divided over workgroups"""

@@ -76,7 +76,7 @@ def refused(L, desc, which):
 
 BOTH = [dict(dtype=2), dict(dtype=-1), dict(heads=0), dict(heads=1026), dict(kv_heads=0), dict(kv_heads=3), dict(dim=0), dict(dim=129),
         dict(sequences=-1), dict(sequences=65536), dict(q_len=-1), dict(k_len=-1), dict(q_len=2**28 + 1), dict(k_len=2**30 + 1), dict(scale=0.0),
-        dict(scale=-1.0), dict(scale=float("nan")), dict(scale=float("inf")), dict(cap=-1.0), dict(cap=float("nan")), dict(packed=1),
+        dict(scale=-1.0), dict(scale=float("nan")), dict(scale=float("inf")), dict(scale=1e-30), dict(cap=-1.0), dict(cap=float("nan")), dict(cap=5000.0), dict(cap=1e-6), dict(packed=1),
         dict(packed=1, d_q=P), dict(d_q=P + 2), dict(d_k=P + 1), dict(d_prefix=P + 2), dict(d_slopes=P + 2), dict(q=0), dict(q=P + 1), dict(k=0),
         dict(v=0), dict(y=0), dict(lse=P + 2), dict(q_strides=three(9999, 256, 63)), dict(k_strides=three(9999, -128, 64)),
         dict(v_strides=three(-1, 128, 64)), dict(q_strides=three(9999, 2**22 + 1, 64)), dict(k_strides=three(9999, 63, 64)), dict(v_strides=three(0, 128, 64))]
