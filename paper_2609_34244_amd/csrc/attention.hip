@@ -2,11 +2,10 @@
 //
 // One pass over the keys with a running maximum and sum. Query rows of a key head, (query, head of its
 // group) pairs in that order, are taken 32 a wavefront, so that heads that share keys share their tiles.
-// forward_kernel: 128 rows a workgroup over tiles of 64 keys, two in LDS; two workgroups a CU, so that one's
-// products run beside the other's exponentials. Bound by both: 32 keys of 32 rows are 16 products of 32
-// cycles and 16 values a lane of about 30 cycles.
+// forward_kernel (attention_forward.hip): 128 or 256 rows a workgroup over tiles of 64 keys.
 // split_kernel: 32 rows a workgroup (few queries over long caches), each wavefront with tiles of its own, the
-// keys of a row tile divided over `parts` workgroups; combine_kernel joins them. Bound by reading keys and values.
+// keys of a row tile divided over `parts` workgroups; combine_kernel joins them. Bound by reading keys and values: 32
+// sequences of up to 8192 keys, 8 key heads, 125 us (4.2 TB/s); one of 2048, 32 heads, 12 + 4 us.
 #include <algorithm>
 #include <cmath>
 

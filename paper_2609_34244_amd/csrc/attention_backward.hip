@@ -4,9 +4,12 @@
 // dq = scale dS K, dk = scale dS^T Q, dv = P^T dY. P is formed again in both kernels, so that each
 // sum stays in registers and is added up in one order, without atomics: 7 products instead of 5.
 // rows_kernel (dq): 128 query rows a workgroup, tiles of 64 keys, like the forward pass; it also
-// leaves lse log2(e) and delta of its rows for the other one. keys_kernel (dk, dv): 128 keys a
+// leaves lse log2(e) and delta of its rows for the other one. keys_kernel (dk, dv): 128 keys or two times 128 a
 // workgroup, 32 a wavefront, over tiles of query rows of each head of the group in turn, whose sum
-// the shared heads' gradient is. P and dS are rounded to the operands' type, as the products' operands.
+// the shared heads' gradient is; the values' operands are read from LDS, as with keys, values and both sums in registers a SIMD
+// would hold one wavefront. P and dS are rounded to the operands' type, as the products' operands.
+// Bound as the forward pass is: 4 sequences of 2048, 64 heads on 8: dq 452 us, dk and dv 562 us (912 and 977 TFLOP/s of products), with a
+// cap 509 and 646.
 #include <algorithm>
 #include <cmath>
 
