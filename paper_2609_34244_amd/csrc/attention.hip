@@ -5,7 +5,7 @@
 // forward_kernel (attention_forward.hip): 128 or 256 rows a workgroup over tiles of 64 keys.
 // split_kernel: 32 rows a workgroup (few queries over long caches), each wavefront with tiles of its own, the
 // keys of a row tile divided over `parts` workgroups; combine_kernel joins them. Bound by reading keys and values: 32
-// sequences of up to 8192 keys, 8 key heads, 125 us (4.2 TB/s); one of 2048, 32 heads, 12 + 4 us.
+// sequences of up to 8192 keys, 8 key heads, 128 us (4.1 TB/s); one of 2048, 32 heads, 13 + 4 us.
 #include <algorithm>
 #include <cmath>
 

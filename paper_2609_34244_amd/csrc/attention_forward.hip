@@ -1,8 +1,8 @@
 // Attention's forward pass over many query rows.
 //
 // A workgroup of four or eight wavefronts takes 32 rows each over tiles of 64 keys; keys and values are in LDS twice. Bound by the
-// matrix cores and the vector units, which overlap little: a step of 32 keys is 16 products of 32 cycles and, without a
-// cap or slopes, about 110 vector instructions of 4 cycles (exponentials 8). 8192 queries, 32 heads on 8, slopes: 551 us (998
+// matrix cores and the vector units, which overlap little: a step of 32 keys is 16 products of 32 cycles and
+// vector instructions of about 610 cycles with slopes, 900 with a cap. 8192 queries, 32 heads on 8, slopes: 564 us (975
 // TFLOP/s; 659 with addresses formed at each read, masks in every tile, keys from first to last, and products and exponentials apart); 4
 // sequences of 2048, 64 heads on 8: 330 us (832 TFLOP/s), with a cap 387.
 #include "attention.h"
