@@ -765,7 +765,9 @@ int heddle_attention(const heddle_attention_desc *d, void *d_workspace, int64_t 
  * heddle_attention_backward -- with P = exp(s - lse), dP = dy v^T, D = sum dy y,
  * dS = P (dP - D) (1 - tanh^2 with a cap): dq = scale dS k, dk = scale dS^T q,
  * dv = P^T dy, the last two summed over the heads of a key head, in a fixed
- * order. P and dS are rounded to dtype as operands. No gradient of the slopes.
+ * order. P and dS are rounded to dtype as operands, dS before the scale: in
+ * HEDDLE_T_F16 a dS past 65504 is an infinity, and one below 2^-25 counts as 0.
+ * No gradient of the slopes.
  */
 int heddle_attention_backward(const heddle_attention_desc *d, void *d_workspace, int64_t workspace_bytes, hipStream_t stream);
 int heddle_attention_workspace(const heddle_attention_desc *d, int32_t backward, int64_t *h_bytes);

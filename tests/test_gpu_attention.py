@@ -340,3 +340,19 @@ def test_refusals(H):
         with pytest.raises(H.HeddleError) as e:
             call()
         assert e.value.code == H.HEDDLE_E_INVAL
+
+
+@pytest.mark.parametrize("a,b,c,want", [(2.0 ** -12, 2.0 ** -11, 2.0 ** 10, 2.0 ** -13), (2.0 ** -7, 2.0 ** -6, 2.0 ** 10, 2.0 ** -3),
+                                        (2.0 ** -13, 2.0 ** -12, 2.0 ** 10, 0.0), (2.0 ** 8, 2.0 ** 8, 2.0 ** -3, 2.0 ** 13),
+                                        (2.0 ** 9, 2.0 ** 9, 2.0 ** -4, float("inf"))])
+def test_range_of_float16_gradients(H, a, b, c, want):
+    """Two keys of equal scores, values b and -b, dy a: y = 0, D = 0, dS = a b / 2 and -a b / 2, dq = 2 c dS for keys c and
+    -c. dS is 2^-24 (the smallest float16), 2^-14, 2^-26 (0 when rounded), 2^15 and 2^17 (past the largest). P is off by
+    some 2^-22, far from half a step of dS, and all else is a power of two: dq is what it should be, to its rounding."""
+    q, k, v, dy = torch.zeros(1, 1, 1, 16), torch.zeros(1, 2, 1, 16), torch.zeros(1, 2, 1, 16), torch.zeros(1, 1, 1, 16)
+    k[0, :, 0, 0], v[0, :, 0, 0], dy[..., 0] = torch.tensor([c, -c]), torch.tensor([b, -b]), a
+    q, k, v, dy = (t.half().cuda() for t in (q, k, v, dy))
+    lse = torch.empty(1, 1, 1, device="cuda")
+    y = H.heddle_attention(q, k, v, scale=1.0, lse=lse)
+    dq = float(H.heddle_attention_backward(dy, q, k, v, y, lse, scale=1.0)["dq"][0, 0, 0, 0])
+    assert dq == want or abs(dq - want) <= 2.0 ** -11 * want, dq
