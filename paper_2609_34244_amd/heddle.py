@@ -1007,6 +1007,8 @@ def heddle_expert_balance_backward(logits, picked, counts, rows, dloss=None, sca
     pr = (0, 0) if residual is None else _matrix(residual, "residual", (t, e), logits.dtype, gpu)
     if dloss is not None and (dloss.numel() != 1 or str(dloss.dtype) != "torch.float32" or dloss.get_device() != gpu):
         _refuse("dloss: not one float32 value on the logits' GPU")
+    if dloss is not None and dloss.requires_grad:
+        _unrecorded("dloss")
     desc = _BALANCE.pack(_dtype(logits, "logits"), e, k, size, t, scale, pl, ldl, pp, ldp, _ints(counts, "counts", e, gpu),
                          _ints(rows, "rows", 1, gpu), 0, 0, 0, 0 if dloss is None else dloss.data_ptr(), *pr,
                          *_matrix(out, "out", (t, e), logits.dtype, gpu))

@@ -174,3 +174,15 @@ def test_refusals(H):
         with pytest.raises(H.HeddleError) as e:
             call()
         assert e.value.code == H.HEDDLE_E_INVAL
+
+
+def test_loss_gradient_requires_grad(H):
+    z, p = torch.ones(4, 8, device="cuda"), torch.zeros(4, 2, dtype=torch.int64, device="cuda")
+    got = H.heddle_expert_balance(z, p)
+    given = torch.full((1,), 0.5, device="cuda")
+    want = H.heddle_expert_balance_backward(z, p, got["counts"], got["rows"], dloss=given)
+    given.requires_grad_(True)
+    with pytest.raises(H.HeddleError, match="no_grad"):
+        H.heddle_expert_balance_backward(z, p, got["counts"], got["rows"], dloss=given)
+    with torch.no_grad():
+        assert torch.equal(H.heddle_expert_balance_backward(z, p, got["counts"], got["rows"], dloss=given), want)
