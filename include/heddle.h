@@ -758,7 +758,8 @@ typedef struct heddle_attention_desc {
 
 /*
  * heddle_attention -- probabilities are rounded to dtype as operands of the
- * product with v; their sum is of the values before that rounding.
+ * product with v; their sum is of the values before that rounding. Scores are
+ * fp32, and may be any that are finite there.
  */
 int heddle_attention(const heddle_attention_desc *d, void *d_workspace, int64_t workspace_bytes, hipStream_t stream);
 /*
@@ -767,6 +768,8 @@ int heddle_attention(const heddle_attention_desc *d, void *d_workspace, int64_t 
  * dv = P^T dy, the last two summed over the heads of a key head, in a fixed
  * order. P and dS are rounded to dtype as operands, dS before the scale: in
  * HEDDLE_T_F16 a dS past 65504 is an infinity, and one below 2^-25 counts as 0.
+ * P comes from the 24 bits of lse: it is off by some 2^-22 |s| of itself, so
+ * that scores past 2^20 leave it hardly a digit, and past 2^27 it may overflow.
  * No gradient of the slopes.
  */
 int heddle_attention_backward(const heddle_attention_desc *d, void *d_workspace, int64_t workspace_bytes, hipStream_t stream);

@@ -312,6 +312,8 @@ enum Mode { kPlain = 0, kCap = 1, kSlopes = 2 };
 // cancel (offset_of() has them for lse). slope: in these units. distance: from register 0's key to the row's place.
 template <int MODE> HEDDLE_INLINE float unit_of(const Args &a) { return MODE & kCap ? 2 * a.cap2 : a.scale2; }
 template <int MODE> HEDDLE_INLINE float offset_of(const Args &a) { return MODE & kCap ? a.cap2 : 0.0f; }
+// the same where the mode is not a constant
+__device__ inline float unit_of(const Args &a) { return a.cap2 > 0 ? 2 * a.cap2 : a.scale2; }
 template <int MODE> HEDDLE_INLINE float slope_of(const Args &a, int head) { return MODE & kSlopes ? a.d_slopes[head] * kLog2e / unit_of<MODE>(a) : 0.0f; }
 template <int MODE> HEDDLE_INLINE float modify(const Args &a, float s, int r, float slope, float distance)
 {
@@ -349,9 +351,10 @@ __device__ inline int limit_of(const Args &a, const Sequence &q, int r)
 template <int DP> struct State {
     f32x16 o[DP / 32];
     float m, l;
+    bool far;                                 // (of forward_kernel)
     __device__ inline void init()
     {
-        m = -INFINITY, l = 0;
+        m = -INFINITY, l = 0, far = false;
 #pragma unroll
         for (int d = 0; d < DP / 32; d++) o[d] = f32x16{};
     }
@@ -364,6 +367,16 @@ template <typename T, int DP> HEDDLE_INLINE f32x16 score(const char *tk, const P
 #pragma unroll
     for (int k = 0; k < DP / 16; k++) s = mfma(row_fragment<DP, T>(tk, at, from, k), q[k], s);
     return s;
+}
+
+// The maximum times the unit is what exponents start from. Its rounding is common to a row's probabilities, but from
+// kFar on past 2^-4 of an exponent, and for scores near 2^28 past float16's range: there the maximum is taken off
+// the scores first, exactly near it. far: whether it is so far for one of the wavefront's rows.
+constexpr float kFar = 1 << 20;
+template <int MODE> HEDDLE_INLINE bool is_far(float base)
+{
+    if constexpr (MODE == kCap) return false;               // (scores to 2 cap log2(e))
+    return __any(fabsf(base) > kFar);
 }
 
 // Probabilities of 32 keys, key `first` the lane's register 0. The maximum follows only when it is 2^8 behind: p then
@@ -381,7 +394,11 @@ HEDDLE_INLINE bool soften(const Args &a, f32x16 &s, float &m, float &was, float 
     was = m;
     m = follow ? fmaxf(m, top) : m;
     here(m);
-    const float base = m == -INFINITY ? 0.0f : m * unit;
+    float base = m == -INFINITY ? 0.0f : m * unit;
+    if (is_far<MODE>(base)) {
+        each<16>([&](int r) { s[r] -= m == -INFINITY ? 0.0f : m; });
+        base = 0;
+    }
     sum = 0;
     each<16>([&](int r) {
         s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], unit, -base));

@@ -14,7 +14,7 @@
 namespace heddle {
 namespace attn {
 
-// 32 rows a workgroup. The sums of a part, where there are several: DP values, the maximum (times log2(e)) and the sum.
+// 32 rows a workgroup. The sums of a part, where there are several: DP values, the maximum (in modify()'s units, whose differences are exact where they count) and the sum.
 template <typename T, int DP, int MODE> __global__ void __launch_bounds__(256) split_kernel(Args a, int64_t tiles)
 {
     typedef Tile<DP, 32, 1> Tk;
@@ -91,7 +91,7 @@ template <typename T, int DP, int MODE> __global__ void __launch_bounds__(256) s
         attend(std::true_type());
     }
     // the four wavefronts' sums
-    const float m = st.m == -INFINITY ? -INFINITY : st.m * unit_of<MODE>(a) + offset_of<MODE>(a), l = st.l + other_half(st.l);
+    const float m = st.m, l = st.l + other_half(st.l), unit = unit_of<MODE>(a);
     float *sums = (float *)&smem[0][0][0], *ms = sums + 4 * 32 * kLine;   // [wave][row][kLine], [wave][row] of m, then of l
     __syncthreads();
 #pragma unroll
@@ -110,7 +110,7 @@ template <typename T, int DP, int MODE> __global__ void __launch_bounds__(256) s
     float f[4], sum = 0;
 #pragma unroll
     for (int w = 0; w < 4; w++) {
-        f[w] = ms[w * 32 + mine] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(ms[w * 32 + mine] - top);
+        f[w] = ms[w * 32 + mine] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((ms[w * 32 + mine] - top) * unit);
         sum += f[w] * ms[128 + w * 32 + mine];
     }
     const float inv = a.parts > 1 ? 1.0f : sum == 0 ? 0.0f : 1.0f / sum;
@@ -131,7 +131,7 @@ template <typename T, int DP, int MODE> __global__ void __launch_bounds__(256) s
     }
     if (sub) return;
     if (a.parts > 1) p[DP] = top, p[DP + 1] = sum;
-    else if (a.lse) a.lse[out.at * a.heads + out.head] = sum == 0 ? -INFINITY : (top + __log2f(sum)) * kLn2;
+    else if (a.lse) a.lse[out.at * a.heads + out.head] = sum == 0 ? -INFINITY : (top * unit + offset_of<MODE>(a) + __log2f(sum)) * kLn2;
 }
 
 // Joins the parts of a row, one wavefront a row: a lane has a part's maximum and sum (parts <= 64), then DP / 64
@@ -162,7 +162,7 @@ template <typename T, int DP> __global__ void __launch_bounds__(256) combine_ker
     float top = m;
 #pragma unroll
     for (int d = 32; d; d /= 2) top = fmaxf(top, __shfl_xor(top, d));
-    const float f = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - top);
+    const float unit = unit_of(a), f = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m - top) * unit);
     float sum = f * l;
 #pragma unroll
     for (int d = 32; d; d /= 2) sum += __shfl_xor(sum, d);
@@ -177,7 +177,7 @@ template <typename T, int DP> __global__ void __launch_bounds__(256) combine_ker
 #pragma unroll
     for (int i = 0; i < kValues; i++)
         if (lane * kValues + i < a.dim) y[lane * kValues + i] = (T)(v[i] * inv);
-    if (a.lse && lane == 0) a.lse[out.at * a.heads + out.head] = sum == 0 ? -INFINITY : (top + __log2f(sum)) * kLn2;
+    if (a.lse && lane == 0) a.lse[out.at * a.heads + out.head] = sum == 0 ? -INFINITY : (top * unit + a.cap2 + __log2f(sum)) * kLn2;
 }
 
 // ---- operands that do not lie on 16-byte boundaries ----

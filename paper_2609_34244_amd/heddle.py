@@ -879,7 +879,8 @@ def heddle_attention_backward(dy, q, k, v, y, lse, scale=None, causal=False, cap
     given tensors are written, dk and dv together). y, lse: what
     heddle_attention returned and kept. Rows past the lengths, or in no
     document, are left as they were. float16: the scores' gradients before the scale,
-    p * (dy v - sum(dy * y)), are float16 operands and need its range."""
+    p * (dy v - sum(dy * y)), are float16 operands and need its range. Probabilities
+    are formed again from lse: scores past 2^20 leave them hardly a digit."""
     gpu, dt, head, qs, ks = _attention_inputs(q, k, v, scale, causal, cap, slopes, prefix, q_lengths, k_lengths, q_offsets,
                                               k_offsets)
     if lse is None or y is None:
