@@ -726,9 +726,10 @@ int heddle_grad_norm_workspace(const heddle_grad_desc *grads, int32_t count, int
  * written. Head h reads key head h / (heads / kv_heads).
  *
  * Values run over dim side by side; strides [3] are elements from one sequence
- * (ignored where packed), row and head to the next; a row's at most HEDDLE_MAX_LD,
- * one of a dimension of size 1 is not looked at. Any
- * address and strides will do: full speed for 16-byte addresses, strides of
+ * (ignored where packed), row and head to the next, at least dim; a row's at most
+ * HEDDLE_MAX_LD, one of a dimension of size 1 is not looked at. In an output each
+ * steps over all that the smaller ones reach. Any address, order of dimensions and
+ * such strides will do: full speed for 16-byte addresses, strides of
  * whole eights and dim a multiple of 8 (other operands are copied to scratch).
  * lse: [all query rows][heads] fp32, log(sum_j exp(s)). Inputs of
  * sequences' rows are finite: a product of 0 and an infinity or NaN of a key that

@@ -244,6 +244,45 @@ Args base_args(const heddle_attention_desc *d)
     return a;
 }
 
+// A tensor as runs of `cols` values at up to three distances, the smallest first. Dimensions that go on a run, or its
+// repetition, are part of it.
+typedef __int128 Wide;                        // (distances between sequences have no bound)
+struct Runs {
+    const char *name;
+    const void *p;                            // NULL: not given, or of no values
+    int64_t cols;
+    int levels;
+    int64_t size[3], step[3];
+    // values from the first to the last, of the first n levels
+    Wide extent(int n) const
+    {
+        Wide e = cols;
+        for (int i = 0; i < n; i++) e += (Wide)(size[i] - 1) * step[i];
+        return e;
+    }
+    // (distances that each step over all that is smaller; others may do without an overlap, but nothing lays tensors so)
+    bool over_itself() const
+    {
+        for (int i = 0; i < levels; i++)
+            if (step[i] < extent(i)) return true;
+        return false;
+    }
+};
+static Runs runs_of(const heddle_attention_desc *d, const char *name, const void *p, const int64_t *st, bool keys)
+{
+    const int64_t n[3] = {keys ? d->kv_heads : d->heads, keys ? d->k_len : d->q_len, d->packed ? 1 : d->sequences}, step[3] = {st[2], st[1], st[0]};
+    Runs r = {name, n[0] * n[1] * n[2] ? p : nullptr, d->dim, 0, {}, {}};
+    int order[3] = {0, 1, 2};
+    std::stable_sort(order, order + 3, [&](int a, int b) { return step[a] < step[b]; });
+    for (int i : order) {
+        if (n[i] <= 1) continue;
+        if (!r.levels && step[i] == r.cols) r.cols *= n[i];
+        else if (r.levels && step[i] == (Wide)r.size[r.levels - 1] * r.step[r.levels - 1]) r.size[r.levels - 1] *= n[i];
+        else r.size[r.levels] = n[i], r.step[r.levels++] = step[i];
+    }
+    return r;
+}
+
 int check(const heddle_attention_desc *d, bool backward)
 {
     if (!d) return fail(HEDDLE_E_INVAL, "descriptor is NULL");
@@ -262,25 +301,26 @@ int check(const heddle_attention_desc *d, bool backward)
         return fail(HEDDLE_E_INVAL, "d_q, d_k, d_prefix, d_slopes or lse is misaligned");
     const int64_t n = d->packed ? 1 : d->sequences, q_all = n * d->q_len, k_all = n * d->k_len;
     int rc = HEDDLE_OK;
-    auto tensor = [&](const char *name, const void *p, const int64_t *st, bool keys) {
+    auto tensor = [&](const char *name, const void *p, const int64_t *st, bool keys, bool out = false) {
         if (rc || (keys ? k_all : q_all) == 0) return;
         const int64_t heads = keys ? d->kv_heads : d->heads;
         if (!p || ((uintptr_t)p & 1)) rc = fail(HEDDLE_E_INVAL, std::string(name) + " is NULL or not aligned to its values");
         else if ((heads > 1 && st[2] < d->dim) || ((keys ? d->k_len : d->q_len) > 1 && (st[1] < d->dim || st[1] > HEDDLE_MAX_LD)) ||
                  (!d->packed && d->sequences > 1 && st[0] < d->dim))
             rc = fail(HEDDLE_E_INVAL, std::string(name) + ": strides out of range");
+        else if (out && runs_of(d, name, p, st, keys).over_itself()) rc = fail(HEDDLE_E_INVAL, std::string(name) + ": strides let its values overlap");
     };
     tensor("q", d->q, d->q_strides, false);
     tensor("k", d->k, d->k_strides, true);
     tensor("v", d->v, d->v_strides, true);
-    tensor("y", d->y, d->y_strides, false);
+    tensor("y", d->y, d->y_strides, false, !backward);
     if (backward) {
         tensor("dy", d->dy, d->dy_strides, false);
         if (rc == HEDDLE_OK && !d->lse && q_all > 0) rc = fail(HEDDLE_E_INVAL, "lse is NULL");
         if (rc == HEDDLE_OK && !d->dk != !d->dv) rc = fail(HEDDLE_E_INVAL, "dk without dv, or dv without dk");
-        if (d->dq) tensor("dq", d->dq, d->dq_strides, false);
-        if (d->dk) tensor("dk", d->dk, d->dk_strides, true);
-        if (d->dv) tensor("dv", d->dv, d->dv_strides, true);
+        if (d->dq) tensor("dq", d->dq, d->dq_strides, false, true);
+        if (d->dk) tensor("dk", d->dk, d->dk_strides, true, true);
+        if (d->dv) tensor("dv", d->dv, d->dv_strides, true, true);
     }
     return rc;
 }

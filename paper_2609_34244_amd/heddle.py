@@ -852,8 +852,8 @@ def heddle_attention(q, k, v, scale=None, causal=False, cap=0.0, slopes=None, pr
     [sequences, rows, kv_heads, dim], heads a multiple of kv_heads; int32 q_lengths
     and k_lengths [sequences] where rows are not all used (a cache). Or
     documents in one run of rows: [rows, heads, dim] with int32 q_offsets and
-    k_offsets [sequences + 1]. Tensors may have any strides with a head's
-    values side by side.
+    k_offsets [sequences + 1]. Tensors may have any strides from dim on (none that
+    are expanded) with a head's values side by side.
 
     s = scale q k (scale: dim ** -0.5), cap * tanh(s / cap) with a cap (to 4096), minus
     slopes[head] * distance (float32 [heads]). causal: a query sees the keys up to

@@ -1,0 +1,51 @@
+"""Attention's outputs whose strides lay several values on one address are refused.
+Without a GPU; the addresses are of no memory."""
+import pytest
+
+from paper_2609_34244_amd import heddle as H
+from test_layer_abi import TENSORS, attention, no_gpu, refused, three
+
+OUTPUTS = {"y": "forward", "dq": "backward", "dk": "backward", "dv": "backward"}
+
+
+@pytest.fixture(scope="module")
+def L():
+    return H.lib()
+
+
+def sizes(t):
+    """(rows, heads) of attention()'s tensors of 2 sequences, 64 values a head"""
+    return (60, 2) if t in ("k", "v", "dk", "dv") else (40, 4)
+
+
+@pytest.mark.parametrize("t", OUTPUTS)
+def test_outputs_over_themselves(L, t):
+    rows, heads = sizes(t)
+    row, whole = heads * 64, rows * heads * 64
+    for strides in ((whole, 64, 64), (whole, row - 1, 64), (whole, row, 63 + 2), (64, row, 64), (whole - 1, row, 64), (row, row, 64), (rows * 64, 64, rows * 64),
+                    (row - 64, 2 * row, 64), (whole, 64, rows * 64 - 1), (2 ** 62, 64, 64)):
+        if strides[2] >= 64:
+            assert refused(L, attention(**{f"{t}_strides": three(*strides)}), OUTPUTS[t]), strides
+    # packed: no distance between sequences
+    o = dict(packed=1, d_q=1 << 20, d_k=1 << 20)
+    assert refused(L, attention(**o, **{f"{t}_strides": three(0, 64, 64)}), OUTPUTS[t])
+
+
+@no_gpu
+@pytest.mark.parametrize("t", OUTPUTS)
+def test_orders_of_dimensions(L, t):
+    rows, heads = sizes(t)
+    for strides in ((heads * rows * 64, heads * 64, 64), (heads * rows * 64, 64, rows * 64), (heads * 64, 2 * heads * 64, 64), (64, 2 * 64, 2 * rows * 64),
+                    (rows * 64, 64, 2 * rows * 64), (64, 2 * heads * 64, 2 * 64), (rows * heads * 80 + 5, heads * 80, 80), (2 ** 62, heads * 64, 64)):
+        assert not refused(L, attention(**{f"{t}_strides": three(*strides)}), OUTPUTS[t]), strides
+    # one of a dimension: its distance is not looked at
+    one = {f"{x}_strides": three(0, 64, 0) for x in TENSORS}
+    assert not refused(L, attention(sequences=1, heads=1, kv_heads=1, **one), OUTPUTS[t])
+
+
+@no_gpu
+def test_inputs_may_lie_over_themselves(L):
+    for t, which in (("q", "forward"), ("k", "forward"), ("v", "backward"), ("dy", "backward"), ("y", "backward")):
+        rows, heads = sizes(t)
+        assert not refused(L, attention(**{f"{t}_strides": three(rows * heads * 64, 64, 64)}), which)
+        assert not refused(L, attention(**{f"{t}_strides": three(64, heads * 64, 64)}), which)
