@@ -735,8 +735,8 @@ int heddle_grad_norm_workspace(const heddle_grad_desc *grads, int32_t count, int
  * sequences' rows are finite: a product of 0 and an infinity or NaN of a key that
  * some rows do not see may reach those rows too, and one of a row's dy the
  * gradients of keys that it does not see. Outputs lie apart from inputs
- * and from each other (seen where heads lie side by side; tensors with other
- * orders of dimensions may overlap unseen).
+ * and from each other (an overlap is refused; of tensors of unlike strides that
+ * lie in one another's gaps, where one of the first few thousand runs meets).
  */
 typedef struct heddle_attention_desc {
     int32_t dtype, causal, packed, sequences;         /* HEDDLE_T_BF16 or HEDDLE_T_F16; sequences 0 .. HEDDLE_MAX_GROUPS */

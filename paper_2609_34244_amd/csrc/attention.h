@@ -479,7 +479,6 @@ template <typename T, int DP> HEDDLE_INLINE void store_row(T *p, const f32x16 *o
 }
 
 int check(const heddle_attention_desc *d, bool backward);
-int check_overlaps(const heddle_attention_desc *d, bool backward);
 Args base_args(const heddle_attention_desc *d);
 int mode_of(const heddle_attention_desc *d);
 // the launches; mode: of enum Mode

@@ -325,37 +325,55 @@ int check(const heddle_attention_desc *d, bool backward)
     return rc;
 }
 
-// A tensor as rows of all its heads, where it can be seen as such: heads side by side, sequences as rows go on. Other
-// orders of the dimensions are compared by their first value alone.
-static mm::Region region(const heddle_attention_desc *d, const char *name, const void *p, const int64_t *st, bool keys)
+// Whether a value of b (its first n levels), which lies d values after a, is one of a's (its first m levels). Levels
+// of one distance are taken apart together, by the difference of their indices: few come into question. Of others the
+// larger one is, index by index: at most kLooks of them, past which tensors count as apart.
+constexpr int kLooks = 4096;
+static bool meet(const Runs &a, int m, const Runs &b, int n, Wide d, int &looks)
 {
-    const int64_t heads = keys ? d->kv_heads : d->heads, length = keys ? d->k_len : d->q_len, n = d->packed ? 1 : d->sequences;
-    mm::Region r = {name, length * n ? p : nullptr, 1, d->dim, d->dim};
-    const bool side = heads == 1 || st[2] == d->dim;
-    if (!side) return r;
-    r.cols = heads * d->dim;
-    if (n == 1 || st[0] == length * st[1]) r.rows = length * n, r.ld = length * n > 1 ? st[1] : r.cols;
-    else if (length == 1) r.rows = n, r.ld = st[0];
-    else r.rows = length, r.ld = st[1], r.groups = (int)n, r.stride = st[0];
-    return r;
+    if (d >= a.extent(m) || -d >= b.extent(n)) return false;
+    if (m == 0 && n == 0) return true;
+    const bool of_a = m && (!n || a.step[m - 1] >= b.step[n - 1]), of_b = n && (!m || b.step[n - 1] >= a.step[m - 1]);
+    if (of_a) m--;
+    if (of_b) n--;
+    // d + q step, q = index in b - index in a, from the first that lies less than b's extent before a
+    const Wide step = of_a ? a.step[m] : b.step[n], end = a.extent(m), least = 1 - b.extent(n) - d;
+    Wide q = least / step + (least % step > 0);
+    if (q < (of_a ? 1 - a.size[m] : 0)) q = of_a ? 1 - a.size[m] : 0;
+    for (; q <= (of_b ? b.size[n] - 1 : 0) && d + q * step < end && looks > 0; q++) {
+        looks--;
+        if (meet(a, m, b, n, d + q * step, looks)) return true;
+    }
+    return false;
 }
 
-int check_overlaps(const heddle_attention_desc *d, bool backward)
+static int check_apart(const Runs &out, std::initializer_list<const Runs *> others)
 {
-    const mm::Region q = region(d, "q", d->q, d->q_strides, false), k = region(d, "k", d->k, d->k_strides, true), v = region(d, "v", d->v, d->v_strides, true);
-    const mm::Region y = region(d, "y", d->y, d->y_strides, false);
+    if (!out.p) return HEDDLE_OK;
+    for (const Runs *r : others) {
+        int looks = kLooks;
+        if (r->p && meet(out, out.levels, *r, r->levels, ((intptr_t)r->p - (intptr_t)out.p) / 2, looks))
+            return fail(HEDDLE_E_INVAL, std::string(out.name) + " overlaps " + r->name);
+    }
+    return HEDDLE_OK;
+}
+
+static int check_overlaps(const heddle_attention_desc *d, bool backward)
+{
+    const Runs q = runs_of(d, "q", d->q, d->q_strides, false), k = runs_of(d, "k", d->k, d->k_strides, true), v = runs_of(d, "v", d->v, d->v_strides, true);
+    const Runs y = runs_of(d, "y", d->y, d->y_strides, false);
     const int64_t n = d->packed ? 1 : d->sequences, words = n * d->q_len * d->heads;
-    const mm::Region lse = {"lse", words ? d->lse : nullptr, 1, 2 * words, 2 * words};
+    const Runs lse = {"lse", words ? d->lse : nullptr, 2 * words, 0, {}, {}};
     int rc;
     if (!backward) {
-        rc = mm::check_apart(y, {&q, &k, &v, &lse});
-        return rc ? rc : mm::check_apart(lse, {&q, &k, &v});
+        rc = check_apart(y, {&q, &k, &v, &lse});
+        return rc ? rc : check_apart(lse, {&q, &k, &v});
     }
-    const mm::Region dy = region(d, "dy", d->dy, d->dy_strides, false), dq = region(d, "dq", d->dq, d->dq_strides, false);
-    const mm::Region dk = region(d, "dk", d->dk, d->dk_strides, true), dv = region(d, "dv", d->dv, d->dv_strides, true);
-    rc = mm::check_apart(dq, {&q, &k, &v, &y, &dy, &lse, &dk, &dv});
-    if (rc == HEDDLE_OK) rc = mm::check_apart(dk, {&q, &k, &v, &y, &dy, &lse, &dv});
-    return rc ? rc : mm::check_apart(dv, {&q, &k, &v, &y, &dy, &lse});
+    const Runs dy = runs_of(d, "dy", d->dy, d->dy_strides, false), dq = runs_of(d, "dq", d->dq, d->dq_strides, false);
+    const Runs dk = runs_of(d, "dk", d->dk, d->dk_strides, true), dv = runs_of(d, "dv", d->dv, d->dv_strides, true);
+    rc = check_apart(dq, {&q, &k, &v, &y, &dy, &lse, &dk, &dv});
+    if (rc == HEDDLE_OK) rc = check_apart(dk, {&q, &k, &v, &y, &dy, &lse, &dv});
+    return rc ? rc : check_apart(dv, {&q, &k, &v, &y, &dy, &lse});
 }
 
 static int launched(const char *what)
