@@ -722,8 +722,8 @@ int heddle_grad_norm_workspace(const heddle_grad_desc *grads, int32_t count, int
  * d_q[s+1] - 1 of q and d_k[s] .. d_k[s+1] - 1 of k and v are sequence s; a
  * document sees only itself. Offsets are non-decreasing; otherwise what the
  * rows concerned receive is unspecified.
- * Rows of no sequence, and past a sequence's length, are neither used nor
- * written. Head h reads key head h / (heads / kv_heads).
+ * Rows of no sequence, and past a sequence's length, are not used, and not
+ * written unless `clear` names the output: they receive zeros then. Head h reads key head h / (heads / kv_heads).
  *
  * Values run over dim side by side; strides [3] are elements from one sequence
  * (ignored where packed), row and head to the next, at least dim; a row's at most
@@ -743,6 +743,7 @@ typedef struct heddle_attention_desc {
     int64_t q_len, k_len;                             /* q_len * heads, k_len 0 .. HEDDLE_MAX_ROWS */
     int32_t heads, kv_heads, dim;                     /* heads a multiple of kv_heads; dim 1 .. HEDDLE_MAX_HEAD_DIM */
     float scale, cap;                                 /* scale 1e-20 .. 1e20; cap 0: none, or 1e-3 .. 4096 */
+    int32_t clear;                                    /* sum of 1: y or dq, 2: dk, 4: dv; or 0 */
     const int32_t *d_q, *d_k;                         /* offsets [sequences + 1], or lengths [sequences] or NULL */
     const int32_t *d_prefix;                          /* [sequences] or NULL */
     const float *d_slopes;                            /* [heads] or NULL */

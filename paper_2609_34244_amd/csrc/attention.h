@@ -482,6 +482,7 @@ int check(const heddle_attention_desc *d, bool backward);
 Args base_args(const heddle_attention_desc *d);
 int mode_of(const heddle_attention_desc *d);
 // the launches; mode: of enum Mode
+void launch_clear(const heddle_attention_desc *d, const Args &a, bool backward, hipStream_t stream);
 void launch_forward(const heddle_attention_desc *d, const Args &a, int rows, int64_t blocks, hipStream_t stream);
 void launch_rows(const heddle_attention_desc *d, const Args &a, int64_t blocks, hipStream_t stream);
 void launch_keys(const heddle_attention_desc *d, const Args &a, int span, int64_t blocks, int64_t tiles, hipStream_t stream);

@@ -221,6 +221,55 @@ int Copies::launch(hipStream_t stream) const
     return e == hipSuccess ? HEDDLE_OK : hip_fail(e, "attention's copies");
 }
 
+// ---- rows of no sequence ----
+// z: sequences (one where packed). With offsets or lengths that leave no row out, 2 us for the launch.
+struct Outputs {
+    View view[3];
+    int keys[3];                              // of keys' rows
+};
+__global__ void __launch_bounds__(256) clear_kernel(Args a, Outputs o)
+{
+    const View v = o.view[blockIdx.y];
+    const bool keys = o.keys[blockIdx.y];
+    const int32_t *at = keys ? a.d_k : a.d_q;
+    const int rows = keys ? a.k_len : a.q_len, heads = keys ? a.kv_heads : a.heads, per = (a.dim + 7) / 8, line = heads * per, s = blockIdx.z;
+    int first = 0, last = rows;                             // rows before the first and from the last on
+    if (!a.packed) last = at ? clamp_row(at[s], rows) : rows;
+    else if (a.sequences) first = clamp_row(at[0], rows), last = max(first, clamp_row(at[a.sequences], rows));
+    else last = 0;
+    const int64_t all = (int64_t)(first + rows - last) * line;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
+        const int64_t u = i / line, row = u < first ? u : u - first + last;
+        const int rest = (int)(i - u * line), head = rest / per, col = (rest - head * per) * 8;
+        uint16_t *p = (uint16_t *)v.p + s * v.seq + row * v.row + head * v.head + col;
+        if (a.out_vec) {
+            *(s16x8 *)p = s16x8{};
+        } else {
+#pragma unroll
+            for (int k = 0; k < 8; k++)
+                if (col + k < a.dim) p[k] = 0;
+        }
+    }
+}
+void launch_clear(const heddle_attention_desc *d, const Args &a, bool backward, hipStream_t stream)
+{
+    Outputs o = {};
+    int n = 0;
+    int64_t most = 0;
+    auto add = [&](int bit, const View &v, bool keys) {
+        const int64_t line = (int64_t)(keys ? a.kv_heads : a.heads) * ((a.dim + 7) / 8), all = (keys ? a.k_len : a.q_len) * line;
+        if (!(d->clear & bit) || !v.p || all == 0) return;
+        o.view[n] = v, o.keys[n++] = keys;
+        most = std::max(most, all);
+    };
+    add(1, backward ? a.dq : a.y, false);
+    if (backward) add(2, a.dk, true), add(4, a.dv, true);
+    const int64_t z = a.packed ? 1 : a.sequences;
+    if (n == 0 || z == 0) return;
+    const int64_t x = std::max<int64_t>(1, std::min<int64_t>((most + 255) / 256, 512 / z));
+    hipLaunchKernelGGL(clear_kernel, dim3((unsigned)x, (unsigned)n, (unsigned)z), dim3(256), 0, stream, a, o);
+}
+
 // ---- host ----
 int mode_of(const heddle_attention_desc *d) { return (d->cap > 0 ? kCap : 0) | (d->d_slopes ? kSlopes : 0); }
 
@@ -296,6 +345,7 @@ int check(const heddle_attention_desc *d, bool backward)
     if (!(d->scale >= 1e-20f && d->scale <= 1e20f)) return fail(HEDDLE_E_INVAL, "scale out of range");
     // the tanh is off by a few 2^-24 of 1: by 2^-11 of a score of any size at the largest cap
     if (!(d->cap == 0 || (d->cap >= 1e-3f && d->cap <= 4096))) return fail(HEDDLE_E_INVAL, "cap out of range");
+    if (d->clear & ~7) return fail(HEDDLE_E_INVAL, "clear is no sum of 1, 2 and 4");
     if (d->packed && d->sequences > 0 && (!d->d_q || !d->d_k)) return fail(HEDDLE_E_INVAL, "packed sequences without offsets");
     if (((uintptr_t)d->d_q | (uintptr_t)d->d_k | (uintptr_t)d->d_prefix | (uintptr_t)d->d_slopes | (uintptr_t)d->lse) & 3)
         return fail(HEDDLE_E_INVAL, "d_q, d_k, d_prefix, d_slopes or lse is misaligned");
@@ -396,12 +446,14 @@ static void launch_combine(const heddle_attention_desc *d, const Args &a, int64_
 static int forward(const heddle_attention_desc *d, mm::Scratch &s, bool run, hipStream_t stream)
 {
     Args a = base_args(d);
-    if (d->sequences == 0 || a.q_rows == 0) return HEDDLE_OK;
+    if (a.q_rows == 0) return HEDDLE_OK;
+    a.out_vec = !((uintptr_t)d->y & 15) && !((a.y.seq | a.y.row | a.y.head | d->dim) & 7);
+    if (run && d->clear) launch_clear(d, a, false, stream);
+    if (d->sequences == 0) return run && d->clear ? launched("attention") : HEDDLE_OK;
     Copies c;
     c.add(d, a.q, false, s);
     c.add(d, a.k, true, s);
     c.add(d, a.v, true, s);
-    a.out_vec = !((uintptr_t)d->y & 15) && !((a.y.seq | a.y.row | a.y.head | d->dim) & 7);
     // rows of a key head in a sequence, on average
     const int64_t rows = std::max<int64_t>(1, a.q_rows * a.group / d->sequences), keys = a.k_rows / d->sequences;
     // Whether the keys are divided over workgroups, by an estimate in us of both kernels. Measured, 8 sequences of 4000 keys, 32

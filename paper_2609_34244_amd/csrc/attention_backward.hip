@@ -480,7 +480,15 @@ int backward(const heddle_attention_desc *d, mm::Scratch &s, bool run, hipStream
 {
     Args a = base_args(d);
     a.grads = (d->dq ? 1 : 0) | (d->dk ? 2 : 0);
-    if (d->sequences == 0 || !a.grads) return HEDDLE_OK;
+    if (!a.grads) return HEDDLE_OK;
+    auto aligned = [&](const void *p, const View &v) { return !((uintptr_t)p & 15) && !((v.seq | v.row | v.head | d->dim) & 7); };
+    a.out_vec = (!d->dq || aligned(d->dq, a.dq)) && (!d->dk || (aligned(d->dk, a.dk) && aligned(d->dv, a.dv)));
+    auto launched = []() {
+        const hipError_t e = hipGetLastError();
+        return e == hipSuccess ? HEDDLE_OK : hip_fail(e, "attention's gradients");
+    };
+    if (run && d->clear) launch_clear(d, a, true, stream);
+    if (d->sequences == 0) return run && d->clear ? launched() : HEDDLE_OK;
     Copies c;
     if (a.q_rows) c.add(d, a.q, false, s);
     if (a.q_rows) c.add(d, a.y, false, s);
@@ -488,8 +496,6 @@ int backward(const heddle_attention_desc *d, mm::Scratch &s, bool run, hipStream
     if (a.k_rows) c.add(d, a.k, true, s);
     if (a.k_rows) c.add(d, a.v, true, s);
     a.rows = (float2 *)s.take((size_t)a.q_rows * d->heads * 8);
-    auto aligned = [&](const void *p, const View &v) { return !((uintptr_t)p & 15) && !((v.seq | v.row | v.head | d->dim) & 7); };
-    a.out_vec = (!d->dq || aligned(d->dq, a.dq)) && (!d->dk || (aligned(d->dk, a.dk) && aligned(d->dv, a.dv)));
     const int64_t blocks = a.q_rows ? slots_of(d->packed, d->sequences, d->q_len, d->q_len, a.group, 128) * d->kv_heads : 0;
     // Keys a workgroup takes: 32 where there would not be one of 128 keys for every CU (one sequence of 2000, 8 heads: 54 us, 66
     // with pairs of 128); pairs of 128 where that leaves few rounds (4 of 2048, 64 heads on 8: 563 us, 603 with 128; 4 of 1000, 32 heads: 91 and 87).
@@ -502,8 +508,7 @@ int backward(const heddle_attention_desc *d, mm::Scratch &s, bool run, hipStream
     if (const int rc = c.launch(stream)) return rc;
     if (blocks) launch_rows(d, a, blocks, stream);
     if (kblocks) launch_keys(d, a, (int)span, kblocks, ktiles, stream);
-    const hipError_t e = hipGetLastError();
-    return e == hipSuccess ? HEDDLE_OK : hip_fail(e, "attention's gradients");
+    return launched();
 }
 
 }  // namespace attn

@@ -106,7 +106,7 @@ def _tensor_fields(*names):
 class heddle_attention_desc(C.Structure):
     _fields_ = [("dtype", C.c_int32), ("causal", C.c_int32), ("packed", C.c_int32), ("sequences", C.c_int32),
                 ("q_len", C.c_int64), ("k_len", C.c_int64), ("heads", C.c_int32), ("kv_heads", C.c_int32), ("dim", C.c_int32),
-                ("scale", C.c_float), ("cap", C.c_float), ("d_q", C.c_void_p), ("d_k", C.c_void_p), ("d_prefix", C.c_void_p),
+                ("scale", C.c_float), ("cap", C.c_float), ("clear", C.c_int32), ("d_q", C.c_void_p), ("d_k", C.c_void_p), ("d_prefix", C.c_void_p),
                 ("d_slopes", C.c_void_p), *_tensor_fields("q", "k", "v", "y"), ("lse", C.c_void_p),
                 *_tensor_fields("dy", "dq", "dk", "dv")]
 
@@ -779,7 +779,7 @@ def heddle_clip_grad_norm(grads, max_norm, out=None, stream=None):
 
 # ---- attention, layer normalisation and a router's balance ----
 
-_ATTENTION = struct.Struct("@4i2q3i2f4P" + "Pqqq" * 4 + "P" + "Pqqq" * 4)
+_ATTENTION = struct.Struct("@4i2q3i2fi4P" + "Pqqq" * 4 + "P" + "Pqqq" * 4)
 _LAYER_NORM = struct.Struct("@iiqqfPqPPPqPPqPqPqPP")
 _BALANCE = struct.Struct("@iiiiqfPqPqPPPPPPPqPq")
 assert (_ATTENTION.size, _LAYER_NORM.size, _BALANCE.size) == tuple(
@@ -811,7 +811,7 @@ def _ints(t, what, n, gpu, kind="torch.int32"):
     return t.data_ptr()
 
 
-def _attention_inputs(q, k, v, scale, causal, cap, slopes, prefix, q_lengths, k_lengths, q_offsets, k_offsets):
+def _attention_inputs(q, k, v, scale, causal, cap, slopes, prefix, q_lengths, k_lengths, q_offsets, k_offsets, clear):
     """(GPU, packed head of the descriptor, shape of q, shape of k)"""
     packed = q_offsets is not None or k_offsets is not None
     if q.dim() != (3 if packed else 4) or k.dim() != q.dim() or not q.is_cuda:
@@ -834,7 +834,7 @@ def _attention_inputs(q, k, v, scale, causal, cap, slopes, prefix, q_lengths, k_
     if slopes is not None and slopes.requires_grad:
         _unrecorded("slopes")
     head = (_dtype(q, "q"), 1 if causal else 0, 1 if packed else 0, n, qs[-3], ks[-3], qs[-2], ks[-2], qs[-1],
-            qs[-1] ** -0.5 if scale is None else scale, cap, dq, dk, _ints(prefix, "prefix", n, gpu),
+            qs[-1] ** -0.5 if scale is None else scale, cap, clear, dq, dk, _ints(prefix, "prefix", n, gpu),
             _ints(slopes, "slopes", qs[-2], gpu, "torch.float32"),
             *_heads(q, "q", qs, dt, gpu), *_heads(k, "k", ks, dt, gpu), *_heads(v, "v", ks, dt, gpu))
     return gpu, dt, head, qs, ks
@@ -860,9 +860,11 @@ def heddle_attention(q, k, v, scale=None, causal=False, cap=0.0, slopes=None, pr
     its own place, the last query standing at the last key, and the first
     prefix[sequence] keys (int32). lse: float32, q's shape without dim, to keep
     for the backward pass. Returns out (q's shape); rows past the lengths, or in
-    no document, are left as they were."""
+    no document, are zeros where out is not given and left as they were in one that is."""
+    # a fresh output's rows of no sequence are zeros
+    clear = out is None and (q_lengths is not None or q_offsets is not None)
     gpu, dt, head, qs, ks = _attention_inputs(q, k, v, scale, causal, cap, slopes, prefix, q_lengths, k_lengths, q_offsets,
-                                              k_offsets)
+                                              k_offsets, int(clear))
     if out is None:
         out = _fresh(q, qs, stream)
     L = lib()
@@ -878,11 +880,13 @@ def heddle_attention_backward(dy, q, k, v, y, lse, scale=None, causal=False, cap
     """Gradients of heddle_attention: a dict with dq, dk and dv (those wanted;
     given tensors are written, dk and dv together). y, lse: what
     heddle_attention returned and kept. Rows past the lengths, or in no
-    document, are left as they were. float16: the scores' gradients before the scale,
+    document, are zeros in tensors made here and left as they were in given ones. float16: the scores' gradients before the scale,
     p * (dy v - sum(dy * y)), are float16 operands and need its range. Probabilities
     are formed again from lse: scores past 2^20 leave them hardly a digit."""
+    clear_q, clear_k = q_lengths is not None or q_offsets is not None, k_lengths is not None or k_offsets is not None
+    clear = (dq is None and clear_q) + 2 * (dk is None and clear_k) + 4 * (dv is None and clear_k)
     gpu, dt, head, qs, ks = _attention_inputs(q, k, v, scale, causal, cap, slopes, prefix, q_lengths, k_lengths, q_offsets,
-                                              k_offsets)
+                                              k_offsets, clear)
     if lse is None or y is None:
         _refuse("heddle_attention_backward: y and lse are what heddle_attention returned and kept")
     out, at = {}, {"dq": _NONE, "dk": _NONE, "dv": _NONE}

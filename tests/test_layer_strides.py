@@ -49,3 +49,18 @@ def test_inputs_may_lie_over_themselves(L):
         rows, heads = sizes(t)
         assert not refused(L, attention(**{f"{t}_strides": three(rows * heads * 64, 64, 64)}), which)
         assert not refused(L, attention(**{f"{t}_strides": three(64, heads * 64, 64)}), which)
+
+
+def test_rows_to_clear(L):
+    for which in ("forward", "backward"):
+        for clear in (8, -1, 256):
+            assert refused(L, attention(clear=clear), which)
+
+
+@no_gpu
+def test_outputs_to_clear(L):
+    o = dict(packed=1, d_q=1 << 20, d_k=1 << 20)
+    for clear in range(8):
+        for over in (dict(), o, dict(o, sequences=0), dict(dq=0), dict(dk=0, dv=0)):
+            for which in ("forward", "backward"):
+                assert not refused(L, attention(clear=clear, **over), which)
