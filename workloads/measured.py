@@ -100,7 +100,8 @@ class WholeLayer(Layer):
         """documents: int32 offsets of the rows' documents (one without); picked: [tokens, top_k], the
         router's choice without. self.loss: the balance loss of a layer with experts."""
         self.x, t, w = x, x.shape[0], self.w
-        self.documents = torch.tensor([0, t], dtype=torch.int32, device=x.device) if documents is None else documents
+        # (formed on the GPU: a copy from the host would be waited for)
+        self.documents = torch.arange(2, dtype=torch.int32, device=x.device) * t if documents is None else documents
         self.stats = [torch.empty(t, 2, dtype=torch.float32, device=x.device) for _ in range(2)]
         self.n1 = H.heddle_layer_norm(x, w["norm1"], w["shift1"], stats=self.stats[0])
         self.q, self.kv = H.heddle_linear(self.n1, w["q"]), H.heddle_linear(self.n1, w["kv"])
