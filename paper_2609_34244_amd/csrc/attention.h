@@ -19,6 +19,7 @@
 
 #include <utility>
 
+#include "attention_plan.h"
 #include "linear.h"
 
 namespace heddle {

@@ -454,31 +454,16 @@ static int forward(const heddle_attention_desc *d, mm::Scratch &s, bool run, hip
     c.add(d, a.q, false, s);
     c.add(d, a.k, true, s);
     c.add(d, a.v, true, s);
-    // rows of a key head in a sequence, on average
-    const int64_t rows = std::max<int64_t>(1, a.q_rows * a.group / d->sequences), keys = a.k_rows / d->sequences;
-    // Whether the keys are divided over workgroups, by an estimate in us of both kernels. Measured, 8 sequences of 4000 keys, 32
-    // heads on 8: 2, 16, 32, 64 queries 27, 39, 59, 115 us divided, 83, 82, 84, 85 not; 32 of 200 keys, 16 queries: 18 and 14; one of
-    // 16000 keys, 64 queries: 72 and 312; 2 of 600, 600 queries, 8 heads: 21.5 and 19.3.
-    const double tiles128 = (double)d->sequences * ((rows + 127) / 128) * d->kv_heads, tiles32 = (double)d->sequences * ((rows + 31) / 32) * d->kv_heads;
-    const bool split = 8 + 0.0125 * keys * std::max(1.0, tiles32 / 256) < 2 + 0.0205 * keys * std::max(1.0, tiles128 / 360);
-    // 256 rows a workgroup read each tile of keys half as often as 128, but want two rounds of workgroups (2 sequences of 2048, 32
-    // heads: 88 us with 256 rows, 111 with 128; one of 2000, 8 heads: 64 and 50; 3 of 333, 12 heads: 18 and 15)
-    const bool tall = rows >= 512 && d->sequences * ((rows + 255) / 256) * d->kv_heads >= 512;
-    const int T = split ? 32 : tall ? 256 : 128;
+    const ForwardPlan plan = plan_forward({d->sequences, a.q_rows, a.k_rows, d->heads, d->kv_heads});
+    const int T = plan.rows;
     const int64_t slots = slots_of(d->packed, d->sequences, d->q_len, d->q_len, a.group, T), tiles = (d->q_len * a.group + T - 1) / T;
-    int64_t blocks = slots * d->kv_heads;
-    a.parts = 1;
-    if (split) {
-        const int64_t used = std::max<int64_t>(1, d->sequences * ((rows + 31) / 32) * d->kv_heads);
-        // One workgroup a CU at a time. Two rounds of them where there are many anyway: the sequences' lengths differ (32 of up
-        // to 8192 keys, 8 key heads: 126 us, 142 with one part each); one round else (8 of up to 4000: 23.5 us, 26.5 with twice the parts).
-        a.parts = (int32_t)std::max<int64_t>(1, std::min<int64_t>({(used >= 128 ? 512 : 256) / used, keys / 128, 64}));
-        if (a.parts > 1) a.partial = (float *)s.take((size_t)blocks * 32 * a.parts * ((d->dim <= 64 ? 64 : 128) + 2) * 4);
-    }
+    const int64_t blocks = slots * d->kv_heads;
+    a.parts = plan.parts;
+    if (a.parts > 1) a.partial = (float *)s.take((size_t)blocks * 32 * a.parts * ((d->dim <= 64 ? 64 : 128) + 2) * 4);
     if (blocks * (a.parts > 1 ? std::max(a.parts, 8) : 1) > kMostBlocks) return fail(HEDDLE_E_RANGE, "more tiles than a launch holds");
     if (!run) return HEDDLE_OK;
     if (const int rc = c.launch(stream)) return rc;
-    if (!split) {
+    if (!plan.split) {
         launch_forward(d, a, T, blocks, stream);
     } else {
         with_kind(d, [&](auto t, auto dp, auto mode) {

@@ -497,10 +497,7 @@ int backward(const heddle_attention_desc *d, mm::Scratch &s, bool run, hipStream
     if (a.k_rows) c.add(d, a.v, true, s);
     a.rows = (float2 *)s.take((size_t)a.q_rows * d->heads * 8);
     const int64_t blocks = a.q_rows ? slots_of(d->packed, d->sequences, d->q_len, d->q_len, a.group, 128) * d->kv_heads : 0;
-    // Keys a workgroup takes: 32 where there would not be one of 128 keys for every CU (one sequence of 2000, 8 heads: 54 us, 66
-    // with pairs of 128); pairs of 128 where that leaves few rounds (4 of 2048, 64 heads on 8: 563 us, 603 with 128; 4 of 1000, 32 heads: 91 and 87).
-    const int64_t keys = std::max<int64_t>(1, a.k_rows / d->sequences), singles = d->sequences * ((keys + 127) / 128) * d->kv_heads;
-    const int64_t span = singles < 256 ? 32 : singles < 1024 && keys >= 512 ? 256 : 128;
+    const int64_t span = plan_keys({d->sequences, a.q_rows, a.k_rows, d->heads, d->kv_heads});
     const int64_t ktiles = (d->k_len + span - 1) / span;
     const int64_t kblocks = d->dk && a.k_rows ? slots_of(d->packed, d->sequences, d->k_len, d->k_len, 1, span) * d->kv_heads : 0;
     if (std::max(blocks, kblocks) > kMostBlocks) return fail(HEDDLE_E_RANGE, "more tiles than a launch holds");
