@@ -69,13 +69,13 @@ struct Args {
     const int32_t *d_q, *d_k, *d_prefix;
     const float *d_slopes;
     float2 *rows;                             // [heads][query rows]: backward's lse log2(e) and delta
-    float *partial;                           // few queries: [parts][slot rows][DP + 2]
+    float *partial;                           // few queries: [slot][key head][32 rows][parts][DP + 2]
     int64_t q_rows, k_rows;                   // of all sequences (batched: sequences * length)
     int32_t sequences, q_len, k_len, packed;
     int32_t heads, kv_heads, group, dim;
     int32_t causal, parts;
-    int32_t q_vec, out_vec, grads;            // 16-byte rows of q, k, v (dy); 8-byte rows of outputs; which gradients
-    float scale, scale2, cap, cap2, unscale;  // scale2 = scale log2(e); with a cap: 2 scale log2(e) / cap and cap log2(e); -1 / scale2
+    int32_t out_vec, grads;                   // outputs on 16-byte addresses, their strides and dim whole eights; which gradients
+    float scale, scale2, cap2, unscale;       // scale2 = scale log2(e); with a cap: 2 scale log2(e) / cap and cap log2(e); -1 / scale2
 };
 
 // A sequence's rows: first row of its queries and of its keys, counted over all sequences where packed, else in the sequence.
@@ -263,7 +263,9 @@ template <typename T> __device__ inline typename mm::pack8<T>::type global_fragm
     return x;
 }
 
-// eight probabilities as the next product's operand
+// eight probabilities as the next product's operand, rounded to the type that the matrix cores read at full rate: in bf16 y is
+// off by 0.19 to 0.22% where fp32 throughout is off by the 0.17% of its last rounding. A second operand of what the rounding
+// leaves would be half as many products again; in split_kernel, bound by reading, 134 us for 131 (32 sequences of up to 8192 keys).
 template <typename T> __device__ inline typename mm::pack8<T>::type pack(const f32x16 &p, int from)
 {
     typename mm::pack8<T>::type x;
@@ -479,14 +481,12 @@ template <typename T, int DP> HEDDLE_INLINE void store_row(T *p, const f32x16 *o
         }
 }
 
-int check(const heddle_attention_desc *d, bool backward);
 Args base_args(const heddle_attention_desc *d);
 int mode_of(const heddle_attention_desc *d);
-// the launches; mode: of enum Mode
+int backward(const heddle_attention_desc *d, mm::Scratch &s, bool run, hipStream_t stream);
+// the launches
 void launch_clear(const heddle_attention_desc *d, const Args &a, bool backward, hipStream_t stream);
 void launch_forward(const heddle_attention_desc *d, const Args &a, int rows, int64_t blocks, hipStream_t stream);
-void launch_rows(const heddle_attention_desc *d, const Args &a, int64_t blocks, hipStream_t stream);
-void launch_keys(const heddle_attention_desc *d, const Args &a, int span, int64_t blocks, int64_t tiles, hipStream_t stream);
 
 // f(type, padded head width, mode) as constants
 template <typename F> void with_kind(const heddle_attention_desc *d, F f)

@@ -286,7 +286,7 @@ Args base_args(const heddle_attention_desc *d)
     a.q_rows = d->packed ? d->q_len : d->q_len * d->sequences, a.k_rows = d->packed ? d->k_len : d->k_len * d->sequences;
     a.sequences = d->sequences, a.q_len = (int32_t)d->q_len, a.k_len = (int32_t)d->k_len, a.packed = d->packed;
     a.heads = d->heads, a.kv_heads = d->kv_heads, a.group = d->heads / d->kv_heads, a.dim = d->dim, a.causal = d->causal;
-    a.scale = d->scale, a.cap = d->cap;
+    a.scale = d->scale;
     a.scale2 = d->cap > 0 ? 2 * d->scale * kLog2e / d->cap : d->scale * kLog2e;
     a.cap2 = d->cap * kLog2e;
     a.unscale = -1.0f / a.scale2;
@@ -332,7 +332,7 @@ static Runs runs_of(const heddle_attention_desc *d, const char *name, const void
     return r;
 }
 
-int check(const heddle_attention_desc *d, bool backward)
+static int check(const heddle_attention_desc *d, bool backward)
 {
     if (!d) return fail(HEDDLE_E_INVAL, "descriptor is NULL");
     if (d->dtype != HEDDLE_T_BF16 && d->dtype != HEDDLE_T_F16) return fail(HEDDLE_E_INVAL, "dtype is neither BF16 nor F16");
@@ -475,10 +475,7 @@ static int forward(const heddle_attention_desc *d, mm::Scratch &s, bool run, hip
     return launched("attention");
 }
 
-int run_attention(const heddle_attention_desc *d, bool back, void *ws, int64_t bytes, bool run, hipStream_t stream, int64_t *need);
-int backward(const heddle_attention_desc *d, mm::Scratch &s, bool run, hipStream_t stream);
-
-int run_attention(const heddle_attention_desc *d, bool back, void *ws, int64_t bytes, bool run, hipStream_t stream, int64_t *need)
+static int run_attention(const heddle_attention_desc *d, bool back, void *ws, int64_t bytes, bool run, hipStream_t stream, int64_t *need)
 {
     int rc = check(d, back);
     if (rc) return rc;

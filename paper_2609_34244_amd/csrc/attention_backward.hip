@@ -7,7 +7,10 @@
 // leaves lse log2(e) and delta of its rows for the other one. keys_kernel (dk, dv): 128 keys or two times 128 a
 // workgroup, 32 a wavefront, over tiles of query rows of each head of the group in turn, whose sum
 // the shared heads' gradient is; the values' operands are read from LDS, as with keys, values and both sums in registers a SIMD
-// would hold one wavefront. P and dS are rounded to the operands' type, as the products' operands.
+// would hold one wavefront.
+// P and dS are rounded to the operands' type, and D is formed from the y of that type that the caller keeps: in bf16 dq and dk are off by
+// 0.25%, dv by 0.23%, where fp32 throughout is off by the 0.17% of its last rounding. A second operand of what dS's rounding leaves
+// brings dq and dk to 0.18 to 0.19%, and the layer below with its forward pass from 1534 us to 1750, 11 documents of 4092 rows from 194 to 212.
 // Bound as the forward pass is: 4 sequences of 2048, 64 heads on 8: dq 452 us, dk and dv 562 us (912 and 977 TFLOP/s of products), with a
 // cap 509 and 646.
 #include <algorithm>
@@ -461,13 +464,13 @@ template <typename T, int DP, int MODE> __global__ void __launch_bounds__(512) _
     });
 }
 
-void launch_rows(const heddle_attention_desc *d, const Args &a, int64_t blocks, hipStream_t stream)
+static void launch_rows(const heddle_attention_desc *d, const Args &a, int64_t blocks, hipStream_t stream)
 {
     with_kind(d, [&](auto t, auto dp, auto mode) {
         hipLaunchKernelGGL((rows_kernel<decltype(t), dp, mode>), dim3((unsigned)blocks), dim3(256), 0, stream, a);
     });
 }
-void launch_keys(const heddle_attention_desc *d, const Args &a, int span, int64_t blocks, int64_t tiles, hipStream_t stream)
+static void launch_keys(const heddle_attention_desc *d, const Args &a, int span, int64_t blocks, int64_t tiles, hipStream_t stream)
 {
     with_kind(d, [&](auto t, auto dp, auto mode) {
         if (span == 32) hipLaunchKernelGGL((few_keys_kernel<decltype(t), dp, mode>), dim3((unsigned)blocks), dim3(512), 0, stream, a, tiles);
