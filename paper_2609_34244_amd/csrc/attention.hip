@@ -5,7 +5,8 @@
 // forward_kernel (attention_forward.hip): 128 or 256 rows a workgroup over tiles of 64 keys.
 // split_kernel: 32 rows a workgroup (few queries over long caches), each wavefront with tiles of its own, the
 // keys of a row tile divided over `parts` workgroups; combine_kernel joins them. Bound by reading keys and values: 32
-// sequences of up to 8192 keys, 8 key heads, 128 us (4.1 TB/s); one of 2048, 32 heads, 13 + 4 us.
+// sequences of up to 8192 keys, 8 key heads, 129 us (4.1 TB/s); one of 2048, 32 heads, 13 + 3.6 us (a wavefront has two tiles, and
+// its start, its wait for both and the sums' exchange follow one another).
 #include <algorithm>
 #include <cmath>
 

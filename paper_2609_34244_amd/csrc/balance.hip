@@ -4,11 +4,12 @@
 // p = softmax(logits) of a row, c_e = picks of expert e, C = sum c, N = rows with a pick,
 // P_e = sum of p_e over those rows / N, loss = scale E sum_e (c_e / C) P_e;
 // dlogits = dloss scale E / (C N) p (c_e - sum_j p_j c_j) + r.
-// Bound by memory: the logits are read once, and once more for the gradient (p is formed again
+// The logits are read once, and once more for the gradient (p is formed again
 // rather than kept). G lanes to a row, K neighbouring values a lane, so that a wavefront reads 64 / G
 // rows side by side, kAhead of them before the first is used. A workgroup counts picks in LDS with integer atomics, whose order changes nothing;
-// probabilities are summed in fp32 registers, then over workgroups, in one order. 131072 rows of 64 in bf16, top 2: 15 + 6.6 us,
-// the gradient with a residual 21 us (2.4 TB/s).
+// probabilities are summed in fp32 registers, then over workgroups, in one order. 131072 rows of 64 in bf16, top 2: 16 + 6.5 us,
+// the gradient with a residual 21 us: 1.2 and 2.4 TB/s, wavefronts waiting 62 and 66% of the time (forward, a CU has
+// eight wavefronts, and the next rows are loaded when the last are used up).
 #include <algorithm>
 #include <cmath>
 

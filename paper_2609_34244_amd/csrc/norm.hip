@@ -2,14 +2,15 @@
 //
 // mean = sum x / n, rstd = 1 / sqrt(sum (x - mean)^2 / n + eps), xh = (x - mean) rstd, y = xh w + b;
 // g = dy w, dx = rstd (g - mean(g) - xh mean(g xh)) + r, dw = sum over rows of dy xh, db of dy.
-// Bound by memory: a row is read once and stays in registers, TPR lanes to a row, K pieces of 16
+// Memory is read and written once: a row is read once and stays in registers, TPR lanes to a row, K pieces of 16
 // bytes a lane; the variance is summed from the differences to the mean, so that a mean far from
 // zero costs no digits. All sums are fp32.
 // The backward pass takes a row at a time in each of its workgroups (several where a row needs
 // less than one), so that a lane keeps its columns' sums of dy xh and dy in registers; a second
 // kernel adds up the workgroups' sums, in one order. The next row's loads are in flight while a
-// row's two sums are formed. 4096 rows of 4096, bf16: forward 20 us (3.4 TB/s), backward with a residual 33 + 4.6 us (4.0 TB/s
-// without the sums). Rows of more than 512 kLongest values are read again instead.
+// row's two sums are formed. 4096 rows of 4096, bf16: forward 20 us (3.4 TB/s), backward with a residual 34 + 4.4 us (3.9 TB/s
+// without the sums), wavefronts waiting 62 and 55% of the time: forward, each workgroup has one row, and reads the weights and
+// shifts for it from the caches, as many requests to the L2 as for the row. Rows of more than 512 kLongest values are read again instead.
 #include <algorithm>
 #include <cmath>
 
@@ -37,8 +38,8 @@ template <typename T> struct Piece {
     typedef T loose __attribute__((ext_vector_type(16 / sizeof(T)), aligned(sizeof(T))));   // at any address its values may have
 };
 
-// The values from column c on, those past the row's end 0. WHOLE: rows end with a piece (a test for the end made every
-// load wait for the one before: 4096 rows of 4096 in bf16, forward, 31 us instead of 16).
+// The values from column c on, those past the row's end 0. WHOLE: rows end with a piece, and no load
+// waits for a test of the end (4096 rows of 4096 in bf16, forward: 19.8 us, 20.4 with the tests).
 template <typename T, bool WHOLE = false> __device__ inline typename Piece<T>::type load(const T *row, int c, int n)
 {
     typename Piece<T>::type v = {};
