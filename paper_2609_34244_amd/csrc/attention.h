@@ -53,7 +53,8 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 __device__ inline f32x16 mfma(mm::bf16x8 a, mm::bf16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
 __device__ inline f32x16 mfma(mm::f16x8 a, mm::f16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
 
-constexpr int64_t kMostBlocks = (int64_t(1) << 23) - 1;   // of 512 lanes: a launch has fewer than 2^32
+constexpr int kClearing = 256;                // the most workgroups that clear rows
+constexpr int64_t kMostBlocks = (int64_t(1) << 23) - 1 - kClearing;   // of 512 lanes: a launch has fewer than 2^32
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
@@ -74,7 +75,8 @@ struct Args {
     int32_t sequences, q_len, k_len, packed;
     int32_t heads, kv_heads, group, dim;
     int32_t causal, parts;
-    int32_t out_vec, grads;                   // outputs on 16-byte addresses, their strides and dim whole eights; which gradients
+    uint32_t blocks;                          // the launch's workgroups for tiles; those past them clear rows
+    int32_t out_vec, grads;                   // outputs on 16-byte addresses, their strides and dim whole eights; 1: dq wanted, 4, 8: dk, dv to be cleared
     float scale, scale2, cap2, unscale;       // scale2 = scale log2(e); with a cap: 2 scale log2(e) / cap and cap log2(e); -1 / scale2
 };
 
@@ -261,6 +263,35 @@ template <typename T> __device__ inline typename mm::pack8<T>::type global_fragm
     typename mm::pack8<T>::type x = {};
     if (any && col < dim) x = *(const typename mm::pack8<T>::type *)(row + col);
     return x;
+}
+
+// Zeros for an output's rows of no sequence: workgroup b of n that share them. They are workgroups of the kernel that writes the
+// output's other rows; a launch of their own took 2 us, and 3 of the host (11 documents of 4092 rows, 32 heads, training: NEW us, 194).
+HEDDLE_INLINE void clear_rows(const Args &a, const View &v, bool keys, uint32_t b, uint32_t n)
+{
+    const int32_t *at = keys ? a.d_k : a.d_q;
+    const int rows = keys ? a.k_len : a.q_len, heads = keys ? a.kv_heads : a.heads, per = (a.dim + 7) / 8, line = heads * per;
+    const uint32_t sequences = a.packed ? 1 : a.sequences, chunks = max(1u, n / sequences);
+    for (uint32_t x = b; x < sequences * chunks; x += n) {
+        const uint32_t s = x % sequences, chunk = x / sequences;
+        int first = 0, last = rows;                         // rows before the first and from the last on
+        if (!a.packed) last = at ? clamp_row(at[s], rows) : rows;
+        else if (a.sequences) first = clamp_row(at[0], rows), last = max(first, clamp_row(at[a.sequences], rows));
+        else last = 0;
+        const int64_t all = (int64_t)(first + rows - last) * line, step = (int64_t)chunks * blockDim.x;
+        for (int64_t i = (int64_t)chunk * blockDim.x + threadIdx.x; i < all; i += step) {
+            const int64_t u = i / line, row = u < first ? u : u - first + last;
+            const int rest = (int)(i - u * line), head = rest / per, col = (rest - head * per) * 8;
+            uint16_t *p = (uint16_t *)v.p + s * v.seq + row * v.row + head * v.head + col;
+            if (a.out_vec) {
+                *(s16x8 *)p = s16x8{};
+            } else {
+#pragma unroll
+                for (int k = 0; k < 8; k++)
+                    if (col + k < a.dim) p[k] = 0;
+            }
+        }
+    }
 }
 
 // eight probabilities as the next product's operand, rounded to the type that the matrix cores read at full rate: in bf16 y is
@@ -485,8 +516,10 @@ Args base_args(const heddle_attention_desc *d);
 int mode_of(const heddle_attention_desc *d);
 int backward(const heddle_attention_desc *d, mm::Scratch &s, bool run, hipStream_t stream);
 // the launches
-void launch_clear(const heddle_attention_desc *d, const Args &a, bool backward, hipStream_t stream);
-void launch_forward(const heddle_attention_desc *d, const Args &a, int rows, int64_t blocks, hipStream_t stream);
+// workgroups of `threads` that clear rows: 0 unless one of `bits` of the descriptor's `clear` is set
+unsigned clearing(const heddle_attention_desc *d, int bits, bool keys, int threads);
+int clear_all(const heddle_attention_desc *d, const Args &a, bool backward, hipStream_t stream);
+void launch_forward(const heddle_attention_desc *d, Args a, int rows, int64_t blocks, hipStream_t stream);
 
 // f(type, padded head width, mode) as constants
 template <typename F> void with_kind(const heddle_attention_desc *d, F f)

@@ -23,6 +23,7 @@ template <typename T, int DP, int MODE> __global__ void __launch_bounds__(256) s
     static_assert(4 * 32 * kLine * 4 + 4 * 64 * 4 <= 8 * kStage, "the wavefronts' sums fit where the tiles were");
     __shared__ __align__(1024) char smem[4][2][kStage];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, h = lane >> 5, col = lane & 31;
+    if (blockIdx.x >= a.blocks) return clear_rows(a, a.y, false, blockIdx.x - a.blocks, gridDim.x - a.blocks);
     const uint32_t rest = blockIdx.x / (uint32_t)a.kv_heads;
     const int hk = blockIdx.x - rest * a.kv_heads;
     const int64_t slot = rest / (uint32_t)a.parts;
@@ -222,53 +223,27 @@ int Copies::launch(hipStream_t stream) const
     return e == hipSuccess ? HEDDLE_OK : hip_fail(e, "attention's copies");
 }
 
-// ---- rows of no sequence ----
-// z: sequences (one where packed). With offsets or lengths that leave no row out, 2 us for the launch.
-struct Outputs {
-    View view[3];
-    int keys[3];                              // of keys' rows
-};
-__global__ void __launch_bounds__(256) clear_kernel(Args a, Outputs o)
+// ---- rows of no sequence, where there is none ----
+__global__ void __launch_bounds__(256) clear_kernel(Args a, View v, int keys) { clear_rows(a, v, keys, blockIdx.x, gridDim.x); }
+
+unsigned clearing(const heddle_attention_desc *d, int bits, bool keys, int threads)
 {
-    const View v = o.view[blockIdx.y];
-    const bool keys = o.keys[blockIdx.y];
-    const int32_t *at = keys ? a.d_k : a.d_q;
-    const int rows = keys ? a.k_len : a.q_len, heads = keys ? a.kv_heads : a.heads, per = (a.dim + 7) / 8, line = heads * per, s = blockIdx.z;
-    int first = 0, last = rows;                             // rows before the first and from the last on
-    if (!a.packed) last = at ? clamp_row(at[s], rows) : rows;
-    else if (a.sequences) first = clamp_row(at[0], rows), last = max(first, clamp_row(at[a.sequences], rows));
-    else last = 0;
-    const int64_t all = (int64_t)(first + rows - last) * line;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
-        const int64_t u = i / line, row = u < first ? u : u - first + last;
-        const int rest = (int)(i - u * line), head = rest / per, col = (rest - head * per) * 8;
-        uint16_t *p = (uint16_t *)v.p + s * v.seq + row * v.row + head * v.head + col;
-        if (a.out_vec) {
-            *(s16x8 *)p = s16x8{};
-        } else {
-#pragma unroll
-            for (int k = 0; k < 8; k++)
-                if (col + k < a.dim) p[k] = 0;
-        }
-    }
+    if (!(d->clear & bits)) return 0;
+    const int64_t rows = (keys ? d->k_len : d->q_len) * (d->packed ? 1 : d->sequences), all = rows * (keys ? d->kv_heads : d->heads) * ((d->dim + 7) / 8);
+    return (unsigned)std::min<int64_t>((all + threads - 1) / threads, kClearing);
 }
-void launch_clear(const heddle_attention_desc *d, const Args &a, bool backward, hipStream_t stream)
+
+int clear_all(const heddle_attention_desc *d, const Args &a, bool backward, hipStream_t stream)
 {
-    Outputs o = {};
-    int n = 0;
-    int64_t most = 0;
-    auto add = [&](int bit, const View &v, bool keys) {
-        const int64_t line = (int64_t)(keys ? a.kv_heads : a.heads) * ((a.dim + 7) / 8), all = (keys ? a.k_len : a.q_len) * line;
-        if (!(d->clear & bit) || !v.p || all == 0) return;
-        o.view[n] = v, o.keys[n++] = keys;
-        most = std::max(most, all);
+    auto clear = [&](int bit, const View &v, bool keys) {
+        const unsigned n = clearing(d, bit, keys, 256);
+        if (v.p && n) hipLaunchKernelGGL(clear_kernel, dim3(n), dim3(256), 0, stream, a, v, (int)keys);
     };
-    add(1, backward ? a.dq : a.y, false);
-    if (backward) add(2, a.dk, true), add(4, a.dv, true);
-    const int64_t z = a.packed ? 1 : a.sequences;
-    if (n == 0 || z == 0) return;
-    const int64_t x = std::max<int64_t>(1, std::min<int64_t>((most + 255) / 256, 512 / z));
-    hipLaunchKernelGGL(clear_kernel, dim3((unsigned)x, (unsigned)n, (unsigned)z), dim3(256), 0, stream, a, o);
+    clear(1, backward ? a.dq : a.y, false);
+    if (backward) clear(2, a.dk, true), clear(4, a.dv, true);
+    if (!d->clear) return HEDDLE_OK;
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess ? HEDDLE_OK : hip_fail(e, "attention's empty rows");
 }
 
 // ---- host ----
@@ -449,8 +424,7 @@ static int forward(const heddle_attention_desc *d, mm::Scratch &s, bool run, hip
     Args a = base_args(d);
     if (a.q_rows == 0) return HEDDLE_OK;
     a.out_vec = !((uintptr_t)d->y & 15) && !((a.y.seq | a.y.row | a.y.head | d->dim) & 7);
-    if (run && d->clear) launch_clear(d, a, false, stream);
-    if (d->sequences == 0) return run && d->clear ? launched("attention") : HEDDLE_OK;
+    if (d->sequences == 0) return run ? clear_all(d, a, false, stream) : HEDDLE_OK;
     Copies c;
     c.add(d, a.q, false, s);
     c.add(d, a.k, true, s);
@@ -467,9 +441,10 @@ static int forward(const heddle_attention_desc *d, mm::Scratch &s, bool run, hip
     if (!plan.split) {
         launch_forward(d, a, T, blocks, stream);
     } else {
+        a.blocks = (uint32_t)(blocks * a.parts);
         with_kind(d, [&](auto t, auto dp, auto mode) {
             typedef decltype(t) T;
-            hipLaunchKernelGGL((split_kernel<T, dp, mode>), dim3((unsigned)(blocks * a.parts)), dim3(256), 0, stream, a, tiles);
+            hipLaunchKernelGGL((split_kernel<T, dp, mode>), dim3(a.blocks + clearing(d, 1, false, 256)), dim3(256), 0, stream, a, tiles);
         });
         if (a.parts > 1) launch_combine(d, a, blocks, tiles, stream);
     }

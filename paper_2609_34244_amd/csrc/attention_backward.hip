@@ -63,11 +63,12 @@ template <typename T, int DP, int MODE> __global__ void __launch_bounds__(256, 2
     typedef typename mm::pack8<T>::type frag;
     __shared__ __align__(1024) char smem[2][2 * Tk::kBytes];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, h = lane >> 5, col = lane & 31;
+    if (blockIdx.x >= a.blocks) return clear_rows(a, a.dq, false, blockIdx.x - a.blocks, gridDim.x - a.blocks);
     const uint32_t slot = blockIdx.x / (uint32_t)a.kv_heads;
     const int hk = blockIdx.x - slot * a.kv_heads;
     Sequence q;
     int64_t tile;
-    if (!find_tile(a, false, kRows, slot, gridDim.x / (uint32_t)a.kv_heads, q, tile)) return;
+    if (!find_tile(a, false, kRows, slot, a.blocks / (uint32_t)a.kv_heads, q, tile)) return;
     const int s = q.s;
     if (tile * kRows >= (int64_t)q.lq * a.group) return;
     const int rows = q.lq * a.group, r = (int)tile * kRows + wave * 32 + col;
@@ -232,6 +233,12 @@ HEDDLE_INLINE void gather(const Args &a, f32x16 *dk, f32x16 *dv, const char *tq,
     });
 }
 
+HEDDLE_INLINE void clear_keys(const Args &a, uint32_t b, uint32_t n)
+{
+    if (a.grads & 4) clear_rows(a, a.dk, true, b, n);
+    if (a.grads & 8) clear_rows(a, a.dv, true, b, n);
+}
+
 // NW 8: two tiles of 128 keys a workgroup, the sequence's p-th and p-th from the end, which together see as many rows as
 // any other such pair, and share the rows' tiles.
 template <typename T, int DP, int MODE, int NW> __global__ void __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2))) keys_kernel(Args a)
@@ -244,11 +251,12 @@ template <typename T, int DP, int MODE, int NW> __global__ void __launch_bounds_
     __shared__ __align__(1024) char values[NW / 4][Tv::kBytes];
     __shared__ __align__(16) float stats[2][2][kRows];      // what the exponents, or the scores' sums, start from; -delta
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, h = lane >> 5, col = lane & 31;
+    if (blockIdx.x >= a.blocks) return clear_keys(a, blockIdx.x - a.blocks, gridDim.x - a.blocks);
     const uint32_t slot = blockIdx.x / (uint32_t)a.kv_heads;
     const int hk = blockIdx.x - slot * a.kv_heads;
     Sequence q;
     int64_t tile;
-    if (!find_tile(a, true, 32 * NW, slot, gridDim.x / (uint32_t)a.kv_heads, q, tile)) return;
+    if (!find_tile(a, true, 32 * NW, slot, a.blocks / (uint32_t)a.kv_heads, q, tile)) return;
     const int s = q.s;
     if (tile * (32 * NW) >= q.lk) return;
     const int team = wave >> 2, last_tile = (q.lk + 127) / 128 - 1, own = team ? last_tile - (int)tile : (int)tile;
@@ -359,6 +367,7 @@ template <typename T, int DP, int MODE> __global__ void __launch_bounds__(512) _
     __shared__ __align__(1024) char smem[8][kStage], values[Tk::kBytes];
     __shared__ __align__(16) float stats[8][2][32];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, h = lane >> 5, col = lane & 31;
+    if (blockIdx.x >= a.blocks) return clear_keys(a, blockIdx.x - a.blocks, gridDim.x - a.blocks);
     const uint32_t slot = blockIdx.x / (uint32_t)a.kv_heads;
     const int hk = blockIdx.x - slot * a.kv_heads;
     int s;
@@ -464,34 +473,33 @@ template <typename T, int DP, int MODE> __global__ void __launch_bounds__(512) _
     });
 }
 
-static void launch_rows(const heddle_attention_desc *d, const Args &a, int64_t blocks, hipStream_t stream)
+static void launch_rows(const heddle_attention_desc *d, Args a, int64_t blocks, hipStream_t stream)
 {
+    a.blocks = (uint32_t)blocks;
+    const dim3 grid(a.blocks + (d->dq ? clearing(d, 1, false, 256) : 0));
     with_kind(d, [&](auto t, auto dp, auto mode) {
-        hipLaunchKernelGGL((rows_kernel<decltype(t), dp, mode>), dim3((unsigned)blocks), dim3(256), 0, stream, a);
+        hipLaunchKernelGGL((rows_kernel<decltype(t), dp, mode>), grid, dim3(256), 0, stream, a);
     });
 }
-static void launch_keys(const heddle_attention_desc *d, const Args &a, int span, int64_t blocks, int64_t tiles, hipStream_t stream)
+static void launch_keys(const heddle_attention_desc *d, Args a, int span, int64_t blocks, int64_t tiles, hipStream_t stream)
 {
+    a.blocks = (uint32_t)blocks;
+    const dim3 grid(a.blocks + clearing(d, 6, true, 256));
     with_kind(d, [&](auto t, auto dp, auto mode) {
-        if (span == 32) hipLaunchKernelGGL((few_keys_kernel<decltype(t), dp, mode>), dim3((unsigned)blocks), dim3(512), 0, stream, a, tiles);
-        else if (span == 256) hipLaunchKernelGGL((keys_kernel<decltype(t), dp, mode, 8>), dim3((unsigned)blocks), dim3(512), 0, stream, a);
-        else hipLaunchKernelGGL((keys_kernel<decltype(t), dp, mode, 4>), dim3((unsigned)blocks), dim3(256), 0, stream, a);
+        if (span == 32) hipLaunchKernelGGL((few_keys_kernel<decltype(t), dp, mode>), grid, dim3(512), 0, stream, a, tiles);
+        else if (span == 256) hipLaunchKernelGGL((keys_kernel<decltype(t), dp, mode, 8>), grid, dim3(512), 0, stream, a);
+        else hipLaunchKernelGGL((keys_kernel<decltype(t), dp, mode, 4>), grid, dim3(256), 0, stream, a);
     });
 }
 
 int backward(const heddle_attention_desc *d, mm::Scratch &s, bool run, hipStream_t stream)
 {
     Args a = base_args(d);
-    a.grads = (d->dq ? 1 : 0) | (d->dk ? 2 : 0);
-    if (!a.grads) return HEDDLE_OK;
+    if (!d->dq && !d->dk) return HEDDLE_OK;
+    a.grads = (d->dq ? 1 : 0) | (d->clear & 6) * 2;
     auto aligned = [&](const void *p, const View &v) { return !((uintptr_t)p & 15) && !((v.seq | v.row | v.head | d->dim) & 7); };
     a.out_vec = (!d->dq || aligned(d->dq, a.dq)) && (!d->dk || (aligned(d->dk, a.dk) && aligned(d->dv, a.dv)));
-    auto launched = []() {
-        const hipError_t e = hipGetLastError();
-        return e == hipSuccess ? HEDDLE_OK : hip_fail(e, "attention's gradients");
-    };
-    if (run && d->clear) launch_clear(d, a, true, stream);
-    if (d->sequences == 0) return run && d->clear ? launched() : HEDDLE_OK;
+    if (d->sequences == 0) return run ? clear_all(d, a, true, stream) : HEDDLE_OK;
     Copies c;
     if (a.q_rows) c.add(d, a.q, false, s);
     if (a.q_rows) c.add(d, a.y, false, s);
@@ -508,7 +516,8 @@ int backward(const heddle_attention_desc *d, mm::Scratch &s, bool run, hipStream
     if (const int rc = c.launch(stream)) return rc;
     if (blocks) launch_rows(d, a, blocks, stream);
     if (kblocks) launch_keys(d, a, (int)span, kblocks, ktiles, stream);
-    return launched();
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess ? HEDDLE_OK : hip_fail(e, "attention's gradients");
 }
 
 }  // namespace attn

@@ -65,12 +65,13 @@ template <typename T, int DP, int MODE, int NW> __global__ void __launch_bounds_
     typedef typename mm::pack8<T>::type frag;
     __shared__ __align__(1024) char smem[2][2][Tk::kBytes]; // keys, values
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, h = lane >> 5;
+    if (blockIdx.x >= a.blocks) return clear_rows(a, a.y, false, blockIdx.x - a.blocks, gridDim.x - a.blocks);
     // key heads fastest: 8 of them lie on one XCD each, whose L2 then holds its head's keys
     const uint32_t slot = blockIdx.x / (uint32_t)a.kv_heads;
     const int hk = blockIdx.x - slot * a.kv_heads;
     Sequence q;
     int64_t tile;
-    if (!find_tile(a, false, kRows, slot, gridDim.x / (uint32_t)a.kv_heads, q, tile)) return;
+    if (!find_tile(a, false, kRows, slot, a.blocks / (uint32_t)a.kv_heads, q, tile)) return;
     const int s = q.s;
     if (tile * kRows >= (int64_t)q.lq * a.group) return;
     const int r0 = (int)tile * kRows, rows = q.lq * a.group;
@@ -177,11 +178,13 @@ template <typename T, int DP, int MODE, int NW> __global__ void __launch_bounds_
         a.lse[row.at * a.heads + row.head] = l == 0 ? -INFINITY : (st.m * unit_of<MODE>(a) + offset_of<MODE>(a) + __log2f(l)) * kLn2;
 }
 
-void launch_forward(const heddle_attention_desc *d, const Args &a, int rows, int64_t blocks, hipStream_t stream)
+void launch_forward(const heddle_attention_desc *d, Args a, int rows, int64_t blocks, hipStream_t stream)
 {
+    a.blocks = (uint32_t)blocks;
+    const dim3 grid(a.blocks + clearing(d, 1, false, 2 * rows));
     with_kind(d, [&](auto t, auto dp, auto mode) {
-        if (rows == 128) hipLaunchKernelGGL((forward_kernel<decltype(t), dp, mode, 4>), dim3((unsigned)blocks), dim3(256), 0, stream, a);
-        else hipLaunchKernelGGL((forward_kernel<decltype(t), dp, mode, 8>), dim3((unsigned)blocks), dim3(512), 0, stream, a);
+        if (rows == 128) hipLaunchKernelGGL((forward_kernel<decltype(t), dp, mode, 4>), grid, dim3(256), 0, stream, a);
+        else hipLaunchKernelGGL((forward_kernel<decltype(t), dp, mode, 8>), grid, dim3(512), 0, stream, a);
     });
 }
 

@@ -97,3 +97,21 @@ def test_captured(H):
         for n, t in (("y", y), *grads.items()):
             assert not t[~used].any() and bool(torch.isfinite(t).all()), (n, now)
         assert torch.equal(y, H.heddle_attention(q, k, v, q_lengths=lengths, k_lengths=lengths))
+
+
+@pytest.mark.parametrize("n,lq,lk,hq,hk,dim", [(2, 640, 640, 104, 52, 64), (2, 600, 700, 54, 54, 128), (4, 300, 290, 44, 22, 128), (300, 3, 40, 2, 2, 64), (700, 2, 5, 1, 1, 24),
+                                               (40, 1, 3000, 8, 8, 128), (3, 2, 4000, 8, 2, 64)])
+def test_kernels(H, n, lq, lk, hq, hk, dim):
+    """256 and 128 rows and keys a workgroup, few of them, more sequences than workgroups that clear, keys in one part and several"""
+    queries, keys = [(7 * j) % (lq + 1) for j in range(n)], [lk - (31 * j) % lk for j in range(n)]
+    both_ways(H, (n, lq, hq, dim), (n, lk, hk, dim), BF16, used_rows(n, lq, queries), used_rows(n, lk, keys),
+              dict(causal=True, q_lengths=ints(queries), k_lengths=ints(keys)))
+
+
+@pytest.mark.parametrize("lengths,heads,kv_heads", [([700, 0, 513, 640, 1, 1200, 900], 32, 16), ([300, 0, 129, 257, 1], 60, 60), ([640] * 66, 4, 2), ([1, 2, 1], 4, 4)])
+@pytest.mark.parametrize("lead,tail", [(0, 0), (300, 0), (0, 1), (5, 2000)])
+def test_kernels_of_documents(H, lengths, heads, kv_heads, lead, tail):
+    rows, offsets = lead + sum(lengths) + tail, [lead + sum(lengths[:i]) for i in range(len(lengths) + 1)]
+    at = torch.arange(rows, device="cuda")
+    used = (at >= lead) & (at < rows - tail)
+    both_ways(H, (rows, heads, 64), (rows, kv_heads, 64), FP16, used, used, dict(causal=True, q_offsets=ints(offsets), k_offsets=ints(offsets)))
