@@ -266,7 +266,8 @@ template <typename T> __device__ inline typename mm::pack8<T>::type global_fragm
 }
 
 // Zeros for an output's rows of no sequence: workgroup b of n that share them. They are workgroups of the kernel that writes the
-// output's other rows; a launch of their own took 2 us, and 3 of the host (11 documents of 4092 rows, 32 heads, training: NEW us, 194).
+// output's other rows; a launch of their own takes 2 us, and 3 of the host (11 documents of 4092 rows, 32 heads, training: 196.8 us without clearing, 198.3 so, 2% more
+// with launches).
 HEDDLE_INLINE void clear_rows(const Args &a, const View &v, bool keys, uint32_t b, uint32_t n)
 {
     const int32_t *at = keys ? a.d_k : a.d_q;

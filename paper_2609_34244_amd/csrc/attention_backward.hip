@@ -63,7 +63,7 @@ template <typename T, int DP, int MODE> __global__ void __launch_bounds__(256, 2
     typedef typename mm::pack8<T>::type frag;
     __shared__ __align__(1024) char smem[2][2 * Tk::kBytes];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, h = lane >> 5, col = lane & 31;
-    if (blockIdx.x >= a.blocks) return clear_rows(a, a.dq, false, blockIdx.x - a.blocks, gridDim.x - a.blocks);
+    if (__builtin_expect(blockIdx.x >= a.blocks, false)) return clear_rows(a, a.dq, false, blockIdx.x - a.blocks, gridDim.x - a.blocks);
     const uint32_t slot = blockIdx.x / (uint32_t)a.kv_heads;
     const int hk = blockIdx.x - slot * a.kv_heads;
     Sequence q;
@@ -251,7 +251,7 @@ template <typename T, int DP, int MODE, int NW> __global__ void __launch_bounds_
     __shared__ __align__(1024) char values[NW / 4][Tv::kBytes];
     __shared__ __align__(16) float stats[2][2][kRows];      // what the exponents, or the scores' sums, start from; -delta
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, h = lane >> 5, col = lane & 31;
-    if (blockIdx.x >= a.blocks) return clear_keys(a, blockIdx.x - a.blocks, gridDim.x - a.blocks);
+    if (__builtin_expect(blockIdx.x >= a.blocks, false)) return clear_keys(a, blockIdx.x - a.blocks, gridDim.x - a.blocks);
     const uint32_t slot = blockIdx.x / (uint32_t)a.kv_heads;
     const int hk = blockIdx.x - slot * a.kv_heads;
     Sequence q;
@@ -367,7 +367,7 @@ template <typename T, int DP, int MODE> __global__ void __launch_bounds__(512) _
     __shared__ __align__(1024) char smem[8][kStage], values[Tk::kBytes];
     __shared__ __align__(16) float stats[8][2][32];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, h = lane >> 5, col = lane & 31;
-    if (blockIdx.x >= a.blocks) return clear_keys(a, blockIdx.x - a.blocks, gridDim.x - a.blocks);
+    if (__builtin_expect(blockIdx.x >= a.blocks, false)) return clear_keys(a, blockIdx.x - a.blocks, gridDim.x - a.blocks);
     const uint32_t slot = blockIdx.x / (uint32_t)a.kv_heads;
     const int hk = blockIdx.x - slot * a.kv_heads;
     int s;

@@ -65,7 +65,7 @@ template <typename T, int DP, int MODE, int NW> __global__ void __launch_bounds_
     typedef typename mm::pack8<T>::type frag;
     __shared__ __align__(1024) char smem[2][2][Tk::kBytes]; // keys, values
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, h = lane >> 5;
-    if (blockIdx.x >= a.blocks) return clear_rows(a, a.y, false, blockIdx.x - a.blocks, gridDim.x - a.blocks);
+    if (__builtin_expect(blockIdx.x >= a.blocks, false)) return clear_rows(a, a.y, false, blockIdx.x - a.blocks, gridDim.x - a.blocks);
     // key heads fastest: 8 of them lie on one XCD each, whose L2 then holds its head's keys
     const uint32_t slot = blockIdx.x / (uint32_t)a.kv_heads;
     const int hk = blockIdx.x - slot * a.kv_heads;

@@ -518,7 +518,8 @@ def _dtype_codes():
     return _codes
 
 
-_forward_ad = None               # torch.autograd.forward_ad, from the first call on
+class _forward_ad:                # until the first call, then torch.autograd.forward_ad
+    _current_level = 0
 
 
 def _plain(t, what):
@@ -530,16 +531,15 @@ def _plain(t, what):
         if torch.is_grad_enabled():
             _refuse(f"{what}: requires a gradient, and autograd records nothing of this call; use torch.no_grad() and the "
                     "operator's backward call")
-    if _forward_ad is None:
-        from torch.autograd import forward_ad
-        _forward_ad = forward_ad
+    from torch.autograd import forward_ad
+    _forward_ad = forward_ad
     if _forward_ad._current_level >= 0 and _forward_ad.unpack_dual(t).tangent is not None:
         _refuse(f"{what}: has a tangent, and the calls do not propagate those of forward-mode differentiation")
 
 
 def _matrix(t, what, shape, dtype, gpu):
     """(data pointer, ld) of a device matrix whose rows are contiguous"""
-    if t.requires_grad or _forward_ad is None or _forward_ad._current_level >= 0:
+    if t.requires_grad or _forward_ad._current_level >= 0:
         _plain(t, what)
     if t.dtype != dtype or t.get_device() != gpu:
         _refuse(f"{what}: {t.dtype} on {t.device}, not {dtype} on GPU {gpu}")
@@ -558,7 +558,7 @@ def _weights(t, what, shape, dtype, gpu):
 
 
 def _vector(t, what, shape, dtype, gpu):
-    if t.requires_grad or _forward_ad is None or _forward_ad._current_level >= 0:
+    if t.requires_grad or _forward_ad._current_level >= 0:
         _plain(t, what)
     if t.dtype != dtype or t.get_device() != gpu or t.shape != shape or not t.is_contiguous():
         _refuse(f"{what}: not a contiguous {dtype} tensor of shape {shape} on GPU {gpu}")
@@ -802,7 +802,7 @@ _NONE = (0, 0, 0, 0)
 
 def _heads(t, what, shape, dtype, gpu):
     """(data pointer, strides of sequences, rows and heads) of [sequences, rows, heads, dim] or [rows, heads, dim]"""
-    if t.requires_grad or _forward_ad is None or _forward_ad._current_level >= 0:
+    if t.requires_grad or _forward_ad._current_level >= 0:
         _plain(t, what)
     if t.dtype != dtype or t.get_device() != gpu:
         _refuse(f"{what}: {t.dtype} on {t.device}, not {dtype} on GPU {gpu}")
@@ -844,7 +844,7 @@ def _attention_inputs(q, k, v, scale, causal, cap, slopes, prefix, q_lengths, k_
         dq, dk = _ints(q_lengths, "q_lengths", n, gpu), _ints(k_lengths, "k_lengths", n, gpu)
     if ks[-1] != qs[-1]:
         _refuse(f"k: heads of {ks[-1]} values, not {qs[-1]}")
-    if slopes is not None:
+    if slopes is not None and (slopes.requires_grad or _forward_ad._current_level >= 0):
         _plain(slopes, "slopes")
     head = (_dtype(q, "q"), 1 if causal else 0, 1 if packed else 0, n, qs[-3], ks[-3], qs[-2], ks[-2], qs[-1],
             qs[-1] ** -0.5 if scale is None else scale, cap, clear, dq, dk, _ints(prefix, "prefix", n, gpu),
@@ -1025,7 +1025,7 @@ def heddle_expert_balance_backward(logits, picked, counts, rows, dloss=None, sca
     pr = (0, 0) if residual is None else _matrix(residual, "residual", (t, e), logits.dtype, gpu)
     if dloss is not None and (dloss.numel() != 1 or str(dloss.dtype) != "torch.float32" or dloss.get_device() != gpu):
         _refuse("dloss: not one float32 value on the logits' GPU")
-    if dloss is not None:
+    if dloss is not None and (dloss.requires_grad or _forward_ad._current_level >= 0):
         _plain(dloss, "dloss")
     desc = _BALANCE.pack(_dtype(logits, "logits"), e, k, size, t, scale, pl, ldl, pp, ldp, _ints(counts, "counts", e, gpu),
                          _ints(rows, "rows", 1, gpu), 0, 0, 0, 0 if dloss is None else dloss.data_ptr(), *pr,
